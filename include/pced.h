@@ -59,6 +59,7 @@ typedef enum pced_status {
 #define PCED_DEV_STEP_LIMIT 0x10u /* step counter reached max_steps */
 #define PCED_DEV_BAD_BLOCK 0x20u  /* paged caches: a needed block-table entry is missing or outside the pool */
 #define PCED_DEV_BOUNDS 0x40u     /* bounds-checked build only: an index outside its buffer (the access was skipped) */
+#define PCED_DEV_BAD_INDEX 0x80u  /* a position outside the rotation table, or a mask number outside the masks */
 
 /* Static description of a status code (host). */
 const char* pced_status_string(int32_t status);
@@ -407,6 +408,165 @@ int32_t pced_step_launch_count(const pced_step_args* args);
  * "lse_finalize", "adacad_beta", "agg_partials", "agg_select" or "select";
  * NULL when out of range (static storage). */
 const char* pced_step_launch_kind(const pced_step_args* args, int32_t i);
+
+/* ========================================================================
+ * Operators of a decode step over paged caches, for programs that have their
+ * own layers: kv_append -> block_select -> paged_attention in every layer,
+ * lm_head_logprobs -> logits_process -> contrastive_select after the last.
+ * The pool is laid out as pced_step's paged caches are, so one cache serves
+ * both.
+ *
+ * pced_paged_cache describes one layer's cache of S sequences (host struct,
+ * device pointers; fields that a call does not name may be NULL):
+ *   k, v         bf16 [num_blocks][Hkv][block_rows][D]
+ *   block_table  int32 [S][max_blocks]: row r of sequence s is row
+ *                r % block_rows of block block_table[s][r / block_rows]
+ *   seq_len      int32 [S]: live rows, the rows appended in this step
+ *                included; 0: an idle sequence
+ *   summary      int8 [num_blocks][Hkv][2][D]: of every block, kv-head and
+ *                channel the largest key (index 0), rounded up, and the
+ *                smallest (index 1), rounded down, in steps of key_step[h],
+ *                clipped to [-127, 127] (a key that is not a number: 127 and
+ *                -127); in steps: the fp32 product of the stored key and
+ *                the fp32 quotient 1 / key_step[h]
+ *   key_step     fp32 [Hkv]: about the largest |key| of a head / 127
+ * block_rows: a multiple of 16; D 64 or 128; S <= 1024; 16-byte aligned
+ * k, v, summary; num_blocks*Hkv*block_rows < 2^31.  A length outside
+ * [0, max_blocks*block_rows] sets PCED_DEV_BAD_LENGTH and is clipped into it;
+ * a table entry outside [0, num_blocks) that a call needs sets
+ * PCED_DEV_BAD_BLOCK, and its rows are neither written nor read.
+ * ======================================================================== */
+typedef struct pced_paged_cache {
+  void* k;
+  void* v;
+  int8_t* summary;
+  const float* key_step;
+  const int32_t* block_table;
+  const int32_t* seq_len;
+  int32_t num_blocks, block_rows, max_blocks, S, Hkv, D;
+} pced_paged_cache;
+
+/* ------------------------------------------------------------------------
+ * pced_kv_append -- the new tokens' keys and values into the pages, rotated
+ * on the way, and their rotated queries beside them.
+ *   q, k, v    bf16 [T][Hq or Hkv][D], token t at t * q_stride (k_stride,
+ *              v_stride) elements, its heads side by side: the parts of one
+ *              projection's output need no copies.  16-byte aligned, strides
+ *              multiples of 8.  q and q_out may both be NULL (with Hq = Hkv)
+ *   q_out      bf16 [T][Hq][D], must not overlap q, k or v
+ *   tok_start  int32 [S+1] (device): tokens [tok_start[s], tok_start[s+1]) are
+ *              the last rows of sequence s, in order; their keys and values
+ *              go to rows seq_len[s] - count ... seq_len[s] - 1.  NULL: T = S,
+ *              one token for every sequence; an idle sequence has none then,
+ *              and zeros in q_out
+ *   rope       fp32 [rope_rows][D]: cosines of the D/2 angles of a position,
+ *              then their sines, rotate-half pairing (f, f + D/2); each
+ *              product and sum is rounded to fp32, the result to bf16.  NULL:
+ *              no rotation.  Any scaling of the angles is the table's matter
+ *   positions  int32 [T] (device), NULL: the rows the tokens go to.  A position
+ *              outside the table sets PCED_DEV_BAD_INDEX; that token is not
+ *              rotated
+ *   status     device int32 word, may be NULL
+ * With cache->summary the blocks' summaries follow: a block whose first row
+ * is appended starts anew, another one takes the new keys in.  Blocks being
+ * appended to belong to one sequence.  Counts that are negative, above the
+ * sequence's rows or beyond T set PCED_DEV_BAD_LENGTH, and that sequence's
+ * tokens are left out.  Supports Hq/Hkv <= 8.
+ * ------------------------------------------------------------------------ */
+pced_status pced_kv_append(const pced_paged_cache* cache, const void* q, int64_t q_stride, const void* k,
+                           int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int32_t Hq,
+                           const int32_t* tok_start, int32_t T, const float* rope, int32_t rope_rows,
+                           const int32_t* positions, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------
+ * pced_block_summaries -- summaries of all live blocks of the sequences, for
+ * caches that were built elsewhere (documents encoded offline); the rows past
+ * a sequence's last do not count.  Blocks without live rows keep theirs.
+ * ------------------------------------------------------------------------ */
+pced_status pced_block_summaries(const pced_paged_cache* cache, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------
+ * pced_block_select -- the blocks that the new token of every sequence
+ * attends to, for each kv-head: the first n_first, the last n_last, and of
+ * the others those with the highest scores.  With the sums over the heads of
+ * the group, in their order,
+ *   P_d = sum max(q_gd, 0),  N_d = sum min(q_gd, 0)   (fp32),
+ *   m = max_d max(P_d, -N_d),  p = rint(P * (127 / m)),  n = rint(N * (127 / m)),
+ *   score(j) = sum_d p_d max_jd + n_d min_jd,
+ * an upper bound, in steps, of the group's summed q.k over the block.  p, n and
+ * the summaries are whole numbers, so a choice depends on no order of sums.
+ * Ties go to the lowest block.  m zero or not finite: all scores are 0.
+ *   q    bf16 [S][Hq][D], sequence s at s * q_stride elements (16-byte
+ *        aligned, a multiple of 8)
+ *   sel  int32 [S][Hkv][n_sel]: block numbers j (indices into the sequence's
+ *        row of the table) in ascending order; all blocks where there are no
+ *        more than n_sel; -1 after the last
+ * A block without a valid table entry scores below all others.  Needs summary,
+ * n_first, n_last >= 0, n_first + n_last <= n_sel, max_blocks <= 32768.
+ * ------------------------------------------------------------------------ */
+pced_status pced_block_select(const pced_paged_cache* cache, const void* q, int64_t q_stride, int32_t Hq,
+                              int32_t n_sel, int32_t n_first, int32_t n_last, int32_t* sel, int32_t* status,
+                              void* stream);
+
+/* ------------------------------------------------------------------------
+ * pced_paged_attention -- one layer of decode attention, every sequence's new
+ * token over its own cache: o = softmax(scale q K^T) V.
+ *   q, q_stride  as in pced_block_select
+ *   sel, n_sel   int32 [S][Hkv][n_sel] (device): the blocks to attend to, in any
+ *                order, each at most once; -1: none.  A number that is not of
+ *                a live block sets PCED_DEV_BAD_BLOCK and is left out.  NULL: all
+ *   total_rows   host upper bound of the rows attended to, summed over the
+ *                sequences (of one kv-head); sizes the grid only.  0: unknown
+ *   out          [S][Hq][D], fp32 (PCED_OUT_F32) or bf16 (PCED_OUT_BF16)
+ *   lse          fp32 [S][Hq], may be NULL: log of the sum of exp(scale q.k)
+ * A sequence (or a head's choice) without rows has zeros in out and -inf in
+ * lse.  What lies in rows past a sequence's last does not matter.  Probabilities
+ * are held to 16 bits, sums in fp32.  Supports Hq/Hkv <= 8.  The workspace must
+ * be zero-filled before the first call: besides the status word it holds
+ * counters that a call leaves at zero.
+ * ------------------------------------------------------------------------ */
+#define PCED_OUT_F32 0
+#define PCED_OUT_BF16 1
+size_t pced_paged_attention_workspace_size(int32_t S, int32_t Hq, int32_t Hkv, int32_t D);
+pced_status pced_paged_attention(const pced_paged_cache* cache, const void* q, int64_t q_stride, int32_t Hq,
+                                 const int32_t* sel, int32_t n_sel, int64_t total_rows, float scale, void* out,
+                                 int32_t out_type, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * pced_logits_process -- what a request asks of its logits (or
+ * log-probabilities) before a token is chosen: all R rows of a query (its
+ * experts and the amateur) are processed alike, as they share one history.
+ *   x, y         fp32 rows of V entries, row i at i * stride elements, row
+ *                b*R + j belongs to query b; y may be x, and must not overlap
+ *                it otherwise
+ *   history      int32 [B][history_stride]: query b's tokens are its first
+ *                history_len[b] (device int32 [B]) entries; -1 counts as none.
+ *                NULL: no penalties
+ *   penalties    fp32 [B][3] (device): repetition t > 0, frequency f, presence p.
+ *                A token that is in the history c > 0 times:
+ *                  x <- (x > 0 ? x / t : x * t) - (c f + p)
+ *                NULL: none
+ *   bias_ids     int32 [B][n_bias], bias fp32 [B][n_bias] (device): added to the
+ *                token's entry; -1: none; of a token named twice the last
+ *                counts.  NULL (n_bias = 0): none
+ *   mask         uint32 [n_masks][mask_words] (device): bit v % 32 of word v / 32
+ *                is set where token v is allowed; the others become -inf.
+ *                mask_words >= ceil(V / 32).  NULL: none
+ *   mask_row     int32 [B] (device): the mask of each query, -1: none.  NULL:
+ *                mask b for query b.  Another number sets PCED_DEV_BAD_INDEX
+ *                and masks nothing
+ *   status       device int32 word, may be NULL
+ * In this order, each operation rounded to fp32.  A token outside [0, V) sets
+ * PCED_DEV_BAD_TOKEN and is left out; a history_len outside
+ * [0, history_stride] sets PCED_DEV_BAD_LENGTH and is clipped.
+ * pced_contrastive_select never chooses an entry that is -inf in the expert's
+ * and in the amateur's row.
+ * ------------------------------------------------------------------------ */
+pced_status pced_logits_process(const float* x, float* y, int64_t stride, int32_t B, int32_t R, int32_t V,
+                                const int32_t* history, int32_t history_stride, const int32_t* history_len,
+                                const float* penalties, const int32_t* bias_ids, const float* bias, int32_t n_bias,
+                                const uint32_t* mask, int32_t n_masks, int32_t mask_words, const int32_t* mask_row,
+                                int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

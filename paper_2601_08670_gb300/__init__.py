@@ -24,6 +24,7 @@ PCED_DEV_BAD_TOKEN = 0x8
 PCED_DEV_STEP_LIMIT = 0x10
 PCED_DEV_BAD_BLOCK = 0x20
 PCED_DEV_BOUNDS = 0x40
+PCED_DEV_BAD_INDEX = 0x80
 
 
 class PcedError(RuntimeError):
@@ -53,6 +54,13 @@ class StepArgs(ctypes.Structure):
                 ("rope_theta", ctypes.c_float), ("score_mode", ctypes.c_int32), ("aggregation", ctypes.c_int32),
                 ("wait_limit_ns", ctypes.c_uint64), ("expert_base", ctypes.c_int32), ("key_out", ctypes.c_void_p),
                 ("token_out", ctypes.c_void_p), ("expert_out", ctypes.c_void_p), ("score_out", ctypes.c_void_p)]
+
+
+class PagedCacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("summary", ctypes.c_void_p),
+                ("key_step", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
+                ("num_blocks", ctypes.c_int32), ("block_rows", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("S", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32)]
 
 
 _lib = None
@@ -106,6 +114,19 @@ def lib(path: str = LIB_PATH):
         L.pced_select_key_unpack.restype = None
         L.pced_step_commit.argtypes = [P, I32, P, P, P, P, I32, P, P]
         L.pced_step_commit.restype = I32
+        C = ctypes.POINTER(PagedCacheStruct)
+        L.pced_kv_append.argtypes = [C, P, I64, P, I64, P, I64, P, I32, P, I32, P, I32, P, P, P]
+        L.pced_kv_append.restype = I32
+        L.pced_block_summaries.argtypes = [C, P, P]
+        L.pced_block_summaries.restype = I32
+        L.pced_block_select.argtypes = [C, P, I64, I32, I32, I32, I32, P, P, P]
+        L.pced_block_select.restype = I32
+        L.pced_paged_attention_workspace_size.argtypes = [I32, I32, I32, I32]
+        L.pced_paged_attention_workspace_size.restype = SZ
+        L.pced_paged_attention.argtypes = [C, P, I64, I32, P, I32, I64, F, P, I32, P, P, SZ, P]
+        L.pced_paged_attention.restype = I32
+        L.pced_logits_process.argtypes = [P, P, I64, I32, I32, I32, P, I32, P, P, P, P, I32, P, I32, I32, P, P, P]
+        L.pced_logits_process.restype = I32
         _lib = L
     return _lib
 
@@ -260,6 +281,216 @@ def relevance(ret_scores, ret_mode: int = RET_DENSE, rer_logits=None, eps: float
     _check(lib().pced_relevance(_ptr(ret_scores), int(ret_mode), _ptr(rer_logits), ret_scores.numel(), float(eps),
                                 _ptr(r), _stream(stream)), "pced_relevance")
     return r
+
+
+# ------------------------------------------- operators over paged caches
+def _empty(shape, dtype, device, stream):
+    """torch.empty in the memory of the stream that will write it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _is(t, dtype, shape):
+    return t.dtype == dtype and t.shape == shape and t.is_contiguous()
+
+
+def _tokens(t, heads, D):
+    """[T, heads, D] bf16 with a token's heads side by side."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != D or (heads and t.shape[1] != heads):
+        return False
+    st = t.stride()
+    return st[2] == 1 and (st[1] == D or t.shape[1] == 1)
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+class PagedCache:
+    """One layer's paged cache of S sequences (pced_paged_cache in pced.h):
+
+    ``k``, ``v``       bf16 [num_blocks, Hkv, block_rows, D], the layout of pced_step's paged caches
+    ``block_table``    int32 [S, max_blocks]
+    ``seq_len``        int32 [S]: live rows, the rows appended in this step included
+    ``summary``        int8 [num_blocks, Hkv, 2, D] and
+    ``key_step``       fp32 [Hkv]: the blocks' key summaries, for block_select (optional)
+
+    k and v may be None where only block_select is called (block_rows is then needed).  The tensors are held,
+    and their addresses taken once: change their contents, not their storage."""
+
+    def __init__(self, k, v, block_table, seq_len, *, block_rows=None, summary=None, key_step=None):
+        _require(k is not None or (summary is not None and block_rows is not None),
+                 "k, or a summary and block_rows, are needed")
+        if k is not None:
+            _require(k.dim() == 4, "k: [num_blocks, Hkv, block_rows, D]")
+            nb, Hkv, P, D = k.shape
+            _require(block_rows is None or block_rows == P, "block_rows differs from k's")
+        else:
+            _require(summary.dim() == 4, "summary: [num_blocks, Hkv, 2, D]")
+            nb, Hkv, P, D = summary.shape[0], summary.shape[1], int(block_rows), summary.shape[3]
+        for name, t in (("k", k), ("v", v)):
+            _require(t is None or _is(t, torch.bfloat16, (nb, Hkv, P, D)),
+                     f"{name}: contiguous bf16 [num_blocks, Hkv, block_rows, D]")
+        _require(summary is None or _is(summary, torch.int8, (nb, Hkv, 2, D)),
+                 "summary: contiguous int8 [num_blocks, Hkv, 2, D]")
+        _require(key_step is None or _is(key_step, torch.float32, (Hkv,)), "key_step: fp32 [Hkv]")
+        _require(block_table.dim() == 2 and block_table.dtype == torch.int32 and block_table.is_contiguous(),
+                 "block_table: contiguous int32 [S, max_blocks]")
+        S = block_table.shape[0]
+        _require(_is(seq_len, torch.int32, (S,)), "seq_len: contiguous int32 [S]")
+        self.k, self.v, self.block_table, self.seq_len, self.summary, self.key_step = (k, v, block_table, seq_len,
+                                                                                       summary, key_step)
+        self.num_blocks, self.Hkv, self.block_rows, self.D, self.S = nb, Hkv, P, D, S
+        self.max_blocks = block_table.shape[1]
+        self.device = block_table.device
+        for t in (k, v, seq_len, summary, key_step):
+            _require(t is None or t.device == self.device, "a cache's tensors lie on one device")
+        self.struct = PagedCacheStruct(_ptr(k), _ptr(v), _ptr(summary), _ptr(key_step), _ptr(block_table),
+                                       _ptr(seq_len), nb, P, self.max_blocks, S, Hkv, D)
+        self.ref = ctypes.byref(self.struct)
+
+
+def rope_table(theta: float, D: int, rows: int, device="cuda") -> torch.Tensor:
+    """Rotation table of kv_append, fp32 [rows, D]: cosines, then sines, of the
+    angles fp32(p * fp32(theta^(-2f/D))), which pced_step rotates by."""
+    f = torch.tensor([theta ** (-2.0 * i / D) for i in range(D // 2)], dtype=torch.float32, device=device)
+    angle = (torch.arange(rows, dtype=torch.float32, device=device)[:, None] * f).double()
+    return torch.cat([angle.cos(), angle.sin()], dim=1).float()
+
+
+def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=None, q_out=None, status=None,
+              stream=None):
+    """pced_kv_append: k, v bf16 [T, Hkv, D] into the last rows of the sequences, q bf16 [T, Hq, D] (or None)
+    rotated into q_out, which is returned.  The parts of one projection's output need no copies (strides between
+    tokens).  rope: fp32 [rows, D] (rope_table), None: no rotation; tok_start: int32 [S + 1], None: one token per
+    sequence; positions: int32 [T], None: the rows themselves.  Device conditions go to the int32 tensor status."""
+    T, D = k.shape[0], cache.D
+    _require(_tokens(k, cache.Hkv, D), "k: bf16 [T, Hkv, D], a token's heads side by side")
+    _require(_tokens(v, cache.Hkv, D) and v.shape[0] == T, "v: as k")
+    Hq, q_stride = cache.Hkv, 0
+    if q is not None:
+        _require(_tokens(q, 0, D) and q.shape[0] == T, "q: bf16 [T, Hq, D], a token's heads side by side")
+        Hq, q_stride = q.shape[1], _row_stride(q)
+        if q_out is None:
+            q_out = _empty((T, Hq, D), torch.bfloat16, q.device, stream)
+        _require(_is(q_out, torch.bfloat16, (T, Hq, D)), "q_out: contiguous bf16 [T, Hq, D]")
+    else:
+        _require(q_out is None, "q_out without q")
+    rope_rows = 0
+    if rope is not None:
+        _require(rope.dtype == torch.float32 and rope.dim() == 2 and rope.shape[1] == D and rope.is_contiguous(),
+                 "rope: contiguous fp32 [rows, D]")
+        rope_rows = rope.shape[0]
+    _require(tok_start is None or _is(tok_start, torch.int32, (cache.S + 1,)), "tok_start: int32 [S + 1]")
+    _require(positions is None or _is(positions, torch.int32, (T,)), "positions: int32 [T]")
+    _check(lib().pced_kv_append(cache.ref, _ptr(q), q_stride, k.data_ptr(), _row_stride(k), v.data_ptr(),
+                                _row_stride(v), _ptr(q_out), Hq, _ptr(tok_start), T, _ptr(rope), rope_rows,
+                                _ptr(positions), _ptr(status), _stream(stream)), "pced_kv_append")
+    return q_out
+
+
+def block_summaries(cache: PagedCache, status=None, stream=None):
+    """pced_block_summaries: cache.summary from the cached keys of all live blocks; returns it."""
+    _check(lib().pced_block_summaries(cache.ref, _ptr(status), _stream(stream)), "pced_block_summaries")
+    return cache.summary
+
+
+def block_select(cache: PagedCache, q, n_sel: int, n_first: int = 1, n_last: int = 1, sel=None, status=None,
+                 stream=None):
+    """pced_block_select: int32 [S, Hkv, n_sel], the blocks that q bf16 [S, Hq, D] attends to in ascending order
+    (-1 after the last): the first n_first, the last n_last and those with the highest scores."""
+    _require(_tokens(q, 0, cache.D) and q.shape[0] == cache.S, "q: bf16 [S, Hq, D], a token's heads side by side")
+    if sel is None:
+        sel = _empty((cache.S, cache.Hkv, n_sel), torch.int32, q.device, stream)
+    _require(_is(sel, torch.int32, (cache.S, cache.Hkv, n_sel)), "sel: contiguous int32 [S, Hkv, n_sel]")
+    _check(lib().pced_block_select(cache.ref, q.data_ptr(), _row_stride(q), q.shape[1], n_sel, n_first, n_last,
+                                   sel.data_ptr(), _ptr(status), _stream(stream)), "pced_block_select")
+    return sel
+
+
+OUT_F32, OUT_BF16 = 0, 1
+
+
+def paged_attention_workspace_size(S, Hq, Hkv, D) -> int:
+    return int(lib().pced_paged_attention_workspace_size(S, Hq, Hkv, D))
+
+
+def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=None, out=None, lse=None, ws=None,
+                    stream=None):
+    """pced_paged_attention: q bf16 [S, Hq, D] over the cache, or over the blocks sel int32 [S, Hkv, n_sel]; returns
+    out [S, Hq, D], fp32 unless a bf16 `out` is passed.  lse: fp32 [S, Hq] that receives the log of the softmax's sum.
+    total_rows: upper bound of the rows attended to (of one kv-head, over all sequences), 0: unknown.  A workspace of
+    the caller's own is zeroed before its first use (workspace())."""
+    S, D = cache.S, cache.D
+    _require(_tokens(q, 0, D) and q.shape[0] == S, "q: bf16 [S, Hq, D], a token's heads side by side")
+    Hq = q.shape[1]
+    n_sel = 0
+    if sel is not None:
+        _require(sel.dtype == torch.int32 and sel.dim() == 3 and sel.shape[:2] == (S, cache.Hkv)
+                 and sel.is_contiguous(), "sel: contiguous int32 [S, Hkv, n_sel]")
+        n_sel = sel.shape[2]
+    if out is None:
+        out = _empty((S, Hq, D), torch.float32, q.device, stream)
+    _require(out.dtype in (torch.float32, torch.bfloat16) and out.shape == (S, Hq, D) and out.is_contiguous(),
+             "out: contiguous fp32 or bf16 [S, Hq, D]")
+    _require(lse is None or _is(lse, torch.float32, (S, Hq)), "lse: contiguous fp32 [S, Hq]")
+    if ws is None:
+        ws = _empty(max(256, paged_attention_workspace_size(S, Hq, cache.Hkv, D)), torch.uint8, q.device, stream)
+        with torch.cuda.stream(stream):  # (None: the current one)
+            ws.zero_()
+    _check(lib().pced_paged_attention(cache.ref, q.data_ptr(), _row_stride(q), Hq, _ptr(sel), n_sel, total_rows,
+                                      1.0 / math.sqrt(D) if scale is None else scale, out.data_ptr(),
+                                      OUT_F32 if out.dtype == torch.float32 else OUT_BF16, _ptr(lse), ws.data_ptr(),
+                                      ws.numel(), _stream(stream)), "pced_paged_attention")
+    return out
+
+
+def logits_process(logits, rows_per_query: int, history=None, history_len=None, penalties=None, bias_ids=None,
+                   bias=None, mask=None, mask_row=None, out=None, status=None, stream=None):
+    """pced_logits_process: fp32 [B * rows_per_query, V] (rows may be strided) with the penalties of repeated tokens
+    (history int32 [B, n], history_len int32 [B], penalties fp32 [B, 3]: repetition, frequency, presence), biases
+    (bias_ids int32 and bias fp32 [B, n]) and masks (int32 words [n_masks, ceil(V / 32)], bit set: allowed; mask_row
+    int32 [B], -1: none) applied.  out: another buffer of that shape and stride, or logits itself (in place);
+    returned."""
+    _require(logits.dtype == torch.float32 and logits.dim() == 2 and logits.stride(1) == 1, "logits: fp32 [rows, V]")
+    rows, V = logits.shape
+    stride = logits.stride(0) if rows > 1 else V
+    _require(rows_per_query >= 1 and rows % rows_per_query == 0, "rows: a multiple of rows_per_query")
+    B = rows // rows_per_query
+    if out is None:
+        out = _empty((rows, stride), torch.float32, logits.device, stream)[:, :V]
+    _require(out.dtype == torch.float32 and out.shape == logits.shape and out.stride(1) == 1
+             and (rows == 1 or out.stride(0) == stride), "out: fp32 of the shape and stride of logits")
+    n_hist = n_bias = n_masks = words = 0
+    if history is not None:
+        n_hist = history.shape[-1]
+        _require(_is(history, torch.int32, (B, n_hist)), "history: contiguous int32 [B, n]")
+        _require(history_len is not None and _is(history_len, torch.int32, (B,)), "history_len: int32 [B]")
+        _require(penalties is not None and _is(penalties, torch.float32, (B, 3)), "penalties: fp32 [B, 3]")
+        if n_hist == 0:
+            history = history_len = penalties = None
+    else:
+        _require(history_len is None and penalties is None, "history_len and penalties need a history")
+    if bias_ids is not None:
+        n_bias = bias_ids.shape[-1]
+        _require(_is(bias_ids, torch.int32, (B, n_bias)), "bias_ids: contiguous int32 [B, n]")
+        _require(bias is not None and _is(bias, torch.float32, (B, n_bias)), "bias: contiguous fp32 [B, n]")
+    else:
+        _require(bias is None, "bias needs bias_ids")
+    if mask is not None:
+        _require(mask.dim() == 2 and mask.dtype == torch.int32 and mask.is_contiguous(),
+                 "mask: contiguous int32 [n_masks, words]")
+        n_masks, words = mask.shape
+        _require(mask_row is None or _is(mask_row, torch.int32, (B,)), "mask_row: int32 [B]")
+    else:
+        _require(mask_row is None, "mask_row needs a mask")
+    _check(lib().pced_logits_process(logits.data_ptr(), out.data_ptr(), stride, B, rows_per_query, V, _ptr(history),
+                                     n_hist, _ptr(history_len), _ptr(penalties), _ptr(bias_ids), _ptr(bias), n_bias,
+                                     _ptr(mask), n_masks, words, _ptr(mask_row), _ptr(status), _stream(stream)),
+           "pced_logits_process")
+    return out
 
 
 def dims(B, N, L, Hq, Hkv, D, V) -> Dims:

@@ -1,0 +1,157 @@
+// logits.cu -- penalties for repeated tokens, biases and grammar masks on logits
+// (pced_logits_process).
+//
+//   x <- (x > 0 ? x / t : x t) - (c f + p)   where the token is in the history c > 0 times
+//   x <- x + bias;   x <- -inf where the mask's bit is clear
+//
+// A CTA takes LOG_CHUNK tokens of some of a query's rows.  It counts the
+// history's tokens of its chunk in shared memory (whole numbers: the order does
+// not matter) and marks the biased ones, then streams the rows: each thread
+// holds its tokens' counts, biases and mask bits in registers for all of them.
+#include <math.h>
+
+#include "common.cuh"
+
+namespace pced {
+
+constexpr int LOG_THREADS = 256;
+constexpr int LOG_TOK = 8;  // tokens of a thread
+constexpr int LOG_CHUNK = LOG_THREADS * LOG_TOK;
+
+struct LogitsArgs {
+  const float* x;
+  float* y;
+  int64_t stride;
+  int32_t R, V, rows;  // rows: of a CTA
+  const int32_t* history;
+  int32_t history_stride;
+  const int32_t* history_len;
+  const float* penalties;
+  const int32_t* bias_ids;
+  const float* bias;
+  int32_t n_bias;
+  const uint32_t* mask;
+  int32_t n_masks, mask_words;
+  const int32_t* mask_row;
+  int* status;
+};
+
+// VEC: a thread's tokens are two runs of four, moved as 16 bytes
+template <bool VEC>
+__global__ void __launch_bounds__(LOG_THREADS) logits_process_kernel(LogitsArgs a) {
+  __shared__ int32_t count[LOG_CHUNK];
+  __shared__ int32_t named[LOG_CHUNK];  // 1 + the last bias entry of the token
+  const int tid = threadIdx.x, b = blockIdx.z;
+  const int v0 = blockIdx.x * LOG_CHUNK;
+  const int r0 = blockIdx.y * a.rows, r1 = min(a.R, r0 + a.rows);
+  const bool reports = blockIdx.x == 0 && blockIdx.y == 0;
+  pdl_wait();
+  const bool penalise = a.history && a.penalties;
+  float rep = 1.f, freq = 0.f, pres = 0.f;
+  for (int i = tid; i < LOG_CHUNK; i += LOG_THREADS) count[i] = named[i] = 0;
+  __syncthreads();
+  if (penalise) {
+    rep = a.penalties[3 * b], freq = a.penalties[3 * b + 1], pres = a.penalties[3 * b + 2];
+    int n = a.history_len[b];
+    if (n < 0 || n > a.history_stride) {
+      if (reports && tid == 0) dev_flag(a.status, PCED_DEV_BAD_LENGTH);
+      n = n < 0 ? 0 : a.history_stride;
+    }
+    const int32_t* hist = a.history + (int64_t)b * a.history_stride;
+    for (int i = tid; i < n; i += LOG_THREADS) {
+      const int t = hist[i];
+      if ((unsigned)(t - v0) < (unsigned)LOG_CHUNK && t < a.V) atomicAdd(&count[t - v0], 1);
+      if (reports && (t < -1 || t >= a.V)) dev_flag(a.status, PCED_DEV_BAD_TOKEN);
+    }
+  }
+  for (int i = tid; i < a.n_bias; i += LOG_THREADS) {
+    const int t = a.bias_ids[(int64_t)b * a.n_bias + i];
+    if ((unsigned)(t - v0) < (unsigned)LOG_CHUNK && t < a.V) atomicMax(&named[t - v0], i + 1);
+    if (reports && (t < -1 || t >= a.V)) dev_flag(a.status, PCED_DEV_BAD_TOKEN);
+  }
+  const uint32_t* mask = nullptr;
+  if (a.mask) {
+    const int m = a.mask_row ? a.mask_row[b] : b;
+    if (m >= 0 && m < a.n_masks) mask = a.mask + (int64_t)m * a.mask_words;
+    else if (m != -1 && reports && tid == 0) dev_flag(a.status, PCED_DEV_BAD_INDEX);
+  }
+  __syncthreads();
+  // this thread's tokens
+  float cnt[LOG_TOK], add[LOG_TOK];
+  bool allowed[LOG_TOK];
+#pragma unroll
+  for (int e = 0; e < LOG_TOK; ++e) {
+    const int i = VEC ? (e / 4 * LOG_THREADS + tid) * 4 + e % 4 : e * LOG_THREADS + tid;
+    const int v = v0 + i;
+    cnt[e] = (float)count[i];
+    const int w = named[i];
+    add[e] = w ? a.bias[(int64_t)b * a.n_bias + w - 1] : 0.f;
+    allowed[e] = !mask || (v < a.V && (mask[v >> 5] >> (v & 31) & 1u));
+  }
+  for (int r = r0; r < r1; ++r) {
+    const int64_t row = ((int64_t)b * a.R + r) * a.stride + v0;
+    float x[LOG_TOK];
+#pragma unroll
+    for (int e = 0; e < LOG_TOK; e += VEC ? 4 : 1) {
+      const int i = VEC ? (e / 4 * LOG_THREADS + tid) * 4 : e * LOG_THREADS + tid;
+      if (v0 + i >= a.V) continue;
+      if (VEC) *reinterpret_cast<float4*>(x + e) = *reinterpret_cast<const float4*>(a.x + row + i);
+      else x[e] = a.x[row + i];
+    }
+#pragma unroll
+    for (int e = 0; e < LOG_TOK; ++e) {
+      if (cnt[e] > 0.f)
+        x[e] = __fsub_rn(x[e] > 0.f ? __fdiv_rn(x[e], rep) : __fmul_rn(x[e], rep),
+                         __fadd_rn(__fmul_rn(cnt[e], freq), pres));
+      if (add[e] != 0.f) x[e] += add[e];
+      if (!allowed[e]) x[e] = -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < LOG_TOK; e += VEC ? 4 : 1) {
+      const int i = VEC ? (e / 4 * LOG_THREADS + tid) * 4 : e * LOG_THREADS + tid;
+      if (v0 + i >= a.V) continue;
+      if (VEC) *reinterpret_cast<float4*>(a.y + row + i) = *reinterpret_cast<const float4*>(x + e);
+      else a.y[row + i] = x[e];
+    }
+  }
+}
+
+}  // namespace pced
+
+using namespace pced;
+using namespace pced_host;
+
+extern "C" pced_status pced_logits_process(const float* x, float* y, int64_t stride, int32_t B, int32_t R, int32_t V,
+                                           const int32_t* history, int32_t history_stride,
+                                           const int32_t* history_len, const float* penalties,
+                                           const int32_t* bias_ids, const float* bias, int32_t n_bias,
+                                           const uint32_t* mask, int32_t n_masks, int32_t mask_words,
+                                           const int32_t* mask_row, int32_t* status, void* stream) {
+  const char* fn = "pced_logits_process";
+  if (!x || !y) return fail(PCED_ERR_INVALID_ARG, "%s: null pointer", fn);
+  if (B < 1 || R < 1 || V < 1 || B > 65535 || stride < V) return fail(PCED_ERR_INVALID_ARG, "%s: bad sizes", fn);
+  if (!history != !penalties || !history != !history_len || (history && history_stride < 1))
+    return fail(PCED_ERR_INVALID_ARG, "%s: history, history_len and penalties go together", fn);
+  if (n_bias < 0 || !bias_ids != !bias || (n_bias > 0) != (bias_ids != nullptr))
+    return fail(PCED_ERR_INVALID_ARG, "%s: bias_ids, bias and n_bias go together", fn);
+  if (mask ? n_masks < 1 || mask_words < (V - 1) / 32 + 1 || (!mask_row && n_masks < B) : mask_row != nullptr)
+    return fail(PCED_ERR_INVALID_ARG, "%s: masks too few or too short", fn);
+  const void* words[] = {x, y, history, history_len, penalties, bias_ids, bias, mask, mask_row, status};
+  for (const void* p : words)
+    if (((uintptr_t)p) & 3u) return fail(PCED_ERR_INVALID_ARG, "%s: misaligned pointer", fn);
+  if (num_sms() <= 0) return fail(PCED_ERR_NO_DEVICE, "%s: no CUDA device", fn);
+  LogitsArgs a;
+  a.x = x, a.y = y, a.stride = stride;
+  a.R = R, a.V = V;
+  a.history = history, a.history_stride = history_stride, a.history_len = history_len;
+  a.penalties = penalties;
+  a.bias_ids = bias_ids, a.bias = bias, a.n_bias = n_bias;
+  a.mask = mask, a.n_masks = n_masks, a.mask_words = mask_words, a.mask_row = mask_row;
+  a.status = status;
+  a.rows = R;
+  const bool vec = V % 4 == 0 && stride % 4 == 0 && (((uintptr_t)x | (uintptr_t)y) & 15u) == 0;
+  const dim3 grid((V - 1) / LOG_CHUNK + 1, 1, B);
+  const cudaError_t e = vec ? launch_pdl(logits_process_kernel<true>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a)
+                            : launch_pdl(logits_process_kernel<false>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a);
+  return e == cudaSuccess ? PCED_OK : cuda_status(e, "logits_process launch");
+}
