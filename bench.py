@@ -165,6 +165,7 @@ def source_hash(files) -> str:
 
 KERNEL_SOURCES = {
     "attention": ["paper_2601_08670_gb300/csrc/attention.cu", "paper_2601_08670_gb300/csrc/attention.cuh",
+                  "paper_2601_08670_gb300/csrc/attention_tile.cuh",
                    "paper_2601_08670_gb300/csrc/common.cuh"],
     "lm_head": ["paper_2601_08670_gb300/csrc/lm_head.cu", "paper_2601_08670_gb300/csrc/lm_head.cuh",
                 "paper_2601_08670_gb300/csrc/lm_epilogue.cuh", "paper_2601_08670_gb300/csrc/common.cuh",

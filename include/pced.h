@@ -431,7 +431,8 @@ const char* pced_step_launch_kind(const pced_step_args* args, int32_t i);
  *                the fp32 quotient 1 / key_step[h]
  *   key_step     fp32 [Hkv]: about the largest |key| of a head / 127
  * block_rows: a multiple of 16; D 64 or 128; S <= 1024; 16-byte aligned
- * k, v, summary; num_blocks*Hkv*block_rows < 2^31.  A length outside
+ * k, v, summary; num_blocks*Hkv*block_rows and (max_blocks+1)*block_rows
+ * below 2^31.  A length outside
  * [0, max_blocks*block_rows] sets PCED_DEV_BAD_LENGTH and is clipped into it;
  * a table entry outside [0, num_blocks) that a call needs sets
  * PCED_DEV_BAD_BLOCK, and its rows are neither written nor read.
@@ -513,8 +514,9 @@ pced_status pced_block_select(const pced_paged_cache* cache, const void* q, int6
  * token over its own cache: o = softmax(scale q K^T) V.
  *   q, q_stride  as in pced_block_select
  *   sel, n_sel   int32 [S][Hkv][n_sel] (device): the blocks to attend to, in any
- *                order, each at most once; -1: none.  A number that is not of
- *                a live block sets PCED_DEV_BAD_BLOCK and is left out.  NULL: all
+ *                order, each at most once; -1 after the last.  A number that is
+ *                not of a live block sets PCED_DEV_BAD_BLOCK and is left out.
+ *                NULL: all
  *   total_rows   host upper bound of the rows attended to, summed over the
  *                sequences (of one kv-head); sizes the grid only.  0: unknown
  *   out          [S][Hq][D], fp32 (PCED_OUT_F32) or bf16 (PCED_OUT_BF16)

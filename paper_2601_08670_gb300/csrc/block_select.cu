@@ -171,7 +171,8 @@ extern "C" pced_status pced_block_select(const pced_paged_cache* cache, const vo
   a.status = status;
   const auto kernel = c.D == 128 ? block_select_kernel<128> : block_select_kernel<64>;
   const size_t smem = (size_t)c.max_blocks * 4;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BSEL_MAX_BLOCKS * 4);
+  static bool done[2][64];
+  cudaError_t e = allow_smem(kernel, BSEL_MAX_BLOCKS * 4, done[c.D == 128]);
   if (e != cudaSuccess) return cuda_status(e, "block_select shared memory");
   e = launch_pdl(kernel, dim3(c.Hkv, c.S), BSEL_THREADS, smem, (cudaStream_t)stream, a);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "block_select launch");

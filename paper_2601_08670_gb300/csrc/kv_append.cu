@@ -272,6 +272,8 @@ pced_status check_paged_cache(const pced_paged_cache* c, const char* fn) {
     return fail(PCED_ERR_INVALID_ARG, "%s: misaligned cache pointer", fn);
   if (c->D != 64 && c->D != 128) return fail(PCED_ERR_UNSUPPORTED, "%s: head dim %d", fn, c->D);
   if (c->S > PAGED_MAX_S) return fail(PCED_ERR_UNSUPPORTED, "%s: %d sequences, at most %d", fn, c->S, PAGED_MAX_S);
+  if ((int64_t)c->max_blocks * c->block_rows + c->block_rows > INT32_MAX)
+    return fail(PCED_ERR_UNSUPPORTED, "%s: a sequence's table holds 2^31 rows or more", fn);
   // (Hkv is the y extent of a grid)
   if (c->Hkv > 65535 || (int64_t)c->num_blocks * c->Hkv >= (INT64_C(1) << 31) ||
       (int64_t)c->num_blocks * c->Hkv * c->block_rows >= (INT64_C(1) << 31))

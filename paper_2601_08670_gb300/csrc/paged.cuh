@@ -8,14 +8,10 @@ namespace pced {
 constexpr int PAGED_MAX_S = 1024;  // sequences of a call (their lengths and prefixes lie in shared memory)
 constexpr int PAGED_MAX_G = 8;     // query heads per kv-head
 
-// rows that a sequence's part of the table can hold
-__host__ __device__ __forceinline__ int64_t paged_rows(const pced_paged_cache& c) {
-  return (int64_t)c.max_blocks * c.block_rows;
-}
 // live rows of sequence s, clipped into what its table can hold
 __device__ __forceinline__ int paged_len(const pced_paged_cache& c, int s, int* status) {
   const int n = c.seq_len[s];
-  const int cap = (int)min(paged_rows(c), (int64_t)INT32_MAX);
+  const int cap = c.max_blocks * c.block_rows;
   if (n >= 0 && n <= cap) return n;
   dev_flag(status, PCED_DEV_BAD_LENGTH);
   return n < 0 ? 0 : cap;
@@ -58,5 +54,20 @@ namespace pced_host {
 pced_status check_paged_cache(const pced_paged_cache* c, const char* fn);
 // ... and of a call's query heads over it
 pced_status check_paged_heads(const pced_paged_cache* c, int32_t Hq, const char* fn);
+// host.cu: make_tmap_kv with `blocks` of the D / 64 column blocks in a copy
+pced_status make_tmap_kv_part(CUtensorMap* map, const void* base, uint64_t rows, uint32_t D, uint32_t box_rows,
+                              uint32_t blocks);
+// more than 48 KB of dynamic shared memory for a kernel: asked for once per device
+template <typename K>
+inline cudaError_t allow_smem(K kernel, size_t bytes, bool (&done)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (done[dev]) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  done[dev] = e == cudaSuccess;
+  return e;
+}
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 }  // namespace pced_host

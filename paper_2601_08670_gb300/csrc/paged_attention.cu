@@ -1,16 +1,28 @@
 // paged_attention.cu -- one layer of decode attention over a paged cache, over
 // all blocks or the selected ones (pced_paged_attention).
 //
-// One CTA per (sequence, kv-head): its warps take the rows in turn, each with a
-// running maximum and sum per query head, and meet in shared memory at the end.
-#include <math.h>
-
+//   o = sum_r exp2(x_r - m) v_r / sum_r exp2(x_r - m),  x_r = scale log2(e) q.k_r
+//
+// Split over the rows: every (sequence, kv-head) is a segment of 64-row tiles,
+// the tiles of all segments are cut into equal contiguous ranges, one per CTA,
+// and the parts of a segment that several CTAs hold meet through records in
+// the workspace, merged by the CTA that comes last (in the order of the CTAs,
+// so that the result does not depend on who that is).  A producer warp brings
+// the tiles with TMA: 32 tiles at a time, each lane finds one tile's segment,
+// its place in the selection and its pool block, so the dependent loads of the
+// lookups are paid once per 32 tiles.  Where a tile is not 64 live rows of one
+// block (a block of another size, a sequence's end) it is put together from
+// 16-row boxes, the rows that one consumer warp takes, and rows past the live
+// ones are neither brought nor used.  The math on a tile is that of the slab
+// kernels (attention_tile.cuh).
+#include "attention_tile.cuh"
 #include "paged.cuh"
 
 namespace pced {
 
-constexpr int PATT_THREADS = 256;
-constexpr int PATT_WARPS = PATT_THREADS / 32;
+constexpr int PATT_MAX_CTAS = 256;  // sizes the records and counters of the workspace
+constexpr int PATT_GRAN = 16;       // rows of a consumer warp, and of a small box
+constexpr int PATT_MIN_TILES = 4;   // tiles of a CTA where there are few
 
 struct PagedAttArgs {
   pced_paged_cache c;
@@ -23,85 +35,366 @@ struct PagedAttArgs {
   void* out;
   int32_t out_bf16;
   float* lse;
+  float* rec_o;     // [2 * CTAs][G][D] unnormalised partial outputs
+  float2* rec_ml;   // [2 * CTAs][G] (running max in log2 units, sum of exp2)
+  int32_t* parts;   // [CTAs] records written of the segment that begins in a CTA and goes on past it (0 between calls)
   int* status;
 };
 
+// The tiles [t0, t1) of segment (s, h) that a CTA holds; nt tiles in all.
+struct PagedPiece {
+  int32_t s, h;
+  int64_t t0, t1, nt;
+};
+
+// Positions: sequence s begins at Hkv * pre[s]; its heads follow one another, nt tiles each.
+__device__ __forceinline__ PagedPiece paged_piece(const int64_t* pre, int32_t S, int32_t Hkv, int64_t p, int64_t end) {
+  int32_t lo = 0, hi = S - 1;
+  while (lo < hi) {  // the last sequence that begins at or before p (sequences without tiles begin where the next does)
+    const int32_t mid = (lo + hi + 1) >> 1;
+    if (pre[mid] * Hkv <= p) lo = mid;
+    else hi = mid - 1;
+  }
+  PagedPiece pc;
+  pc.s = lo;
+  pc.nt = pre[lo + 1] - pre[lo];
+  const int64_t off = p - pre[lo] * Hkv;
+  pc.h = (int32_t)((((uint64_t)off | (uint64_t)pc.nt) >> 32) ? off / pc.nt : (uint32_t)off / (uint32_t)pc.nt);
+  pc.t0 = off - pc.h * pc.nt;
+  pc.t1 = min(pc.nt, pc.t0 + (end - p));
+  return pc;
+}
+
 template <int D>
-__global__ void __launch_bounds__(PATT_THREADS) paged_attention_kernel(PagedAttArgs a) {
-  constexpr int E = D / 32;  // channels of a lane
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int h = blockIdx.x, s = blockIdx.y, G = a.G, P = a.c.block_rows;
-  __shared__ float ms[PATT_WARPS][PAGED_MAX_G], ls[PATT_WARPS][PAGED_MAX_G];
-  __shared__ float os[PATT_WARPS][PAGED_MAX_G][D];
+struct PagedCfg : AttCfg<D> {
+  using B = AttCfg<D>;
+  static constexpr size_t BARS = (2 * B::STAGES + 2) * 8;
+  static constexpr size_t DESC = (size_t)B::STAGES * 4;
+  static constexpr size_t SMEM = 1024 + (size_t)B::STAGES * B::STAGE_BYTES + BARS + (size_t)B::PARTIALS * 4 +
+                                 (PAGED_MAX_S + 1) * 8 + PAGED_MAX_S * 4 + DESC + 64;
+};
+
+// Writes four outputs of a finished segment (all 256 consumer threads; the
+// first G*D/4 hold outputs), normalised.
+__device__ __forceinline__ void write_out(const PagedAttArgs& a, int s, int h, int D, int hh, int idx0, float mx,
+                                          float lsum, const float (&acc)[4]) {
+  const float w = mx == -INFINITY ? 0.f : 1.f / lsum;
+  float y[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = mx == -INFINITY ? 0.f : acc[j] * w;
+  const int64_t at = ((int64_t)s * a.Hq + (int64_t)h * a.G) * D + idx0;
+  if (a.out_bf16)
+    *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + at) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+  else
+    *reinterpret_cast<float4*>((float*)a.out + at) = make_float4(y[0], y[1], y[2], y[3]);
+  if (a.lse && idx0 % D == 0)
+    a.lse[(int64_t)s * a.Hq + h * a.G + hh] = mx == -INFINITY ? -INFINITY : (mx + log2f(lsum)) * 0.6931471805599453f;
+}
+
+// The records of the segment that begins in CTA c, n of them, merged: slots
+// 2c + 1, 2(c + 1), 2(c + 2), ...
+__device__ __forceinline__ void merge_records(const PagedAttArgs& a, int c, int n, int D, int hh, int idx0, float& mx,
+                                              float& lsum, float (&acc)[4]) {
+  constexpr int BATCH = 4;  // records in flight
+  const int GD = a.G * D;
+  for (int i0 = 0; i0 < n; i0 += BATCH) {
+    float2 ml[BATCH];
+    float4 o[BATCH];
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) {
+      const int i = i0 + q;
+      ml[q] = make_float2(-INFINITY, 0.f);
+      o[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i >= n) continue;
+      const int64_t slot = i == 0 ? 2 * (int64_t)c + 1 : 2 * ((int64_t)c + i);
+      ml[q] = __ldcg(a.rec_ml + slot * a.G + hh);
+      o[q] = __ldcg(reinterpret_cast<const float4*>(a.rec_o + slot * GD + idx0));
+    }
+    float M = mx;
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) M = fmaxf(M, ml[q].x);
+    const float f = mx == -INFINITY ? 0.f : exp2f(mx - M);
+    lsum *= f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] *= f;
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) {
+      const float e = ml[q].x == -INFINITY ? 0.f : exp2f(ml[q].x - M);
+      acc[0] += o[q].x * e;
+      acc[1] += o[q].y * e;
+      acc[2] += o[q].z * e;
+      acc[3] += o[q].w * e;
+      lsum += ml[q].y * e;
+    }
+    mx = M;
+  }
+}
+
+// SMALL: block_rows is no multiple of 64, so every tile comes in 16-row boxes,
+// each of its own block.
+template <int D, bool PK, bool SMALL>
+__global__ void __launch_bounds__(ATT_THREADS, 1)
+    paged_attention_kernel(const __grid_constant__ CUtensorMap ktile, const __grid_constant__ CUtensorMap vtile,
+                           const __grid_constant__ CUtensorMap kbox, const __grid_constant__ CUtensorMap vbox,
+                           PagedAttArgs a) {
+  using C = PagedCfg<D>;
+  constexpr int NG = ATT_BLOCK_N / PATT_GRAN;  // small boxes of a tile
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* gbase = smem_raw + (base - raw);
+  // layout: stages | full[STAGES] | empty[STAGES] | partials full | partials empty | partials | tables
+  const uint32_t bar_full = base + C::STAGES * C::STAGE_BYTES;
+  const uint32_t bar_empty = bar_full + C::STAGES * 8;
+  const uint32_t bar_pfull = bar_empty + C::STAGES * 8, bar_pempty = bar_pfull + 8;
+  float* ms = reinterpret_cast<float*>(gbase + C::STAGES * C::STAGE_BYTES + C::BARS);
+  float* ls = ms + ATT_CONSUMERS * ATT_MAX_G;
+  float* os = ls + ATT_CONSUMERS * ATT_MAX_G;
+  int64_t* pre = reinterpret_cast<int64_t*>(ms + C::PARTIALS);  // [S + 1] tiles of one head before sequence s
+  int32_t* lens = reinterpret_cast<int32_t*>(pre + PAGED_MAX_S + 1);
+  uint32_t* desc = reinterpret_cast<uint32_t*>(lens + PAGED_MAX_S);  // [STAGES] live rows of a tile's 16-row parts, a byte each
+  int32_t* last_here = reinterpret_cast<int32_t*>(desc + C::STAGES);
+
+  const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
+  const int32_t S = a.c.S, Hkv = a.c.Hkv, G = a.G, GD = G * D, P = a.c.block_rows;
+
+  if (tid == 0) {
+    for (int i = 0; i < C::STAGES; ++i) {
+      mbar_init(bar_full + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 4);  // the four warps of the consuming warpgroup
+    }
+    mbar_init(bar_pfull, ATT_CONSUMERS);
+    mbar_init(bar_pempty, ATT_CONSUMERS);
+    mbar_fence_init();
+  }
+  if (warp == ATT_CONSUMERS && lane == 0) {
+    tma_prefetch_desc(&ktile);
+    tma_prefetch_desc(&vtile);
+    tma_prefetch_desc(&kbox);
+    tma_prefetch_desc(&vbox);
+  }
   pdl_wait();
-  const int n = paged_len(a.c, s, a.status);
-  const int nb = (n + P - 1) / P;
-  float q[PAGED_MAX_G][E], o[PAGED_MAX_G][E], m[PAGED_MAX_G], l[PAGED_MAX_G];
+  for (int i = tid; i < S; i += ATT_THREADS) lens[i] = paged_len(a.c, i, a.status);
+  __syncthreads();
+  if (warp == 0) {  // prefix of the tiles
+    const int chunk = (S + 31) / 32, b0 = min(S, lane * chunk), b1 = min(S, b0 + chunk);
+    auto tiles = [&](int i) -> int64_t {
+      int64_t rows = lens[i];
+      if (a.sel) rows = min((int64_t)a.n_sel, (rows + P - 1) / P) * P;
+      return (rows + ATT_BLOCK_N - 1) / ATT_BLOCK_N;
+    };
+    int64_t own = 0;
+    for (int i = b0; i < b1; ++i) own += tiles(i);
+    int64_t incl = own;
 #pragma unroll
-  for (int g = 0; g < PAGED_MAX_G; ++g) {
-    m[g] = -INFINITY, l[g] = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      o[g][e] = 0.f;
-      q[g][e] = g < G ? __bfloat162float(a.q[s * a.q_stride + (int64_t)(h * G + g) * D + lane + 32 * e]) : 0.f;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
     }
-  }
-  const int blocks = a.sel ? a.n_sel : nb;
-  for (int i = 0; i < blocks; ++i) {
-    const int j = a.sel ? a.sel[((int64_t)s * a.c.Hkv + h) * a.n_sel + i] : i;
-    if (j == -1) continue;
-    if (j < 0 || j >= nb) {
-      dev_flag(a.status, PCED_DEV_BAD_BLOCK);
-      continue;
+    int64_t run = incl - own;
+    for (int i = b0; i < b1; ++i) {
+      pre[i] = run;
+      run += tiles(i);
     }
-    const int blk = paged_block(a.c, s, j, a.status);
-    if (blk < 0) continue;
-    const int64_t base = ((int64_t)blk * a.c.Hkv + h) * P * D;
-    const int live = min(P, n - j * P);
-    for (int r = warp; r < live; r += PATT_WARPS) {
-      const __nv_bfloat16* k = (const __nv_bfloat16*)a.c.k + base + (int64_t)r * D + lane;
-      const __nv_bfloat16* v = (const __nv_bfloat16*)a.c.v + base + (int64_t)r * D + lane;
-      float kf[E], vf[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) kf[e] = __bfloat162float(k[32 * e]), vf[e] = __bfloat162float(v[32 * e]);
-#pragma unroll
-      for (int g = 0; g < PAGED_MAX_G; ++g) {
-        if (g >= G) break;
-        float x = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x += q[g][e] * kf[e];
-        x = warp_sum(x) * a.scale_log2;
-        const float mn = fmaxf(m[g], x), f = m[g] == -INFINITY ? 0.f : exp2f(m[g] - mn);
-        const float p = mn == -INFINITY ? 0.f : exp2f(x - mn);
-        l[g] = l[g] * f + p;
-        m[g] = mn;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[g][e] = o[g][e] * f + p * vf[e];
-      }
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < PAGED_MAX_G; ++g) {
-    if (lane == 0) ms[warp][g] = m[g], ls[warp][g] = l[g];
-#pragma unroll
-    for (int e = 0; e < E; ++e) os[warp][g][lane + 32 * e] = o[g][e];
+    if (lane == 31) pre[S] = incl;
   }
   __syncthreads();
-  for (int i = tid; i < G * D; i += PATT_THREADS) {
-    const int g = i / D, d = i % D;
-    float mx = -INFINITY, sum = 0.f, acc = 0.f;
-    for (int w = 0; w < PATT_WARPS; ++w) mx = fmaxf(mx, ms[w][g]);
-    for (int w = 0; w < PATT_WARPS; ++w) {
-      const float f = ms[w][g] == -INFINITY ? 0.f : exp2f(ms[w][g] - mx);
-      sum += ls[w][g] * f;
-      acc += os[w][g][d] * f;
+  const int64_t total = pre[S] * Hkv;
+  const int64_t per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)PATT_MIN_TILES);
+  const int64_t r_begin = min(total, (int64_t)blockIdx.x * per);
+  const int64_t r_end = min(total, r_begin + per);
+
+  if (warp == ATT_CONSUMERS) {
+    // ------------------------------------------------------------ producer
+    const uint64_t pol = policy_evict_first();
+    uint32_t st = 0, ph = 0;
+    int64_t it = 0;
+    bool ok = true;
+    for (int64_t p0 = r_begin; p0 < r_end && ok; p0 += 32) {
+      // this lane's tile: pool row of each of its parts, live rows of the parts
+      int32_t row[SMALL ? NG : 1];
+      uint32_t live4 = 0;
+      row[0] = 0;
+      if (p0 + lane < r_end) {
+        const PagedPiece pc = paged_piece(pre, S, Hkv, p0 + lane, r_end);
+        const int32_t n = lens[pc.s];
+        const int32_t nb = (n + P - 1) / P;
+        const int32_t* sel = a.sel ? a.sel + ((int64_t)pc.s * Hkv + pc.h) * a.n_sel : nullptr;
+        const int32_t places = sel ? min(a.n_sel, nb) : nb;
+#pragma unroll
+        for (int i = 0; i < (SMALL ? NG : 1); ++i) {
+          const int64_t r = pc.t0 * ATT_BLOCK_N + i * PATT_GRAN;  // row of the list
+          const int32_t place = (int32_t)(r / P), at = (int32_t)(r - (int64_t)place * P);
+          row[i] = 0;
+          if (place >= places) continue;
+          const int32_t j = sel ? sel[place] : place;
+          if (j < 0 || j >= nb) {
+            if (j != -1) dev_flag(a.status, PCED_DEV_BAD_BLOCK);
+            continue;
+          }
+          const int32_t blk = paged_block(a.c, pc.s, j, a.status);
+          if (blk < 0) continue;
+          row[i] = (int32_t)(((int64_t)blk * Hkv + pc.h) * P) + at;
+          const int64_t left = (int64_t)n - (int64_t)j * P - at;  // live rows from here on
+          if (SMALL) {
+            live4 |= (uint32_t)max((int64_t)0, min(left, (int64_t)PATT_GRAN)) << (8 * i);
+          } else {
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+              live4 |= (uint32_t)max((int64_t)0, min(left - g * PATT_GRAN, (int64_t)PATT_GRAN)) << (8 * g);
+          }
+        }
+      }
+      const int nt = (int)min((int64_t)32, r_end - p0);
+      for (int t = 0; t < nt; ++t, ++it) {
+        if (!mbar_wait_warp(bar_empty + 8 * st, ph ^ 1u, a.status)) {
+          ok = false;
+          break;
+        }
+        const uint32_t fb = bar_full + 8 * st, sk = base + st * C::STAGE_BYTES, sv = sk + C::TILE_BYTES;
+        const uint32_t lv = __shfl_sync(0xffffffffu, live4, t);
+        const int32_t r0 = __shfl_sync(0xffffffffu, row[0], t);
+        const uint32_t on = elect_one();
+        if (on) desc[st] = lv;
+        // (more than 48 live rows of one block: the whole tile at once)
+        if (!SMALL && lv >> 24) {
+          mbar_arrive_expect_tx_if(on, fb, C::STAGE_BYTES);
+          if (on) {
+            tma_load_3d(sk, &ktile, fb, 0, r0, 0, pol);
+            tma_load_3d(sv, &vtile, fb, 0, r0, 0, pol);
+          }
+        } else {
+          // parts with live rows; a lane for each box of K and V
+          const int boxes = ((lv & 0xFFu) != 0) + ((lv & 0xFF00u) != 0) + ((lv & 0xFF0000u) != 0) + (lv >> 24 != 0);
+          mbar_arrive_expect_tx_if(on, fb, boxes * (2 * D * 2 * PATT_GRAN));
+          __syncwarp();
+          const int g = lane / (2 * C::BOXES) % NG, half = lane % C::BOXES, v = lane / C::BOXES & 1;
+          int32_t rg = r0 + g * PATT_GRAN;
+          if (SMALL) {
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+              const int32_t x = __shfl_sync(0xffffffffu, row[i], t);
+              if (i == g) rg = x;
+            }
+          }
+          if (lane < 2 * C::BOXES * NG && (lv >> (8 * g) & 0xFFu))
+            tma_load_3d((v ? sv : sk) + half * C::BOX_BYTES + g * PATT_GRAN * 128, v ? &vbox : &kbox, fb, 0, rg, half,
+                        pol);
+        }
+        if (++st == C::STAGES) {
+          st = 0;
+          ph ^= 1u;
+        }
+      }
     }
-    const float y = mx == -INFINITY ? 0.f : acc / sum;
-    const int64_t at = ((int64_t)s * a.Hq + h * G + g) * D + d;
-    if (a.out_bf16) ((__nv_bfloat16*)a.out)[at] = __float2bfloat16_rn(y);
-    else ((float*)a.out)[at] = y;
-    if (a.lse && d == 0)
-      a.lse[(int64_t)s * a.Hq + h * G + g] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * 0.6931471805599453f;
+    if (!ok) {
+      // let copies already in flight land before the CTA exits
+      for (int64_t j = (it >= C::STAGES ? it - C::STAGES : 0); j < it; ++j)
+        mbar_wait(bar_full + 8 * (uint32_t)(j % C::STAGES), (uint32_t)(j / C::STAGES) & 1u, a.status);
+    }
+    return;
+  }
+
+  // -------------------------------------------------------------- consumers
+  const int wg = warp >> 2, kb = PATT_GRAN * (warp & 3);
+  const int g = lane >> 2, tq = lane & 3;
+  const bool own = tid < GD / 4;
+  const int hh = own ? tid / (D / 4) : 0, idx0 = own ? 4 * tid : 0;
+  // sequences without rows
+  for (int s = blockIdx.x; s < S; s += gridDim.x)
+    if (pre[s] == pre[s + 1] && own) {
+      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int h = 0; h < Hkv; ++h) write_out(a, s, h, D, hh, idx0, -INFINITY, 0.f, zero);
+    }
+  // B column g of S^T = K Q^T is head g; with PK columns 4-7 repeat heads 0-3
+  const int qh = PK ? (g & 3) : g;
+  const bool hv = qh < G;
+  uint32_t it = 0, st = 0, use = 0, np = 0;  // tile counter (parity), its stage and use of the stage; pieces done
+  for (int64_t p = r_begin; p < r_end; ++np) {
+    const PagedPiece pc = paged_piece(pre, S, Hkv, p, r_end);
+    p += pc.t1 - pc.t0;
+    uint32_t qf[C::KSTEPS][2];
+    {
+      const uint32_t* qrow = reinterpret_cast<const uint32_t*>(
+          a.q + pc.s * a.q_stride + ((int64_t)pc.h * G + (hv ? qh : 0)) * D);
+#pragma unroll
+      for (int j = 0; j < C::KSTEPS; ++j) {
+        qf[j][0] = hv ? qrow[8 * j + tq] : 0u;
+        qf[j][1] = hv ? qrow[8 * j + 4 + tq] : 0u;
+      }
+    }
+    WarpAcc<D> A;
+    acc_reset(A);
+    bool ok = true;
+    for (int64_t t = pc.t0; t < pc.t1; ++t, ++it, st = st + 1 == C::STAGES ? (++use, 0u) : st + 1) {
+      if ((int)(it & 1u) != wg) continue;
+      // (the release of the stage's previous use, by the other warpgroup, comes
+      // first: the parity below then means this tile's phase)
+      if ((use > 0 && !mbar_wait(bar_empty + 8 * st, (use - 1u) & 1u, a.status)) ||
+          !mbar_wait(bar_full + 8 * st, use & 1u, a.status)) {
+        ok = false;
+        break;
+      }
+      const int live = desc[st] >> (8 * (warp & 3)) & 0xFFu;
+      if (live) {
+        const uint32_t sk = base + st * C::STAGE_BYTES;
+        tile_math<D, PK>(A, qf, sk, sk + C::TILE_BYTES, kb, kb + live, a.scale_log2, lane);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_empty + 8 * st);
+    }
+    if (!ok) return;
+    // scores that are all not numbers moved no maximum: their sum shall not be dropped with it
+    if (__any_sync(0xffffffffu, (A.m0 == -INFINITY && A.l0 != A.l0) || (A.m1 == -INFINITY && A.l1 != A.l1))) {
+      A.m0 = A.m0 == -INFINITY ? 0.f : A.m0;
+      A.m1 = A.m1 == -INFINITY ? 0.f : A.m1;
+    }
+    if (PK) pack_fold<D>(A);
+    // the previous piece's partials have been read
+    if (np > 0 && !mbar_wait(bar_pempty, (np - 1u) & 1u, a.status)) return;
+    store_partial<D>(A, ms, ls, os, G, warp, lane);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_pfull);
+    if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
+    float mx = -INFINITY, lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    if (own) load_merged<D>(ms, ls, os, G, hh, idx0, mx, lsum, acc);
+    if (pc.t0 == 0 && pc.t1 == pc.nt) {
+      if (own) write_out(a, pc.s, pc.h, D, hh, idx0, mx, lsum, acc);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_pempty);
+      continue;
+    }
+    // a part of a segment: record 2c of CTA c when it began in an earlier CTA,
+    // 2c + 1 when it begins here; the CTA that writes the last one merges them
+    const int64_t seg0 = pre[pc.s] * Hkv + pc.h * pc.nt;  // the segment's first position
+    const int first = (int)(seg0 / per), n = (int)((seg0 + pc.nt - 1) / per) - first + 1;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (pc.t0 == 0 ? 1 : 0);
+    if (own) {
+      *reinterpret_cast<float4*>(a.rec_o + slot * GD + idx0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      if (idx0 % D == 0) a.rec_ml[slot * G + hh] = make_float2(mx, lsum);
+      __threadfence();
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_pempty);
+    if (!mbar_wait(bar_pempty, np & 1u, a.status)) return;  // all warps' records are written
+    if (tid == 0) *last_here = atom_acq_rel_gpu_add(a.parts + first, 1) == n - 1;
+    // (a second round of the same two barriers hands the answer over)
+    ++np;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_pfull);
+    if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
+    if (*last_here) {
+      __threadfence();
+      mx = -INFINITY, lsum = 0.f;
+      acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+      if (own) {
+        merge_records(a, first, n, D, hh, idx0, mx, lsum, acc);
+        write_out(a, pc.s, pc.h, D, hh, idx0, mx, lsum, acc);
+      }
+      if (tid == 0) a.parts[first] = 0;
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_pempty);
   }
 }
 
@@ -110,9 +403,35 @@ __global__ void __launch_bounds__(PATT_THREADS) paged_attention_kernel(PagedAttA
 using namespace pced;
 using namespace pced_host;
 
+static size_t place_records(PagedAttArgs* a, void* ws, int32_t G, int32_t D) {
+  Carver cv(ws ? (char*)ws + 256 : nullptr);
+  int32_t* parts = cv.take<int32_t>(PATT_MAX_CTAS);
+  float* rec_o = cv.take<float>((size_t)2 * PATT_MAX_CTAS * G * D);
+  float2* rec_ml = cv.take<float2>((size_t)2 * PATT_MAX_CTAS * G);
+  if (a) a->parts = parts, a->rec_o = rec_o, a->rec_ml = rec_ml;
+  return 256 + cv.used();
+}
+
 extern "C" size_t pced_paged_attention_workspace_size(int32_t S, int32_t Hq, int32_t Hkv, int32_t D) {
   if (S < 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || D < 1) return 0;
-  return 256;
+  return place_records(nullptr, nullptr, Hq / Hkv, D);
+}
+
+template <int D, bool PK, bool SMALL>
+static cudaError_t launch_paged(const CUtensorMap (&maps)[4], const PagedAttArgs& a, int ctas, cudaStream_t stream) {
+  const auto kernel = paged_attention_kernel<D, PK, SMALL>;
+  static bool done[64];
+  const cudaError_t e = allow_smem(kernel, PagedCfg<D>::SMEM, done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(ctas), ATT_THREADS, PagedCfg<D>::SMEM, stream, maps[0], maps[1], maps[2], maps[3], a);
+}
+template <int D>
+static cudaError_t launch_paged_d(const CUtensorMap (&maps)[4], const PagedAttArgs& a, int ctas, cudaStream_t stream) {
+  const bool pk = a.G <= 4, small = a.c.block_rows % ATT_BLOCK_N != 0;  // pk: hi and lo parts of P share one MMA
+  return pk ? (small ? launch_paged<D, true, true>(maps, a, ctas, stream)
+                     : launch_paged<D, true, false>(maps, a, ctas, stream))
+            : (small ? launch_paged<D, false, true>(maps, a, ctas, stream)
+                     : launch_paged<D, false, false>(maps, a, ctas, stream));
 }
 
 extern "C" pced_status pced_paged_attention(const pced_paged_cache* cache, const void* q, int64_t q_stride, int32_t Hq,
@@ -135,7 +454,15 @@ extern "C" pced_status pced_paged_attention(const pced_paged_cache* cache, const
   if (!isfinite(scale) || total_rows < 0) return fail(PCED_ERR_INVALID_ARG, "%s: scale or total_rows", fn);
   if (!aligned(workspace, 256) || workspace_bytes < pced_paged_attention_workspace_size(c.S, Hq, c.Hkv, c.D))
     return fail(PCED_ERR_WORKSPACE, "%s: workspace too small or misaligned", fn);
-  if (num_sms() <= 0) return fail(PCED_ERR_NO_DEVICE, "%s: no CUDA device", fn);
+  const int sms = num_sms();
+  if (sms <= 0) return fail(PCED_ERR_NO_DEVICE, "%s: no CUDA device", fn);
+  // the pool as rows of D elements: whole tiles, and 16 rows of 64 columns
+  const uint64_t rows = (uint64_t)c.num_blocks * c.Hkv * c.block_rows;
+  CUtensorMap maps[4];
+  const void* pools[2] = {c.k, c.v};
+  for (int i = 0; i < 4 && st == PCED_OK; ++i)
+    st = make_tmap_kv_part(&maps[i], pools[i & 1], rows, c.D, i < 2 ? ATT_BLOCK_N : PATT_GRAN, i < 2 ? c.D / 64 : 1);
+  if (st != PCED_OK) return st;
   PagedAttArgs a;
   a.c = c;
   a.q = (const __nv_bfloat16*)q;
@@ -146,9 +473,15 @@ extern "C" pced_status pced_paged_attention(const pced_paged_cache* cache, const
   a.out = out, a.out_bf16 = out_type == PCED_OUT_BF16;
   a.lse = lse;
   a.status = (int*)workspace;
-  const dim3 grid(c.Hkv, c.S);
-  const cudaError_t e =
-      c.D == 128 ? launch_pdl(paged_attention_kernel<128>, grid, PATT_THREADS, 0, (cudaStream_t)stream, a)
-                 : launch_pdl(paged_attention_kernel<64>, grid, PATT_THREADS, 0, (cudaStream_t)stream, a);
+  place_records(&a, workspace, a.G, c.D);
+  // a CTA for every SM, fewer where the caller's bound of the rows needs no more
+  int64_t ctas = sms < PATT_MAX_CTAS ? sms : PATT_MAX_CTAS;
+  if (total_rows > 0) {
+    const int64_t tiles = (total_rows / ATT_BLOCK_N + c.S) * c.Hkv;
+    const int64_t want = (tiles + PATT_MIN_TILES - 1) / PATT_MIN_TILES;
+    if (want < ctas) ctas = want;
+  }
+  const cudaError_t e = c.D == 128 ? launch_paged_d<128>(maps, a, (int)ctas, (cudaStream_t)stream)
+                                   : launch_paged_d<64>(maps, a, (int)ctas, (cudaStream_t)stream);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "paged_attention launch");
 }

@@ -56,7 +56,7 @@ def test_long_and_ragged(cuda_ok, heads, P, lens):
 @pytest.mark.parametrize("heads", [(8, 2, 64), (28, 4, 128), (32, 8, 128), (6, 1, 128)])
 @pytest.mark.parametrize("P", [16, 48, 64, 128])
 def test_selected_blocks(cuda_ok, heads, P):
-    # any order, places without a block anywhere, a head without any, more places than blocks
+    # any order, any number, a head without any, more places than blocks
     Hq, Hkv, D = heads
     rng = np.random.default_rng([Hq, P, 5])
     lens = [0, 1, P, P + 1, 5 * P - 1, 9 * P + 7, 1500]
@@ -68,8 +68,7 @@ def test_selected_blocks(cuda_ok, heads, P):
         nb = (n + P - 1) // P
         for h in range(Hkv):
             k = int(rng.integers(0, min(nb, n_sel) + 1))
-            places = rng.permutation(n_sel)[:k]
-            sel[s, h, places] = rng.permutation(nb)[:k]
+            sel[s, h, :k] = rng.permutation(nb)[:k]
     sel[5, 0] = -1
     out, lse = run(c, q, sel=sel)
     ref.check_attention(c, q, out, lse, sel=sel)
