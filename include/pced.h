@@ -429,7 +429,7 @@ const char* pced_step_launch_kind(const pced_step_args* args, int32_t i);
  *                clipped to [-127, 127] (a key that is not a number: 127 and
  *                -127); in steps: the fp32 product of the stored key and
  *                the fp32 quotient 1 / key_step[h]
- *   key_step     fp32 [Hkv]: about the largest |key| of a head / 127
+ *   key_step     fp32 [Hkv], > 0: about the largest |key| of a head / 127
  * block_rows: a multiple of 16; D 64 or 128; S <= 1024; 16-byte aligned
  * k, v, summary; num_blocks*Hkv*block_rows and (max_blocks+1)*block_rows
  * below 2^31.  A length outside

@@ -296,16 +296,15 @@ def _is(t, dtype, shape):
     return t.dtype == dtype and t.shape == shape and t.is_contiguous()
 
 
-def _tokens(t, heads, D):
-    """[T, heads, D] bf16 with a token's heads side by side."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != D or (heads and t.shape[1] != heads):
-        return False
-    st = t.stride()
-    return st[2] == 1 and (st[1] == D or t.shape[1] == 1)
-
-
-def _row_stride(t):
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+def _token_stride(t, T, heads, D, what):
+    """Elements between the tokens of t: bf16 [T, heads (0: any), D], a token's heads side by side.  (A small call's
+    time is what its checks take on the host, so they ask each tensor once.)"""
+    if t.dtype == torch.bfloat16 and t.dim() == 3:
+        n, H, d = t.shape
+        st, sh, sd = t.stride()
+        if n == T and d == D and (H == heads or not heads) and sd == 1 and (sh == D or H == 1):
+            return st if n > 1 else H * D
+    raise ValueError(f"{what}: bf16 [{T}, {heads or 'Hq'}, {D}], a token's heads side by side")
 
 
 class PagedCache:
@@ -366,28 +365,29 @@ def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=N
     rotated into q_out, which is returned.  The parts of one projection's output need no copies (strides between
     tokens).  rope: fp32 [rows, D] (rope_table), None: no rotation; tok_start: int32 [S + 1], None: one token per
     sequence; positions: int32 [T], None: the rows themselves.  Device conditions go to the int32 tensor status."""
-    T, D = k.shape[0], cache.D
-    _require(_tokens(k, cache.Hkv, D), "k: bf16 [T, Hkv, D], a token's heads side by side")
-    _require(_tokens(v, cache.Hkv, D) and v.shape[0] == T, "v: as k")
-    Hq, q_stride = cache.Hkv, 0
+    T, Hkv, D = k.shape[0], cache.Hkv, cache.D
+    k_stride, v_stride = _token_stride(k, T, Hkv, D, "k"), _token_stride(v, T, Hkv, D, "v")
+    Hq, q_stride = Hkv, 0
     if q is not None:
-        _require(_tokens(q, 0, D) and q.shape[0] == T, "q: bf16 [T, Hq, D], a token's heads side by side")
-        Hq, q_stride = q.shape[1], _row_stride(q)
+        q_stride = _token_stride(q, T, 0, D, "q")
+        Hq = q.shape[1]
         if q_out is None:
             q_out = _empty((T, Hq, D), torch.bfloat16, q.device, stream)
-        _require(_is(q_out, torch.bfloat16, (T, Hq, D)), "q_out: contiguous bf16 [T, Hq, D]")
+        else:
+            _require(_is(q_out, torch.bfloat16, (T, Hq, D)), "q_out: contiguous bf16 [T, Hq, D]")
     else:
         _require(q_out is None, "q_out without q")
     rope_rows = 0
     if rope is not None:
-        _require(rope.dtype == torch.float32 and rope.dim() == 2 and rope.shape[1] == D and rope.is_contiguous(),
-                 "rope: contiguous fp32 [rows, D]")
         rope_rows = rope.shape[0]
+        _require(_is(rope, torch.float32, (rope_rows, D)), "rope: contiguous fp32 [rows, D]")
     _require(tok_start is None or _is(tok_start, torch.int32, (cache.S + 1,)), "tok_start: int32 [S + 1]")
     _require(positions is None or _is(positions, torch.int32, (T,)), "positions: int32 [T]")
-    _check(lib().pced_kv_append(cache.ref, _ptr(q), q_stride, k.data_ptr(), _row_stride(k), v.data_ptr(),
-                                _row_stride(v), _ptr(q_out), Hq, _ptr(tok_start), T, _ptr(rope), rope_rows,
-                                _ptr(positions), _ptr(status), _stream(stream)), "pced_kv_append")
+    rc = lib().pced_kv_append(cache.ref, _ptr(q), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
+                              _ptr(q_out), Hq, _ptr(tok_start), T, _ptr(rope), rope_rows, _ptr(positions),
+                              _ptr(status), _stream(stream))
+    if rc:
+        _check(rc, "pced_kv_append")
     return q_out
 
 
@@ -401,12 +401,15 @@ def block_select(cache: PagedCache, q, n_sel: int, n_first: int = 1, n_last: int
                  stream=None):
     """pced_block_select: int32 [S, Hkv, n_sel], the blocks that q bf16 [S, Hq, D] attends to in ascending order
     (-1 after the last): the first n_first, the last n_last and those with the highest scores."""
-    _require(_tokens(q, 0, cache.D) and q.shape[0] == cache.S, "q: bf16 [S, Hq, D], a token's heads side by side")
+    q_stride = _token_stride(q, cache.S, 0, cache.D, "q")
     if sel is None:
         sel = _empty((cache.S, cache.Hkv, n_sel), torch.int32, q.device, stream)
-    _require(_is(sel, torch.int32, (cache.S, cache.Hkv, n_sel)), "sel: contiguous int32 [S, Hkv, n_sel]")
-    _check(lib().pced_block_select(cache.ref, q.data_ptr(), _row_stride(q), q.shape[1], n_sel, n_first, n_last,
-                                   sel.data_ptr(), _ptr(status), _stream(stream)), "pced_block_select")
+    else:
+        _require(_is(sel, torch.int32, (cache.S, cache.Hkv, n_sel)), "sel: contiguous int32 [S, Hkv, n_sel]")
+    rc = lib().pced_block_select(cache.ref, q.data_ptr(), q_stride, q.shape[1], n_sel, n_first, n_last,
+                                 sel.data_ptr(), _ptr(status), _stream(stream))
+    if rc:
+        _check(rc, "pced_block_select")
     return sel
 
 
@@ -424,26 +427,29 @@ def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=N
     total_rows: upper bound of the rows attended to (of one kv-head, over all sequences), 0: unknown.  A workspace of
     the caller's own is zeroed before its first use (workspace())."""
     S, D = cache.S, cache.D
-    _require(_tokens(q, 0, D) and q.shape[0] == S, "q: bf16 [S, Hq, D], a token's heads side by side")
+    q_stride = _token_stride(q, S, 0, D, "q")
     Hq = q.shape[1]
     n_sel = 0
     if sel is not None:
-        _require(sel.dtype == torch.int32 and sel.dim() == 3 and sel.shape[:2] == (S, cache.Hkv)
-                 and sel.is_contiguous(), "sel: contiguous int32 [S, Hkv, n_sel]")
-        n_sel = sel.shape[2]
+        n_sel = sel.shape[-1]
+        _require(_is(sel, torch.int32, (S, cache.Hkv, n_sel)), "sel: contiguous int32 [S, Hkv, n_sel]")
+    kind = OUT_F32
     if out is None:
         out = _empty((S, Hq, D), torch.float32, q.device, stream)
-    _require(out.dtype in (torch.float32, torch.bfloat16) and out.shape == (S, Hq, D) and out.is_contiguous(),
-             "out: contiguous fp32 or bf16 [S, Hq, D]")
+    else:
+        kind = OUT_F32 if out.dtype == torch.float32 else OUT_BF16
+        _require(_is(out, torch.float32 if kind == OUT_F32 else torch.bfloat16, (S, Hq, D)),
+                 "out: contiguous fp32 or bf16 [S, Hq, D]")
     _require(lse is None or _is(lse, torch.float32, (S, Hq)), "lse: contiguous fp32 [S, Hq]")
     if ws is None:
         ws = _empty(max(256, paged_attention_workspace_size(S, Hq, cache.Hkv, D)), torch.uint8, q.device, stream)
         with torch.cuda.stream(stream):  # (None: the current one)
             ws.zero_()
-    _check(lib().pced_paged_attention(cache.ref, q.data_ptr(), _row_stride(q), Hq, _ptr(sel), n_sel, total_rows,
-                                      1.0 / math.sqrt(D) if scale is None else scale, out.data_ptr(),
-                                      OUT_F32 if out.dtype == torch.float32 else OUT_BF16, _ptr(lse), ws.data_ptr(),
-                                      ws.numel(), _stream(stream)), "pced_paged_attention")
+    rc = lib().pced_paged_attention(cache.ref, q.data_ptr(), q_stride, Hq, _ptr(sel), n_sel, total_rows,
+                                    1.0 / math.sqrt(D) if scale is None else scale, out.data_ptr(), kind, _ptr(lse),
+                                    ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "pced_paged_attention")
     return out
 
 
@@ -461,8 +467,10 @@ def logits_process(logits, rows_per_query: int, history=None, history_len=None, 
     B = rows // rows_per_query
     if out is None:
         out = _empty((rows, stride), torch.float32, logits.device, stream)[:, :V]
-    _require(out.dtype == torch.float32 and out.shape == logits.shape and out.stride(1) == 1
-             and (rows == 1 or out.stride(0) == stride), "out: fp32 of the shape and stride of logits")
+    elif out is not logits:
+        _require(out.dtype == torch.float32 and out.shape == (rows, V)
+                 and out.stride() == (stride if rows > 1 else out.stride(0), 1),
+                 "out: fp32 of the shape and stride of logits")
     n_hist = n_bias = n_masks = words = 0
     if history is not None:
         n_hist = history.shape[-1]
@@ -486,10 +494,11 @@ def logits_process(logits, rows_per_query: int, history=None, history_len=None, 
         _require(mask_row is None or _is(mask_row, torch.int32, (B,)), "mask_row: int32 [B]")
     else:
         _require(mask_row is None, "mask_row needs a mask")
-    _check(lib().pced_logits_process(logits.data_ptr(), out.data_ptr(), stride, B, rows_per_query, V, _ptr(history),
-                                     n_hist, _ptr(history_len), _ptr(penalties), _ptr(bias_ids), _ptr(bias), n_bias,
-                                     _ptr(mask), n_masks, words, _ptr(mask_row), _ptr(status), _stream(stream)),
-           "pced_logits_process")
+    rc = lib().pced_logits_process(logits.data_ptr(), out.data_ptr(), stride, B, rows_per_query, V, _ptr(history),
+                                   n_hist, _ptr(history_len), _ptr(penalties), _ptr(bias_ids), _ptr(bias), n_bias,
+                                   _ptr(mask), n_masks, words, _ptr(mask_row), _ptr(status), _stream(stream))
+    if rc:
+        _check(rc, "pced_logits_process")
     return out
 
 

@@ -7,11 +7,18 @@
 // n_sel-th highest of a row's scores is found by a radix select over 24-bit
 // keys, eight bits a pass; one more pass writes the blocks above it and, of
 // those at it, the lowest, in ascending order.
+#include <cooperative_groups.h>
+
 #include "paged.cuh"
 
 namespace pced {
 
+namespace cg = cooperative_groups;
+
 constexpr int BSEL_THREADS = 256;
+constexpr int BSEL_BATCH = 8;    // blocks of a half-warp in flight
+constexpr int BSEL_CLUSTER = 8;  // most CTAs of a row
+constexpr int BSEL_MIN_PART = 128;  // blocks that a CTA of a shared row has at least
 constexpr int BSEL_MAX_BLOCKS = 32768;   // scores of a row lie in shared memory
 constexpr uint32_t BSEL_ZERO = 1u << 22;         // key of score 0: |score| <= 2 * 128 * 127 * 127 < 2^22
 constexpr uint32_t BSEL_FORCED = (1u << 24) - 1;  // key of a block that is chosen whatever its score
@@ -25,33 +32,46 @@ struct SelectArgs {
   int* status;
 };
 
+// A cluster of CTAs shares a row: each scores its part of the blocks, BSEL_BATCH
+// of them in flight per half-warp, and puts the keys into the first CTA's shared
+// memory, which selects alone.
 template <int D>
 __global__ void __launch_bounds__(BSEL_THREADS) block_select_kernel(SelectArgs a) {
-  extern __shared__ uint32_t keys[];  // [blocks of the sequence]
+  extern __shared__ uint32_t keys[];  // [blocks of the sequence]; in the part being scored the pool blocks first
   __shared__ __align__(16) int8_t pooled[2 * D];
   __shared__ float wmax[BSEL_THREADS / 32];
   __shared__ uint32_t hist[256];
   __shared__ uint32_t found[2];  // bin of the threshold's digit, entries wanted from it
   __shared__ uint32_t wcnt[BSEL_THREADS / 32];
+  cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int s = blockIdx.y, h = blockIdx.x;
+  const int ctas = cluster.num_blocks(), rank = cluster.block_rank();
+  const int s = blockIdx.y, h = blockIdx.x / ctas;
+  if (ctas > 1) cluster.barrier_arrive();  // (the first CTA runs before its memory is written)
   pdl_wait();
-  int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
   const int n = paged_len(a.c, s, a.status);
   const int nb = (n + a.c.block_rows - 1) / a.c.block_rows;
   if (nb <= a.n_sel) {  // all of them
-    for (int i = tid; i < a.n_sel; i += BSEL_THREADS) sel[i] = i < nb ? i : -1;
+    if (rank == 0) {
+      int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
+      for (int i = tid; i < a.n_sel; i += BSEL_THREADS) sel[i] = i < nb ? i : -1;
+    }
+    if (ctas > 1) cluster.barrier_wait();
     return;
   }
+  const int part = (nb + ctas - 1) / ctas, j_lo = min(nb, rank * part), j_hi = min(nb, j_lo + part);
+  for (int j = j_lo + tid; j < j_hi; j += BSEL_THREADS) keys[j] = (uint32_t)paged_block(a.c, s, j, a.status);
   // ---- the pooled query
   float p = 0.f, m = 0.f;
   if (tid < 2 * D) {
-    const int d = tid % D;
-    const __nv_bfloat16* q = a.q + s * a.q_stride + (int64_t)h * a.G * D + d;
-    for (int g = 0; g < a.G; ++g) {
-      const float x = __bfloat162float(q[g * D]);
-      p = __fadd_rn(p, tid < D ? (x > 0.f ? x : 0.f) : (x < 0.f ? x : 0.f));
-      if (x != x) p = x;
+    const __nv_bfloat16* q = a.q + s * a.q_stride + (int64_t)h * a.G * D + tid % D;
+    float x[PAGED_MAX_G];
+#pragma unroll
+    for (int g = 0; g < PAGED_MAX_G; ++g) x[g] = g < a.G ? __bfloat162float(q[g * D]) : 0.f;
+#pragma unroll
+    for (int g = 0; g < PAGED_MAX_G; ++g) {
+      p = __fadd_rn(p, tid < D ? (x[g] > 0.f ? x[g] : 0.f) : (x[g] < 0.f ? x[g] : 0.f));
+      if (x[g] != x[g]) p = x[g];
     }
     m = p != p ? INFINITY : fabsf(p);
   }
@@ -63,25 +83,37 @@ __global__ void __launch_bounds__(BSEL_THREADS) block_select_kernel(SelectArgs a
   if (tid < 2 * D)
     pooled[tid] = m > 0.f && m < INFINITY ? (int8_t)(int)rintf(__fmul_rn(p, __fdiv_rn(127.f, m))) : (int8_t)0;
   __syncthreads();
+  if (ctas > 1) cluster.barrier_wait();
   // ---- scores: 2D / 16 lanes a block
-  constexpr int LANES = 2 * D / 16;
+  constexpr int LANES = 2 * D / 16, STRIDE = BSEL_THREADS / LANES;
+  uint32_t* out = ctas > 1 ? cluster.map_shared_rank(keys, 0) : keys;
   const int l = tid % LANES;
   const int4 pq = reinterpret_cast<const int4*>(pooled)[l];
-  for (int j0 = 0; j0 < nb; j0 += BSEL_THREADS / LANES) {
-    const int j = j0 + tid / LANES;
-    int sc = 0, blk = -1;
-    if (j < nb) {
-      blk = paged_block(a.c, s, j, a.status);
-      if (blk >= 0) {
-        const int4 w = reinterpret_cast<const int4*>(a.c.summary + ((int64_t)blk * a.c.Hkv + h) * 2 * D)[l];
-        sc = __dp4a(w.x, pq.x, __dp4a(w.y, pq.y, __dp4a(w.z, pq.z, __dp4a(w.w, pq.w, 0))));
-      }
+  for (int j0 = j_lo + tid / LANES; j0 - tid / LANES < j_hi; j0 += BSEL_BATCH * STRIDE) {
+    int4 w[BSEL_BATCH];
+    int blk[BSEL_BATCH];
+#pragma unroll
+    for (int u = 0; u < BSEL_BATCH; ++u) {
+      const int j = j0 + u * STRIDE;
+      blk[u] = j < j_hi ? (int)keys[j] : -1;
+      w[u] = make_int4(0, 0, 0, 0);
+      if (blk[u] >= 0)
+        w[u] = reinterpret_cast<const int4*>(a.c.summary + ((int64_t)blk[u] * a.c.Hkv + h) * 2 * D)[l];
     }
 #pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) sc += __shfl_xor_sync(0xffffffffu, sc, o);
-    if (l == 0 && j < nb)
-      keys[j] = j < a.n_first || j >= nb - a.n_last ? BSEL_FORCED : (blk < 0 ? 0u : BSEL_ZERO + (uint32_t)sc);
+    for (int u = 0; u < BSEL_BATCH; ++u) {
+      const int j = j0 + u * STRIDE;
+      int sc = __dp4a(w[u].x, pq.x, __dp4a(w[u].y, pq.y, __dp4a(w[u].z, pq.z, __dp4a(w[u].w, pq.w, 0))));
+#pragma unroll
+      for (int o = 1; o < LANES; o <<= 1) sc += __shfl_xor_sync(0xffffffffu, sc, o);
+      if (l == 0 && j < j_hi)
+        out[j] = j < a.n_first || j >= nb - a.n_last ? BSEL_FORCED : (blk[u] < 0 ? 0u : BSEL_ZERO + (uint32_t)sc);
+    }
   }
+  if (ctas > 1) cluster.sync();
+  else __syncthreads();
+  if (rank > 0) return;
+  int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
   // ---- threshold: the n_sel-th highest key
   uint32_t prefix = 0, want = a.n_sel;  // digits found so far; entries wanted among the keys that share them
   for (int shift = 16; shift >= 0; shift -= 8) {
@@ -174,6 +206,10 @@ extern "C" pced_status pced_block_select(const pced_paged_cache* cache, const vo
   static bool done[2][64];
   cudaError_t e = allow_smem(kernel, BSEL_MAX_BLOCKS * 4, done[c.D == 128]);
   if (e != cudaSuccess) return cuda_status(e, "block_select shared memory");
-  e = launch_pdl(kernel, dim3(c.Hkv, c.S), BSEL_THREADS, smem, (cudaStream_t)stream, a);
+  int ctas = 1;
+  while (ctas < BSEL_CLUSTER && (int64_t)c.Hkv * c.S * ctas < 4 * (int64_t)num_sms() &&
+         c.max_blocks >= 2 * ctas * BSEL_MIN_PART)
+    ctas *= 2;
+  e = launch_cluster(kernel, dim3(c.Hkv * ctas, c.S), ctas, BSEL_THREADS, smem, (cudaStream_t)stream, true, a);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "block_select launch");
 }

@@ -93,166 +93,238 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
   return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
 
-// A CTA takes one item and one kv-head: the rows of K and V and the group's
-// queries.  D/16 lanes share a row of one head (a unit), each with eight channels
-// and their eight rotation partners, so a thread sees the same channels of every
-// key row it takes and holds their bounds in registers.
-template <int D, bool ONE>
-__global__ void __launch_bounds__(APP_THREADS) kv_append_kernel(AppendArgs a) {
-  constexpr int LANES = D / 16;
-  const int tid = threadIdx.x, h = blockIdx.y, G = a.G, P = a.c.block_rows;
-  pdl_wait();
-  AppendItem it;
-  if (ONE) {
-    it.s = it.t0 = blockIdx.x;
-    const int n = paged_len(a.c, it.s, a.status);
-    it.r0 = n - 1;
-    it.m = n > 0;
-    if (n == 0) {  // an idle sequence: no query either
-      for (int i = tid; i < G * D / 8; i += blockDim.x)
-        reinterpret_cast<uint4*>(a.q_out + ((int64_t)it.t0 * a.Hq + h * G) * D)[i] = make_uint4(0, 0, 0, 0);
-      return;
-    }
-  } else {
-    it = find_item(a, blockIdx.x);
-    if (it.s < 0) return;
+// One head's row of a token: eight channels and their eight rotation partners.
+struct HeadRow {
+  uint4 a, b;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int half) {
+    a = *reinterpret_cast<const uint4*>(p);
+    b = *reinterpret_cast<const uint4*>(p + half);
   }
-  const int blk = paged_block(a.c, it.s, it.r0 / P, a.status);
-  const int64_t row0 = ((int64_t)blk * a.c.Hkv + h) * P + it.r0 % P;
-  const bool summarise = a.c.summary != nullptr;
-  const float inv = summarise ? __fdiv_rn(1.f, a.c.key_step[h]) : 0.f;
-  const int l = tid % LANES, f = 8 * l;
-  KeyBounds lo[8], hi[8];
-  const int units = it.m * (G + 2);
-  for (int u = tid / LANES; u < units; u += blockDim.x / LANES) {
-    const int i = u / (G + 2), role = u - i * (G + 2);  // role 0: key, 1: value, then queries
-    const int64_t t = it.t0 + i;
-    const __nv_bfloat16* src;
-    __nv_bfloat16* dst;
-    if (role < 2) {
-      src = (role ? a.v + t * a.v_stride : a.k + t * a.k_stride) + h * D;
-      dst = (__nv_bfloat16*)(role ? a.c.v : a.c.k) + (row0 + i) * D;
-    } else {
-      const int head = h * G + role - 2;
-      src = a.q + t * a.q_stride + (int64_t)head * D;
-      dst = a.q_out + (t * a.Hq + head) * D;
-    }
-    uint4 w0 = *reinterpret_cast<const uint4*>(src + f), w1 = *reinterpret_cast<const uint4*>(src + f + D / 2);
-    if (a.rope && role != 1) {
-      const int p = a.positions ? a.positions[t] : it.r0 + i;
-      if (p >= 0 && p < a.rope_rows) {
-        float x[8], y[8], co[8], si[8];
-        unpack8(w0, x);
-        unpack8(w1, y);
-        const float4* tc = reinterpret_cast<const float4*>(a.rope + (int64_t)p * D + f);
-        const float4* ts = reinterpret_cast<const float4*>(a.rope + (int64_t)p * D + D / 2 + f);
-        *reinterpret_cast<float4*>(co) = tc[0], *reinterpret_cast<float4*>(co + 4) = tc[1];
-        *reinterpret_cast<float4*>(si) = ts[0], *reinterpret_cast<float4*>(si + 4) = ts[1];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float u0 = __fsub_rn(__fmul_rn(x[e], co[e]), __fmul_rn(y[e], si[e]));
-          y[e] = __fadd_rn(__fmul_rn(y[e], co[e]), __fmul_rn(x[e], si[e]));
-          x[e] = u0;
-        }
-        w0 = pack8(x);
-        w1 = pack8(y);
-      } else if (l == 0) {
-        dev_flag(a.status, PCED_DEV_BAD_INDEX);
-      }
-    }
-    if (role >= 2 || blk >= 0) {
-      *reinterpret_cast<uint4*>(dst + f) = w0;
-      *reinterpret_cast<uint4*>(dst + f + D / 2) = w1;
-    }
-    if (role == 0 && summarise) {
-      float x[8], y[8];
-      unpack8(w0, x);
-      unpack8(w1, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) lo[e].take(x[e], inv), hi[e].take(y[e], inv);
-    }
+  __device__ __forceinline__ void store(__nv_bfloat16* p, int half) const {
+    *reinterpret_cast<uint4*>(p) = a;
+    *reinterpret_cast<uint4*>(p + half) = b;
   }
-  if (!summarise) return;
-  // the bounds of all units, channel by channel
-  __shared__ float bounds[2][APP_THREADS / 32][D];
-  const int lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  __device__ __forceinline__ void rotate(const float (&co)[8], const float (&si)[8]) {
+    float x[8], y[8];
+    unpack8(a, x);
+    unpack8(b, y);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-#pragma unroll
-    for (int o = LANES; o < 32; o <<= 1) {
-      lo[e].merge(__shfl_xor_sync(0xffffffffu, lo[e].mx, o), __shfl_xor_sync(0xffffffffu, lo[e].mn, o));
-      hi[e].merge(__shfl_xor_sync(0xffffffffu, hi[e].mx, o), __shfl_xor_sync(0xffffffffu, hi[e].mn, o));
+    for (int e = 0; e < 8; ++e) {
+      const float u = __fsub_rn(__fmul_rn(x[e], co[e]), __fmul_rn(y[e], si[e]));
+      y[e] = __fadd_rn(__fmul_rn(y[e], co[e]), __fmul_rn(x[e], si[e]));
+      x[e] = u;
     }
-    if (lane < LANES) {
-      bounds[0][warp][f + e] = lo[e].mx, bounds[1][warp][f + e] = lo[e].mn;
-      bounds[0][warp][f + D / 2 + e] = hi[e].mx, bounds[1][warp][f + D / 2 + e] = hi[e].mn;
-    }
+    a = pack8(x);
+    b = pack8(y);
   }
-  __syncthreads();
-  if (blk < 0) return;
-  uint32_t* sum = reinterpret_cast<uint32_t*>(a.c.summary + ((int64_t)blk * a.c.Hkv + h) * 2 * D);
-  const bool fresh = it.r0 % P == 0;
-  for (int i = tid; i < 2 * D / 4; i += blockDim.x) {  // four channels of one bound
-    const int which = i / (D / 4), d = 4 * (i % (D / 4));
-    const uint32_t old = fresh ? 0u : sum[i];
-    float x[4];
+};
+// cosines and sines of eight angles of position p; false (flagged) outside the table
+__device__ __forceinline__ bool load_angles(const AppendArgs& a, int D, int p, int f, float (&co)[8], float (&si)[8]) {
+  if (p < 0 || p >= a.rope_rows) {
+    dev_flag(a.status, PCED_DEV_BAD_INDEX);
+    return false;
+  }
+  const float4* tc = reinterpret_cast<const float4*>(a.rope + (int64_t)p * D + f);
+  const float4* ts = reinterpret_cast<const float4*>(a.rope + (int64_t)p * D + D / 2 + f);
+  *reinterpret_cast<float4*>(co) = tc[0], *reinterpret_cast<float4*>(co + 4) = tc[1];
+  *reinterpret_cast<float4*>(si) = ts[0], *reinterpret_cast<float4*>(si + 4) = ts[1];
+  return true;
+}
+// a block's summary taken up to date with the bounds of eight channels from f on
+// (half: 0) or their partners (half: D / 2)
+__device__ __forceinline__ void update_summary(int8_t* summary, int D, int f, const uint32_t (&mx)[4],
+                                               const uint32_t (&mn)[4], float inv, bool fresh) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[e] = bounds[which][0][d + e];
-      for (int w = 1; w < warps; ++w)
-        x[e] = which ? fminf(x[e], bounds[1][w][d + e]) : fmaxf(x[e], bounds[0][w][d + e]);
-      if (!fresh) x[e] = which ? fminf(x[e], unpack_s8(old, e)) : fmaxf(x[e], unpack_s8(old, e));
+  for (int which = 0; which < 2; ++which) {
+    uint2* at = reinterpret_cast<uint2*>(summary + which * D + f);
+    const uint32_t(&k)[4] = which ? mn : mx;
+    uint2 w = make_uint2(steps4(k[0], k[1], !which, inv), steps4(k[2], k[3], !which, inv));
+    if (!fresh) {
+      const uint2 old = *at;
+      w = which ? make_uint2(__vmins4(w.x, old.x), __vmins4(w.y, old.y))
+                : make_uint2(__vmaxs4(w.x, old.x), __vmaxs4(w.y, old.y));
     }
-    sum[i] = pack_s8(x[0], x[1], x[2], x[3]);
+    *at = w;
   }
 }
 
-// ------------------------------------------------------------------ summaries
-constexpr int SUM_THREADS = 128;
+// One token per sequence: a CTA per (sequence, kv-head), D/16 lanes for each row
+// of a head (key, value, the group's queries).
+template <int D>
+__global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(AppendArgs a) {
+  constexpr int LANES = D / 16;
+  const int tid = threadIdx.x, s = blockIdx.x, h = blockIdx.y, G = a.G, P = a.c.block_rows;
+  const int role = tid / LANES, f = 8 * (tid % LANES);  // role 0: key, 1: value, then queries
+  if (role >= G + 2) return;
+  pdl_wait();
+  HeadRow r;
+  __nv_bfloat16* dst = nullptr;
+  if (role >= 2) {
+    const int head = h * G + role - 2;
+    r.load(a.q + s * a.q_stride + (int64_t)head * D + f, D / 2);
+    dst = a.q_out + ((int64_t)s * a.Hq + head) * D + f;
+  } else {
+    r.load((role ? a.v + s * a.v_stride : a.k + s * a.k_stride) + h * D + f, D / 2);
+  }
+  const int n = paged_len(a.c, s, a.status);
+  if (n == 0) {  // an idle sequence: no query either
+    r.a = r.b = make_uint4(0, 0, 0, 0);
+    if (role >= 2) r.store(dst, D / 2);
+    return;
+  }
+  if (a.rope && role != 1) {
+    float co[8], si[8];
+    if (load_angles(a, D, a.positions ? a.positions[s] : n - 1, f, co, si)) r.rotate(co, si);
+  }
+  if (role >= 2) {
+    r.store(dst, D / 2);
+    return;
+  }
+  const int blk = paged_block(a.c, s, (n - 1) / P, a.status), at = (n - 1) % P;
+  if (blk < 0) return;
+  const int64_t page = (int64_t)blk * a.c.Hkv + h;
+  r.store((__nv_bfloat16*)(role ? a.c.v : a.c.k) + (page * P + at) * D + f, D / 2);
+  if (role == 0 && a.c.summary) {
+    const float inv = __fdiv_rn(1.f, a.c.key_step[h]);
+    const uint32_t lo[4] = {r.a.x, r.a.y, r.a.z, r.a.w}, hi[4] = {r.b.x, r.b.y, r.b.z, r.b.w};
+    update_summary(a.c.summary + page * 2 * D, D, f, lo, lo, inv, at == 0);
+    update_summary(a.c.summary + page * 2 * D, D, f + D / 2, hi, hi, inv, at == 0);
+  }
+}
+
+// Any number of tokens: a CTA takes one item and one kv-head.  D/16 lanes share a
+// row, each with the same channels of all its heads, so a position's angles are
+// read once for all of them, and a thread holds the bounds of its channels' keys
+// in registers.
+constexpr int APP_HEADS = 3;  // heads whose loads a thread has in flight
 
 template <int D>
-__global__ void __launch_bounds__(SUM_THREADS) block_summaries_kernel(pced_paged_cache c, int* status) {
-  constexpr int LANES = D / 8, ROWS = SUM_THREADS / LANES;  // a lane holds eight channels
-  const int tid = threadIdx.x, s = blockIdx.y, j = blockIdx.x / c.Hkv, h = blockIdx.x % c.Hkv, P = c.block_rows;
-  __shared__ float bounds[2][SUM_THREADS / 32][D];
+__global__ void __launch_bounds__(APP_THREADS) kv_append_kernel(AppendArgs a) {
+  constexpr int LANES = D / 16, UNITS = APP_THREADS / LANES, WARPS = APP_THREADS / 32;
+  const int tid = threadIdx.x, h = blockIdx.y, G = a.G, P = a.c.block_rows;
+  __shared__ uint32_t bounds[WARPS][2][D / 2];  // of each warp: largest, smallest keys
   pdl_wait();
-  const int live = min(P, paged_len(c, s, status) - j * P);
-  if (live <= 0) return;
-  const int blk = paged_block(c, s, j, status);
-  if (blk < 0) return;
-  const int64_t at = (int64_t)blk * c.Hkv + h;
-  const float inv = __fdiv_rn(1.f, c.key_step[h]);
+  const AppendItem it = find_item(a, blockIdx.x);
+  if (it.s < 0) return;
+  const int blk = paged_block(a.c, it.s, it.r0 / P, a.status);
+  const int64_t page = (int64_t)blk * a.c.Hkv + h;
   const int f = 8 * (tid % LANES);
-  const __nv_bfloat16* k = (const __nv_bfloat16*)c.k + at * P * D + f;
-  KeyBounds b[8];
-#pragma unroll 8
-  for (int r = tid / LANES; r < live; r += ROWS) {
-    float x[8];
-    unpack8(*reinterpret_cast<const uint4*>(k + (int64_t)r * D), x);
+  KeyBounds2 kb[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) b[e].take(x[e], inv);
+  for (int e = 0; e < 8; ++e) kb[e].reset();
+  for (int i = tid / LANES; i < it.m; i += UNITS) {
+    const int64_t t = it.t0 + i;
+    const int64_t row = (page * P + it.r0 % P + i) * D + f;
+    float co[8], si[8];
+    const bool rotated = a.rope && load_angles(a, D, a.positions ? a.positions[t] : it.r0 + i, f, co, si);
+    for (int r0 = 0; r0 < G + 2; r0 += APP_HEADS) {  // role 0: key, 1: value, then queries
+      HeadRow x[APP_HEADS];
+#pragma unroll
+      for (int u = 0; u < APP_HEADS; ++u) {
+        const int role = r0 + u;
+        if (role >= G + 2) break;
+        const __nv_bfloat16* src = role == 0   ? a.k + t * a.k_stride + h * D
+                                   : role == 1 ? a.v + t * a.v_stride + h * D
+                                               : a.q + t * a.q_stride + (int64_t)(h * G + role - 2) * D;
+        x[u].load(src + f, D / 2);
+      }
+#pragma unroll
+      for (int u = 0; u < APP_HEADS; ++u) {
+        const int role = r0 + u;
+        if (role >= G + 2) break;
+        if (rotated && role != 1) x[u].rotate(co, si);
+        if (role >= 2) {
+          x[u].store(a.q_out + (t * a.Hq + h * G + role - 2) * D + f, D / 2);
+        } else if (blk >= 0) {
+          x[u].store((__nv_bfloat16*)(role ? a.c.v : a.c.k) + row, D / 2);
+        }
+        if (role == 0) {
+          const uint32_t w[8] = {x[u].a.x, x[u].a.y, x[u].a.z, x[u].a.w, x[u].b.x, x[u].b.y, x[u].b.z, x[u].b.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) kb[e].take(w[e]);
+        }
+      }
+    }
   }
+  if (!a.c.summary || blk < 0) return;
   const int lane = tid & 31, warp = tid >> 5;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
 #pragma unroll
-    for (int o = LANES; o < 32; o <<= 1)
-      b[e].merge(__shfl_xor_sync(0xffffffffu, b[e].mx, o), __shfl_xor_sync(0xffffffffu, b[e].mn, o));
-    if (lane < LANES) bounds[0][warp][f + e] = b[e].mx, bounds[1][warp][f + e] = b[e].mn;
+    for (int o = LANES; o < 32; o <<= 1) kb[e].merge_xor(o);
+    if (lane < LANES) {
+      const int at = f / 2 + (e < 4 ? e : D / 4 + e - 4);
+      bounds[warp][0][at] = kb[e].top();
+      bounds[warp][1][at] = kb[e].bottom();
+    }
   }
   __syncthreads();
-  if (tid < 2 * D / 4) {
-    const int which = tid / (D / 4), d = 4 * (tid % (D / 4));
-    float x[4];
+  if (tid < D / 8) {  // eight channels
+    uint32_t mx[4], mn[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      x[e] = bounds[which][0][d + e];
+      KeyBounds2 b;
+      b.reset();
 #pragma unroll
-      for (int w = 1; w < SUM_THREADS / 32; ++w)
-        x[e] = which ? fminf(x[e], bounds[1][w][d + e]) : fmaxf(x[e], bounds[0][w][d + e]);
+      for (int w = 0; w < WARPS; ++w) b.merge(bounds[w][0][4 * tid + e], bounds[w][1][4 * tid + e]);
+      mx[e] = b.top(), mn[e] = b.bottom();
     }
-    reinterpret_cast<uint32_t*>(c.summary + at * 2 * D)[tid] = pack_s8(x[0], x[1], x[2], x[3]);
+    update_summary(a.c.summary + page * 2 * D, D, 8 * tid, mx, mn, __fdiv_rn(1.f, a.c.key_step[h]), it.r0 % P == 0);
   }
+}
+
+// ------------------------------------------------------------------ summaries
+// A warp takes up to SUM_ROWS rows of one block and kv-head, D/8 lanes a row; the
+// warps of a block (a power of two of them) meet in shared memory.
+constexpr int SUM_WARPS = 8;
+constexpr int SUM_ROWS = 32;
+constexpr int SUM_BATCH = 8;  // loads of a lane in flight
+
+template <int D>
+__global__ void __launch_bounds__(32 * SUM_WARPS) block_summaries_kernel(pced_paged_cache c, int split, int* status) {
+  constexpr int LANES = D / 8, ROWS = 32 / LANES;  // lanes of a row, rows of a load
+  __shared__ uint32_t bounds[SUM_WARPS][2][D / 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = blockIdx.y, P = c.block_rows;
+  const int unit = blockIdx.x * (SUM_WARPS / split) + warp / split;  // block and kv-head
+  const int j = unit / c.Hkv, h = unit % c.Hkv, part = warp % split;
+  pdl_wait();
+  const int live = j < c.max_blocks ? min(P, paged_len(c, s, status) - j * P) : 0;
+  const int blk = live > 0 ? paged_block(c, s, j, status) : -1;
+  const int64_t page = (int64_t)blk * c.Hkv + h;
+  KeyBounds2 kb[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) kb[e].reset();
+  const int f = 8 * (lane % LANES);
+  if (blk >= 0) {
+    const __nv_bfloat16* k = (const __nv_bfloat16*)c.k + page * P * D + f;
+    const int step = split * ROWS;
+    for (int r = part * ROWS + lane / LANES; r < live; r += SUM_BATCH * step) {
+      uint4 w[SUM_BATCH];
+#pragma unroll
+      for (int u = 0; u < SUM_BATCH; ++u)
+        w[u] = *reinterpret_cast<const uint4*>(k + (int64_t)min(r + u * step, live - 1) * D);  // (a row twice: no harm)
+#pragma unroll
+      for (int u = 0; u < SUM_BATCH; ++u) kb[0].take(w[u].x), kb[1].take(w[u].y), kb[2].take(w[u].z), kb[3].take(w[u].w);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int o = LANES; o < 32; o <<= 1) kb[e].merge_xor(o);
+    if (split > 1 && lane < LANES) {
+      bounds[warp][0][f / 2 + e] = kb[e].top();
+      bounds[warp][1][f / 2 + e] = kb[e].bottom();
+    }
+  }
+  if (split > 1) __syncthreads();
+  if (part > 0 || lane >= LANES || blk < 0) return;
+  uint32_t mx[4], mn[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    for (int w = 1; w < split; ++w) kb[e].merge(bounds[warp + w][0][f / 2 + e], bounds[warp + w][1][f / 2 + e]);
+    mx[e] = kb[e].top(), mn[e] = kb[e].bottom();
+  }
+  update_summary(c.summary + page * 2 * D, D, f, mx, mn, __fdiv_rn(1.f, c.key_step[h]), true);
 }
 
 }  // namespace pced
@@ -290,12 +362,6 @@ pced_status check_paged_heads(const pced_paged_cache* c, int32_t Hq, const char*
 
 }  // namespace pced_host
 
-template <bool ONE>
-static cudaError_t launch_append(const AppendArgs& a, dim3 grid, int threads, cudaStream_t s) {
-  return a.c.D == 128 ? launch_pdl(kv_append_kernel<128, ONE>, grid, threads, 0, s, a)
-                      : launch_pdl(kv_append_kernel<64, ONE>, grid, threads, 0, s, a);
-}
-
 extern "C" pced_status pced_kv_append(const pced_paged_cache* cache, const void* q, int64_t q_stride, const void* k,
                                       int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int32_t Hq,
                                       const int32_t* tok_start, int32_t T, const float* rope, int32_t rope_rows,
@@ -331,13 +397,15 @@ extern "C" pced_status pced_kv_append(const pced_paged_cache* cache, const void*
   a.status = status;
   cudaError_t e;
   if (!tok_start) {
-    const int threads = ((a.G + 2) * (c.D / 16) + 31) / 32 * 32;  // a unit for every head
-    e = launch_append<true>(a, dim3(c.S, c.Hkv), threads, (cudaStream_t)stream);
+    const int threads = (a.G + 2) * (c.D / 16);
+    e = launch_pdl(c.D == 128 ? kv_append_one_kernel<128> : kv_append_one_kernel<64>, dim3(c.S, c.Hkv), threads, 0,
+                   (cudaStream_t)stream, a);
   } else {
     // blocks touched: at most two more than whole ones for every sequence with tokens
     const int64_t items = (int64_t)T / c.block_rows + 2 * (int64_t)(T < c.S ? T : c.S);
     if (items >= (INT64_C(1) << 31)) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
-    e = launch_append<false>(a, dim3((unsigned)items, c.Hkv), APP_THREADS, (cudaStream_t)stream);
+    e = launch_pdl(c.D == 128 ? kv_append_kernel<128> : kv_append_kernel<64>, dim3((unsigned)items, c.Hkv), APP_THREADS,
+                   0, (cudaStream_t)stream, a);
   }
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "kv_append launch");
 }
@@ -349,12 +417,13 @@ extern "C" pced_status pced_block_summaries(const pced_paged_cache* cache, int32
   const pced_paged_cache& c = *cache;
   if (!c.k || !c.summary || !c.key_step) return fail(PCED_ERR_INVALID_ARG, "%s: null pointer", fn);
   if (!aligned(status, 4)) return fail(PCED_ERR_INVALID_ARG, "%s: misaligned pointer", fn);
-  const int64_t gx = (int64_t)c.max_blocks * c.Hkv;
-  if (gx >= (INT64_C(1) << 31)) return fail(PCED_ERR_UNSUPPORTED, "%s: max_blocks * Hkv >= 2^31", fn);
+  int split = 1;  // warps of a block's rows
+  while (split < SUM_WARPS && split * SUM_ROWS < c.block_rows) split *= 2;
+  const int64_t gx = ((int64_t)c.max_blocks * c.Hkv + SUM_WARPS / split - 1) / (SUM_WARPS / split);
+  if ((int64_t)c.max_blocks * c.Hkv >= (INT64_C(1) << 31) - SUM_WARPS)
+    return fail(PCED_ERR_UNSUPPORTED, "%s: max_blocks * Hkv >= 2^31", fn);
   if (num_sms() <= 0) return fail(PCED_ERR_NO_DEVICE, "%s: no CUDA device", fn);
-  const dim3 grid((unsigned)gx, c.S);
-  const cudaError_t e =
-      c.D == 128 ? launch_pdl(block_summaries_kernel<128>, grid, SUM_THREADS, 0, (cudaStream_t)stream, c, status)
-                 : launch_pdl(block_summaries_kernel<64>, grid, SUM_THREADS, 0, (cudaStream_t)stream, c, status);
+  const cudaError_t e = launch_pdl(c.D == 128 ? block_summaries_kernel<128> : block_summaries_kernel<64>,
+                                   dim3((unsigned)gx, c.S), 32 * SUM_WARPS, 0, (cudaStream_t)stream, c, split, status);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "block_summaries launch");
 }

@@ -17,6 +17,7 @@ namespace pced {
 constexpr int LOG_THREADS = 256;
 constexpr int LOG_TOK = 8;  // tokens of a thread
 constexpr int LOG_CHUNK = LOG_THREADS * LOG_TOK;
+constexpr int LOG_ROWS = 4;  // rows in flight
 
 struct LogitsArgs {
   const float* x;
@@ -36,7 +37,33 @@ struct LogitsArgs {
   int* status;
 };
 
-// VEC: a thread's tokens are two runs of four, moved as 16 bytes
+// Token e of this thread, from the chunk's first.  VEC: they are two runs of four,
+// moved as 16 bytes.
+template <bool VEC>
+__device__ __forceinline__ int token_of(int e) {
+  return VEC ? (e / 4 * LOG_THREADS + (int)threadIdx.x) * 4 + e % 4 : e * LOG_THREADS + (int)threadIdx.x;
+}
+template <bool VEC>
+__device__ __forceinline__ void load_row(const LogitsArgs& a, int64_t at, int v0, float (&x)[LOG_TOK]) {
+#pragma unroll
+  for (int e = 0; e < LOG_TOK; e += VEC ? 4 : 1) {
+    const int i = token_of<VEC>(e);
+    if (v0 + i >= a.V) continue;
+    if (VEC) *reinterpret_cast<float4*>(x + e) = *reinterpret_cast<const float4*>(a.x + at + i);
+    else x[e] = a.x[at + i];
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store_row(const LogitsArgs& a, int64_t at, int v0, const float (&x)[LOG_TOK]) {
+#pragma unroll
+  for (int e = 0; e < LOG_TOK; e += VEC ? 4 : 1) {
+    const int i = token_of<VEC>(e);
+    if (v0 + i >= a.V) continue;
+    if (VEC) *reinterpret_cast<float4*>(a.y + at + i) = *reinterpret_cast<const float4*>(x + e);
+    else a.y[at + i] = x[e];
+  }
+}
+
 template <bool VEC>
 __global__ void __launch_bounds__(LOG_THREADS) logits_process_kernel(LogitsArgs a) {
   __shared__ int32_t count[LOG_CHUNK];
@@ -78,40 +105,33 @@ __global__ void __launch_bounds__(LOG_THREADS) logits_process_kernel(LogitsArgs 
   __syncthreads();
   // this thread's tokens
   float cnt[LOG_TOK], add[LOG_TOK];
-  bool allowed[LOG_TOK];
+  uint32_t allowed = 0;
 #pragma unroll
   for (int e = 0; e < LOG_TOK; ++e) {
-    const int i = VEC ? (e / 4 * LOG_THREADS + tid) * 4 + e % 4 : e * LOG_THREADS + tid;
-    const int v = v0 + i;
+    const int i = token_of<VEC>(e), v = v0 + i;
     cnt[e] = (float)count[i];
     const int w = named[i];
     add[e] = w ? a.bias[(int64_t)b * a.n_bias + w - 1] : 0.f;
-    allowed[e] = !mask || (v < a.V && (mask[v >> 5] >> (v & 31) & 1u));
+    if (!mask || (v < a.V && (mask[v >> 5] >> (v & 31) & 1u))) allowed |= 1u << e;
   }
-  for (int r = r0; r < r1; ++r) {
-    const int64_t row = ((int64_t)b * a.R + r) * a.stride + v0;
-    float x[LOG_TOK];
+  const int64_t row0 = (int64_t)b * a.R * a.stride + v0;
+  for (int r = r0; r < r1; r += LOG_ROWS) {
+    float x[LOG_ROWS][LOG_TOK];
 #pragma unroll
-    for (int e = 0; e < LOG_TOK; e += VEC ? 4 : 1) {
-      const int i = VEC ? (e / 4 * LOG_THREADS + tid) * 4 : e * LOG_THREADS + tid;
-      if (v0 + i >= a.V) continue;
-      if (VEC) *reinterpret_cast<float4*>(x + e) = *reinterpret_cast<const float4*>(a.x + row + i);
-      else x[e] = a.x[row + i];
-    }
+    for (int u = 0; u < LOG_ROWS; ++u)
+      if (r + u < r1) load_row<VEC>(a, row0 + (r + u) * a.stride, v0, x[u]);
 #pragma unroll
-    for (int e = 0; e < LOG_TOK; ++e) {
-      if (cnt[e] > 0.f)
-        x[e] = __fsub_rn(x[e] > 0.f ? __fdiv_rn(x[e], rep) : __fmul_rn(x[e], rep),
-                         __fadd_rn(__fmul_rn(cnt[e], freq), pres));
-      if (add[e] != 0.f) x[e] += add[e];
-      if (!allowed[e]) x[e] = -INFINITY;
-    }
+    for (int u = 0; u < LOG_ROWS; ++u) {
+      if (r + u >= r1) break;
 #pragma unroll
-    for (int e = 0; e < LOG_TOK; e += VEC ? 4 : 1) {
-      const int i = VEC ? (e / 4 * LOG_THREADS + tid) * 4 : e * LOG_THREADS + tid;
-      if (v0 + i >= a.V) continue;
-      if (VEC) *reinterpret_cast<float4*>(a.y + row + i) = *reinterpret_cast<const float4*>(x + e);
-      else a.y[row + i] = x[e];
+      for (int e = 0; e < LOG_TOK; ++e) {
+        float& y = x[u][e];
+        if (cnt[e] > 0.f)
+          y = __fsub_rn(y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep), __fadd_rn(__fmul_rn(cnt[e], freq), pres));
+        if (add[e] != 0.f) y += add[e];
+        if (!(allowed >> e & 1u)) y = -INFINITY;
+      }
+      store_row<VEC>(a, row0 + (r + u) * a.stride, v0, x[u]);
     }
   }
 }
@@ -148,9 +168,12 @@ extern "C" pced_status pced_logits_process(const float* x, float* y, int64_t str
   a.bias_ids = bias_ids, a.bias = bias, a.n_bias = n_bias;
   a.mask = mask, a.n_masks = n_masks, a.mask_words = mask_words, a.mask_row = mask_row;
   a.status = status;
-  a.rows = R;
+  // CTAs for about four a SM; a chunk's tokens are counted again for every part of the rows
+  const int chunks = (V - 1) / LOG_CHUNK + 1;
+  const int64_t parts = 4 * (int64_t)num_sms() / ((int64_t)chunks * B);
+  a.rows = parts < 1 ? R : (int)((R + parts - 1) / parts);
   const bool vec = V % 4 == 0 && stride % 4 == 0 && (((uintptr_t)x | (uintptr_t)y) & 15u) == 0;
-  const dim3 grid((V - 1) / LOG_CHUNK + 1, 1, B);
+  const dim3 grid(chunks, (R - 1) / a.rows + 1, B);
   const cudaError_t e = vec ? launch_pdl(logits_process_kernel<true>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a)
                             : launch_pdl(logits_process_kernel<false>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "logits_process launch");

@@ -25,26 +25,46 @@ __device__ __forceinline__ int paged_block(const pced_paged_cache& c, int s, int
 }
 
 // ------------------------------------------------------------- key summaries
-// Largest and smallest key of a channel in whole steps: the bounds of what one
-// thread has seen (fp32 holds these whole numbers exactly).
-struct KeyBounds {
-  float mx = -127.f, mn = 127.f;
-  __device__ __forceinline__ void take(float k, float inv_step) {
-    const float x = __fmul_rn(k, inv_step);
-    // (fmaxf and fminf drop what is not a number)
-    mx = x != x ? 127.f : fmaxf(mx, fminf(ceilf(x), 127.f));
-    mn = x != x ? -127.f : fminf(mn, fmaxf(floorf(x), -127.f));
+// Largest and smallest of two channels' keys, as bf16 pairs (one instruction for
+// two keys each; not-a-number wins).  The product with 1 / key_step, rounded,
+// and ceil, floor and the clipping are monotone, so they are taken of the bounds
+// alone: counted per key they bound the summaries of 272 caches at 150 us.
+struct KeyBounds2 {
+  __nv_bfloat162 mx, mn;
+  __device__ __forceinline__ void reset() {
+    mx = __float2bfloat162_rn(-INFINITY);
+    mn = __float2bfloat162_rn(INFINITY);
   }
-  __device__ __forceinline__ void merge(float mx2, float mn2) {
-    mx = fmaxf(mx, mx2);
-    mn = fminf(mn, mn2);
+  __device__ __forceinline__ void take(uint32_t k) { merge(k, k); }
+  __device__ __forceinline__ void merge(uint32_t mx2, uint32_t mn2) {
+    mx = __hmax2_nan(mx, *reinterpret_cast<const __nv_bfloat162*>(&mx2));
+    mn = __hmin2_nan(mn, *reinterpret_cast<const __nv_bfloat162*>(&mn2));
+  }
+  __device__ __forceinline__ uint32_t top() const { return *reinterpret_cast<const uint32_t*>(&mx); }
+  __device__ __forceinline__ uint32_t bottom() const { return *reinterpret_cast<const uint32_t*>(&mn); }
+  // with the bounds of lane ^ o
+  __device__ __forceinline__ void merge_xor(int o) {
+    const uint32_t x = __shfl_xor_sync(0xffffffffu, top(), o), y = __shfl_xor_sync(0xffffffffu, bottom(), o);
+    merge(x, y);
   }
 };
-__device__ __forceinline__ uint32_t pack_s8(float a, float b, float c, float d) {
-  return ((uint32_t)(int)a & 0xFFu) | ((uint32_t)(int)b & 0xFFu) << 8 | ((uint32_t)(int)c & 0xFFu) << 16 |
-         ((uint32_t)(int)d & 0xFFu) << 24;
+// whole steps of a largest key, and of a smallest one
+__device__ __forceinline__ int steps_up(float k, float inv_step) {
+  const float x = __fmul_rn(k, inv_step);
+  return x != x ? 127 : (int)fminf(fmaxf(ceilf(x), -127.f), 127.f);
 }
-__device__ __forceinline__ float unpack_s8(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
+__device__ __forceinline__ int steps_down(float k, float inv_step) {
+  const float x = __fmul_rn(k, inv_step);
+  return x != x ? -127 : (int)fminf(fmaxf(floorf(x), -127.f), 127.f);
+}
+// the steps of four channels (two words of bf16), a byte each
+__device__ __forceinline__ uint32_t steps4(uint32_t a, uint32_t b, bool up, float inv) {
+  const float k[4] = {bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)};
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w |= ((uint32_t)(up ? steps_up(k[i], inv) : steps_down(k[i], inv)) & 0xFFu) << (8 * i);
+  return w;
+}
 
 }  // namespace pced
 
