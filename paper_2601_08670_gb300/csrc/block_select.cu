@@ -4,9 +4,8 @@
 // The score of a block is the dot product of the group's pooled query (its
 // positive and its negative parts, in 127 steps) with the block's largest and
 // smallest keys: 2D products of 8-bit numbers, four a dp4a, exact in 32 bits.  The
-// n_sel-th highest of a row's scores is found by a radix select over 24-bit
-// keys, eight bits a pass; one more pass writes the blocks above it and, of
-// those at it, the lowest, in ascending order.
+// lowest chosen score of a row is found by a radix select, eight bits a pass; the
+// blocks above it and, of those at it, the lowest are written in ascending order.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -16,12 +15,11 @@ namespace pced {
 namespace cg = cooperative_groups;
 
 constexpr int BSEL_THREADS = 256;
-constexpr int BSEL_BATCH = 8;    // blocks of a half-warp in flight
+constexpr int BSEL_BATCH = 8;    // blocks of a group of lanes in flight
 constexpr int BSEL_CLUSTER = 8;  // most CTAs of a row
 constexpr int BSEL_MIN_PART = 128;  // blocks that a CTA of a shared row has at least
-constexpr int BSEL_MAX_BLOCKS = 32768;   // scores of a row lie in shared memory
-constexpr uint32_t BSEL_ZERO = 1u << 22;         // key of score 0: |score| <= 2 * 128 * 127 * 127 < 2^22
-constexpr uint32_t BSEL_FORCED = (1u << 24) - 1;  // key of a block that is chosen whatever its score
+constexpr int BSEL_MAX_BLOCKS = 32768;  // scores of a row lie in shared memory
+constexpr int32_t BSEL_WORST = -(1 << 22);  // of a bad block: below -2 * 128 * 127 * 127
 
 struct SelectArgs {
   pced_paged_cache c;
@@ -32,23 +30,53 @@ struct SelectArgs {
   int* status;
 };
 
+// Place j of the i-th block of a cluster's CTA: the CTAs take turns at 32 blocks.
+__device__ __forceinline__ int place_of(int i, int ctas, int rank) { return (i / 32 * ctas + rank) * 32 + i % 32; }
+
+// Exclusive prefix over the CTA's threads of x (all threads; wsum: a word per warp).
+__device__ __forceinline__ uint32_t cta_prefix(uint32_t x, uint32_t* wsum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t incl = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) wsum[warp] = incl;
+  __syncthreads();
+  uint32_t before = incl - x;
+  for (int w = 0; w < warp; ++w) before += wsum[w];
+  return before;
+}
+
 // A cluster of CTAs shares a row: each scores its part of the blocks, BSEL_BATCH
-// of them in flight per half-warp, and puts the keys into the first CTA's shared
-// memory, which selects alone.
+// of them in flight per group of lanes, and puts the scores into the first CTA's
+// shared memory, which selects alone.
 template <int D>
-__global__ void __launch_bounds__(BSEL_THREADS) block_select_kernel(SelectArgs a) {
-  extern __shared__ uint32_t keys[];  // [blocks of the sequence]; in the part being scored the pool blocks first
+__global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArgs a) {
+  extern __shared__ int32_t scores[];  // [blocks of the sequence]; before a block's score, its pool block
   __shared__ __align__(16) int8_t pooled[2 * D];
   __shared__ float wmax[BSEL_THREADS / 32];
+  __shared__ int2 wrange[BSEL_THREADS / 32];
   __shared__ uint32_t hist[256];
-  __shared__ uint32_t found[2];  // bin of the threshold's digit, entries wanted from it
-  __shared__ uint32_t wcnt[BSEL_THREADS / 32];
+  __shared__ uint32_t found[3];  // digit of the threshold, entries wanted at it, entries there are
+  __shared__ uint32_t wsum[BSEL_THREADS / 32];
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ctas = cluster.num_blocks(), rank = cluster.block_rank();
   const int s = blockIdx.y, h = blockIdx.x / ctas;
   if (ctas > 1) cluster.barrier_arrive();  // (the first CTA runs before its memory is written)
   pdl_wait();
+  // the length, this thread's part of the queries and its first table entry arrive together
+  const int j_tid = place_of(tid, ctas, rank);
+  const int32_t* table = a.c.block_table + (int64_t)s * a.c.max_blocks;
+  int entry = j_tid < a.c.max_blocks ? table[j_tid] : 0;
+  float x[PAGED_MAX_G];
+  if (tid < 2 * D) {
+    const __nv_bfloat16* q = a.q + s * a.q_stride + (int64_t)h * a.G * D + tid % D;
+#pragma unroll
+    for (int g = 0; g < PAGED_MAX_G; ++g) x[g] = g < a.G ? __bfloat162float(q[g * D]) : 0.f;
+  }
   const int n = paged_len(a.c, s, a.status);
   const int nb = (n + a.c.block_rows - 1) / a.c.block_rows;
   if (nb <= a.n_sel) {  // all of them
@@ -59,15 +87,19 @@ __global__ void __launch_bounds__(BSEL_THREADS) block_select_kernel(SelectArgs a
     if (ctas > 1) cluster.barrier_wait();
     return;
   }
-  const int part = (nb + ctas - 1) / ctas, j_lo = min(nb, rank * part), j_hi = min(nb, j_lo + part);
-  for (int j = j_lo + tid; j < j_hi; j += BSEL_THREADS) keys[j] = (uint32_t)paged_block(a.c, s, j, a.status);
+  for (int i = tid, j = j_tid; j < nb;) {
+    if (entry < 0 || entry >= a.c.num_blocks) {
+      dev_flag(a.status, PCED_DEV_BAD_BLOCK);
+      entry = -1;
+    }
+    scores[j] = entry;
+    i += BSEL_THREADS;
+    j = place_of(i, ctas, rank);
+    if (j < nb) entry = table[j];
+  }
   // ---- the pooled query
   float p = 0.f, m = 0.f;
   if (tid < 2 * D) {
-    const __nv_bfloat16* q = a.q + s * a.q_stride + (int64_t)h * a.G * D + tid % D;
-    float x[PAGED_MAX_G];
-#pragma unroll
-    for (int g = 0; g < PAGED_MAX_G; ++g) x[g] = g < a.G ? __bfloat162float(q[g * D]) : 0.f;
 #pragma unroll
     for (int g = 0; g < PAGED_MAX_G; ++g) {
       p = __fadd_rn(p, tid < D ? (x[g] > 0.f ? x[g] : 0.f) : (x[g] < 0.f ? x[g] : 0.f));
@@ -79,6 +111,7 @@ __global__ void __launch_bounds__(BSEL_THREADS) block_select_kernel(SelectArgs a
   if (lane == 0) wmax[warp] = m;
   __syncthreads();
   m = wmax[0];
+#pragma unroll
   for (int w = 1; w < BSEL_THREADS / 32; ++w) m = fmaxf(m, wmax[w]);
   if (tid < 2 * D)
     pooled[tid] = m > 0.f && m < INFINITY ? (int8_t)(int)rintf(__fmul_rn(p, __fdiv_rn(127.f, m))) : (int8_t)0;
@@ -86,87 +119,115 @@ __global__ void __launch_bounds__(BSEL_THREADS) block_select_kernel(SelectArgs a
   if (ctas > 1) cluster.barrier_wait();
   // ---- scores: 2D / 16 lanes a block
   constexpr int LANES = 2 * D / 16, STRIDE = BSEL_THREADS / LANES;
-  uint32_t* out = ctas > 1 ? cluster.map_shared_rank(keys, 0) : keys;
+  int32_t* out = ctas > 1 ? cluster.map_shared_rank(scores, 0) : scores;
   const int l = tid % LANES;
   const int4 pq = reinterpret_cast<const int4*>(pooled)[l];
-  for (int j0 = j_lo + tid / LANES; j0 - tid / LANES < j_hi; j0 += BSEL_BATCH * STRIDE) {
+  for (int i0 = 0; place_of(i0, ctas, rank) < nb; i0 += BSEL_BATCH * STRIDE) {
     int4 w[BSEL_BATCH];
     int blk[BSEL_BATCH];
 #pragma unroll
     for (int u = 0; u < BSEL_BATCH; ++u) {
-      const int j = j0 + u * STRIDE;
-      blk[u] = j < j_hi ? (int)keys[j] : -1;
+      const int j = place_of(i0 + u * STRIDE + tid / LANES, ctas, rank);
+      blk[u] = j < nb ? scores[j] : -1;
       w[u] = make_int4(0, 0, 0, 0);
       if (blk[u] >= 0)
         w[u] = reinterpret_cast<const int4*>(a.c.summary + ((int64_t)blk[u] * a.c.Hkv + h) * 2 * D)[l];
     }
 #pragma unroll
     for (int u = 0; u < BSEL_BATCH; ++u) {
-      const int j = j0 + u * STRIDE;
+      const int j = place_of(i0 + u * STRIDE + tid / LANES, ctas, rank);
       int sc = __dp4a(w[u].x, pq.x, __dp4a(w[u].y, pq.y, __dp4a(w[u].z, pq.z, __dp4a(w[u].w, pq.w, 0))));
 #pragma unroll
       for (int o = 1; o < LANES; o <<= 1) sc += __shfl_xor_sync(0xffffffffu, sc, o);
-      if (l == 0 && j < j_hi)
-        out[j] = j < a.n_first || j >= nb - a.n_last ? BSEL_FORCED : (blk[u] < 0 ? 0u : BSEL_ZERO + (uint32_t)sc);
+      if (l == 0 && j < nb) out[j] = blk[u] < 0 ? BSEL_WORST : sc;
     }
   }
   if (ctas > 1) cluster.sync();
   else __syncthreads();
   if (rank > 0) return;
-  int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
-  // ---- threshold: the n_sel-th highest key
-  uint32_t prefix = 0, want = a.n_sel;  // digits found so far; entries wanted among the keys that share them
-  for (int shift = 16; shift >= 0; shift -= 8) {
-    hist[tid] = 0;
-    __syncthreads();
-    for (int j = tid; j < nb; j += BSEL_THREADS)
-      if (shift == 16 || keys[j] >> (shift + 8) == prefix) atomicAdd(&hist[keys[j] >> shift & 255u], 1u);
-    __syncthreads();
-    if (warp == 0) {  // the bin that holds the want-th from above
-      uint32_t own = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) own += hist[8 * lane + i];
-      uint32_t above = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t v = __shfl_down_sync(0xffffffffu, above, o);
-        if (lane + o < 32) above += v;
-      }
-      above -= own;
-      if (above < want && want <= above + own) {
-        int b = 8 * lane + 7;
-        while (above + hist[b] < want) above += hist[b--];
-        found[0] = b;
-        found[1] = want - above;
-      }
-    }
-    __syncthreads();
-    prefix = prefix << 8 | found[0];
-    want = found[1];
-    __syncthreads();
+
+  // ---- the lowest score chosen among the blocks [lo, hi) between the first and the last ones
+  const int lo = min(a.n_first, nb), hi = max(lo, nb - a.n_last);
+  uint32_t want = a.n_sel - (a.n_first + a.n_last);  // of them; fewer than there are, as nb > n_sel
+  int2 range = make_int2(INT32_MAX, INT32_MIN);
+  for (int j = lo + tid; j < hi; j += BSEL_THREADS) {
+    range.x = min(range.x, scores[j]);
+    range.y = max(range.y, scores[j]);
   }
-  // ---- the chosen, in order; of those at the threshold the first `want`
-  uint32_t above0 = 0, ties0 = 0;  // before this round's blocks
-  for (int j0 = 0; j0 < nb; j0 += BSEL_THREADS) {
-    const int j = j0 + tid;
-    const uint32_t key = j < nb ? keys[j] : 0u;
-    const bool above = j < nb && key > prefix, tie = j < nb && key == prefix;
-    const uint32_t ba = __ballot_sync(0xffffffffu, above), bt = __ballot_sync(0xffffffffu, tie);
-    if (lane == 0) wcnt[warp] = __popc(ba) | __popc(bt) << 16;
-    __syncthreads();
-    const uint32_t below = (1u << lane) - 1u;
-    uint32_t na = above0 + __popc(ba & below), nt = ties0 + __popc(bt & below);
-    for (int w = 0; w < BSEL_THREADS / 32; ++w) {
-      const uint32_t x = wcnt[w];
-      above0 += x & 0xFFFFu;
-      ties0 += x >> 16;
-      if (w < warp) {
-        na += x & 0xFFFFu;
-        nt += x >> 16;
+  range.x = __reduce_min_sync(0xffffffffu, range.x);
+  range.y = __reduce_max_sync(0xffffffffu, range.y);
+  if (lane == 0) wrange[warp] = range;
+  hist[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < BSEL_THREADS / 32; ++w) {
+    range.x = min(range.x, wrange[w].x);
+    range.y = max(range.y, wrange[w].y);
+  }
+  // Scores as distances from the lowest, eight bits a pass from the highest bit
+  // that any of them has; the search ends early where a digit's entries are all wanted.
+  uint32_t floor = 0;  // distance of the threshold
+  if (want > 0) {
+    int shift = max(0, 32 - __clz(range.y - range.x) - 8), bits = 32;  // bits: of the distance not fixed yet
+    while (true) {
+      for (int j = lo + tid; j < hi; j += BSEL_THREADS) {
+        const uint32_t d = (uint32_t)(scores[j] - range.x);
+        if (bits == 32 || (d ^ floor) >> bits == 0) atomicAdd(&hist[d >> shift & 255u], 1u);
       }
+      __syncthreads();
+      if (warp == 0) {  // the digit that holds the want-th from above
+        uint32_t own = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) own += hist[8 * lane + i];
+        uint32_t above = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t v = __shfl_down_sync(0xffffffffu, above, o);
+          if (lane + o < 32) above += v;
+        }
+        above -= own;
+        if (above < want && want <= above + own) {
+          int b = 8 * lane + 7;
+          while (above + hist[b] < want) above += hist[b--];
+          found[0] = b, found[1] = want - above, found[2] = hist[b];
+        }
+      }
+      __syncthreads();
+      floor |= found[0] << shift;
+      want = found[1];
+      if (shift == 0 || want == found[2]) break;  // (then all from `floor` on are chosen)
+      bits = shift;
+      shift = max(0, shift - 8);
+      hist[tid] = 0;
+      __syncthreads();
     }
-    if (above || (tie && nt < want)) sel[na + min(nt, want)] = j;
-    __syncthreads();
+    if (want == found[2]) want = UINT32_MAX;  // of those at the threshold, or in its digit, all
+  }
+  // ---- the chosen, in order; each thread takes consecutive blocks
+  const bool none = a.n_sel == a.n_first + a.n_last;
+  const int per = (nb + BSEL_THREADS - 1) / BSEL_THREADS, j0 = min(nb, tid * per), j1 = min(nb, j0 + per);
+  // (2: chosen, 1: at the threshold)
+  auto rate = [&](int j) -> uint32_t {
+    if (j < lo || j >= hi) return 2;
+    if (none) return 0;
+    const uint32_t d = (uint32_t)(scores[j] - range.x);
+    if (want == UINT32_MAX) return d >= floor ? 2 : 0;
+    return d > floor ? 2 : d == floor;
+  };
+  uint32_t above = 0, ties = 0;
+  for (int j = j0; j < j1; ++j) {
+    const uint32_t r = rate(j);
+    above += r >> 1;
+    ties += r & 1u;
+  }
+  const uint32_t before = cta_prefix(above << 16 | ties, wsum);
+  above = before >> 16, ties = before & 0xFFFFu;
+  int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
+  for (int j = j0; j < j1; ++j) {
+    const uint32_t r = rate(j);
+    if (r == 2 || (r == 1 && ties < want)) sel[above + min(ties, want)] = j;
+    above += r >> 1;
+    ties += r & 1u;
   }
 }
 
@@ -207,7 +268,7 @@ extern "C" pced_status pced_block_select(const pced_paged_cache* cache, const vo
   cudaError_t e = allow_smem(kernel, BSEL_MAX_BLOCKS * 4, done[c.D == 128]);
   if (e != cudaSuccess) return cuda_status(e, "block_select shared memory");
   int ctas = 1;
-  while (ctas < BSEL_CLUSTER && (int64_t)c.Hkv * c.S * ctas < 4 * (int64_t)num_sms() &&
+  while (ctas < BSEL_CLUSTER && (int64_t)c.Hkv * c.S * ctas < 2 * (int64_t)num_sms() &&
          c.max_blocks >= 2 * ctas * BSEL_MIN_PART)
     ctas *= 2;
   e = launch_cluster(kernel, dim3(c.Hkv * ctas, c.S), ctas, BSEL_THREADS, smem, (cudaStream_t)stream, true, a);

@@ -48,13 +48,20 @@ __device__ __forceinline__ int blocks_touched(int3 r, int P) {
 // Item `want` of the call: its sequence by the prefix of blocks touched.  All
 // threads; s = -1 past the last.
 __device__ __forceinline__ AppendItem find_item(const AppendArgs& a, int want) {
+  constexpr int PER = PAGED_MAX_S / APP_THREADS;  // sequences of a thread
   __shared__ int wsum[APP_THREADS / 32];
   __shared__ AppendItem it;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, P = a.c.block_rows;
-  const int per = (a.c.S + APP_THREADS - 1) / APP_THREADS;
-  const int s0 = min(a.c.S, tid * per), s1 = min(a.c.S, s0 + per);
-  int own = 0;
-  for (int s = s0; s < s1; ++s) own += blocks_touched(new_rows(a, s), P);
+  const int per = (a.c.S + APP_THREADS - 1) / APP_THREADS, s0 = tid * per;
+  int3 r[PER];
+  int nb[PER], own = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool in = i < per && s0 + i < a.c.S;
+    r[i] = in ? new_rows(a, s0 + i) : make_int3(0, 0, 0);
+    nb[i] = blocks_touched(r[i], P);
+    own += nb[i];
+  }
   int incl = own;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -65,21 +72,18 @@ __device__ __forceinline__ AppendItem find_item(const AppendArgs& a, int want) {
   if (tid == 0) it.s = -1;
   __syncthreads();
   int at = incl - own;
-  for (int w = 0; w < warp; ++w) at += wsum[w];
-  if (want >= at && want < at + own) {
-    for (int s = s0; s < s1; ++s) {
-      const int3 r = new_rows(a, s);
-      const int nb = blocks_touched(r, P);
-      if (want < at + nb) {
-        const int first = r.z - r.y, j = first / P + (want - at);
-        it.s = s;
-        it.r0 = max(first, j * P);
-        it.m = min(r.z, (j + 1) * P) - it.r0;
-        it.t0 = r.x + (it.r0 - first);
-        break;
-      }
-      at += nb;
+#pragma unroll
+  for (int w = 0; w < APP_THREADS / 32; ++w) at += w < warp ? wsum[w] : 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (want >= at && want < at + nb[i]) {
+      const int first = r[i].z - r[i].y, j = first / P + (want - at);
+      it.s = s0 + i;
+      it.r0 = max(first, j * P);
+      it.m = min(r[i].z, (j + 1) * P) - it.r0;
+      it.t0 = r[i].x + (it.r0 - first);
     }
+    at += nb[i];
   }
   __syncthreads();
   return it;
@@ -199,7 +203,7 @@ __global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(A
 constexpr int APP_HEADS = 3;  // heads whose loads a thread has in flight
 
 template <int D>
-__global__ void __launch_bounds__(APP_THREADS) kv_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(APP_THREADS, 3) kv_append_kernel(AppendArgs a) {
   constexpr int LANES = D / 16, UNITS = APP_THREADS / LANES, WARPS = APP_THREADS / 32;
   const int tid = threadIdx.x, h = blockIdx.y, G = a.G, P = a.c.block_rows;
   __shared__ uint32_t bounds[WARPS][2][D / 2];  // of each warp: largest, smallest keys
