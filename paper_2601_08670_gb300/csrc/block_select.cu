@@ -30,9 +30,6 @@ struct SelectArgs {
   int* status;
 };
 
-// Place j of the i-th block of a cluster's CTA: the CTAs take turns at 32 blocks.
-__device__ __forceinline__ int place_of(int i, int ctas, int rank) { return (i / 32 * ctas + rank) * 32 + i % 32; }
-
 // Exclusive prefix over the CTA's threads of x (all threads; wsum: a word per warp).
 __device__ __forceinline__ uint32_t cta_prefix(uint32_t x, uint32_t* wsum) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -49,12 +46,50 @@ __device__ __forceinline__ uint32_t cta_prefix(uint32_t x, uint32_t* wsum) {
   return before;
 }
 
-// A cluster of CTAs shares a row: each scores its part of the blocks, BSEL_BATCH
-// of them in flight per group of lanes, and puts the scores into the first CTA's
-// shared memory, which selects alone.
+// Scores of the BSEL_BATCH * 32 / LANES blocks whose pool numbers lie in the
+// lanes from `first` on (-1: none): LANES lanes share a block, BSEL_BATCH blocks
+// of theirs are in flight.  With LANES >= BSEL_BATCH the sums cross the lanes in
+// halves, so that in the end LANES / BSEL_BATCH lanes hold each block's.
+template <int D>
+struct Scorer {
+  static constexpr int LANES = 2 * D / 16, SIDE = 32 / LANES;  // lanes of a block, blocks side by side
+  int4 w[BSEL_BATCH];
+  __device__ __forceinline__ void load(const int8_t* summary, int64_t page, int entry, int first, int lane) {
+#pragma unroll
+    for (int u = 0; u < BSEL_BATCH; ++u) {
+      const int blk = __shfl_sync(0xffffffffu, entry, first + u * SIDE + lane / LANES);
+      w[u] = make_int4(0, 0, 0, 0);
+      if (blk >= 0) w[u] = reinterpret_cast<const int4*>(summary + blk * page)[lane % LANES];
+    }
+  }
+  // the score of block first + slot() * SIDE + lane / LANES
+  __device__ __forceinline__ int sum(int4 pq, int lane) const {
+    int v[BSEL_BATCH];
+#pragma unroll
+    for (int u = 0; u < BSEL_BATCH; ++u)
+      v[u] = __dp4a(w[u].x, pq.x, __dp4a(w[u].y, pq.y, __dp4a(w[u].z, pq.z, __dp4a(w[u].w, pq.w, 0))));
+    int o = LANES / 2;
+#pragma unroll
+    for (int half = BSEL_BATCH / 2; half > 0; half /= 2, o /= 2) {
+      const bool upper = lane & o;
+#pragma unroll
+      for (int u = 0; u < half; ++u) {
+        const int give = upper ? v[u] : v[u + half], keep = upper ? v[u + half] : v[u];
+        v[u] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      }
+    }
+    for (; o > 0; o /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    return v[0];
+  }
+  static __device__ __forceinline__ int slot(int lane) { return lane % LANES / (LANES / BSEL_BATCH); }
+  static __device__ __forceinline__ bool writes(int lane) { return lane % (LANES / BSEL_BATCH) == 0; }
+};
+
+// A cluster of CTAs shares a row: their warps take turns at 32 blocks and put the
+// scores into the first CTA's shared memory, which selects alone.
 template <int D>
 __global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArgs a) {
-  extern __shared__ int32_t scores[];  // [blocks of the sequence]; before a block's score, its pool block
+  extern __shared__ int32_t scores[];  // [blocks of the sequence]
   __shared__ __align__(16) int8_t pooled[2 * D];
   __shared__ float wmax[BSEL_THREADS / 32];
   __shared__ int2 wrange[BSEL_THREADS / 32];
@@ -68,9 +103,10 @@ __global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArg
   if (ctas > 1) cluster.barrier_arrive();  // (the first CTA runs before its memory is written)
   pdl_wait();
   // the length, this thread's part of the queries and its first table entry arrive together
-  const int j_tid = place_of(tid, ctas, rank);
   const int32_t* table = a.c.block_table + (int64_t)s * a.c.max_blocks;
-  int entry = j_tid < a.c.max_blocks ? table[j_tid] : 0;
+  const int stride = ctas * BSEL_THREADS;
+  int j = (warp * ctas + rank) * 32 + lane;
+  int entry = j < a.c.max_blocks ? table[j] : -1;
   float x[PAGED_MAX_G];
   if (tid < 2 * D) {
     const __nv_bfloat16* q = a.q + s * a.q_stride + (int64_t)h * a.G * D + tid % D;
@@ -87,16 +123,19 @@ __global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArg
     if (ctas > 1) cluster.barrier_wait();
     return;
   }
-  for (int i = tid, j = j_tid; j < nb;) {
-    if (entry < 0 || entry >= a.c.num_blocks) {
+  const int64_t page = (int64_t)a.c.Hkv * 2 * D;  // bytes of a block's summaries
+  const int8_t* summary = a.c.summary + h * 2 * D;
+  Scorer<D> sc;
+  const auto check = [&](int j) {  // the lane's entry, -1 where there is no such block
+    if (j >= nb) {
+      entry = -1;
+    } else if (entry < 0 || entry >= a.c.num_blocks) {
       dev_flag(a.status, PCED_DEV_BAD_BLOCK);
       entry = -1;
     }
-    scores[j] = entry;
-    i += BSEL_THREADS;
-    j = place_of(i, ctas, rank);
-    if (j < nb) entry = table[j];
-  }
+  };
+  check(j);
+  sc.load(summary, page, entry, 0, lane);  // the first blocks come while the queries are pooled
   // ---- the pooled query
   float p = 0.f, m = 0.f;
   if (tid < 2 * D) {
@@ -117,30 +156,22 @@ __global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArg
     pooled[tid] = m > 0.f && m < INFINITY ? (int8_t)(int)rintf(__fmul_rn(p, __fdiv_rn(127.f, m))) : (int8_t)0;
   __syncthreads();
   if (ctas > 1) cluster.barrier_wait();
-  // ---- scores: 2D / 16 lanes a block
-  constexpr int LANES = 2 * D / 16, STRIDE = BSEL_THREADS / LANES;
+  // ---- scores
+  constexpr int LANES = Scorer<D>::LANES, SIDE = Scorer<D>::SIDE;
   int32_t* out = ctas > 1 ? cluster.map_shared_rank(scores, 0) : scores;
-  const int l = tid % LANES;
-  const int4 pq = reinterpret_cast<const int4*>(pooled)[l];
-  for (int i0 = 0; place_of(i0, ctas, rank) < nb; i0 += BSEL_BATCH * STRIDE) {
-    int4 w[BSEL_BATCH];
-    int blk[BSEL_BATCH];
+  const int4 pq = reinterpret_cast<const int4*>(pooled)[lane % LANES];
+  for (int jw = j - lane; jw < nb; jw += stride) {  // 32 blocks of this warp
+    const int next = jw + stride + lane < a.c.max_blocks ? table[jw + stride + lane] : -1;
 #pragma unroll
-    for (int u = 0; u < BSEL_BATCH; ++u) {
-      const int j = place_of(i0 + u * STRIDE + tid / LANES, ctas, rank);
-      blk[u] = j < nb ? scores[j] : -1;
-      w[u] = make_int4(0, 0, 0, 0);
-      if (blk[u] >= 0)
-        w[u] = reinterpret_cast<const int4*>(a.c.summary + ((int64_t)blk[u] * a.c.Hkv + h) * 2 * D)[l];
+    for (int first = 0; first < 32; first += BSEL_BATCH * SIDE) {
+      if (first > 0 || jw != j - lane) sc.load(summary, page, entry, first, lane);
+      const int mine = first + Scorer<D>::slot(lane) * SIDE + lane / LANES;
+      const int blk = __shfl_sync(0xffffffffu, entry, mine);
+      const int v = sc.sum(pq, lane);
+      if (Scorer<D>::writes(lane) && jw + mine < nb) out[jw + mine] = blk < 0 ? BSEL_WORST : v;
     }
-#pragma unroll
-    for (int u = 0; u < BSEL_BATCH; ++u) {
-      const int j = place_of(i0 + u * STRIDE + tid / LANES, ctas, rank);
-      int sc = __dp4a(w[u].x, pq.x, __dp4a(w[u].y, pq.y, __dp4a(w[u].z, pq.z, __dp4a(w[u].w, pq.w, 0))));
-#pragma unroll
-      for (int o = 1; o < LANES; o <<= 1) sc += __shfl_xor_sync(0xffffffffu, sc, o);
-      if (l == 0 && j < nb) out[j] = blk[u] < 0 ? BSEL_WORST : sc;
-    }
+    entry = next;
+    check(jw + stride + lane);
   }
   if (ctas > 1) cluster.sync();
   else __syncthreads();

@@ -23,7 +23,7 @@ struct AppendArgs {
   int* status;
 };
 
-constexpr int APP_THREADS = 256;
+constexpr int APP_THREADS = 128;
 
 // tokens [t0, t0 + m) of one sequence, which go to rows r0 ... of one block
 struct AppendItem {
@@ -157,7 +157,7 @@ __device__ __forceinline__ void update_summary(int8_t* summary, int D, int f, co
 template <int D>
 __global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(AppendArgs a) {
   constexpr int LANES = D / 16;
-  const int tid = threadIdx.x, s = blockIdx.x, h = blockIdx.y, G = a.G, P = a.c.block_rows;
+  const int tid = threadIdx.x, s = blockIdx.y, h = blockIdx.x, G = a.G, P = a.c.block_rows;
   const int role = tid / LANES, f = 8 * (tid % LANES);  // role 0: key, 1: value, then queries
   if (role >= G + 2) return;
   pdl_wait();
@@ -203,12 +203,13 @@ __global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(A
 constexpr int APP_HEADS = 3;  // heads whose loads a thread has in flight
 
 template <int D>
-__global__ void __launch_bounds__(APP_THREADS, 3) kv_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a) {
   constexpr int LANES = D / 16, UNITS = APP_THREADS / LANES, WARPS = APP_THREADS / 32;
-  const int tid = threadIdx.x, h = blockIdx.y, G = a.G, P = a.c.block_rows;
+  // (the heads of an item side by side: their parts of a token's row are neighbours in memory)
+  const int tid = threadIdx.x, h = blockIdx.x % a.c.Hkv, G = a.G, P = a.c.block_rows;
   __shared__ uint32_t bounds[WARPS][2][D / 2];  // of each warp: largest, smallest keys
   pdl_wait();
-  const AppendItem it = find_item(a, blockIdx.x);
+  const AppendItem it = find_item(a, blockIdx.x / a.c.Hkv);
   if (it.s < 0) return;
   const int blk = paged_block(a.c, it.s, it.r0 / P, a.status);
   const int64_t page = (int64_t)blk * a.c.Hkv + h;
@@ -350,8 +351,7 @@ pced_status check_paged_cache(const pced_paged_cache* c, const char* fn) {
   if (c->S > PAGED_MAX_S) return fail(PCED_ERR_UNSUPPORTED, "%s: %d sequences, at most %d", fn, c->S, PAGED_MAX_S);
   if ((int64_t)c->max_blocks * c->block_rows + c->block_rows > INT32_MAX)
     return fail(PCED_ERR_UNSUPPORTED, "%s: a sequence's table holds 2^31 rows or more", fn);
-  // (Hkv is the y extent of a grid)
-  if (c->Hkv > 65535 || (int64_t)c->num_blocks * c->Hkv >= (INT64_C(1) << 31) ||
+  if ((int64_t)c->num_blocks * c->Hkv >= (INT64_C(1) << 31) ||
       (int64_t)c->num_blocks * c->Hkv * c->block_rows >= (INT64_C(1) << 31))
     return fail(PCED_ERR_UNSUPPORTED, "%s: more than 2^31 rows in the pool", fn);
   return PCED_OK;
@@ -402,13 +402,13 @@ extern "C" pced_status pced_kv_append(const pced_paged_cache* cache, const void*
   cudaError_t e;
   if (!tok_start) {
     const int threads = (a.G + 2) * (c.D / 16);
-    e = launch_pdl(c.D == 128 ? kv_append_one_kernel<128> : kv_append_one_kernel<64>, dim3(c.S, c.Hkv), threads, 0,
+    e = launch_pdl(c.D == 128 ? kv_append_one_kernel<128> : kv_append_one_kernel<64>, dim3(c.Hkv, c.S), threads, 0,
                    (cudaStream_t)stream, a);
   } else {
     // blocks touched: at most two more than whole ones for every sequence with tokens
     const int64_t items = (int64_t)T / c.block_rows + 2 * (int64_t)(T < c.S ? T : c.S);
-    if (items >= (INT64_C(1) << 31)) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
-    e = launch_pdl(c.D == 128 ? kv_append_kernel<128> : kv_append_kernel<64>, dim3((unsigned)items, c.Hkv), APP_THREADS,
+    if (items * c.Hkv >= (INT64_C(1) << 31)) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
+    e = launch_pdl(c.D == 128 ? kv_append_kernel<128> : kv_append_kernel<64>, dim3((unsigned)(items * c.Hkv)), APP_THREADS,
                    0, (cudaStream_t)stream, a);
   }
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "kv_append launch");

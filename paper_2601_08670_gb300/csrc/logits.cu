@@ -17,14 +17,15 @@ namespace pced {
 constexpr int LOG_THREADS = 256;
 constexpr int LOG_TOK = 8;  // tokens of a thread
 constexpr int LOG_CHUNK = LOG_THREADS * LOG_TOK;
-constexpr int LOG_ROWS = 2;  // rows in flight
+constexpr int LOG_CTAS = 4;  // CTAs that an SM holds
+constexpr int LOG_WAVES = 3;  // CTAs for so many SM fillings, where there are rows enough
+constexpr int LOG_HIST = 8;  // history tokens of a thread in flight
 
 struct LogitsArgs {
   const float* x;
   float* y;
   int64_t stride;
-  int32_t R, V, chunks;
-  int64_t total, per;  // rows of all chunks; of a CTA
+  int32_t R, V, rows;  // rows: of a CTA
   const int32_t* history;
   int32_t history_stride;
   const int32_t* history_len;
@@ -65,95 +66,89 @@ __device__ __forceinline__ void store_row(const LogitsArgs& a, int64_t at, int v
   }
 }
 
-// Rows of the call are cut into equal contiguous ranges of (query, chunk, row), one
-// per CTA, so a CTA counts a chunk's tokens once for all rows it has of it.
 template <bool VEC>
-__global__ void __launch_bounds__(LOG_THREADS, 4) logits_process_kernel(LogitsArgs a) {
+__global__ void __launch_bounds__(LOG_THREADS, LOG_CTAS) logits_process_kernel(LogitsArgs a) {
   __shared__ __align__(16) int32_t count[LOG_CHUNK];
-  __shared__ __align__(16) int32_t named[LOG_CHUNK];  // 1 + the last bias entry of the token
-  const int tid = threadIdx.x;
+  __shared__ __align__(16) int32_t named[LOG_CHUNK];  // 1 + the last bias entry of the token; then the bias itself
+  const int tid = threadIdx.x, b = blockIdx.z, v0 = blockIdx.x * LOG_CHUNK;
+  const int r0 = blockIdx.y * a.rows, r1 = min(a.R, r0 + a.rows);
+  const bool reports = blockIdx.x == 0 && blockIdx.y == 0;
+  for (int i = tid; i < LOG_CHUNK / 4; i += LOG_THREADS) {
+    reinterpret_cast<int4*>(count)[i] = make_int4(0, 0, 0, 0);
+    reinterpret_cast<int4*>(named)[i] = make_int4(0, 0, 0, 0);
+  }
   pdl_wait();
-  const int64_t end = min(a.total, (blockIdx.x + 1) * a.per);
-  for (int64_t at = blockIdx.x * a.per; at < end;) {
-    const int group = (int)(at / a.R), r0 = (int)(at - (int64_t)group * a.R);
-    const int r1 = (int)min((int64_t)a.R, r0 + (end - at));
-    at += r1 - r0;
-    const int b = group / a.chunks, v0 = (group - b * a.chunks) * LOG_CHUNK;
-    const bool reports = v0 == 0 && r0 == 0;
-    const int64_t row0 = (int64_t)b * a.R * a.stride + v0;
-    float x[LOG_ROWS][LOG_TOK];  // the first rows come while the tokens are counted
+  const int64_t row0 = (int64_t)b * a.R * a.stride + v0;
+  float x[LOG_TOK];  // the first row comes while the tokens are counted
+  load_row<VEC>(a, row0 + r0 * a.stride, v0, x);
+  int n = 0, m = -1;
+  float rep = 1.f, freq = 0.f, pres = 0.f;
+  if (a.history) {
+    n = a.history_len[b];
+    rep = a.penalties[3 * b], freq = a.penalties[3 * b + 1], pres = a.penalties[3 * b + 2];
+  }
+  if (a.mask) m = a.mask_row ? a.mask_row[b] : b;
+  if (n < 0 || n > a.history_stride) {
+    if (reports && tid == 0) dev_flag(a.status, PCED_DEV_BAD_LENGTH);
+    n = n < 0 ? 0 : a.history_stride;
+  }
+  if (m < -1 || m >= a.n_masks) {
+    if (reports && tid == 0) dev_flag(a.status, PCED_DEV_BAD_INDEX);
+    m = -1;
+  }
+  __syncthreads();
+  // bits to keep of this thread's tokens: none where the mask forbids them
+  uint32_t keep[LOG_TOK];
 #pragma unroll
-    for (int u = 0; u < LOG_ROWS; ++u)
-      if (r0 + u < r1) load_row<VEC>(a, row0 + (r0 + u) * a.stride, v0, x[u]);
-    float rep = 1.f, freq = 0.f, pres = 0.f;
-    for (int i = tid; i < LOG_CHUNK / 4; i += LOG_THREADS) {
-      reinterpret_cast<int4*>(count)[i] = make_int4(0, 0, 0, 0);
-      reinterpret_cast<int4*>(named)[i] = make_int4(0, 0, 0, 0);
-    }
-    __syncthreads();
-    if (a.history) {
-      rep = a.penalties[3 * b], freq = a.penalties[3 * b + 1], pres = a.penalties[3 * b + 2];
-      int n = a.history_len[b];
-      if (n < 0 || n > a.history_stride) {
-        if (reports && tid == 0) dev_flag(a.status, PCED_DEV_BAD_LENGTH);
-        n = n < 0 ? 0 : a.history_stride;
-      }
-      const int32_t* hist = a.history + (int64_t)b * a.history_stride;
-      for (int i0 = tid; i0 < n; i0 += 4 * LOG_THREADS) {
-        int t[4];
+  for (int e = 0; e < LOG_TOK; ++e) {
+    const int v = v0 + token_of<VEC>(e);
+    keep[e] = 0xFFFFFFFFu;
+    if (m >= 0 && v < a.V) keep[e] = a.mask[(int64_t)m * a.mask_words + (v >> 5)] >> (v & 31) & 1u ? 0xFFFFFFFFu : 0u;
+  }
+  const int32_t* hist = a.history + (int64_t)b * a.history_stride;
+  for (int i0 = tid; i0 < n; i0 += LOG_HIST * LOG_THREADS) {
+    int t[LOG_HIST];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) t[u] = i0 + u * LOG_THREADS < n ? hist[i0 + u * LOG_THREADS] : -1;
+    for (int u = 0; u < LOG_HIST; ++u) t[u] = i0 + u * LOG_THREADS < n ? hist[i0 + u * LOG_THREADS] : -1;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if ((unsigned)(t[u] - v0) < (unsigned)LOG_CHUNK && t[u] < a.V) atomicAdd(&count[t[u] - v0], 1);
-          if (reports && (t[u] < -1 || t[u] >= a.V)) dev_flag(a.status, PCED_DEV_BAD_TOKEN);
-        }
-      }
+    for (int u = 0; u < LOG_HIST; ++u) {
+      if ((unsigned)(t[u] - v0) < (unsigned)LOG_CHUNK && t[u] < a.V) atomicAdd(&count[t[u] - v0], 1);
+      if (reports && (t[u] < -1 || t[u] >= a.V)) dev_flag(a.status, PCED_DEV_BAD_TOKEN);
     }
-    for (int i = tid; i < a.n_bias; i += LOG_THREADS) {
-      const int t = a.bias_ids[(int64_t)b * a.n_bias + i];
-      if ((unsigned)(t - v0) < (unsigned)LOG_CHUNK && t < a.V) atomicMax(&named[t - v0], i + 1);
-      if (reports && (t < -1 || t >= a.V)) dev_flag(a.status, PCED_DEV_BAD_TOKEN);
-    }
-    const uint32_t* mask = nullptr;
-    if (a.mask) {
-      const int m = a.mask_row ? a.mask_row[b] : b;
-      if (m >= 0 && m < a.n_masks) mask = a.mask + (int64_t)m * a.mask_words;
-      else if (m != -1 && reports && tid == 0) dev_flag(a.status, PCED_DEV_BAD_INDEX);
-    }
-    __syncthreads();
-    // this thread's tokens
-    float cnt[LOG_TOK], add[LOG_TOK];
-    uint32_t allowed = 0;
+  }
+  for (int i = tid; i < a.n_bias; i += LOG_THREADS) {
+    const int t = a.bias_ids[(int64_t)b * a.n_bias + i];
+    if ((unsigned)(t - v0) < (unsigned)LOG_CHUNK && t < a.V) atomicMax(&named[t - v0], i + 1);
+    if (reports && (t < -1 || t >= a.V)) dev_flag(a.status, PCED_DEV_BAD_TOKEN);
+  }
+  __syncthreads();
+  // Which of the warp's places hold a repeated or a biased token: only there are
+  // the counts and biases looked at again, row by row.
+  uint32_t special = 0;
+#pragma unroll
+  for (int e = 0; e < LOG_TOK; ++e) {
+    const int i = token_of<VEC>(e), w = named[i];
+    if (w) named[i] = __float_as_int(a.bias[(int64_t)b * a.n_bias + w - 1]);  // (this thread's own from here on)
+    if (__any_sync(0xffffffffu, w | count[i])) special |= 1u << e;
+  }
+  for (int r = r0; r < r1; ++r) {
+    float next[LOG_TOK];  // ... and each other one while the one before it is processed
+    if (r + 1 < r1) load_row<VEC>(a, row0 + (r + 1) * a.stride, v0, next);
 #pragma unroll
     for (int e = 0; e < LOG_TOK; ++e) {
-      const int i = token_of<VEC>(e), v = v0 + i;
-      cnt[e] = (float)count[i];
-      const int w = named[i];
-      add[e] = w ? a.bias[(int64_t)b * a.n_bias + w - 1] : 0.f;
-      if (!mask || (v < a.V && (mask[v >> 5] >> (v & 31) & 1u))) allowed |= 1u << e;
-    }
-    __syncthreads();  // (the next group's counts overwrite these)
-    for (int r = r0; r < r1; r += LOG_ROWS) {
-      if (r > r0) {
-#pragma unroll
-        for (int u = 0; u < LOG_ROWS; ++u)
-          if (r + u < r1) load_row<VEC>(a, row0 + (r + u) * a.stride, v0, x[u]);
+      if (special >> e & 1u) {
+        const int i = token_of<VEC>(e);
+        const float cnt = (float)count[i], add = __int_as_float(named[i]);
+        if (cnt > 0.f)
+          x[e] = __fsub_rn(x[e] > 0.f ? __fdiv_rn(x[e], rep) : __fmul_rn(x[e], rep),
+                           __fadd_rn(__fmul_rn(cnt, freq), pres));
+        if (add != 0.f) x[e] += add;
       }
-#pragma unroll
-      for (int u = 0; u < LOG_ROWS; ++u) {
-        if (r + u >= r1) break;
-#pragma unroll
-        for (int e = 0; e < LOG_TOK; ++e) {
-          float& y = x[u][e];
-          if (cnt[e] > 0.f)
-            y = __fsub_rn(y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep), __fadd_rn(__fmul_rn(cnt[e], freq), pres));
-          if (add[e] != 0.f) y += add[e];
-          if (!(allowed >> e & 1u)) y = -INFINITY;
-        }
-        store_row<VEC>(a, row0 + (r + u) * a.stride, v0, x[u]);
-      }
+      x[e] = __uint_as_float((__float_as_uint(x[e]) & keep[e]) | (~keep[e] & 0xFF800000u));  // or -inf
     }
+    store_row<VEC>(a, row0 + r * a.stride, v0, x);
+#pragma unroll
+    for (int e = 0; e < LOG_TOK; ++e) x[e] = next[e];
   }
 }
 
@@ -170,7 +165,7 @@ extern "C" pced_status pced_logits_process(const float* x, float* y, int64_t str
                                            const int32_t* mask_row, int32_t* status, void* stream) {
   const char* fn = "pced_logits_process";
   if (!x || !y) return fail(PCED_ERR_INVALID_ARG, "%s: null pointer", fn);
-  if (B < 1 || R < 1 || V < 1 || B > 65535 || (int64_t)B * ((V - 1) / LOG_CHUNK + 1) > INT32_MAX || stride < V) return fail(PCED_ERR_INVALID_ARG, "%s: bad sizes", fn);
+  if (B < 1 || R < 1 || V < 1 || B > 65535 || R > 65535 || stride < V) return fail(PCED_ERR_INVALID_ARG, "%s: bad sizes", fn);
   if (!history != !penalties || !history != !history_len || (history && history_stride < 1))
     return fail(PCED_ERR_INVALID_ARG, "%s: history, history_len and penalties go together", fn);
   if (n_bias < 0 || !bias_ids != !bias || (n_bias > 0) != (bias_ids != nullptr))
@@ -189,12 +184,12 @@ extern "C" pced_status pced_logits_process(const float* x, float* y, int64_t str
   a.bias_ids = bias_ids, a.bias = bias, a.n_bias = n_bias;
   a.mask = mask, a.n_masks = n_masks, a.mask_words = mask_words, a.mask_row = mask_row;
   a.status = status;
-  a.chunks = (V - 1) / LOG_CHUNK + 1;
-  a.total = (int64_t)a.chunks * B * R;
-  const int64_t ctas = 4 * (int64_t)num_sms();  // what the SMs hold at a time
-  a.per = (a.total + ctas - 1) / ctas;
+  const int chunks = (V - 1) / LOG_CHUNK + 1;
+  const int64_t total = (int64_t)chunks * B * R, ctas = LOG_WAVES * LOG_CTAS * (int64_t)num_sms();
+  const int64_t parts = min((int64_t)R, max((int64_t)1, R / max((int64_t)1, total / ctas)));
+  a.rows = (int)((R + parts - 1) / parts);
   const bool vec = V % 4 == 0 && stride % 4 == 0 && (((uintptr_t)x | (uintptr_t)y) & 15u) == 0;
-  const dim3 grid((unsigned)((a.total + a.per - 1) / a.per));
+  const dim3 grid(chunks, (R - 1) / a.rows + 1, B);
   const cudaError_t e = vec ? launch_pdl(logits_process_kernel<true>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a)
                             : launch_pdl(logits_process_kernel<false>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "logits_process launch");

@@ -22,7 +22,7 @@ namespace pced {
 
 constexpr int PATT_MAX_CTAS = 256;  // sizes the records and counters of the workspace
 constexpr int PATT_GRAN = 16;       // rows of a consumer warp, and of a small box
-constexpr int PATT_MIN_TILES = 4;   // tiles of a CTA where there are few
+constexpr int PATT_MIN_TILES = 1;   // tiles of a CTA where there are few
 
 struct PagedAttArgs {
   pced_paged_cache c;
