@@ -95,7 +95,7 @@ __device__ __forceinline__ void write_out(const PagedAttArgs& a, int s, int h, i
 // 2c + 1, 2(c + 1), 2(c + 2), ...
 __device__ __forceinline__ void merge_records(const PagedAttArgs& a, int c, int n, int D, int hh, int idx0, float& mx,
                                               float& lsum, float (&acc)[4]) {
-  constexpr int BATCH = 4;  // records in flight
+  constexpr int BATCH = 8;  // records in flight
   const int GD = a.G * D;
   for (int i0 = 0; i0 < n; i0 += BATCH) {
     float2 ml[BATCH];
@@ -218,13 +218,13 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
       if (p0 + lane < r_end) {
         const PagedPiece pc = paged_piece(pre, S, Hkv, p0 + lane, r_end);
         const int32_t n = lens[pc.s];
-        const int32_t nb = (n + P - 1) / P;
+        const int32_t nb = (int32_t)((uint32_t)(n + P - 1) / (uint32_t)P);
         const int32_t* sel = a.sel ? a.sel + ((int64_t)pc.s * Hkv + pc.h) * a.n_sel : nullptr;
         const int32_t places = sel ? min(a.n_sel, nb) : nb;
 #pragma unroll
         for (int i = 0; i < (SMALL ? NG : 1); ++i) {
-          const int64_t r = pc.t0 * ATT_BLOCK_N + i * PATT_GRAN;  // row of the list
-          const int32_t place = (int32_t)(r / P), at = (int32_t)(r - (int64_t)place * P);
+          const uint32_t r = (uint32_t)pc.t0 * ATT_BLOCK_N + i * PATT_GRAN;  // row of the list
+          const int32_t place = (int32_t)(r / (uint32_t)P), at = (int32_t)(r - (uint32_t)place * P);
           row[i] = 0;
           if (place >= places) continue;
           const int32_t j = sel ? sel[place] : place;
@@ -372,11 +372,11 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
     if (own) {
       *reinterpret_cast<float4*>(a.rec_o + slot * GD + idx0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
       if (idx0 % D == 0) a.rec_ml[slot * G + hh] = make_float2(mx, lsum);
-      __threadfence();
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_pempty);
     if (!mbar_wait(bar_pempty, np & 1u, a.status)) return;  // all warps' records are written
+    // (its release and acquire at gpu scope carry what the barriers ordered for the other threads)
     if (tid == 0) *last_here = atom_acq_rel_gpu_add(a.parts + first, 1) == n - 1;
     // (a second round of the same two barriers hands the answer over)
     ++np;
@@ -384,7 +384,6 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
     if (lane == 0) mbar_arrive(bar_pfull);
     if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
     if (*last_here) {
-      __threadfence();
       mx = -INFINITY, lsum = 0.f;
       acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
       if (own) {
