@@ -22,7 +22,8 @@ namespace pced {
 
 constexpr int PATT_MAX_CTAS = 256;  // sizes the records and counters of the workspace
 constexpr int PATT_GRAN = 16;       // rows of a consumer warp, and of a small box
-constexpr int PATT_MIN_TILES = 1;   // tiles of a CTA where there are few
+constexpr int PATT_EPI = 3;         // epilogue warps
+constexpr int PATT_THREADS = (ATT_CONSUMERS + 1 + PATT_EPI) * 32;
 
 struct PagedAttArgs {
   pced_paged_cache c;
@@ -43,39 +44,63 @@ struct PagedAttArgs {
 
 // The tiles [t0, t1) of segment (s, h) that a CTA holds; nt tiles in all.
 struct PagedPiece {
-  int32_t s, h;
-  int64_t t0, t1, nt;
+  int32_t s, h, t0, t1, nt;
+};
+// Positions: sequence s begins at base[s]; its heads follow one another, tiles[s] each.
+struct PagedPlan {
+  const int32_t* base;   // [S + 1]
+  const int32_t* tiles;  // [S]
+  int32_t S, Hkv;
+  __device__ __forceinline__ PagedPiece at(int32_t p, int32_t end) const {
+    int32_t lo = 0, hi = S - 1;
+    while (lo < hi) {  // the last sequence that begins at or before p (one without tiles begins where the next does)
+      const int32_t mid = (lo + hi + 1) >> 1;
+      if (base[mid] <= p) lo = mid;
+      else hi = mid - 1;
+    }
+    PagedPiece pc;
+    pc.s = lo;
+    pc.nt = tiles[lo];
+    const uint32_t off = p - base[lo];
+    pc.h = off / (uint32_t)pc.nt;
+    pc.t0 = off - pc.h * pc.nt;
+    pc.t1 = min(pc.nt, pc.t0 + (end - p));
+    return pc;
+  }
+  // the piece after one that ended at its segment's end, at position p < end
+  __device__ __forceinline__ PagedPiece after(PagedPiece pc, int32_t p, int32_t end) const {
+    if (++pc.h == Hkv) {
+      pc.h = 0;
+      do ++pc.s;
+      while (tiles[pc.s] == 0);
+      pc.nt = tiles[pc.s];
+    }
+    pc.t0 = 0;
+    pc.t1 = min(pc.nt, end - p);
+    return pc;
+  }
 };
 
-// Positions: sequence s begins at Hkv * pre[s]; its heads follow one another, nt tiles each.
-__device__ __forceinline__ PagedPiece paged_piece(const int64_t* pre, int32_t S, int32_t Hkv, int64_t p, int64_t end) {
-  int32_t lo = 0, hi = S - 1;
-  while (lo < hi) {  // the last sequence that begins at or before p (sequences without tiles begin where the next does)
-    const int32_t mid = (lo + hi + 1) >> 1;
-    if (pre[mid] * Hkv <= p) lo = mid;
-    else hi = mid - 1;
-  }
-  PagedPiece pc;
-  pc.s = lo;
-  pc.nt = pre[lo + 1] - pre[lo];
-  const int64_t off = p - pre[lo] * Hkv;
-  pc.h = (int32_t)((((uint64_t)off | (uint64_t)pc.nt) >> 32) ? off / pc.nt : (uint32_t)off / (uint32_t)pc.nt);
-  pc.t0 = off - pc.h * pc.nt;
-  pc.t1 = min(pc.nt, pc.t0 + (end - p));
-  return pc;
+// Barrier of the epilogue's warps (bounded); `phase` is the caller's phase bit.
+__device__ __forceinline__ bool bar_sync_warps(uint32_t bar, uint32_t& phase, int lane, int* status) {
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+  const bool ok = mbar_wait(bar, phase, status);
+  phase ^= 1u;
+  return ok;
 }
 
 template <int D>
 struct PagedCfg : AttCfg<D> {
   using B = AttCfg<D>;
-  static constexpr size_t BARS = (2 * B::STAGES + 2) * 8;
+  static constexpr size_t BARS = (2 * B::STAGES + 4) * 8;
   static constexpr size_t DESC = (size_t)B::STAGES * 4;
   static constexpr size_t SMEM = 1024 + (size_t)B::STAGES * B::STAGE_BYTES + BARS + (size_t)B::PARTIALS * 4 +
-                                 (PAGED_MAX_S + 1) * 8 + PAGED_MAX_S * 4 + DESC + 64;
+                                 (3 * PAGED_MAX_S + 1) * 4 + DESC + 64;
+  static_assert(BARS % 16 == 0, "the partials are read as float4");
 };
 
-// Writes four outputs of a finished segment (all 256 consumer threads; the
-// first G*D/4 hold outputs), normalised.
+// Writes four outputs of a finished segment, normalised.
 __device__ __forceinline__ void write_out(const PagedAttArgs& a, int s, int h, int D, int hh, int idx0, float mx,
                                           float lsum, const float (&acc)[4]) {
   const float w = mx == -INFINITY ? 0.f : 1.f / lsum;
@@ -130,10 +155,64 @@ __device__ __forceinline__ void merge_records(const PagedAttArgs& a, int c, int 
   }
 }
 
+// A piece's partials, merged, into the output (a whole segment) or into a record,
+// and the segment's records into the output where this was the last of them to
+// come.  NT threads, whole warps, with a barrier of their own; seq0: the position at
+// which the piece's sequence begins; bar_read: told when the partials have been
+// read (0: nobody waits).
+template <int D, int NT>
+__device__ __forceinline__ bool finish_piece(const PagedAttArgs& a, const PagedPiece& pc, int32_t seq0, int32_t per,
+                                             const float* ms, const float* ls, const float* os, int et, uint32_t bar,
+                                             uint32_t& phase, uint32_t bar_read, int32_t* last_here) {
+  const int G = a.G, GD = G * D, lane = et & 31;
+  const bool whole = pc.t0 == 0 && pc.t1 == pc.nt;
+  // a part of a segment: record 2c of CTA c when it began in an earlier CTA,
+  // 2c + 1 when it begins here
+  const int64_t slot = 2 * (int64_t)blockIdx.x + (pc.t0 == 0 ? 1 : 0);
+  for (int i = et; i < GD / 4; i += NT) {
+    const int hh = i / (D / 4), idx0 = 4 * i;
+    float mx = -INFINITY, lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    load_merged<D>(ms, ls, os, G, hh, idx0, mx, lsum, acc);
+    if (whole) {
+      write_out(a, pc.s, pc.h, D, hh, idx0, mx, lsum, acc);
+    } else {
+      *reinterpret_cast<float4*>(a.rec_o + slot * GD + idx0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      if (idx0 % D == 0) a.rec_ml[slot * G + hh] = make_float2(mx, lsum);
+    }
+  }
+  __syncwarp();
+  if (bar_read && lane == 0) mbar_arrive(bar_read);
+  if (whole) return true;
+  const int32_t seg0 = seq0 + pc.h * pc.nt;  // the segment's first position
+  const int first = (uint32_t)seg0 / (uint32_t)per;
+  const int n = (int)((uint32_t)(seg0 + pc.nt - 1) / (uint32_t)per) - first + 1;
+  if (!bar_sync_warps(bar, phase, lane, a.status)) return false;  // all of this CTA's record is written
+  // (its release and acquire at gpu scope carry what the barriers order for the other threads)
+  if (et == 0) *last_here = atom_acq_rel_gpu_add(a.parts + first, 1) == n - 1;
+  if (!bar_sync_warps(bar, phase, lane, a.status)) return false;
+  if (*last_here) {
+    for (int i = et; i < GD / 4; i += NT) {
+      float mx = -INFINITY, lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+      merge_records(a, first, n, D, i / (D / 4), 4 * i, mx, lsum, acc);
+      write_out(a, pc.s, pc.h, D, i / (D / 4), 4 * i, mx, lsum, acc);
+    }
+    if (et == 0) a.parts[first] = 0;
+  }
+  return true;
+}
+
+// Roles: eight consumer warps (the math, and each piece's partials into shared
+// memory), a producer warp (lookups and TMA) and PATT_EPI warps that finish the
+// pieces, so that the consumers go on with the next piece at once: while they
+// finished pieces themselves, a CTA with a segment's end in its range took 2.5 us
+// longer than one without (17.0 and 14.5 us of the 9 x 2081 rows' 19).
+//
+// (Only a CTA's last piece is the consumers' own matter: they are more, and idle.)
+//
 // SMALL: block_rows is no multiple of 64, so every tile comes in 16-row boxes,
 // each of its own block.
 template <int D, bool PK, bool SMALL>
-__global__ void __launch_bounds__(ATT_THREADS, 1)
+__global__ void __launch_bounds__(PATT_THREADS, 1)
     paged_attention_kernel(const __grid_constant__ CUtensorMap ktile, const __grid_constant__ CUtensorMap vtile,
                            const __grid_constant__ CUtensorMap kbox, const __grid_constant__ CUtensorMap vbox,
                            PagedAttArgs a) {
@@ -141,22 +220,24 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
   constexpr int NG = ATT_BLOCK_N / PATT_GRAN;  // small boxes of a tile
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
-  const uint32_t base = (raw + 1023u) & ~1023u;
-  uint8_t* gbase = smem_raw + (base - raw);
-  // layout: stages | full[STAGES] | empty[STAGES] | partials full | partials empty | partials | tables
-  const uint32_t bar_full = base + C::STAGES * C::STAGE_BYTES;
+  const uint32_t smem0 = (raw + 1023u) & ~1023u;
+  uint8_t* gbase = smem_raw + (smem0 - raw);
+  // layout: stages | full[STAGES] | empty[STAGES] | partials full | partials empty | epilogue | last piece | partials | tables
+  const uint32_t bar_full = smem0 + C::STAGES * C::STAGE_BYTES;
   const uint32_t bar_empty = bar_full + C::STAGES * 8;
   const uint32_t bar_pfull = bar_empty + C::STAGES * 8, bar_pempty = bar_pfull + 8;
+  const uint32_t bar_epi = bar_pempty + 8, bar_last = bar_epi + 8;
   float* ms = reinterpret_cast<float*>(gbase + C::STAGES * C::STAGE_BYTES + C::BARS);
   float* ls = ms + ATT_CONSUMERS * ATT_MAX_G;
   float* os = ls + ATT_CONSUMERS * ATT_MAX_G;
-  int64_t* pre = reinterpret_cast<int64_t*>(ms + C::PARTIALS);  // [S + 1] tiles of one head before sequence s
-  int32_t* lens = reinterpret_cast<int32_t*>(pre + PAGED_MAX_S + 1);
+  int32_t* base = reinterpret_cast<int32_t*>(ms + C::PARTIALS);  // [S + 1]
+  int32_t* tiles = base + PAGED_MAX_S + 1;
+  int32_t* lens = tiles + PAGED_MAX_S;
   uint32_t* desc = reinterpret_cast<uint32_t*>(lens + PAGED_MAX_S);  // [STAGES] live rows of a tile's 16-row parts, a byte each
   int32_t* last_here = reinterpret_cast<int32_t*>(desc + C::STAGES);
 
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
-  const int32_t S = a.c.S, Hkv = a.c.Hkv, G = a.G, GD = G * D, P = a.c.block_rows;
+  const int32_t S = a.c.S, Hkv = a.c.Hkv, G = a.G, P = a.c.block_rows;
 
   if (tid == 0) {
     for (int i = 0; i < C::STAGES; ++i) {
@@ -164,7 +245,9 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
       mbar_init(bar_empty + 8 * i, 4);  // the four warps of the consuming warpgroup
     }
     mbar_init(bar_pfull, ATT_CONSUMERS);
-    mbar_init(bar_pempty, ATT_CONSUMERS);
+    mbar_init(bar_pempty, PATT_EPI);
+    mbar_init(bar_epi, PATT_EPI);
+    mbar_init(bar_last, ATT_CONSUMERS);
     mbar_fence_init();
   }
   if (warp == ATT_CONSUMERS && lane == 0) {
@@ -174,49 +257,51 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
     tma_prefetch_desc(&vbox);
   }
   pdl_wait();
-  for (int i = tid; i < S; i += ATT_THREADS) lens[i] = paged_len(a.c, i, a.status);
-  __syncthreads();
-  if (warp == 0) {  // prefix of the tiles
-    const int chunk = (S + 31) / 32, b0 = min(S, lane * chunk), b1 = min(S, b0 + chunk);
-    auto tiles = [&](int i) -> int64_t {
-      int64_t rows = lens[i];
-      if (a.sel) rows = min((int64_t)a.n_sel, (rows + P - 1) / P) * P;
-      return (rows + ATT_BLOCK_N - 1) / ATT_BLOCK_N;
-    };
-    int64_t own = 0;
-    for (int i = b0; i < b1; ++i) own += tiles(i);
-    int64_t incl = own;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    int64_t run = incl - own;
-    for (int i = b0; i < b1; ++i) {
-      pre[i] = run;
-      run += tiles(i);
-    }
-    if (lane == 31) pre[S] = incl;
+  for (int i = tid; i < S; i += PATT_THREADS) {
+    const int32_t n = paged_len(a.c, i, a.status);
+    uint32_t rows = n;
+    if (a.sel) rows = min((uint32_t)a.n_sel, (rows + P - 1) / P) * P;
+    lens[i] = n;
+    tiles[i] = (rows + ATT_BLOCK_N - 1) / ATT_BLOCK_N;
   }
   __syncthreads();
-  const int64_t total = pre[S] * Hkv;
-  const int64_t per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)PATT_MIN_TILES);
-  const int64_t r_begin = min(total, (int64_t)blockIdx.x * per);
-  const int64_t r_end = min(total, r_begin + per);
+  if (warp == 0) {  // prefix of the tiles of all heads
+    const int chunk = (S + 31) / 32, b0 = min(S, lane * chunk), b1 = min(S, b0 + chunk);
+    int32_t own = 0;
+    for (int i = b0; i < b1; ++i) own += tiles[i] * Hkv;
+    int32_t incl = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    int32_t run = incl - own;
+    for (int i = b0; i < b1; ++i) {
+      base[i] = run;
+      run += tiles[i] * Hkv;
+    }
+    if (lane == 31) base[S] = incl;
+  }
+  __syncthreads();
+  const PagedPlan plan = {base, tiles, S, Hkv};
+  const int32_t total = base[S];
+  const int32_t per = (int32_t)((uint32_t)(total + gridDim.x - 1) / gridDim.x);  // tiles of a CTA
+  const int32_t r_begin = (int32_t)min((int64_t)total, (int64_t)blockIdx.x * per);
+  const int32_t r_end = min(total - r_begin, per) + r_begin;
 
   if (warp == ATT_CONSUMERS) {
     // ------------------------------------------------------------ producer
     const uint64_t pol = policy_evict_first();
-    uint32_t st = 0, ph = 0;
-    int64_t it = 0;
+    uint32_t st = 0, ph = 0, it = 0;
     bool ok = true;
-    for (int64_t p0 = r_begin; p0 < r_end && ok; p0 += 32) {
+    for (int32_t p0 = r_begin; p0 < r_end && ok; p0 += 32) {
       // this lane's tile: pool row of each of its parts, live rows of the parts
       int32_t row[SMALL ? NG : 1];
       uint32_t live4 = 0;
       row[0] = 0;
-      if (p0 + lane < r_end) {
-        const PagedPiece pc = paged_piece(pre, S, Hkv, p0 + lane, r_end);
+      const int nt = min(32, r_end - p0);
+      if (lane < nt) {
+        const PagedPiece pc = plan.at(p0 + lane, r_end);
         const int32_t n = lens[pc.s];
         const int32_t nb = (int32_t)((uint32_t)(n + P - 1) / (uint32_t)P);
         const int32_t* sel = a.sel ? a.sel + ((int64_t)pc.s * Hkv + pc.h) * a.n_sel : nullptr;
@@ -234,24 +319,22 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
           }
           const int32_t blk = paged_block(a.c, pc.s, j, a.status);
           if (blk < 0) continue;
-          row[i] = (int32_t)(((int64_t)blk * Hkv + pc.h) * P) + at;
-          const int64_t left = (int64_t)n - (int64_t)j * P - at;  // live rows from here on
+          row[i] = (blk * Hkv + pc.h) * P + at;
+          const int32_t left = n - j * P - at;  // live rows from here on
           if (SMALL) {
-            live4 |= (uint32_t)max((int64_t)0, min(left, (int64_t)PATT_GRAN)) << (8 * i);
+            live4 |= (uint32_t)max(0, min(left, PATT_GRAN)) << (8 * i);
           } else {
 #pragma unroll
-            for (int g = 0; g < NG; ++g)
-              live4 |= (uint32_t)max((int64_t)0, min(left - g * PATT_GRAN, (int64_t)PATT_GRAN)) << (8 * g);
+            for (int g = 0; g < NG; ++g) live4 |= (uint32_t)max(0, min(left - g * PATT_GRAN, PATT_GRAN)) << (8 * g);
           }
         }
       }
-      const int nt = (int)min((int64_t)32, r_end - p0);
       for (int t = 0; t < nt; ++t, ++it) {
         if (!mbar_wait_warp(bar_empty + 8 * st, ph ^ 1u, a.status)) {
           ok = false;
           break;
         }
-        const uint32_t fb = bar_full + 8 * st, sk = base + st * C::STAGE_BYTES, sv = sk + C::TILE_BYTES;
+        const uint32_t fb = bar_full + 8 * st, sk = smem0 + st * C::STAGE_BYTES, sv = sk + C::TILE_BYTES;
         const uint32_t lv = __shfl_sync(0xffffffffu, live4, t);
         const int32_t r0 = __shfl_sync(0xffffffffu, row[0], t);
         const uint32_t on = elect_one();
@@ -289,61 +372,79 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
     }
     if (!ok) {
       // let copies already in flight land before the CTA exits
-      for (int64_t j = (it >= C::STAGES ? it - C::STAGES : 0); j < it; ++j)
-        mbar_wait(bar_full + 8 * (uint32_t)(j % C::STAGES), (uint32_t)(j / C::STAGES) & 1u, a.status);
+      for (uint32_t j = (it >= C::STAGES ? it - C::STAGES : 0); j < it; ++j)
+        mbar_wait(bar_full + 8 * (j % C::STAGES), (j / C::STAGES) & 1u, a.status);
+    }
+    return;
+  }
+
+  if (warp > ATT_CONSUMERS) {
+    // ------------------------------------------------------------ epilogue
+    const int et = tid - (ATT_CONSUMERS + 1) * 32;
+    // sequences without rows
+    for (int s = blockIdx.x; s < S; s += gridDim.x)
+      if (tiles[s] == 0) {
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int i = et; i < a.Hq * (D / 4); i += PATT_EPI * 32)
+          write_out(a, s, 0, D, i / (D / 4), 4 * i, -INFINITY, 0.f, zero);
+      }
+    if (r_begin >= r_end) return;
+    PagedPiece pc = plan.at(r_begin, r_end);
+    uint32_t phase = 0;
+    for (int32_t p = r_begin + pc.t1 - pc.t0, np = 0; p < r_end; p += pc.t1 - pc.t0, ++np) {
+      if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
+      if (!finish_piece<D, PATT_EPI * 32>(a, pc, base[pc.s], per, ms, ls, os, et, bar_epi, phase, bar_pempty, last_here))
+        return;
+      pc = plan.after(pc, p, r_end);
     }
     return;
   }
 
   // -------------------------------------------------------------- consumers
+  if (r_begin >= r_end) return;
   const int wg = warp >> 2, kb = PATT_GRAN * (warp & 3);
   const int g = lane >> 2, tq = lane & 3;
-  const bool own = tid < GD / 4;
-  const int hh = own ? tid / (D / 4) : 0, idx0 = own ? 4 * tid : 0;
-  // sequences without rows
-  for (int s = blockIdx.x; s < S; s += gridDim.x)
-    if (pre[s] == pre[s + 1] && own) {
-      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int h = 0; h < Hkv; ++h) write_out(a, s, h, D, hh, idx0, -INFINITY, 0.f, zero);
-    }
   // B column g of S^T = K Q^T is head g; with PK columns 4-7 repeat heads 0-3
   const int qh = PK ? (g & 3) : g;
   const bool hv = qh < G;
-  uint32_t it = 0, st = 0, use = 0, np = 0;  // tile counter (parity), its stage and use of the stage; pieces done
-  for (int64_t p = r_begin; p < r_end; ++np) {
-    const PagedPiece pc = paged_piece(pre, S, Hkv, p, r_end);
-    p += pc.t1 - pc.t0;
-    uint32_t qf[C::KSTEPS][2];
-    {
-      const uint32_t* qrow = reinterpret_cast<const uint32_t*>(
-          a.q + pc.s * a.q_stride + ((int64_t)pc.h * G + (hv ? qh : 0)) * D);
+  uint32_t qf[C::KSTEPS][2];
+  const auto load_q = [&](const PagedPiece& pc) {
+    const uint32_t* qrow = reinterpret_cast<const uint32_t*>(
+        a.q + pc.s * a.q_stride + ((int64_t)pc.h * G + (hv ? qh : 0)) * D);
 #pragma unroll
-      for (int j = 0; j < C::KSTEPS; ++j) {
-        qf[j][0] = hv ? qrow[8 * j + tq] : 0u;
-        qf[j][1] = hv ? qrow[8 * j + 4 + tq] : 0u;
-      }
+    for (int j = 0; j < C::KSTEPS; ++j) {
+      qf[j][0] = hv ? qrow[8 * j + tq] : 0u;
+      qf[j][1] = hv ? qrow[8 * j + 4 + tq] : 0u;
     }
+  };
+  PagedPiece pc = plan.at(r_begin, r_end);
+  load_q(pc);
+  uint32_t it = 0, st = 0, use = 0, np = 0;  // tile counter, its stage and use of the stage; pieces done
+  for (int32_t p = r_begin;; ++np) {
+    p += pc.t1 - pc.t0;
     WarpAcc<D> A;
     acc_reset(A);
-    bool ok = true;
-    for (int64_t t = pc.t0; t < pc.t1; ++t, ++it, st = st + 1 == C::STAGES ? (++use, 0u) : st + 1) {
+    for (int32_t t = pc.t0; t < pc.t1; ++t, ++it, st = st + 1 == C::STAGES ? (++use, 0u) : st + 1) {
       if ((int)(it & 1u) != wg) continue;
       // (the release of the stage's previous use, by the other warpgroup, comes
       // first: the parity below then means this tile's phase)
       if ((use > 0 && !mbar_wait(bar_empty + 8 * st, (use - 1u) & 1u, a.status)) ||
-          !mbar_wait(bar_full + 8 * st, use & 1u, a.status)) {
-        ok = false;
-        break;
-      }
+          !mbar_wait(bar_full + 8 * st, use & 1u, a.status))
+        return;
       const int live = desc[st] >> (8 * (warp & 3)) & 0xFFu;
       if (live) {
-        const uint32_t sk = base + st * C::STAGE_BYTES;
+        const uint32_t sk = smem0 + st * C::STAGE_BYTES;
         tile_math<D, PK>(A, qf, sk, sk + C::TILE_BYTES, kb, kb + live, a.scale_log2, lane);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_empty + 8 * st);
     }
-    if (!ok) return;
+    const bool more = p < r_end;
+    const PagedPiece last = pc;
+    if (more) {  // the next piece's queries come while this one's partials go
+      pc = plan.after(pc, p, r_end);
+      load_q(pc);
+    }
     // scores that are all not numbers moved no maximum: their sum shall not be dropped with it
     if (__any_sync(0xffffffffu, (A.m0 == -INFINITY && A.l0 != A.l0) || (A.m1 == -INFINITY && A.l1 != A.l1))) {
       A.m0 = A.m0 == -INFINITY ? 0.f : A.m0;
@@ -355,45 +456,12 @@ __global__ void __launch_bounds__(ATT_THREADS, 1)
     store_partial<D>(A, ms, ls, os, G, warp, lane);
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_pfull);
-    if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
-    float mx = -INFINITY, lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    if (own) load_merged<D>(ms, ls, os, G, hh, idx0, mx, lsum, acc);
-    if (pc.t0 == 0 && pc.t1 == pc.nt) {
-      if (own) write_out(a, pc.s, pc.h, D, hh, idx0, mx, lsum, acc);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_pempty);
-      continue;
-    }
-    // a part of a segment: record 2c of CTA c when it began in an earlier CTA,
-    // 2c + 1 when it begins here; the CTA that writes the last one merges them
-    const int64_t seg0 = pre[pc.s] * Hkv + pc.h * pc.nt;  // the segment's first position
-    const int first = (int)(seg0 / per), n = (int)((seg0 + pc.nt - 1) / per) - first + 1;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (pc.t0 == 0 ? 1 : 0);
-    if (own) {
-      *reinterpret_cast<float4*>(a.rec_o + slot * GD + idx0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-      if (idx0 % D == 0) a.rec_ml[slot * G + hh] = make_float2(mx, lsum);
-    }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar_pempty);
-    if (!mbar_wait(bar_pempty, np & 1u, a.status)) return;  // all warps' records are written
-    // (its release and acquire at gpu scope carry what the barriers ordered for the other threads)
-    if (tid == 0) *last_here = atom_acq_rel_gpu_add(a.parts + first, 1) == n - 1;
-    // (a second round of the same two barriers hands the answer over)
-    ++np;
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar_pfull);
-    if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
-    if (*last_here) {
-      mx = -INFINITY, lsum = 0.f;
-      acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-      if (own) {
-        merge_records(a, first, n, D, hh, idx0, mx, lsum, acc);
-        write_out(a, pc.s, pc.h, D, hh, idx0, mx, lsum, acc);
-      }
-      if (tid == 0) a.parts[first] = 0;
-    }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar_pempty);
+    if (more) continue;
+    // the CTA's last piece
+    uint32_t phase = 0;
+    if (mbar_wait(bar_pfull, np & 1u, a.status))
+      finish_piece<D, ATT_CT>(a, last, base[last.s], per, ms, ls, os, tid, bar_last, phase, 0, last_here + 1);
+    return;
   }
 }
 
@@ -422,7 +490,7 @@ static cudaError_t launch_paged(const CUtensorMap (&maps)[4], const PagedAttArgs
   static bool done[64];
   const cudaError_t e = allow_smem(kernel, PagedCfg<D>::SMEM, done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, dim3(ctas), ATT_THREADS, PagedCfg<D>::SMEM, stream, maps[0], maps[1], maps[2], maps[3], a);
+  return launch_pdl(kernel, dim3(ctas), PATT_THREADS, PagedCfg<D>::SMEM, stream, maps[0], maps[1], maps[2], maps[3], a);
 }
 template <int D>
 static cudaError_t launch_paged_d(const CUtensorMap (&maps)[4], const PagedAttArgs& a, int ctas, cudaStream_t stream) {
@@ -450,6 +518,9 @@ extern "C" pced_status pced_paged_attention(const pced_paged_cache* cache, const
   if (q_stride % 8 || q_stride < (int64_t)Hq * c.D)
     return fail(PCED_ERR_INVALID_ARG, "%s: q_stride no multiple of 8 or below a token's heads", fn);
   if (sel ? n_sel < 1 : n_sel != 0) return fail(PCED_ERR_INVALID_ARG, "%s: n_sel without sel, or below 1", fn);
+  // (positions of tiles are 32-bit numbers)
+  if (((int64_t)c.max_blocks * c.block_rows / ATT_BLOCK_N + 2) * c.S * c.Hkv > INT32_MAX)
+    return fail(PCED_ERR_UNSUPPORTED, "%s: tables of 2^31 tiles or more", fn);
   if (!isfinite(scale) || total_rows < 0) return fail(PCED_ERR_INVALID_ARG, "%s: scale or total_rows", fn);
   if (!aligned(workspace, 256) || workspace_bytes < pced_paged_attention_workspace_size(c.S, Hq, c.Hkv, c.D))
     return fail(PCED_ERR_WORKSPACE, "%s: workspace too small or misaligned", fn);
@@ -477,8 +548,7 @@ extern "C" pced_status pced_paged_attention(const pced_paged_cache* cache, const
   int64_t ctas = sms < PATT_MAX_CTAS ? sms : PATT_MAX_CTAS;
   if (total_rows > 0) {
     const int64_t tiles = (total_rows / ATT_BLOCK_N + c.S) * c.Hkv;
-    const int64_t want = (tiles + PATT_MIN_TILES - 1) / PATT_MIN_TILES;
-    if (want < ctas) ctas = want;
+    if (tiles < ctas) ctas = tiles;
   }
   const cudaError_t e = c.D == 128 ? launch_paged_d<128>(maps, a, (int)ctas, (cudaStream_t)stream)
                                    : launch_paged_d<64>(maps, a, (int)ctas, (cudaStream_t)stream);
