@@ -15,7 +15,7 @@ namespace pced {
 namespace cg = cooperative_groups;
 
 constexpr int BSEL_THREADS = 256;
-constexpr int BSEL_BATCH = 8;    // blocks of a group of lanes in flight
+constexpr int BSEL_BATCH = 4;    // blocks of a group of lanes in flight
 constexpr int BSEL_CLUSTER = 8;  // most CTAs of a row
 constexpr int BSEL_MIN_PART = 128;  // blocks that a CTA of a shared row has at least
 constexpr int BSEL_MAX_BLOCKS = 32768;  // scores of a row lie in shared memory
@@ -88,7 +88,7 @@ struct Scorer {
 // A cluster of CTAs shares a row: their warps take turns at 32 blocks and put the
 // scores into the first CTA's shared memory, which selects alone.
 template <int D>
-__global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArgs a) {
+__global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArgs a) {
   extern __shared__ int32_t scores[];  // [blocks of the sequence]
   __shared__ __align__(16) int8_t pooled[2 * D];
   __shared__ float wmax[BSEL_THREADS / 32];
@@ -246,8 +246,10 @@ __global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArg
     return d > floor ? 2 : d == floor;
   };
   uint32_t above = 0, ties = 0;
+  uint64_t rates = 0;  // of the first 32 of them, two bits each
   for (int j = j0; j < j1; ++j) {
     const uint32_t r = rate(j);
+    if (j - j0 < 32) rates |= (uint64_t)r << (2 * (j - j0));
     above += r >> 1;
     ties += r & 1u;
   }
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(BSEL_THREADS, 4) block_select_kernel(SelectArg
   above = before >> 16, ties = before & 0xFFFFu;
   int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
   for (int j = j0; j < j1; ++j) {
-    const uint32_t r = rate(j);
+    const uint32_t r = j - j0 < 32 ? (uint32_t)(rates >> (2 * (j - j0))) & 3u : rate(j);
     if (r == 2 || (r == 1 && ties < want)) sel[above + min(ties, want)] = j;
     above += r >> 1;
     ties += r & 1u;
