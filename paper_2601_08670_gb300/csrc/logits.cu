@@ -70,9 +70,9 @@ template <bool VEC>
 __global__ void __launch_bounds__(LOG_THREADS, LOG_CTAS) logits_process_kernel(LogitsArgs a) {
   __shared__ __align__(16) int32_t count[LOG_CHUNK];
   __shared__ __align__(16) int32_t named[LOG_CHUNK];  // 1 + the last bias entry of the token; then the bias itself
-  const int tid = threadIdx.x, b = blockIdx.z, v0 = blockIdx.x * LOG_CHUNK;
+  const int tid = threadIdx.x, b = blockIdx.x, v0 = blockIdx.z * LOG_CHUNK;
   const int r0 = blockIdx.y * a.rows, r1 = min(a.R, r0 + a.rows);
-  const bool reports = blockIdx.x == 0 && blockIdx.y == 0;
+  const bool reports = blockIdx.z == 0 && blockIdx.y == 0;
   for (int i = tid; i < LOG_CHUNK / 4; i += LOG_THREADS) {
     reinterpret_cast<int4*>(count)[i] = make_int4(0, 0, 0, 0);
     reinterpret_cast<int4*>(named)[i] = make_int4(0, 0, 0, 0);
@@ -165,7 +165,7 @@ extern "C" pced_status pced_logits_process(const float* x, float* y, int64_t str
                                            const int32_t* mask_row, int32_t* status, void* stream) {
   const char* fn = "pced_logits_process";
   if (!x || !y) return fail(PCED_ERR_INVALID_ARG, "%s: null pointer", fn);
-  if (B < 1 || R < 1 || V < 1 || B > 65535 || R > 65535 || stride < V) return fail(PCED_ERR_INVALID_ARG, "%s: bad sizes", fn);
+  if (B < 1 || R < 1 || V < 1 || B > 65535 || R > 65535 || V > 65535 * LOG_CHUNK || stride < V) return fail(PCED_ERR_INVALID_ARG, "%s: bad sizes", fn);
   if (!history != !penalties || !history != !history_len || (history && history_stride < 1))
     return fail(PCED_ERR_INVALID_ARG, "%s: history, history_len and penalties go together", fn);
   if (n_bias < 0 || !bias_ids != !bias || (n_bias > 0) != (bias_ids != nullptr))
@@ -189,7 +189,8 @@ extern "C" pced_status pced_logits_process(const float* x, float* y, int64_t str
   const int64_t parts = min((int64_t)R, max((int64_t)1, R / max((int64_t)1, total / ctas)));
   a.rows = (int)((R + parts - 1) / parts);
   const bool vec = V % 4 == 0 && stride % 4 == 0 && (((uintptr_t)x | (uintptr_t)y) & 15u) == 0;
-  const dim3 grid(chunks, (R - 1) / a.rows + 1, B);
+  // (the first chunks come first: low token numbers are the frequent ones, and repeated tokens cost time)
+  const dim3 grid(B, (R - 1) / a.rows + 1, chunks);
   const cudaError_t e = vec ? launch_pdl(logits_process_kernel<true>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a)
                             : launch_pdl(logits_process_kernel<false>, grid, LOG_THREADS, 0, (cudaStream_t)stream, a);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "logits_process launch");
