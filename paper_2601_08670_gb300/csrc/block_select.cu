@@ -258,7 +258,10 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
   for (int j = j0; j < j1; ++j) {
     const uint32_t r = j - j0 < 32 ? (uint32_t)(rates >> (2 * (j - j0))) & 3u : rate(j);
-    if (r == 2 || (r == 1 && ties < want)) sel[above + min(ties, want)] = j;
+    if (r == 2 || (r == 1 && ties < want)) {
+      const uint32_t at = above + min(ties, want);
+      if (PCED_IN_BOUNDS(at < (uint32_t)a.n_sel && j < nb, a.status)) sel[at] = j;
+    }
     above += r >> 1;
     ties += r & 1u;
   }

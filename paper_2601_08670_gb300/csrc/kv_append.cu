@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(A
   const int blk = paged_block(a.c, s, (n - 1) / P, a.status), at = (n - 1) % P;
   if (blk < 0) return;
   const int64_t page = (int64_t)blk * a.c.Hkv + h;
+  if (!PCED_IN_BOUNDS(in_pool(a.c, page, at), a.status)) return;
   r.store((__nv_bfloat16*)(role ? a.c.v : a.c.k) + (page * P + at) * D + f, D / 2);
   if (role == 0 && a.c.summary) {
     const float inv = __fdiv_rn(1.f, a.c.key_step[h]);
@@ -238,6 +239,7 @@ __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a)
         const int role = r0 + u;
         if (role >= G + 2) break;
         if (rotated && role != 1) x[u].rotate(co, si);
+        if (!PCED_IN_BOUNDS(t < a.T && (blk < 0 || in_pool(a.c, page, it.r0 % P + i)), a.status)) continue;
         if (role >= 2) {
           x[u].store(a.q_out + (t * a.Hq + h * G + role - 2) * D + f, D / 2);
         } else if (blk >= 0) {
@@ -329,7 +331,8 @@ __global__ void __launch_bounds__(32 * SUM_WARPS) block_summaries_kernel(pced_pa
     for (int w = 1; w < split; ++w) kb[e].merge(bounds[warp + w][0][f / 2 + e], bounds[warp + w][1][f / 2 + e]);
     mx[e] = kb[e].top(), mn[e] = kb[e].bottom();
   }
-  update_summary(c.summary + page * 2 * D, D, f, mx, mn, __fdiv_rn(1.f, c.key_step[h]), true);
+  if (PCED_IN_BOUNDS(in_pool(c, page, live - 1), status))
+    update_summary(c.summary + page * 2 * D, D, f, mx, mn, __fdiv_rn(1.f, c.key_step[h]), true);
 }
 
 }  // namespace pced

@@ -23,6 +23,10 @@ __device__ __forceinline__ int paged_block(const pced_paged_cache& c, int s, int
   dev_flag(status, PCED_DEV_BAD_BLOCK);
   return -1;
 }
+// row r of page (block, kv-head) lies in the pool (guards of the bounds-checked build)
+__device__ __forceinline__ bool in_pool(const pced_paged_cache& c, int64_t page, int r) {
+  return page >= 0 && page < (int64_t)c.num_blocks * c.Hkv && r >= 0 && r < c.block_rows;
+}
 
 // ------------------------------------------------------------- key summaries
 // Largest and smallest of two channels' keys, as bf16 pairs (one instruction for

@@ -169,6 +169,8 @@ __device__ __forceinline__ bool finish_piece(const PagedAttArgs& a, const PagedP
   // a part of a segment: record 2c of CTA c when it began in an earlier CTA,
   // 2c + 1 when it begins here
   const int64_t slot = 2 * (int64_t)blockIdx.x + (pc.t0 == 0 ? 1 : 0);
+  if (!PCED_IN_BOUNDS(pc.s >= 0 && pc.s < a.c.S && pc.h >= 0 && pc.h < a.c.Hkv && slot < 2 * PATT_MAX_CTAS, a.status))
+    return false;
   for (int i = et; i < GD / 4; i += NT) {
     const int hh = i / (D / 4), idx0 = 4 * i;
     float mx = -INFINITY, lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -186,6 +188,7 @@ __device__ __forceinline__ bool finish_piece(const PagedAttArgs& a, const PagedP
   const int32_t seg0 = seq0 + pc.h * pc.nt;  // the segment's first position
   const int first = (uint32_t)seg0 / (uint32_t)per;
   const int n = (int)((uint32_t)(seg0 + pc.nt - 1) / (uint32_t)per) - first + 1;
+  if (!PCED_IN_BOUNDS(first >= 0 && n >= 2 && first + n <= (int)gridDim.x, a.status)) return false;
   if (!bar_sync_warps(bar, phase, lane, a.status)) return false;  // all of this CTA's record is written
   // (its release and acquire at gpu scope carry what the barriers order for the other threads)
   if (et == 0) *last_here = atom_acq_rel_gpu_add(a.parts + first, 1) == n - 1;
@@ -319,6 +322,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
           }
           const int32_t blk = paged_block(a.c, pc.s, j, a.status);
           if (blk < 0) continue;
+          if (!PCED_IN_BOUNDS(in_pool(a.c, (int64_t)blk * Hkv + pc.h, at), a.status)) continue;
           row[i] = (blk * Hkv + pc.h) * P + at;
           const int32_t left = n - j * P - at;  // live rows from here on
           if (SMALL) {
