@@ -523,7 +523,7 @@ pced_status pced_block_select(const pced_paged_cache* cache, const void* q, int6
  *   lse          fp32 [S][Hq], may be NULL: log of the sum of exp(scale q.k)
  * A sequence (or a head's choice) without rows has zeros in out and -inf in
  * lse.  What lies in rows past a sequence's last does not matter.  Probabilities
- * are held to 16 bits, sums in fp32.  Supports Hq/Hkv <= 8 and
+ * are held to 24 bits, sums in fp32.  Supports Hq/Hkv <= 8 and
  * S*Hkv*(max_blocks*block_rows/64 + 2) < 2^31.  The workspace must
  * be zero-filled before the first call: besides the status word it holds
  * counters that a call leaves at zero.

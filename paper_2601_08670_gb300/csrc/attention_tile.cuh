@@ -49,8 +49,12 @@ __device__ __forceinline__ void acc_reset(WarpAcc<D>& A) {
 // of heads 0-3 and columns 4-7 the lo parts of the same heads (qf repeats
 // heads 0-3 in columns 4-7, so the threads owning those columns, tq >= 2,
 // hold the same scores as lane ^ 2), and o of head h is column h plus column
-// h + 4 (summed once per piece, see pack_fold).
-template <int D, bool PK = false>
+// h + 4 (summed once per piece, see pack_fold).  With P3 a third part follows, in an
+// MMA of its own, so P keeps the 24 bits it was computed with, and a tile's sums
+// are added to o in fp32, rounded to nearest (the MMA's own accumulation cuts
+// off): error of the output against 64 bits 2.4e-6 without, 1.7e-7 with it, the time
+// of memory-bound calls the same.
+template <int D, bool PK = false, bool P3 = false>
 __device__ __forceinline__ void tile_math(WarpAcc<D>& A, const uint32_t (&qf)[D / 16][2], uint32_t sk, uint32_t sv,
                                           int kb, int nvalid, float scale_log2, int lane) {
   using C = AttCfg<D>;
@@ -112,6 +116,13 @@ __device__ __forceinline__ void tile_math(WarpAcc<D>& A, const uint32_t (&qf)[D 
   const bool lo_cols = PK && tq >= 2;
   const uint32_t bh0 = movmatrix_t(lo_cols ? q01 : h01), bh1 = movmatrix_t(lo_cols ? q23 : h23);
   const uint32_t bl0 = PK ? 0u : movmatrix_t(q01), bl1 = PK ? 0u : movmatrix_t(q23);
+  uint32_t bt0 = 0u, bt1 = 0u;
+  if (P3) {
+    const uint32_t t01 = pack_bf16((p0 - bf16_lo(h01)) - bf16_lo(q01), (p1 - bf16_hi(h01)) - bf16_hi(q01));
+    const uint32_t t23 = pack_bf16((p2 - bf16_lo(h23)) - bf16_lo(q23), (p3 - bf16_hi(h23)) - bf16_hi(q23));
+    bt0 = movmatrix_t(lo_cols ? 0u : t01);
+    bt1 = movmatrix_t(lo_cols ? 0u : t23);
+  }
   // ---- O^T += V^T P^T; rows of V past the live length are zeroed
   const bool partial = kb + 16 > nvalid;
   const int klo = kb + 2 * tq, khi = klo + 8;
@@ -132,8 +143,17 @@ __device__ __forceinline__ void tile_math(WarpAcc<D>& A, const uint32_t (&qf)[D 
       a2 &= mhi;
       a3 &= mhi;
     }
-    mma_bf16(A.o[i], a0, a1, a2, a3, bh0, bh1);
-    if (!PK) mma_bf16(A.o[i], a0, a1, a2, a3, bl0, bl1);
+    if (P3) {
+      float t[4] = {};
+      mma_bf16(t, a0, a1, a2, a3, bt0, bt1);
+      if (!PK) mma_bf16(t, a0, a1, a2, a3, bl0, bl1);
+      mma_bf16(t, a0, a1, a2, a3, bh0, bh1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) A.o[i][j] += t[j];
+    } else {
+      mma_bf16(A.o[i], a0, a1, a2, a3, bh0, bh1);
+      if (!PK) mma_bf16(A.o[i], a0, a1, a2, a3, bl0, bl1);
+    }
   }
 }
 

@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
       const int live = desc[st] >> (8 * (warp & 3)) & 0xFFu;
       if (live) {
         const uint32_t sk = smem0 + st * C::STAGE_BYTES;
-        tile_math<D, PK>(A, qf, sk, sk + C::TILE_BYTES, kb, kb + live, a.scale_log2, lane);
+        tile_math<D, PK, true>(A, qf, sk, sk + C::TILE_BYTES, kb, kb + live, a.scale_log2, lane);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_empty + 8 * st);
