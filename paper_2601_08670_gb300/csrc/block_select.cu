@@ -14,7 +14,7 @@ namespace pced {
 
 namespace cg = cooperative_groups;
 
-constexpr int BSEL_THREADS = 256;
+constexpr int BSEL_THREADS = 256;  // (also the values of a digit)
 constexpr int BSEL_BATCH = 4;    // blocks of a group of lanes in flight
 constexpr int BSEL_CLUSTER = 8;  // most CTAs of a row
 constexpr int BSEL_MIN_PART = 128;  // blocks that a CTA of a shared row has at least
@@ -42,7 +42,8 @@ __device__ __forceinline__ uint32_t cta_prefix(uint32_t x, uint32_t* wsum) {
   if (lane == 31) wsum[warp] = incl;
   __syncthreads();
   uint32_t before = incl - x;
-  for (int w = 0; w < warp; ++w) before += wsum[w];
+#pragma unroll
+  for (int w = 0; w < BSEL_THREADS / 32 - 1; ++w) before += w < warp ? wsum[w] : 0u;
   return before;
 }
 
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   __shared__ __align__(16) int8_t pooled[2 * D];
   __shared__ float wmax[BSEL_THREADS / 32];
   __shared__ int2 wrange[BSEL_THREADS / 32];
-  __shared__ uint32_t hist[256];
+  __shared__ __align__(16) uint32_t hist[BSEL_THREADS];
   __shared__ uint32_t found[3];  // digit of the threshold, entries wanted at it, entries there are
   __shared__ uint32_t wsum[BSEL_THREADS / 32];
   cg::cluster_group cluster = cg::this_cluster();
@@ -177,6 +178,27 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   else __syncthreads();
   if (rank > 0) return;
 
+  int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
+  const auto choose = [&](uint32_t at, int j) {
+    if (PCED_IN_BOUNDS(at < (uint32_t)a.n_sel && j < nb, a.status)) sel[at] = j;
+  };
+  if (nb <= BSEL_THREADS) {
+    // ---- few blocks, one a thread: chosen where fewer than `want` others come before it
+    const bool forced = tid < a.n_first || tid >= nb - a.n_last;
+    // (scores fall with the number within equal ones, so that no two keys are the same)
+    const uint32_t key = (uint32_t)((tid < nb ? scores[tid] : BSEL_WORST) - BSEL_WORST) << 8 | (255u - tid);
+    hist[tid] = forced || tid >= nb ? 0u : key;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int i = 0; i < (nb + 3) / 4; ++i) {
+      const uint4 k = reinterpret_cast<const uint4*>(hist)[i];
+      before += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+    }
+    const bool chosen = tid < nb && (forced || before < (uint32_t)(a.n_sel - a.n_first - a.n_last));
+    const uint32_t at = cta_prefix(chosen, wsum);
+    if (chosen) choose(at, tid);
+    return;
+  }
   // ---- the lowest score chosen among the blocks [lo, hi) between the first and the last ones
   const int lo = min(a.n_first, nb), hi = max(lo, nb - a.n_last);
   uint32_t want = a.n_sel - (a.n_first + a.n_last);  // of them; fewer than there are, as nb > n_sel
@@ -206,23 +228,20 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
         if (bits == 32 || (d ^ floor) >> bits == 0) atomicAdd(&hist[d >> shift & 255u], 1u);
       }
       __syncthreads();
-      if (warp == 0) {  // the digit that holds the want-th from above
-        uint32_t own = 0;
+      // the digit that holds the want-th from above: a thread each, suffix sums
+      const uint32_t own = hist[tid];
+      uint32_t above = own;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) own += hist[8 * lane + i];
-        uint32_t above = own;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t v = __shfl_down_sync(0xffffffffu, above, o);
-          if (lane + o < 32) above += v;
-        }
-        above -= own;
-        if (above < want && want <= above + own) {
-          int b = 8 * lane + 7;
-          while (above + hist[b] < want) above += hist[b--];
-          found[0] = b, found[1] = want - above, found[2] = hist[b];
-        }
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_down_sync(0xffffffffu, above, o);
+        if (lane + o < 32) above += v;
       }
+      if (lane == 0) wsum[warp] = above;
+      __syncthreads();
+      above -= own;
+#pragma unroll
+      for (int w = 1; w < BSEL_THREADS / 32; ++w) above += w > warp ? wsum[w] : 0u;
+      if (above < want && want <= above + own) found[0] = tid, found[1] = want - above, found[2] = own;
       __syncthreads();
       floor |= found[0] << shift;
       want = found[1];
@@ -255,13 +274,9 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   }
   const uint32_t before = cta_prefix(above << 16 | ties, wsum);
   above = before >> 16, ties = before & 0xFFFFu;
-  int32_t* sel = a.sel + ((int64_t)s * a.c.Hkv + h) * a.n_sel;
   for (int j = j0; j < j1; ++j) {
     const uint32_t r = j - j0 < 32 ? (uint32_t)(rates >> (2 * (j - j0))) & 3u : rate(j);
-    if (r == 2 || (r == 1 && ties < want)) {
-      const uint32_t at = above + min(ties, want);
-      if (PCED_IN_BOUNDS(at < (uint32_t)a.n_sel && j < nb, a.status)) sel[at] = j;
-    }
+    if (r == 2 || (r == 1 && ties < want)) choose(above + min(ties, want), j);
     above += r >> 1;
     ties += r & 1u;
   }
