@@ -109,11 +109,9 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   int j = (warp * ctas + rank) * 32 + lane;
   int entry = j < a.c.max_blocks ? table[j] : -1;
   float x[PAGED_MAX_G];
-  if (tid < 2 * D) {
-    const __nv_bfloat16* q = a.q + s * a.q_stride + (int64_t)h * a.G * D + tid % D;
+  const __nv_bfloat16* q = a.q + s * a.q_stride + (int64_t)h * a.G * D + tid % D;
 #pragma unroll
-    for (int g = 0; g < PAGED_MAX_G; ++g) x[g] = g < a.G ? __bfloat162float(q[g * D]) : 0.f;
-  }
+  for (int g = 0; g < PAGED_MAX_G; ++g) x[g] = g < a.G ? __bfloat162float(q[g * D]) : 0.f;
   const int n = paged_len(a.c, s, a.status);
   const int nb = (n + a.c.block_rows - 1) / a.c.block_rows;
   if (nb <= a.n_sel) {  // all of them
@@ -138,16 +136,14 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   check(j);
   sc.load(summary, page, entry, 0, lane);  // the first blocks come while the queries are pooled
   // ---- the pooled query
-  float p = 0.f, m = 0.f;
-  if (tid < 2 * D) {
+  float p = 0.f;  // part tid: D positive ones, then D negative ones (and with D = 64 these again)
 #pragma unroll
-    for (int g = 0; g < PAGED_MAX_G; ++g) {
-      p = __fadd_rn(p, tid < D ? (x[g] > 0.f ? x[g] : 0.f) : (x[g] < 0.f ? x[g] : 0.f));
-      if (x[g] != x[g]) p = x[g];
-    }
-    m = p != p ? INFINITY : fabsf(p);
+  for (int g = 0; g < PAGED_MAX_G; ++g) {
+    if (g >= a.G) break;
+    p = __fadd_rn(p, tid < D ? (x[g] > 0.f ? x[g] : 0.f) : (x[g] < 0.f ? x[g] : 0.f));
+    if (x[g] != x[g]) p = x[g];
   }
-  m = warp_max(m);
+  float m = warp_max(p != p ? INFINITY : fabsf(p));
   if (lane == 0) wmax[warp] = m;
   __syncthreads();
   m = wmax[0];
@@ -162,9 +158,10 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   int32_t* out = ctas > 1 ? cluster.map_shared_rank(scores, 0) : scores;
   const int4 pq = reinterpret_cast<const int4*>(pooled)[lane % LANES];
   for (int jw = j - lane; jw < nb; jw += stride) {  // 32 blocks of this warp
-    const int next = jw + stride + lane < a.c.max_blocks ? table[jw + stride + lane] : -1;
+    const int next = jw + stride + lane < nb ? table[jw + stride + lane] : -1;
 #pragma unroll
     for (int first = 0; first < 32; first += BSEL_BATCH * SIDE) {
+      if (jw + first >= nb) break;
       if (first > 0 || jw != j - lane) sc.load(summary, page, entry, first, lane);
       const int mine = first + Scorer<D>::slot(lane) * SIDE + lane / LANES;
       const int blk = __shfl_sync(0xffffffffu, entry, mine);
@@ -190,7 +187,8 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
     hist[tid] = forced || tid >= nb ? 0u : key;
     __syncthreads();
     uint32_t before = 0;
-    for (int i = 0; i < (nb + 3) / 4; ++i) {
+    const int n4 = 32 * warp < nb ? (nb + 3) / 4 : 0;  // (a warp without blocks has nothing to count)
+    for (int i = 0; i < n4; ++i) {
       const uint4 k = reinterpret_cast<const uint4*>(hist)[i];
       before += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
     }
