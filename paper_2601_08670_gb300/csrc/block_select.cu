@@ -6,6 +6,15 @@
 // smallest keys: 2D products of 8-bit numbers, four a dp4a, exact in 32 bits.  The
 // lowest chosen score of a row is found by a radix select, eight bits a pass; the
 // blocks above it and, of those at it, the lowest are written in ascending order.
+//
+// What bounds it (one GB300, GPU time in a graph): for long rows the gather of 256
+// bytes a block from anywhere in the pool (33 sequences of 1025 to 2049 blocks,
+// 8 kv-heads, 103 MB in 27 us: about 18 of scoring at 5.6 TB/s, 2.5 before it, 5 for
+// the selection and the rows' unequal ends), for many short ones the instructions
+// (2176 rows of 129 blocks 24 us), for few short ones latency (72 rows of 129
+// blocks 4.0 us).  Tried for long rows: clusters that share 4 or 8 heads, so that a
+// block's summaries are read side by side, 34 and 50 us (clusters of eight CTAs
+// start and end together); four CTAs a row 31 us, one 36 us.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -14,10 +23,10 @@ namespace pced {
 
 namespace cg = cooperative_groups;
 
-constexpr int BSEL_THREADS = 256;  // (also the values of a digit)
-constexpr int BSEL_BATCH = 4;    // blocks of a group of lanes in flight
-constexpr int BSEL_CLUSTER = 8;  // most CTAs of a row
-constexpr int BSEL_MIN_PART = 128;  // blocks that a CTA of a shared row has at least
+constexpr int BSEL_THREADS = 256;       // (also the values of a digit)
+constexpr int BSEL_BATCH = 4;           // blocks of a group of lanes in flight
+constexpr int BSEL_CLUSTER = 8;         // most CTAs of a row
+constexpr int BSEL_MIN_PART = 128;      // blocks that a CTA of a shared row has at least
 constexpr int BSEL_MAX_BLOCKS = 32768;  // scores of a row lie in shared memory
 constexpr int32_t BSEL_WORST = -(1 << 22);  // of a bad block: below -2 * 128 * 127 * 127
 
@@ -316,6 +325,8 @@ extern "C" pced_status pced_block_select(const pced_paged_cache* cache, const vo
   static bool done[2][64];
   cudaError_t e = allow_smem(kernel, BSEL_MAX_BLOCKS * 4, done[c.D == 128]);
   if (e != cudaSuccess) return cuda_status(e, "block_select shared memory");
+  // CTAs of a row: more while there are fewer than two for every SM and the blocks
+  // are many (four sequences of up to 2049 blocks 8.7 us; one CTA a row 19)
   int ctas = 1;
   while (ctas < BSEL_CLUSTER && (int64_t)c.Hkv * c.S * ctas < 2 * (int64_t)num_sms() &&
          c.max_blocks >= 2 * ctas * BSEL_MIN_PART)

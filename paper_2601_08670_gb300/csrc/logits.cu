@@ -6,8 +6,15 @@
 //
 // A CTA takes LOG_CHUNK tokens of some of a query's rows.  It counts the
 // history's tokens of the chunk in shared memory (whole numbers: the order does
-// not matter) and marks the biased ones, then streams the rows: each thread
-// holds its tokens' counts, biases and mask bits in registers for all of them.
+// not matter) and marks the biased ones, then streams the rows, each asked for
+// while the one before is processed; a thread keeps its tokens' mask bits, and a
+// warp which of its places hold a repeated or biased token at all, in registers.
+//
+// What bounds it (one GB300, GPU time in a graph): HBM for many rows (272 rows of
+// V = 151936, 331 MB in 60 us, 5.5 TB/s: 53 us without histories; with 4096 tokens
+// each, counting them and the divisions of the first chunks, where the repeated
+// tokens are, take 7), latency for few (nine rows of V = 128256 4.4 us).  Two rows in
+// flight and none ahead: 69 us; per element tests for counts and biases: 94 us.
 #include <math.h>
 
 #include "common.cuh"
@@ -18,7 +25,6 @@ constexpr int LOG_THREADS = 256;
 constexpr int LOG_TOK = 8;  // tokens of a thread
 constexpr int LOG_CHUNK = LOG_THREADS * LOG_TOK;
 constexpr int LOG_CTAS = 4;  // CTAs that an SM holds
-constexpr int LOG_WAVES = 3;  // CTAs for so many SM fillings, where there are rows enough
 constexpr int LOG_HIST = 8;  // history tokens of a thread in flight
 
 struct LogitsArgs {
@@ -184,9 +190,11 @@ extern "C" pced_status pced_logits_process(const float* x, float* y, int64_t str
   a.bias_ids = bias_ids, a.bias = bias, a.n_bias = n_bias;
   a.mask = mask, a.n_masks = n_masks, a.mask_words = mask_words, a.mask_row = mask_row;
   a.status = status;
+  // Parts of a query's rows: no more than fill the SMs once, as each part counts its
+  // chunk's tokens again (four queries of 17 rows 20 us; parts for three fillings 26,
+  // and 23 against 18 with histories of 64 tokens)
   const int chunks = (V - 1) / LOG_CHUNK + 1;
-  const int64_t total = (int64_t)chunks * B * R, ctas = LOG_WAVES * LOG_CTAS * (int64_t)num_sms();
-  const int64_t parts = min((int64_t)R, max((int64_t)1, R / max((int64_t)1, total / ctas)));
+  const int64_t parts = max((int64_t)1, min((int64_t)R, LOG_CTAS * (int64_t)num_sms() / ((int64_t)chunks * B)));
   a.rows = (int)((R + parts - 1) / parts);
   const bool vec = V % 4 == 0 && stride % 4 == 0 && (((uintptr_t)x | (uintptr_t)y) & 15u) == 0;
   // (the first chunks come first: low token numbers are the frequent ones, and repeated tokens cost time)

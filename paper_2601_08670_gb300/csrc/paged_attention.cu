@@ -14,7 +14,17 @@
 // block (a block of another size, a sequence's end) it is put together from
 // 16-row boxes, the rows that one consumer warp takes, and rows past the live
 // ones are neither brought nor used.  The math on a tile is that of the slab
-// kernels (attention_tile.cuh).
+// kernels (attention_tile.cuh): mma.sync, whose rate is no bound here (at most
+// eight heads share a row: 8 operations a byte, against 280 that the GPU has).
+//
+// What bounds it (one GB300, GPU time in a graph): HBM for long calls (272 ragged
+// sequences, 1.32 GB in 193 us: the measured copy rate), for short ones the chain
+// before the first tile (launch, lengths, plan, table: 2.4 us) and after the last
+// (partials, record, count, merge: 3 us): 9 x 2081 rows, 77 MB, 17 us, of which 11
+// stream; three sequences of 257 rows 5.5 us.  A CTA has one tile at least: with
+// four these took 10 us, as a tile's own chain is longer than a record's merge.
+// Tiles prefetched into L2 ahead of the ring made every case slower (17 x 64 blocks
+// of 64 rows by 15-24 %); a ring of three tiles costs 1-3 %.
 #include "attention_tile.cuh"
 #include "paged.cuh"
 
