@@ -25,6 +25,7 @@ struct AppendArgs {
   const float* rope;
   int32_t rope_rows;
   const int32_t* positions;
+  int32_t heads;  // kv-heads of a CTA (any number of tokens): a power of two that divides Hkv, at most its units
   int* status;
 };
 
@@ -204,23 +205,29 @@ __global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(A
   }
 }
 
-// Any number of tokens: a CTA takes one item and one kv-head.  D/16 lanes share a
-// row, each with the same channels of all its heads, so a position's angles are
-// read once for all of them, and a thread holds the bounds of its channels' keys
-// in registers.  (A page and kv-head has one CTA, so its summary has one writer.)
+// Any number of tokens: a CTA takes one item and a kv-head, or `heads` of them.  D/16 lanes (a
+// unit) share a row of one kv-head and its group, each with the same channels of all
+// these heads, so a position's angles are read once for them, and a thread holds the
+// bounds of its channels' keys in registers.  (A page and kv-head has one CTA, so its
+// summary has one writer.)  SEVERAL: more than one kv-head, where items have so few
+// rows that a CTA's units would idle (272 sequences of two tokens: 17.5 us with one,
+// 7.1 with eight; but 33 of 32 tokens, with two, 14.3 against 9.0).
 // Sixteen documents: 134 us with a unit per head's row (angles read again for every
 // head), 89 us this way at 2 CTAs of 256 threads an SM, 81 us at 3, 78 us with an
 // item's heads side by side in the grid, 76 us with 6 CTAs of 128 threads.
 constexpr int APP_HEADS = 3;  // heads whose loads a thread has in flight (six, at 2/3 of the CTAs: 1 % less time)
 
-template <int D>
+template <int D, bool SEVERAL>
 __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a) {
-  constexpr int LANES = D / 16, UNITS = APP_THREADS / LANES, WARPS = APP_THREADS / 32;
+  constexpr int LANES = D / 16, UNITS = APP_THREADS / LANES;
+  constexpr int SIDE = 32 / LANES;  // units of a warp
   // (the heads of an item side by side: their parts of a token's row are neighbours in memory)
-  const int tid = threadIdx.x, h = blockIdx.x % a.c.Hkv, G = a.G, P = a.c.block_rows;
-  __shared__ uint32_t bounds[WARPS][2][D / 2];  // of each warp: largest, smallest keys
+  const int tid = threadIdx.x, unit = tid / LANES, G = a.G, P = a.c.block_rows;
+  const int heads = SEVERAL ? a.heads : 1;
+  const int per_item = a.c.Hkv / heads, h0 = blockIdx.x % per_item * heads, h = h0 + (unit & (heads - 1));
+  __shared__ uint32_t bounds[UNITS][2][D / 2];  // largest, smallest keys
   pdl_wait();
-  const AppendItem it = find_item(a, blockIdx.x / a.c.Hkv);
+  const AppendItem it = find_item(a, blockIdx.x / per_item);
   if (it.s < 0) return;
   const int blk = paged_block(a.c, it.s, it.r0 / P, a.status);
   const int64_t page = (int64_t)blk * a.c.Hkv + h;
@@ -228,7 +235,7 @@ __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a)
   KeyBounds2 kb[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) kb[e].reset();
-  for (int i = tid / LANES; i < it.m; i += UNITS) {
+  for (int i = unit / heads; i < it.m; i += UNITS / heads) {
     const int64_t t = it.t0 + i;
     const int64_t row = (page * P + it.r0 % P + i) * D + f;
     float co[8], si[8];
@@ -264,29 +271,33 @@ __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a)
     }
   }
   if (!a.c.summary || blk < 0) return;
-  const int lane = tid & 31, warp = tid >> 5;
+  // units of the same head meet: in the warp, then in shared memory
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int o = LANES; o < 32; o <<= 1)
+    if (o >= LANES * heads)
 #pragma unroll
-    for (int o = LANES; o < 32; o <<= 1) kb[e].merge_xor(o);
-    if (lane < LANES) {
+    for (int e = 0; e < 8; ++e) kb[e].merge_xor(o);
+  if (unit % SIDE < heads) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
       const int at = f / 2 + (e < 4 ? e : D / 4 + e - 4);
-      bounds[warp][0][at] = kb[e].top();
-      bounds[warp][1][at] = kb[e].bottom();
+      bounds[unit][0][at] = kb[e].top();
+      bounds[unit][1][at] = kb[e].bottom();
     }
   }
   __syncthreads();
-  if (tid < D / 8) {  // eight channels
+  for (int i = tid; i < heads * (D / 8); i += APP_THREADS) {  // eight channels of a head
+    const int hh = i / (D / 8), d = 8 * (i % (D / 8));
     uint32_t mx[4], mn[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       KeyBounds2 b;
       b.reset();
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) b.merge(bounds[w][0][4 * tid + e], bounds[w][1][4 * tid + e]);
+      for (int u = hh; u < UNITS; u += max(heads, SIDE)) b.merge(bounds[u][0][d / 2 + e], bounds[u][1][d / 2 + e]);
       mx[e] = b.top(), mn[e] = b.bottom();
     }
-    update_summary(a.c.summary + page * 2 * D, D, 8 * tid, mx, mn, __fdiv_rn(1.f, a.c.key_step[h]), it.r0 % P == 0);
+    update_summary(a.c.summary + ((int64_t)blk * a.c.Hkv + h0 + hh) * 2 * D, D, d, mx, mn,
+                   __fdiv_rn(1.f, a.c.key_step[h0 + hh]), it.r0 % P == 0);
   }
 }
 
@@ -423,8 +434,13 @@ extern "C" pced_status pced_kv_append(const pced_paged_cache* cache, const void*
     // blocks touched: at most two more than whole ones for every sequence with tokens
     const int64_t items = (int64_t)T / c.block_rows + 2 * (int64_t)(T < c.S ? T : c.S);
     if (items * c.Hkv >= (INT64_C(1) << 31)) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
-    e = launch_pdl(c.D == 128 ? kv_append_kernel<128> : kv_append_kernel<64>, dim3((unsigned)(items * c.Hkv)), APP_THREADS,
-                   0, (cudaStream_t)stream, a);
+    const int units = APP_THREADS / (c.D / 16);
+    const int64_t rows = T / items > 0 ? T / items : 1;  // of an item, about
+    a.heads = 1;
+    while (2 * a.heads * rows <= units && c.Hkv % (2 * a.heads) == 0) a.heads *= 2;
+    const auto kernel = a.heads > 1 ? (c.D == 128 ? kv_append_kernel<128, true> : kv_append_kernel<64, true>)
+                                    : (c.D == 128 ? kv_append_kernel<128, false> : kv_append_kernel<64, false>);
+    e = launch_pdl(kernel, dim3((unsigned)(items * (c.Hkv / a.heads))), APP_THREADS, 0, (cudaStream_t)stream, a);
   }
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "kv_append launch");
 }
