@@ -165,6 +165,40 @@ __device__ __forceinline__ void merge_records(const PagedAttArgs& a, int c, int 
   }
 }
 
+// The eight warps' partials (store_partial) merged for outputs idx0 ... idx0 + 3 of
+// head hh: load_merged without its branches, so that all eight warps' values are in
+// flight (a piece took the epilogue 1.2 us with them; a warp without rows has a sum
+// and an o of zero).
+template <int D>
+__device__ __forceinline__ void merge_partials(const float* ms, const float* ls, const float* os, int G, int hh,
+                                               int idx0, float& mx, float& lsum, float (&acc)[4]) {
+  constexpr int W = ATT_CONSUMERS;
+  float m[W], l[W];
+  float4 o[W];
+#pragma unroll
+  for (int w = 0; w < W; w += 4) {
+    *reinterpret_cast<float4*>(m + w) = *reinterpret_cast<const float4*>(ms + hh * W + w);
+    *reinterpret_cast<float4*>(l + w) = *reinterpret_cast<const float4*>(ls + hh * W + w);
+  }
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+    o[w] = *reinterpret_cast<const float4*>(os + (w * G + hh) * AttCfg<D>::OROW + (idx0 - hh * D));
+  mx = m[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) mx = fmaxf(mx, m[w]);
+  const float M = mx == -INFINITY ? 0.f : mx;
+  lsum = acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float e = exp2f(m[w] - M);
+    acc[0] += o[w].x * e;
+    acc[1] += o[w].y * e;
+    acc[2] += o[w].z * e;
+    acc[3] += o[w].w * e;
+    lsum += l[w] * e;
+  }
+}
+
 // A piece's partials, merged, into the output (a whole segment) or into a record,
 // and the segment's records into the output where this was the last of them to
 // come.  NT threads, whole warps, with a barrier of their own; seq0: the position at
@@ -183,8 +217,8 @@ __device__ __forceinline__ bool finish_piece(const PagedAttArgs& a, const PagedP
     return false;
   for (int i = et; i < GD / 4; i += NT) {
     const int hh = i / (D / 4), idx0 = 4 * i;
-    float mx = -INFINITY, lsum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    load_merged<D>(ms, ls, os, G, hh, idx0, mx, lsum, acc);
+    float mx, lsum, acc[4];
+    merge_partials<D>(ms, ls, os, G, hh, idx0, mx, lsum, acc);
     if (whole) {
       write_out(a, pc.s, pc.h, D, hh, idx0, mx, lsum, acc);
     } else {
