@@ -32,7 +32,7 @@ namespace pced {
 
 constexpr int PATT_MAX_CTAS = 256;  // sizes the records and counters of the workspace
 constexpr int PATT_GRAN = 16;       // rows of a consumer warp, and of a small box
-constexpr int PATT_EPI = 3;         // epilogue warps
+constexpr int PATT_EPI = 4;         // epilogue warps
 constexpr int PATT_THREADS = (ATT_CONSUMERS + 1 + PATT_EPI) * 32;
 
 struct PagedAttArgs {
