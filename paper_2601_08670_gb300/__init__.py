@@ -1,13 +1,17 @@
 """GB300 (sm_103a) decode step of Parallel Context-of-Experts Decoding.
 
-Thin ctypes binding of ``libpced.so`` (C ABI declared in ``include/pced.h``):
-argument marshalling only, every step of the computation runs in the
-library's CUDA kernels.  PyTorch supplies device memory and streams.  There is
-no CPU fallback: if the library is not built, every call raises.
+Thin binding of ``libpced.so`` (C ABI declared in ``include/pced.h``), through
+ctypes, and for the calls over paged caches and on logits through a small
+CPython module beside it (``pced_calls.so``): argument marshalling only, every
+step of the computation runs in the library's CUDA kernels.  PyTorch supplies
+device memory and streams.  There is no CPU fallback: if the library is not
+built, every call raises.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import math
 import os
 
@@ -129,6 +133,24 @@ def lib(path: str = LIB_PATH):
         L.pced_logits_process.restype = I32
         _lib = L
     return _lib
+
+
+_calls = None
+
+
+def _native():
+    """The CPython module of the calls over paged caches and on logits (raises if it has not been built)."""
+    global _calls
+    if _calls is None:
+        lib()
+        path = os.path.join(os.path.dirname(LIB_PATH), "pced_calls.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with paper_2601_08670_gb300.build.build()")
+        loader = importlib.machinery.ExtensionFileLoader("pced_calls", path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("pced_calls", loader))
+        loader.exec_module(module)
+        _calls = module
+    return _calls
 
 
 def _check(rc: int, what: str):
@@ -296,15 +318,8 @@ def _is(t, dtype, shape):
     return t.dtype == dtype and t.shape == shape and t.is_contiguous()
 
 
-def _token_stride(t, T, heads, D, what):
-    """Elements between the tokens of t: bf16 [T, heads (0: any), D], a token's heads side by side.  (A small call's
-    time is what its checks take on the host, so they ask each tensor once.)"""
-    if t.dtype == torch.bfloat16 and t.dim() == 3:
-        n, H, d = t.shape
-        st, sh, sd = t.stride()
-        if n == T and d == D and (H == heads or not heads) and sd == 1 and (sh == D or H == 1):
-            return st if n > 1 else H * D
-    raise ValueError(f"{what}: bf16 [{T}, {heads or 'Hq'}, {D}], a token's heads side by side")
+def _handle(stream):
+    return None if stream is None else stream.cuda_stream
 
 
 class PagedCache:
@@ -348,7 +363,8 @@ class PagedCache:
             _require(t is None or t.device == self.device, "a cache's tensors lie on one device")
         self.struct = PagedCacheStruct(_ptr(k), _ptr(v), _ptr(summary), _ptr(key_step), _ptr(block_table),
                                        _ptr(seq_len), nb, P, self.max_blocks, S, Hkv, D)
-        self.ref = ctypes.byref(self.struct)
+        self.at = ctypes.addressof(self.struct)
+        self.gpu = self.device.index if self.device.type == "cuda" else -1
 
 
 def rope_table(theta: float, D: int, rows: int, device="cuda") -> torch.Tensor:
@@ -365,27 +381,10 @@ def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=N
     rotated into q_out, which is returned.  The parts of one projection's output need no copies (strides between
     tokens).  rope: fp32 [rows, D] (rope_table), None: no rotation; tok_start: int32 [S + 1], None: one token per
     sequence; positions: int32 [T], None: the rows themselves.  Device conditions go to the int32 tensor status."""
-    T, Hkv, D = k.shape[0], cache.Hkv, cache.D
-    k_stride, v_stride = _token_stride(k, T, Hkv, D, "k"), _token_stride(v, T, Hkv, D, "v")
-    Hq, q_stride = Hkv, 0
-    if q is not None:
-        q_stride = _token_stride(q, T, 0, D, "q")
-        Hq = q.shape[1]
-        if q_out is None:
-            q_out = _empty((T, Hq, D), torch.bfloat16, q.device, stream)
-        else:
-            _require(_is(q_out, torch.bfloat16, (T, Hq, D)), "q_out: contiguous bf16 [T, Hq, D]")
-    else:
-        _require(q_out is None, "q_out without q")
-    rope_rows = 0
-    if rope is not None:
-        rope_rows = rope.shape[0]
-        _require(_is(rope, torch.float32, (rope_rows, D)), "rope: contiguous fp32 [rows, D]")
-    _require(tok_start is None or _is(tok_start, torch.int32, (cache.S + 1,)), "tok_start: int32 [S + 1]")
-    _require(positions is None or _is(positions, torch.int32, (T,)), "positions: int32 [T]")
-    rc = lib().pced_kv_append(cache.ref, _ptr(q), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
-                              _ptr(q_out), Hq, _ptr(tok_start), T, _ptr(rope), rope_rows, _ptr(positions),
-                              _ptr(status), _stream(stream))
+    if q_out is None and q is not None:
+        q_out = _empty((q.shape[0], q.shape[1], cache.D), torch.bfloat16, q.device, stream)
+    rc = (_calls or _native()).kv_append(cache.at, cache.gpu, q, k, v, rope, tok_start, positions, q_out, status,
+                                         _handle(stream))
     if rc:
         _check(rc, "pced_kv_append")
     return q_out
@@ -393,7 +392,9 @@ def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=N
 
 def block_summaries(cache: PagedCache, status=None, stream=None):
     """pced_block_summaries: cache.summary from the cached keys of all live blocks; returns it."""
-    _check(lib().pced_block_summaries(cache.ref, _ptr(status), _stream(stream)), "pced_block_summaries")
+    rc = (_calls or _native()).block_summaries(cache.at, cache.gpu, status, _handle(stream))
+    if rc:
+        _check(rc, "pced_block_summaries")
     return cache.summary
 
 
@@ -401,13 +402,9 @@ def block_select(cache: PagedCache, q, n_sel: int, n_first: int = 1, n_last: int
                  stream=None):
     """pced_block_select: int32 [S, Hkv, n_sel], the blocks that q bf16 [S, Hq, D] attends to in ascending order
     (-1 after the last): the first n_first, the last n_last and those with the highest scores."""
-    q_stride = _token_stride(q, cache.S, 0, cache.D, "q")
     if sel is None:
         sel = _empty((cache.S, cache.Hkv, n_sel), torch.int32, q.device, stream)
-    else:
-        _require(_is(sel, torch.int32, (cache.S, cache.Hkv, n_sel)), "sel: contiguous int32 [S, Hkv, n_sel]")
-    rc = lib().pced_block_select(cache.ref, q.data_ptr(), q_stride, q.shape[1], n_sel, n_first, n_last,
-                                 sel.data_ptr(), _ptr(status), _stream(stream))
+    rc = (_calls or _native()).block_select(cache.at, cache.gpu, q, n_sel, n_first, n_last, sel, status, _handle(stream))
     if rc:
         _check(rc, "pced_block_select")
     return sel
@@ -426,28 +423,16 @@ def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=N
     out [S, Hq, D], fp32 unless a bf16 `out` is passed.  lse: fp32 [S, Hq] that receives the log of the softmax's sum.
     total_rows: upper bound of the rows attended to (of one kv-head, over all sequences), 0: unknown.  A workspace of
     the caller's own is zeroed before its first use (workspace())."""
-    S, D = cache.S, cache.D
-    q_stride = _token_stride(q, S, 0, D, "q")
-    Hq = q.shape[1]
-    n_sel = 0
-    if sel is not None:
-        n_sel = sel.shape[-1]
-        _require(_is(sel, torch.int32, (S, cache.Hkv, n_sel)), "sel: contiguous int32 [S, Hkv, n_sel]")
-    kind = OUT_F32
     if out is None:
-        out = _empty((S, Hq, D), torch.float32, q.device, stream)
-    else:
-        kind = OUT_F32 if out.dtype == torch.float32 else OUT_BF16
-        _require(_is(out, torch.float32 if kind == OUT_F32 else torch.bfloat16, (S, Hq, D)),
-                 "out: contiguous fp32 or bf16 [S, Hq, D]")
-    _require(lse is None or _is(lse, torch.float32, (S, Hq)), "lse: contiguous fp32 [S, Hq]")
+        out = _empty((cache.S, q.shape[1], cache.D), torch.float32, q.device, stream)
     if ws is None:
-        ws = _empty(max(256, paged_attention_workspace_size(S, Hq, cache.Hkv, D)), torch.uint8, q.device, stream)
+        ws = _empty(max(256, paged_attention_workspace_size(cache.S, q.shape[1], cache.Hkv, cache.D)), torch.uint8,
+                    q.device, stream)
         with torch.cuda.stream(stream):  # (None: the current one)
             ws.zero_()
-    rc = lib().pced_paged_attention(cache.ref, q.data_ptr(), q_stride, Hq, _ptr(sel), n_sel, total_rows,
-                                    1.0 / math.sqrt(D) if scale is None else scale, out.data_ptr(), kind, _ptr(lse),
-                                    ws.data_ptr(), ws.numel(), _stream(stream))
+    rc = (_calls or _native()).paged_attention(cache.at, cache.gpu, q, sel, total_rows,
+                                               1.0 / math.sqrt(cache.D) if scale is None else scale, out, lse, ws,
+                                               _handle(stream))
     if rc:
         _check(rc, "pced_paged_attention")
     return out
@@ -460,43 +445,11 @@ def logits_process(logits, rows_per_query: int, history=None, history_len=None, 
     (bias_ids int32 and bias fp32 [B, n]) and masks (int32 words [n_masks, ceil(V / 32)], bit set: allowed; mask_row
     int32 [B], -1: none) applied.  out: another buffer of that shape and stride, or logits itself (in place);
     returned."""
-    _require(logits.dtype == torch.float32 and logits.dim() == 2 and logits.stride(1) == 1, "logits: fp32 [rows, V]")
-    rows, V = logits.shape
-    stride = logits.stride(0) if rows > 1 else V
-    _require(rows_per_query >= 1 and rows % rows_per_query == 0, "rows: a multiple of rows_per_query")
-    B = rows // rows_per_query
     if out is None:
-        out = _empty((rows, stride), torch.float32, logits.device, stream)[:, :V]
-    elif out is not logits:
-        _require(out.dtype == torch.float32 and out.shape == (rows, V)
-                 and out.stride() == (stride if rows > 1 else out.stride(0), 1),
-                 "out: fp32 of the shape and stride of logits")
-    n_hist = n_bias = n_masks = words = 0
-    if history is not None:
-        n_hist = history.shape[-1]
-        _require(_is(history, torch.int32, (B, n_hist)), "history: contiguous int32 [B, n]")
-        _require(history_len is not None and _is(history_len, torch.int32, (B,)), "history_len: int32 [B]")
-        _require(penalties is not None and _is(penalties, torch.float32, (B, 3)), "penalties: fp32 [B, 3]")
-        if n_hist == 0:
-            history = history_len = penalties = None
-    else:
-        _require(history_len is None and penalties is None, "history_len and penalties need a history")
-    if bias_ids is not None:
-        n_bias = bias_ids.shape[-1]
-        _require(_is(bias_ids, torch.int32, (B, n_bias)), "bias_ids: contiguous int32 [B, n]")
-        _require(bias is not None and _is(bias, torch.float32, (B, n_bias)), "bias: contiguous fp32 [B, n]")
-    else:
-        _require(bias is None, "bias needs bias_ids")
-    if mask is not None:
-        _require(mask.dim() == 2 and mask.dtype == torch.int32 and mask.is_contiguous(),
-                 "mask: contiguous int32 [n_masks, words]")
-        n_masks, words = mask.shape
-        _require(mask_row is None or _is(mask_row, torch.int32, (B,)), "mask_row: int32 [B]")
-    else:
-        _require(mask_row is None, "mask_row needs a mask")
-    rc = lib().pced_logits_process(logits.data_ptr(), out.data_ptr(), stride, B, rows_per_query, V, _ptr(history),
-                                   n_hist, _ptr(history_len), _ptr(penalties), _ptr(bias_ids), _ptr(bias), n_bias,
-                                   _ptr(mask), n_masks, words, _ptr(mask_row), _ptr(status), _stream(stream))
+        rows, V = logits.shape
+        out = _empty((rows, logits.stride(0) if rows > 1 else V), torch.float32, logits.device, stream)[:, :V]
+    rc = (_calls or _native()).logits_process(logits, rows_per_query, history, history_len, penalties, bias_ids, bias,
+                                              mask, mask_row, out, status, _handle(stream))
     if rc:
         _check(rc, "pced_logits_process")
     return out

@@ -157,3 +157,32 @@ def test_binding_refuses_bad_tensors(pced):
         with pytest.raises(ValueError):
             call()
             pytest.fail(f"call {i} was accepted")
+
+
+def test_binding_refuses_tensors_off_the_gpu(pced):
+    # right in everything but where they lie: host memory is never handed to a kernel
+    bf, i32 = torch.bfloat16, torch.int32
+    k = torch.zeros((4, 2, 16, 64), dtype=bf)
+    c = pced.PagedCache(k, k.clone(), torch.zeros((3, 2), dtype=i32), torch.ones(3, dtype=i32),
+                        summary=torch.zeros((4, 2, 2, 64), dtype=torch.int8), key_step=torch.ones(2))
+    q, kv = torch.zeros((3, 8, 64), dtype=bf), torch.zeros((3, 2, 64), dtype=bf)
+    ws = torch.zeros(1 << 22, dtype=torch.uint8)
+    for call in (lambda: pced.kv_append(c, q, kv, kv), lambda: pced.block_summaries(c),
+                 lambda: pced.block_select(c, q, 4), lambda: pced.paged_attention(c, q, ws=ws),
+                 lambda: pced.logits_process(torch.zeros(4, 8), 2)):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()
+
+
+def test_binding_refuses_what_is_no_tensor_or_number(pced):
+    k = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)
+    c = pced.PagedCache(k, k, torch.zeros((3, 2), dtype=torch.int32), torch.ones(3, dtype=torch.int32))
+    q = torch.zeros((3, 8, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        pced.kv_append(c, None, [1, 2], q[:, :2])
+    with pytest.raises(ValueError):
+        pced.block_select(c, q, 1 << 40, sel=torch.zeros((3, 2, 4), dtype=torch.int32))
+    with pytest.raises(TypeError):
+        pced.block_select(c, q, 4.5, sel=torch.zeros((3, 2, 4), dtype=torch.int32))
+    with pytest.raises(ValueError):
+        pced.paged_attention(c, q, total_rows=1, out=q.half(), ws=torch.zeros(256, dtype=torch.uint8))
