@@ -10,9 +10,13 @@
 // tokens (sixteen documents, 18,366 tokens of 32 + 16 heads of 128: 466 MB in 76 us,
 // 6.1 TB/s, 90 % of the copy rate), latency where there are few (nine tokens:
 // 2.6 us, a launch and three round trips).
+#include <cooperative_groups.h>
+
 #include "paged.cuh"
 
 namespace pced {
+
+namespace cg = cooperative_groups;
 
 struct AppendArgs {
   pced_paged_cache c;
@@ -205,29 +209,43 @@ __global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(A
   }
 }
 
-// Any number of tokens: a CTA takes one item and a kv-head, or `heads` of them.  D/16 lanes (a
-// unit) share a row of one kv-head and its group, each with the same channels of all
-// these heads, so a position's angles are read once for them, and a thread holds the
-// bounds of its channels' keys in registers.  (A page and kv-head has one CTA, so its
-// summary has one writer.)  SEVERAL: more than one kv-head, where items have so few
-// rows that a CTA's units would idle (272 sequences of two tokens: 17.5 us with one,
-// 7.1 with eight; but 33 of 32 tokens, with two, 14.3 against 9.0).
+// Any number of tokens: a CTA takes one item and a kv-head, or `heads` of them.  D/16
+// lanes (a unit) share a row of one kv-head and its group, each with the same channels
+// of all these heads, so a position's angles are read once for them, and a thread
+// holds the bounds of its channels' keys in registers.  (A page and kv-head has one
+// CTA, or one cluster, so its summary has one writer.)  APP_SEVERAL: more than one
+// kv-head, where items have so few rows that a CTA's units would idle (272 sequences
+// of two tokens: 17.5 us with one, 6.7 with eight; but 33 of 32 tokens, with two, 14.3
+// against 9.0).  APP_SHARED: where CTAs are few and their rows many, a cluster shares
+// the item's rows, and its first CTA brings the bounds together (four sequences of 94
+// to 568 tokens in 256-row pages, two kv-heads: 16.0 us, 9.0 with clusters of eight;
+// but four documents in 64-row pages, eight kv-heads, 21.0 us, 24.1 with two).
 // Sixteen documents: 134 us with a unit per head's row (angles read again for every
 // head), 89 us this way at 2 CTAs of 256 threads an SM, 81 us at 3, 78 us with an
 // item's heads side by side in the grid, 76 us with 6 CTAs of 128 threads.
+constexpr int APP_CLUSTER = 8;  // most CTAs of an item and kv-head
 constexpr int APP_HEADS = 3;  // heads whose loads a thread has in flight (six, at 2/3 of the CTAs: 1 % less time)
 
-template <int D, bool SEVERAL>
+enum AppendMode { APP_ONE_HEAD, APP_SEVERAL, APP_SHARED };
+
+template <int D, AppendMode MODE>
 __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a) {
   constexpr int LANES = D / 16, UNITS = APP_THREADS / LANES;
   constexpr int SIDE = 32 / LANES;  // units of a warp
   // (the heads of an item side by side: their parts of a token's row are neighbours in memory)
   const int tid = threadIdx.x, unit = tid / LANES, G = a.G, P = a.c.block_rows;
-  const int heads = SEVERAL ? a.heads : 1;
-  const int per_item = a.c.Hkv / heads, h0 = blockIdx.x % per_item * heads, h = h0 + (unit & (heads - 1));
+  const int heads = MODE == APP_SEVERAL ? a.heads : 1;
+  uint32_t group = blockIdx.x;
+  int ctas = 1, rank = 0;
+  if constexpr (MODE == APP_SHARED) {
+    ctas = cg::this_cluster().num_blocks(), rank = cg::this_cluster().block_rank();
+    group /= ctas;
+  }
+  const int per_item = a.c.Hkv / heads;
+  const int h0 = group % per_item * heads, h = h0 + (unit & (heads - 1));
   __shared__ uint32_t bounds[UNITS][2][D / 2];  // largest, smallest keys
   pdl_wait();
-  const AppendItem it = find_item(a, blockIdx.x / per_item);
+  const AppendItem it = find_item(a, group / per_item);
   if (it.s < 0) return;
   const int blk = paged_block(a.c, it.s, it.r0 / P, a.status);
   const int64_t page = (int64_t)blk * a.c.Hkv + h;
@@ -235,7 +253,12 @@ __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a)
   KeyBounds2 kb[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) kb[e].reset();
-  for (int i = unit / heads; i < it.m; i += UNITS / heads) {
+  int i0 = 0, i_end = it.m;  // this CTA's rows
+  if constexpr (MODE == APP_SHARED) {
+    const int part = (it.m + ctas - 1) / ctas;
+    i0 = rank * part, i_end = min(it.m, i0 + part);
+  }
+  for (int i = i0 + unit / heads; i < i_end; i += UNITS / heads) {
     const int64_t t = it.t0 + i;
     const int64_t row = (page * P + it.r0 % P + i) * D + f;
     float co[8], si[8];
@@ -285,8 +308,9 @@ __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a)
       bounds[unit][1][at] = kb[e].bottom();
     }
   }
-  __syncthreads();
-  for (int i = tid; i < heads * (D / 8); i += APP_THREADS) {  // eight channels of a head
+  if constexpr (MODE == APP_SHARED) cg::this_cluster().sync();
+  else __syncthreads();
+  for (int i = tid; rank == 0 && i < heads * (D / 8); i += APP_THREADS) {  // eight channels of a head
     const int hh = i / (D / 8), d = 8 * (i % (D / 8));
     uint32_t mx[4], mn[4];
 #pragma unroll
@@ -294,11 +318,18 @@ __global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a)
       KeyBounds2 b;
       b.reset();
       for (int u = hh; u < UNITS; u += max(heads, SIDE)) b.merge(bounds[u][0][d / 2 + e], bounds[u][1][d / 2 + e]);
+      if constexpr (MODE == APP_SHARED) {
+        for (int r = 1; r < ctas; ++r) {
+          const auto& of = *cg::this_cluster().map_shared_rank(&bounds, r);
+          for (int u = 0; u < UNITS; u += SIDE) b.merge(of[u][0][d / 2 + e], of[u][1][d / 2 + e]);
+        }
+      }
       mx[e] = b.top(), mn[e] = b.bottom();
     }
     update_summary(a.c.summary + ((int64_t)blk * a.c.Hkv + h0 + hh) * 2 * D, D, d, mx, mn,
                    __fdiv_rn(1.f, a.c.key_step[h0 + hh]), it.r0 % P == 0);
   }
+  if constexpr (MODE == APP_SHARED) cg::this_cluster().sync();  // (the others' bounds stay until they are read)
 }
 
 // ------------------------------------------------------------------ summaries
@@ -433,14 +464,26 @@ extern "C" pced_status pced_kv_append(const pced_paged_cache* cache, const void*
   } else {
     // blocks touched: at most two more than whole ones for every sequence with tokens
     const int64_t items = (int64_t)T / c.block_rows + 2 * (int64_t)(T < c.S ? T : c.S);
-    if (items * c.Hkv >= (INT64_C(1) << 31)) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
+    if (items * c.Hkv * APP_CLUSTER >= (INT64_C(1) << 31)) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
     const int units = APP_THREADS / (c.D / 16);
     const int64_t rows = T / items > 0 ? T / items : 1;  // of an item, about
     a.heads = 1;
     while (2 * a.heads * rows <= units && c.Hkv % (2 * a.heads) == 0) a.heads *= 2;
-    const auto kernel = a.heads > 1 ? (c.D == 128 ? kv_append_kernel<128, true> : kv_append_kernel<64, true>)
-                                    : (c.D == 128 ? kv_append_kernel<128, false> : kv_append_kernel<64, false>);
-    e = launch_pdl(kernel, dim3((unsigned)(items * (c.Hkv / a.heads))), APP_THREADS, 0, (cudaStream_t)stream, a);
+    const int64_t groups = items * (c.Hkv / a.heads);
+    // rows of a full item, about; CTAs of a cluster for them, while that leaves each its units' worth
+    const int64_t full = min((int64_t)c.block_rows, (int64_t)T / (T < c.S ? T : c.S));
+    int ctas = 1;
+    while (a.heads == 1 && ctas < APP_CLUSTER && groups * ctas < num_sms() && full >= 2 * ctas * units) ctas *= 2;
+    const dim3 grid((unsigned)(groups * ctas));
+    if (ctas > 1)
+      e = launch_cluster(c.D == 128 ? kv_append_kernel<128, APP_SHARED> : kv_append_kernel<64, APP_SHARED>, grid, ctas,
+                         APP_THREADS, 0, (cudaStream_t)stream, true, a);
+    else if (a.heads > 1)
+      e = launch_pdl(c.D == 128 ? kv_append_kernel<128, APP_SEVERAL> : kv_append_kernel<64, APP_SEVERAL>, grid,
+                     APP_THREADS, 0, (cudaStream_t)stream, a);
+    else
+      e = launch_pdl(c.D == 128 ? kv_append_kernel<128, APP_ONE_HEAD> : kv_append_kernel<64, APP_ONE_HEAD>, grid,
+                     APP_THREADS, 0, (cudaStream_t)stream, a);
   }
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "kv_append launch");
 }

@@ -238,3 +238,11 @@ def test_summaries_flag_bad_blocks(cuda_ok):
     want = ref.summaries(dict(c, table=good), old)
     want[good[0, 1]] = 0
     assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 1, 128), (28, 4, 128)])
+@pytest.mark.parametrize("P", [128, 256, 512])
+def test_items_shared_by_clusters(cuda_ok, heads, P):
+    # few sequences of many tokens in large pages: several CTAs bring a page's summary together
+    run([780, 700, 3 * P], [780, 650, 3 * P - 1], heads, P)
+    run([2 * P + 1], [2 * P], heads, P, packed=False)

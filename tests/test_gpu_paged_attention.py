@@ -201,3 +201,27 @@ def test_agrees_with_slab_attention(cuda_ok):
     want = pced.decode_attention(q.cuda(), *slab, torch.zeros(1, dtype=torch.int64, device="cuda"), one, one, Hkv, n)
     _, _, tol, _ = ref.attention(c, q)
     assert np.all(np.abs(ref.f64(out) - ref.f64(want)).max(axis=2) <= 2 * tol)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64), (16, 2, 64), (32, 8, 128), (28, 4, 128), (5, 5, 64)])
+def test_segments_of_one_tile_among_longer_ones(cuda_ok, heads):
+    # a warpgroup finishes a segment of one tile by itself, both meet for longer ones: every order of the two, idle
+    # sequences between them, and enough of them that a CTA holds many
+    Hq, Hkv, D = heads
+    rng = np.random.default_rng([Hq, 21])
+    lens = [int(x) for x in rng.choice([0, 1, 5, 17, 33, 64, 65, 100, 128, 129, 200], size=500)]
+    c = ref.make_cache(rng, lens, Hkv, D, 64)
+    q = ref.rng_bf16(rng, (len(lens), Hq, D))
+    out, lse = run(c, q)
+    ref.check_attention(c, q, out, lse)
+
+
+@pytest.mark.parametrize("heads,n", [((4, 1, 64), 60_000), ((1, 1, 128), 30_000), ((8, 1, 128), 30_000), ((7, 1, 64), 12_000)])
+def test_one_segment_over_all_ctas(cuda_ok, heads, n):
+    # so many records that their merge is shared among the threads
+    Hq, Hkv, D = heads
+    rng = np.random.default_rng([Hq, n])
+    c = ref.make_cache(rng, [n, 3], Hkv, D, 256)
+    q = ref.rng_bf16(rng, (2, Hq, D))
+    out, lse = run(c, q)
+    ref.check_attention(c, q, out, lse)
