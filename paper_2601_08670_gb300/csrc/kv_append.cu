@@ -217,19 +217,21 @@ __global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(A
 // kv-head, where items have so few rows that a CTA's units would idle (272 sequences
 // of two tokens: 17.5 us with one, 6.7 with eight; but 33 of 32 tokens, with two, 14.3
 // against 9.0).  APP_SHARED: where CTAs are few and their rows many, a cluster shares
-// the item's rows, and its first CTA brings the bounds together (four sequences of 94
-// to 568 tokens in 256-row pages, two kv-heads: 16.0 us, 9.0 with clusters of eight;
-// but four documents in 64-row pages, eight kv-heads, 21.0 us, 24.1 with two).
+// the item's rows, and its first CTA brings the bounds together (eight sequences of 278
+// tokens in 256-row pages: 44.3 us, 21.0 with clusters of four; but where the CTAs of
+// clusters no longer fit the SMs at once, four documents of 64-row pages, 24.1 us
+// became 29.7).
 // Sixteen documents: 134 us with a unit per head's row (angles read again for every
 // head), 89 us this way at 2 CTAs of 256 threads an SM, 81 us at 3, 78 us with an
 // item's heads side by side in the grid, 76 us with 6 CTAs of 128 threads.
+constexpr int APP_CTAS = 6;     // CTAs that an SM holds
 constexpr int APP_CLUSTER = 8;  // most CTAs of an item and kv-head
 constexpr int APP_HEADS = 3;  // heads whose loads a thread has in flight (six, at 2/3 of the CTAs: 1 % less time)
 
 enum AppendMode { APP_ONE_HEAD, APP_SEVERAL, APP_SHARED };
 
 template <int D, AppendMode MODE>
-__global__ void __launch_bounds__(APP_THREADS, 6) kv_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(APP_THREADS, APP_CTAS) kv_append_kernel(AppendArgs a) {
   constexpr int LANES = D / 16, UNITS = APP_THREADS / LANES;
   constexpr int SIDE = 32 / LANES;  // units of a warp
   // (the heads of an item side by side: their parts of a token's row are neighbours in memory)
@@ -470,10 +472,13 @@ extern "C" pced_status pced_kv_append(const pced_paged_cache* cache, const void*
     a.heads = 1;
     while (2 * a.heads * rows <= units && c.Hkv % (2 * a.heads) == 0) a.heads *= 2;
     const int64_t groups = items * (c.Hkv / a.heads);
-    // rows of a full item, about; CTAs of a cluster for them, while that leaves each its units' worth
+    // rows of a full item, about; CTAs of a cluster for them, while that leaves each its units' worth and all
+    // fit the SMs at once
     const int64_t full = min((int64_t)c.block_rows, (int64_t)T / (T < c.S ? T : c.S));
     int ctas = 1;
-    while (a.heads == 1 && ctas < APP_CLUSTER && groups * ctas < num_sms() && full >= 2 * ctas * units) ctas *= 2;
+    while (a.heads == 1 && ctas < APP_CLUSTER && 2 * ctas * groups <= APP_CTAS * (int64_t)num_sms() &&
+           full >= 2 * ctas * units)
+      ctas *= 2;
     const dim3 grid((unsigned)(groups * ctas));
     if (ctas > 1)
       e = launch_cluster(c.D == 128 ? kv_append_kernel<128, APP_SHARED> : kv_append_kernel<64, APP_SHARED>, grid, ctas,
