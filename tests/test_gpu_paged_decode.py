@@ -143,3 +143,55 @@ def test_operators_rebuild_the_step(cuda_ok):
                 assert int(token[b]) == int(dec.history[b, step]) and int(expert[b]) == int(dec.expert_trace[b, step])
         tok = dec.history[:, step].long()
     assert dec.status() == 0
+
+
+def test_operators_in_one_graph(cuda_ok):
+    # a layer's calls and the logits' captured together: replays follow the lengths and buffers on the device
+    import numpy as np
+    import paged_ref as ref
+    import paper_2601_08670_gb300 as pced
+    rng = np.random.default_rng(31)
+    Hq, Hkv, D, P, lens = 8, 2, 64, 16, [100, 700, 0, 33]
+    c = ref.make_cache(rng, lens, Hkv, D, P, spare=8, spoil=False)
+    S = len(lens)
+    cache = ref.to_device(c, np.zeros((len(c["k"]), Hkv, 2, D), np.int8))
+    pced.block_summaries(cache)
+    base = {n: getattr(cache, n).clone() for n in ("k", "v", "summary", "seq_len")}
+    qkv = torch.empty((S, Hq + 2 * Hkv, D), dtype=torch.bfloat16, device="cuda")
+    rope = pced.rope_table(1e4, D, 1000)
+    bufs = dict(q=torch.empty((S, Hq, D), dtype=torch.bfloat16, device="cuda"),
+                sel=torch.empty((S, Hkv, 6), dtype=torch.int32, device="cuda"),
+                out=torch.empty((S, Hq, D), device="cuda"), y=torch.empty((S, 500), device="cuda"))
+    ws = pced.workspace(pced.paged_attention_workspace_size(S, Hq, Hkv, D), "cuda")
+    x = torch.from_numpy(rng.normal(size=(S, 500)).astype(np.float32)).cuda()
+    hist, n_hist = torch.zeros((2, 4), dtype=torch.int32, device="cuda"), torch.full((2,), 4, dtype=torch.int32,
+                                                                                    device="cuda")
+    pen = torch.full((2, 3), 1.5, device="cuda")
+    one = (cache.seq_len > 0).to(torch.int32)
+
+    def layer():
+        cache.seq_len.add_(one)
+        pced.kv_append(cache, qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], rope=rope, q_out=bufs["q"])
+        pced.block_select(cache, bufs["q"], 6, sel=bufs["sel"])
+        pced.paged_attention(cache, bufs["q"], sel=bufs["sel"], out=bufs["out"], ws=ws)
+        pced.logits_process(x, 2, history=hist, history_len=n_hist, penalties=pen, out=bufs["y"])
+
+    inputs = [ref.rng_bf16(rng, (S, Hq + 2 * Hkv, D)).cuda() for _ in range(3)]
+    results = []
+    for graphed in (False, True):
+        for n, t in base.items():
+            getattr(cache, n).copy_(t)
+        if graphed:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                layer()
+        got = []
+        for v in inputs:
+            qkv.copy_(v)
+            g.replay() if graphed else layer()
+            got.append([t.clone() for t in (*bufs.values(), cache.k, cache.summary)])
+        results.append(got)
+    torch.cuda.synchronize()
+    assert pced.device_status(ws) == 0
+    for a, b in zip(*results):
+        assert all(torch.equal(s, t) for s, t in zip(a, b))
