@@ -21,7 +21,7 @@
 // sequences, 1.32 GB in 193 us: the measured copy rate), for short ones the chain
 // before the first tile (launch, lengths, plan, table: 2.4 us) and after the last
 // (partials, record, count, merge: 3 us): 9 x 2081 rows, 77 MB, 17 us, of which 11
-// stream; three sequences of 257 rows 5.5 us.  A CTA has one tile at least: with
+// stream; three sequences of 257 rows 5.8 us.  A CTA has one tile at least: with
 // four these took 10 us, as a tile's own chain is longer than a record's merge.
 // Tiles prefetched into L2 ahead of the ring made every case slower (17 x 64 blocks
 // of 64 rows by 15-24 %); a ring of three tiles costs 1-3 %.
