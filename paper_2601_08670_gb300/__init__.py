@@ -410,9 +410,6 @@ def block_select(cache: PagedCache, q, n_sel: int, n_first: int = 1, n_last: int
     return sel
 
 
-OUT_F32, OUT_BF16 = 0, 1
-
-
 def paged_attention_workspace_size(S, Hq, Hkv, D) -> int:
     return int(lib().pced_paged_attention_workspace_size(S, Hq, Hkv, D))
 

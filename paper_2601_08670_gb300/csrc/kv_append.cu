@@ -166,8 +166,10 @@ __device__ __forceinline__ void update_summary(int8_t* summary, int D, int f, co
 // of a head (key, value, the group's queries), so every row's load is asked for at
 // once, beside the length.  Nine tokens 2.6 us; with the kernel for any number of
 // tokens, which looks for its tokens first, 3.1 us.
+constexpr int APP_ONE_THREADS = 8 * (PAGED_MAX_G + 2);  // (D = 128)
+
 template <int D>
-__global__ void __launch_bounds__(32 * (PAGED_MAX_G + 2)) kv_append_one_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(APP_ONE_THREADS) kv_append_one_kernel(AppendArgs a) {
   constexpr int LANES = D / 16;
   const int tid = threadIdx.x, s = blockIdx.y, h = blockIdx.x, G = a.G, P = a.c.block_rows;
   const int role = tid / LANES, f = 8 * (tid % LANES);  // role 0: key, 1: value, then queries

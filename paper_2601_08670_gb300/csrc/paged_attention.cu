@@ -21,7 +21,7 @@
 // sequences, 1.32 GB in 193 us: the measured copy rate), for short ones the chain
 // before the first tile (launch, lengths, plan, table: 2.4 us) and after the last
 // (partials, record, count, merge: 3 us): 9 x 2081 rows, 77 MB, 17 us, of which 11
-// stream; three sequences of 257 rows 5.8 us.  A CTA has one tile at least: with
+// stream; three sequences of 257 rows 5.5 us.  A CTA has one tile at least: with
 // four these took 10 us, as a tile's own chain is longer than a record's merge.
 // Tiles prefetched into L2 ahead of the ring made every case slower (17 x 64 blocks
 // of 64 rows by 15-24 %); a ring of three tiles costs 1-3 %.
@@ -103,7 +103,7 @@ __device__ __forceinline__ bool bar_sync_warps(uint32_t bar, uint32_t& phase, in
 template <int D>
 struct PagedCfg : AttCfg<D> {
   using B = AttCfg<D>;
-  static constexpr size_t BARS = (2 * B::STAGES + 6) * 8;
+  static constexpr size_t BARS = (2 * B::STAGES + 4) * 8;
   static constexpr size_t DESC = (size_t)B::STAGES * 4;
   static constexpr size_t SMEM = 1024 + (size_t)B::STAGES * B::STAGE_BYTES + BARS + (size_t)B::PARTIALS * 4 +
                                  (3 * PAGED_MAX_S + 1) * 4 + DESC + 64;
@@ -176,23 +176,24 @@ __device__ __forceinline__ void merge_records(const PagedAttArgs& a, int c, int 
   }
 }
 
-// The partials (store_partial) of W warps from warp w0 on merged for outputs idx0 ...
-// idx0 + 3 of head hh: load_merged without its branches, so that all warps' values
+// The eight warps' partials (store_partial) merged for outputs idx0 ... idx0 + 3 of
+// head hh: load_merged without its branches, so that all warps' values
 // are in flight (a piece took the epilogue 1.2 us with them; a warp without rows has
 // a sum and an o of zero).
-template <int D, int W>
-__device__ __forceinline__ void merge_partials(const float* ms, const float* ls, const float* os, int w0, int G, int hh,
+template <int D>
+__device__ __forceinline__ void merge_partials(const float* ms, const float* ls, const float* os, int G, int hh,
                                                int idx0, float& mx, float& lsum, float (&acc)[4]) {
+  constexpr int W = ATT_CONSUMERS;
   float m[W], l[W];
   float4 o[W];
 #pragma unroll
   for (int w = 0; w < W; w += 4) {
-    *reinterpret_cast<float4*>(m + w) = *reinterpret_cast<const float4*>(ms + hh * ATT_CONSUMERS + w0 + w);
-    *reinterpret_cast<float4*>(l + w) = *reinterpret_cast<const float4*>(ls + hh * ATT_CONSUMERS + w0 + w);
+    *reinterpret_cast<float4*>(m + w) = *reinterpret_cast<const float4*>(ms + hh * W + w);
+    *reinterpret_cast<float4*>(l + w) = *reinterpret_cast<const float4*>(ls + hh * W + w);
   }
 #pragma unroll
   for (int w = 0; w < W; ++w)
-    o[w] = *reinterpret_cast<const float4*>(os + ((w0 + w) * G + hh) * AttCfg<D>::OROW + (idx0 - hh * D));
+    o[w] = *reinterpret_cast<const float4*>(os + (w * G + hh) * AttCfg<D>::OROW + (idx0 - hh * D));
   mx = m[0];
 #pragma unroll
   for (int w = 1; w < W; ++w) mx = fmaxf(mx, m[w]);
@@ -228,7 +229,7 @@ __device__ __forceinline__ bool finish_piece(const PagedAttArgs& a, const PagedP
   for (int i = et; i < GD / 4; i += NT) {
     const int hh = i / (D / 4), idx0 = 4 * i;
     float mx, lsum, acc[4];
-    merge_partials<D, ATT_CONSUMERS>(ms, ls, os, 0, G, hh, idx0, mx, lsum, acc);
+    merge_partials<D>(ms, ls, os, G, hh, idx0, mx, lsum, acc);
     if (whole) {
       write_out(a, pc.s, pc.h, D, hh, idx0, mx, lsum, acc);
     } else {
@@ -292,9 +293,11 @@ __device__ __forceinline__ bool finish_piece(const PagedAttArgs& a, const PagedP
 // finished pieces themselves, a CTA with a segment's end in its range took 2.5 us
 // longer than one without (17.0 and 14.5 us of the 9 x 2081 rows' 19).
 //
-// (Only a CTA's last piece is the consumers' own matter: they are more, and idle; and
-// a segment of one tile its warpgroup's, while the other one takes the next: 2176
-// segments of 16 to 64 rows 24.3 us, 22.3 so.)
+// (Only a CTA's last piece is the consumers' own matter: they are more, and idle.)
+// A warpgroup that finished segments of one tile alone, while the other one took the
+// next, brought 2176 segments of 16 to 64 rows from 24.3 to 22.3 us, but every other
+// call 1 to 4 % more time, the more the colder the code (a layer of 9 sequences and
+// 16 selected blocks between matrix products: 39.2 us against 37.5).
 //
 // SMALL: block_rows is no multiple of 64, so every tile comes in 16-row boxes,
 // each of its own block.
@@ -309,11 +312,11 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t smem0 = (raw + 1023u) & ~1023u;
   uint8_t* gbase = smem_raw + (smem0 - raw);
-  // layout: stages | full[STAGES] | empty[STAGES] | partials full | partials empty | epilogue | last piece | warpgroups | partials | tables
+  // layout: stages | full[STAGES] | empty[STAGES] | partials full | partials empty | epilogue | last piece | partials | tables
   const uint32_t bar_full = smem0 + C::STAGES * C::STAGE_BYTES;
   const uint32_t bar_empty = bar_full + C::STAGES * 8;
   const uint32_t bar_pfull = bar_empty + C::STAGES * 8, bar_pempty = bar_pfull + 8;
-  const uint32_t bar_epi = bar_pempty + 8, bar_last = bar_epi + 8, bar_wg0 = bar_last + 8;
+  const uint32_t bar_epi = bar_pempty + 8, bar_last = bar_epi + 8;
   float* ms = reinterpret_cast<float*>(gbase + C::STAGES * C::STAGE_BYTES + C::BARS);
   float* ls = ms + ATT_CONSUMERS * ATT_MAX_G;
   float* os = ls + ATT_CONSUMERS * ATT_MAX_G;
@@ -335,7 +338,6 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
     mbar_init(bar_pempty, PATT_EPI);
     mbar_init(bar_epi, PATT_EPI);
     mbar_init(bar_last, ATT_CONSUMERS);
-    for (int i = 0; i < 2; ++i) mbar_init(bar_wg0 + 8 * i, 4);
     mbar_fence_init();
   }
   if (warp == ATT_CONSUMERS && lane == 0) {
@@ -480,14 +482,11 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
     if (r_begin >= r_end) return;
     PagedPiece pc = plan.at(r_begin, r_end);
     uint32_t phase = 0;
-    for (int32_t p = r_begin + pc.t1 - pc.t0, np = 0; p < r_end; p += pc.t1 - pc.t0) {
-      if (pc.nt > 1) {  // (segments of one tile are their warpgroup's matter)
-        if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
-        if (!finish_piece<D, PATT_EPI * 32>(a, pc, base[pc.s], per, ms, ls, os, et, bar_epi, phase, bar_pempty,
-                                            last_here))
-          return;
-        ++np;
-      }
+    for (int32_t p = r_begin + pc.t1 - pc.t0, np = 0; p < r_end; p += pc.t1 - pc.t0, ++np) {
+      if (!mbar_wait(bar_pfull, np & 1u, a.status)) return;
+      if (!finish_piece<D, PATT_EPI * 32>(a, pc, base[pc.s], per, ms, ls, os, et, bar_epi, phase, bar_pempty,
+                                          last_here))
+        return;
       pc = plan.after(pc, p, r_end);
     }
     return;
@@ -496,7 +495,6 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
   // -------------------------------------------------------------- consumers
   if (r_begin >= r_end) return;
   const int wg = warp >> 2, kb = PATT_GRAN * (warp & 3);
-  const uint32_t bar_wg = bar_wg0 + 8 * wg;
   const int g = lane >> 2, tq = lane & 3;
   // B column g of S^T = K Q^T is head g; with PK columns 4-7 repeat heads 0-3
   const int qh = PK ? (g & 3) : g;
@@ -514,10 +512,8 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
   PagedPiece pc = plan.at(r_begin, r_end);
   load_q(pc);
   uint32_t it = 0, st = 0, use = 0, np = 0;  // tile counter, its stage and use of the stage; shared pieces done
-  uint32_t wg_phase = 0;
-  for (int32_t p = r_begin;;) {
+  for (int32_t p = r_begin;; ++np) {
     p += pc.t1 - pc.t0;
-    const bool alone = pc.nt == 1, here = (int)(it & 1u) == wg;  // one tile: the other warpgroup goes on
     WarpAcc<D> A;
     acc_reset(A);
     for (int32_t t = pc.t0; t < pc.t1; ++t, ++it, st = st + 1 == C::STAGES ? (++use, 0u) : st + 1) {
@@ -537,15 +533,9 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
     }
     const bool more = p < r_end;
     const PagedPiece last = pc;
-    if (alone && !here) {
-      if (!more) return;
-      pc = plan.after(pc, p, r_end);
-      if (pc.nt > 1 || (int)(it & 1u) == wg) load_q(pc);
-      continue;
-    }
     if (more) {  // the next piece's queries come while this one's partials go
       pc = plan.after(pc, p, r_end);
-      if (pc.nt > 1 || (int)(it & 1u) == wg) load_q(pc);
+      load_q(pc);
     }
     // scores that are all not numbers moved no maximum: their sum shall not be dropped with it
     if (__any_sync(0xffffffffu, (A.m0 == -INFINITY && A.l0 != A.l0) || (A.m1 == -INFINITY && A.l1 != A.l1))) {
@@ -556,23 +546,9 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
     // the previous piece's partials have been read
     if (np > 0 && !mbar_wait(bar_pempty, (np - 1u) & 1u, a.status)) return;
     store_partial<D>(A, ms, ls, os, G, warp, lane);
-    if (alone) {  // its four warps' partials into the output
-      if (!bar_sync_warps(bar_wg, wg_phase, lane, a.status)) return;
-      for (int i = tid & 127; i < G * (D / 4); i += 128) {
-        float mx, lsum, acc[4];
-        merge_partials<D, 4>(ms, ls, os, 4 * wg, G, i / (D / 4), 4 * i, mx, lsum, acc);
-        write_out(a, last.s, last.h, D, i / (D / 4), 4 * i, mx, lsum, acc);
-      }
-      if (!more) return;
-      if (!bar_sync_warps(bar_wg, wg_phase, lane, a.status)) return;  // (they are read before the next ones come)
-      continue;
-    }
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_pfull);
-    if (more) {
-      ++np;
-      continue;
-    }
+    if (more) continue;
     // the CTA's last piece
     uint32_t phase = 0;
     if (mbar_wait(bar_pfull, np & 1u, a.status))
