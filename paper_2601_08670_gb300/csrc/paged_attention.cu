@@ -639,8 +639,8 @@ extern "C" pced_status pced_paged_attention(const pced_paged_cache* cache, const
   // a CTA for every SM, fewer where the caller's bound of the rows needs no more
   int64_t ctas = sms < PATT_MAX_CTAS ? sms : PATT_MAX_CTAS;
   if (total_rows > 0) {
-    const int64_t tiles = (total_rows / ATT_BLOCK_N + c.S) * c.Hkv;
-    if (tiles < ctas) ctas = tiles;
+    const int64_t tiles = total_rows / ATT_BLOCK_N + c.S;  // of a kv-head
+    if (tiles < ctas) ctas = min(ctas, tiles * c.Hkv);
   }
   const cudaError_t e = c.D == 128 ? launch_paged_d<128>(maps, a, (int)ctas, (cudaStream_t)stream)
                                    : launch_paged_d<64>(maps, a, (int)ctas, (cudaStream_t)stream);
