@@ -482,7 +482,8 @@ pced_status pced_kv_append(const pced_paged_cache* cache, const void* q, int64_t
 /* ------------------------------------------------------------------------
  * pced_block_summaries -- summaries of all live blocks of the sequences, for
  * caches that were built elsewhere (documents encoded offline); the rows past
- * a sequence's last do not count.  Blocks without live rows keep theirs.
+ * a sequence's last do not count.  Blocks without live rows keep theirs.  A block
+ * of several sequences has to be as long in each.
  * ------------------------------------------------------------------------ */
 pced_status pced_block_summaries(const pced_paged_cache* cache, int32_t* status, void* stream);
 
@@ -496,7 +497,7 @@ pced_status pced_block_summaries(const pced_paged_cache* cache, int32_t* status,
  *   score(j) = sum_d p_d max_jd + n_d min_jd,
  * an upper bound, in steps, of the group's summed q.k over the block.  p, n and
  * the summaries are whole numbers, so a choice depends on no order of sums.
- * Ties go to the lowest block.  m zero or not finite: all scores are 0.
+ * Ties go to the lowest block.  Where m or 127 / m is not finite all scores are 0.
  *   q    bf16 [S][Hq][D], sequence s at s * q_stride elements (16-byte
  *        aligned, a multiple of 8)
  *   sel  int32 [S][Hkv][n_sel]: block numbers j (indices into the sequence's
@@ -526,7 +527,9 @@ pced_status pced_block_select(const pced_paged_cache* cache, const void* q, int6
  * are held to 24 bits, sums in fp32.  Supports Hq/Hkv <= 8 and
  * S*Hkv*(max_blocks*block_rows/64 + 2) < 2^31.  The workspace must
  * be zero-filled before the first call: besides the status word it holds
- * counters that a call leaves at zero.
+ * counters that a call leaves at zero (one that set PCED_DEV_TIMEOUT may not:
+ * fill it again).  Calls that can overlap need a workspace each.  An infinite
+ * value among the rows attended to gives infinities or not-a-number.
  * ------------------------------------------------------------------------ */
 #define PCED_OUT_F32 0
 #define PCED_OUT_BF16 1

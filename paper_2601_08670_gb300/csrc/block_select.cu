@@ -158,8 +158,9 @@ __global__ void __launch_bounds__(BSEL_THREADS, 5) block_select_kernel(SelectArg
   m = wmax[0];
 #pragma unroll
   for (int w = 1; w < BSEL_THREADS / 32; ++w) m = fmaxf(m, wmax[w]);
+  const float per_one = __fdiv_rn(127.f, m);  // (infinite where m is zero or next to it)
   if (tid < 2 * D)
-    pooled[tid] = m > 0.f && m < INFINITY ? (int8_t)(int)rintf(__fmul_rn(p, __fdiv_rn(127.f, m))) : (int8_t)0;
+    pooled[tid] = per_one < INFINITY && m < INFINITY ? (int8_t)(int)rintf(__fmul_rn(p, per_one)) : (int8_t)0;
   __syncthreads();
   if (ctas > 1) cluster.barrier_wait();
   // ---- scores

@@ -82,3 +82,18 @@ def test_extreme_summaries(cuda_ok):
         summ[c["table"][0, 30]] = -127
         summ[c["table"][1, 31], :, 1] = 127
     run([1000, 1100], (16, 2, 64), 16, 40, change=change)
+
+
+def test_queries_next_to_zero(cuda_ok):
+    """127 / m is infinite: all scores are 0, so the lowest blocks follow the first and the last ones."""
+    import paper_2601_08670_gb300 as pced
+    rng = np.random.default_rng(5)
+    for blocks in (40, 700):  # counted, and by the radix
+        table, nb = ref.make_table(rng, [blocks * 16], 16)
+        summ = torch.from_numpy(rng.integers(-127, 128, size=(nb, 2, 2, 64)).astype(np.int8)).cuda()
+        cache = pced.PagedCache(None, None, torch.from_numpy(table).cuda(),
+                                torch.tensor([blocks * 16], dtype=torch.int32, device="cuda"), block_rows=16,
+                                summary=summ)
+        q = (ref.rng_bf16(rng, (1, 8, 64)).float().clamp(-2, 2) * 2.0 ** -126).to(torch.bfloat16).cuda()
+        sel = pced.block_select(cache, q, 10, 1, 2).cpu().numpy()
+        assert np.array_equal(sel, np.tile([*range(8), blocks - 2, blocks - 1], (1, 2, 1)))
