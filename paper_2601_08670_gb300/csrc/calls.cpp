@@ -44,6 +44,8 @@ double real(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw Refused("");
   return v;
 }
+// (a tensor without elements has no address, which the library takes for an
+// argument that was not given: where that is not the same, the sizes are checked first)
 void* address(const at::Tensor* t) { return t ? const_cast<void*>(t->const_data_ptr()) : nullptr; }
 
 bool has_shape(const at::Tensor& t, std::initializer_list<int64_t> shape) {
@@ -52,6 +54,10 @@ bool has_shape(const at::Tensor& t, std::initializer_list<int64_t> shape) {
 // contiguous, of this type and shape (None: fine)
 void check(const at::Tensor* t, at::ScalarType type, std::initializer_list<int64_t> shape, const char* what) {
   require(!t || (t->scalar_type() == type && has_shape(*t, shape) && t->is_contiguous()), what);
+}
+// a device status word (None: none)
+void check_status(const at::Tensor* t) {
+  require(!t || (t->scalar_type() == at::kInt && t->numel() > 0), "status: int32, a word at least");
 }
 // elements between the tokens of t: bf16 [T, heads (0: any), D], a token's heads side by side
 int64_t token_stride(const at::Tensor* t, int64_t T, int64_t heads, int64_t D, const char* what) {
@@ -110,10 +116,11 @@ pced_status kv_append(PyObject* const* a) {
     require(rope->dim() == 2, "rope: contiguous fp32 [rows, D]");
     rows = rope->size(0);
     check(rope, at::kFloat, {rows, c.D}, "rope: contiguous fp32 [rows, D]");
+    require(rows > 0, "rope: a table without rows");
   }
   check(start, at::kInt, {c.S + 1}, "tok_start: int32 [S + 1]");
   check(pos, at::kInt, {T}, "positions: int32 [T]");
-  require(!status || status->scalar_type() == at::kInt, "status: int32");
+  check_status(status);
   require(T <= INT32_MAX && rows <= INT32_MAX, "T, rows: below 2^31");
   cache.on_gpu();
   on_gpu({q, k, v, rope, start, pos, out, status}, cache.device);
@@ -129,7 +136,7 @@ pced_status kv_append(PyObject* const* a) {
 pced_status block_summaries(PyObject* const* a) {
   const Cache cache(a[0], a[1]);
   const at::Tensor* status = tensor(a[2], "status");
-  require(!status || status->scalar_type() == at::kInt, "status: int32");
+  check_status(status);
   cache.on_gpu();
   on_gpu({status}, cache.device);
   void* s = stream_of(a[3]);
@@ -145,7 +152,7 @@ pced_status block_select(PyObject* const* a) {
   const int64_t qs = token_stride(q, c.S, 0, c.D, "q: bf16 [S, Hq, D], a token's heads side by side");
   require(sel, "sel: contiguous int32 [S, Hkv, n_sel]");
   check(sel, at::kInt, {c.S, c.Hkv, n_sel}, "sel: contiguous int32 [S, Hkv, n_sel]");
-  require(!status || status->scalar_type() == at::kInt, "status: int32");
+  check_status(status);
   cache.on_gpu();
   on_gpu({q, sel, status}, cache.device);
   void* s = stream_of(a[8]);
@@ -170,6 +177,7 @@ pced_status paged_attention(PyObject* const* a) {
     require(sel->dim() == 3, "sel: contiguous int32 [S, Hkv, n_sel]");
     n_sel = sel->size(2);
     check(sel, at::kInt, {c.S, c.Hkv, n_sel}, "sel: contiguous int32 [S, Hkv, n_sel]");
+    require(n_sel > 0, "sel: no place for a block (None: all blocks)");
   }
   require(out && ws, "out, ws: tensors");
   const bool f32 = out->scalar_type() == at::kFloat;
@@ -225,11 +233,12 @@ pced_status logits_process(PyObject* const* a) {
     require(mask->dim() == 2, "mask: contiguous int32 [n_masks, words]");
     n_masks = mask->size(0), words = mask->size(1);
     check(mask, at::kInt, {n_masks, words}, "mask: contiguous int32 [n_masks, words]");
+    require(n_masks > 0 && words > 0, "mask: no masks, or masks without words");
     check(row, at::kInt, {B}, "mask_row: int32 [B]");
   } else {
     require(!row, "mask_row needs a mask");
   }
-  require(!status || status->scalar_type() == at::kInt, "status: int32");
+  check_status(status);
   for (const int64_t n : {B, R, V, n_hist, n_bias, n_masks, words}) require(n <= INT32_MAX, "sizes: below 2^31");
   require(x->is_cuda(), "logits: on a CUDA device");
   on_gpu({x, hist, len, pen, ids, bias, mask, row, out, status}, x->get_device());
