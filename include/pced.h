@@ -470,9 +470,10 @@ typedef struct pced_paged_cache {
  *   status     device int32 word, may be NULL
  * With cache->summary the blocks' summaries follow: a block whose first row
  * is appended starts anew, another one takes the new keys in.  Blocks being
- * appended to belong to one sequence.  Counts that are negative, above the
- * sequence's rows or beyond T set PCED_DEV_BAD_LENGTH, and that sequence's
- * tokens are left out.  Supports Hq/Hkv <= 8.
+ * appended to belong to one sequence.  A sequence whose starts lie outside
+ * [0, T] or count more tokens than it has rows sets PCED_DEV_BAD_LENGTH and its
+ * tokens are left out (their rows of q_out are not written); where the starts
+ * fall, so are those of every sequence from there on.  Supports Hq/Hkv <= 8.
  * ------------------------------------------------------------------------ */
 pced_status pced_kv_append(const pced_paged_cache* cache, const void* q, int64_t q_stride, const void* k,
                            int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int32_t Hq,

@@ -41,10 +41,11 @@ struct AppendItem {
 };
 
 // New rows of sequence s: {first token, count, live rows}; count 0 where the
-// counts do not fit (flagged).
-__device__ __forceinline__ int3 new_rows(const AppendArgs& a, int s) {
+// counts do not fit (flagged).  falls: its starts fall.
+__device__ __forceinline__ int3 new_rows(const AppendArgs& a, int s, bool& falls) {
   const int n = paged_len(a.c, s, a.status);
   const int t0 = a.tok_start[s], t1 = a.tok_start[s + 1];
+  falls = t1 < t0;
   if (t0 < 0 || t1 < t0 || t1 > a.T || t1 - t0 > n) {
     dev_flag(a.status, PCED_DEV_BAD_LENGTH);
     return make_int3(0, 0, n);
@@ -56,19 +57,23 @@ __device__ __forceinline__ int blocks_touched(int3 r, int P) {
 }
 
 // Item `want` of the call: its sequence by the prefix of blocks touched.  All
-// threads; s = -1 past the last.
+// threads; s = -1 past the last.  Up to where the starts first fall they share
+// the tokens out, so that the launch has an item for every block touched; from
+// there on tokens could be named twice, and no sequence gets any.
 __device__ __forceinline__ AppendItem find_item(const AppendArgs& a, int want) {
   constexpr int PER = PAGED_MAX_S / APP_THREADS;  // sequences of a thread
-  __shared__ int wsum[APP_THREADS / 32];
+  __shared__ int wsum[APP_THREADS / 32], wfall[APP_THREADS / 32];
   __shared__ AppendItem it;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, P = a.c.block_rows;
   const int per = (a.c.S + APP_THREADS - 1) / APP_THREADS, s0 = tid * per;
   int3 r[PER];
-  int nb[PER], own = 0;
+  int nb[PER], own = 0, fall = INT32_MAX;  // the first sequence at which the starts fall
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const bool in = i < per && s0 + i < a.c.S;
-    r[i] = in ? new_rows(a, s0 + i) : make_int3(0, 0, 0);
+    bool falls = false;
+    r[i] = in ? new_rows(a, s0 + i, falls) : make_int3(0, 0, 0);
+    if (falls) fall = min(fall, s0 + i);
     nb[i] = blocks_touched(r[i], P);
     own += nb[i];
   }
@@ -78,15 +83,19 @@ __device__ __forceinline__ AppendItem find_item(const AppendArgs& a, int want) {
     const int v = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += v;
   }
-  if (lane == 31) wsum[warp] = incl;
+  fall = __reduce_min_sync(0xffffffffu, fall);
+  if (lane == 31) wsum[warp] = incl, wfall[warp] = fall;
   if (tid == 0) it.s = -1;
   __syncthreads();
   int at = incl - own;
 #pragma unroll
-  for (int w = 0; w < APP_THREADS / 32; ++w) at += w < warp ? wsum[w] : 0;
+  for (int w = 0; w < APP_THREADS / 32; ++w) {
+    at += w < warp ? wsum[w] : 0;
+    fall = min(fall, wfall[w]);
+  }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    if (want >= at && want < at + nb[i]) {
+    if (want >= at && want < at + nb[i] && s0 + i < fall) {
       const int first = r[i].z - r[i].y, j = first / P + (want - at);
       it.s = s0 + i;
       it.r0 = max(first, j * P);
