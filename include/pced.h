@@ -470,7 +470,9 @@ typedef struct pced_paged_cache {
  *   status     device int32 word, may be NULL
  * With cache->summary the blocks' summaries follow: a block whose first row
  * is appended starts anew, another one takes the new keys in.  Blocks being
- * appended to belong to one sequence.  A sequence whose starts lie outside
+ * appended to belong to one sequence.  Nothing is appended to a sequence whose
+ * length is outside its table (the query of a length above it is rotated as the
+ * last row's without tok_start).  A sequence whose starts lie outside
  * [0, T] or count more tokens than it has rows sets PCED_DEV_BAD_LENGTH and its
  * tokens are left out (their rows of q_out are not written); where the starts
  * fall, so are those of every sequence from there on.  Supports Hq/Hkv <= 8.

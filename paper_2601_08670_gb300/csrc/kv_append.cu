@@ -43,10 +43,11 @@ struct AppendItem {
 // New rows of sequence s: {first token, count, live rows}; count 0 where the
 // counts do not fit (flagged).  falls: its starts fall.
 __device__ __forceinline__ int3 new_rows(const AppendArgs& a, int s, bool& falls) {
-  const int n = paged_len(a.c, s, a.status);
+  bool fits;
+  const int n = paged_len(a.c, s, a.status, fits);
   const int t0 = a.tok_start[s], t1 = a.tok_start[s + 1];
   falls = t1 < t0;
-  if (t0 < 0 || t1 < t0 || t1 > a.T || t1 - t0 > n) {
+  if (!fits || t0 < 0 || t1 < t0 || t1 > a.T || t1 - t0 > n) {
     dev_flag(a.status, PCED_DEV_BAD_LENGTH);
     return make_int3(0, 0, n);
   }
@@ -193,7 +194,8 @@ __global__ void __launch_bounds__(APP_ONE_THREADS) kv_append_one_kernel(AppendAr
   } else {
     r.load((role ? a.v + s * a.v_stride : a.k + s * a.k_stride) + h * D + f, D / 2);
   }
-  const int n = paged_len(a.c, s, a.status);
+  bool fits;
+  const int n = paged_len(a.c, s, a.status, fits);
   if (n == 0) {  // an idle sequence: no query either
     r.a = r.b = make_uint4(0, 0, 0, 0);
     if (role >= 2) r.store(dst, D / 2);
@@ -207,6 +209,7 @@ __global__ void __launch_bounds__(APP_ONE_THREADS) kv_append_one_kernel(AppendAr
     r.store(dst, D / 2);
     return;
   }
+  if (!fits) return;  // (the table's last row is another token's)
   const int blk = paged_block(a.c, s, (n - 1) / P, a.status), at = (n - 1) % P;
   if (blk < 0) return;
   const int64_t page = (int64_t)blk * a.c.Hkv + h;

@@ -8,13 +8,18 @@ namespace pced {
 constexpr int PAGED_MAX_S = 1024;  // sequences of a call (their lengths and prefixes lie in shared memory)
 constexpr int PAGED_MAX_G = 8;     // query heads per kv-head
 
-// live rows of sequence s, clipped into what its table can hold
-__device__ __forceinline__ int paged_len(const pced_paged_cache& c, int s, int* status) {
+// live rows of sequence s, clipped into what its table can hold; fits: they were not
+__device__ __forceinline__ int paged_len(const pced_paged_cache& c, int s, int* status, bool& fits) {
   const int n = c.seq_len[s];
   const int cap = c.max_blocks * c.block_rows;
-  if (n >= 0 && n <= cap) return n;
+  fits = n >= 0 && n <= cap;
+  if (fits) return n;
   dev_flag(status, PCED_DEV_BAD_LENGTH);
   return n < 0 ? 0 : cap;
+}
+__device__ __forceinline__ int paged_len(const pced_paged_cache& c, int s, int* status) {
+  bool fits;
+  return paged_len(c, s, status, fits);
 }
 // pool block of block j of sequence s, -1 where the entry is outside the pool
 __device__ __forceinline__ int paged_block(const pced_paged_cache& c, int s, int j, int* status) {

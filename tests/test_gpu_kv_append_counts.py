@@ -86,3 +86,15 @@ def test_a_fall_among_many_sequences(cuda_ok):
     start = list(range(S + 1))
     start[at + 1] = 3
     check([20] * S, S, start, range(at), P=16)
+
+
+@pytest.mark.parametrize("one", [False, True])
+@pytest.mark.parametrize("bad", [193, 10_000, 2 ** 31 - 1])
+def test_nothing_is_appended_past_the_table(cuda_ok, one, bad):
+    # the last row that the table holds is another token's
+    check([bad, 20, 70], 3, [0, 1, 2, 3], [1, 2], cap=3, one=one)
+
+
+def test_a_full_table_is_no_error(cuda_ok):
+    check([192, 20, 70], 3, None, [0, 1, 2], cap=3, one=True, status=0)
+    check([192, 20, 70], 9, [0, 4, 8, 9], [0, 1, 2], cap=3, status=0)
