@@ -7,7 +7,8 @@ products between the library's operators.
 
     documents   kv_append of whole sequences, block_summaries
     each layer  kv_append -> block_select -> paged_attention
-    each token  lm_head_logprobs -> logits_process -> contrastive_select
+    each token  lm_head_logprobs -> logits_process -> contrastive_select, with the rows made logits again
+                before logits_process and normalised after it
 
 Run: python examples/paged_decode.py [--steps 8] [--blocks 8]
 """
@@ -111,12 +112,14 @@ class Loop:
             pced.paged_attention(cache, q, sel=sel, out=o, ws=self.ws)
             x = x + (o.view(S, -1) @ m.out[layer].T).float()
         self.hidden = rmsnorm(x)
-        lp, _ = pced.lm_head_logprobs(self.hidden, m.unembed)
+        lp, lse = pced.lm_head_logprobs(self.hidden, m.unembed)
         if self.penalties is not None or self.mask is not None:
             use = self.penalties is not None
-            pced.logits_process(lp, self.N + 1, history=self.history if use else None,
+            z = lp.add_(lse[:, None])  # logits: a penalty asks for their sign
+            pced.logits_process(z, self.N + 1, history=self.history if use else None,
                                 history_len=self.n_history if use else None, penalties=self.penalties,
-                                mask=self.mask, out=lp, status=self.status)
+                                mask=self.mask, out=z, status=self.status)
+            lp = z.log_softmax(1)  # (a mask that forbids everything leaves no distribution)
         self.logprobs = lp
         token, expert, _ = pced.contrastive_select(lp, self.beta, self.r, self.gamma)
         self.history[:, self.t], self.expert[:, self.t] = token, expert

@@ -411,8 +411,9 @@ const char* pced_step_launch_kind(const pced_step_args* args, int32_t i);
 
 /* ========================================================================
  * Operators of a decode step over paged caches, for programs that have their
- * own layers: kv_append -> block_select -> paged_attention in every layer,
- * lm_head_logprobs -> logits_process -> contrastive_select after the last.
+ * own layers: kv_append -> block_select -> paged_attention in every layer, and
+ * after the last one lm_head_logprobs -> logits_process -> contrastive_select,
+ * with the rows made logits again before logits_process and normalised after it.
  * The pool is laid out as pced_step's paged caches are, so one cache serves
  * both.
  *
@@ -542,9 +543,14 @@ pced_status pced_paged_attention(const pced_paged_cache* cache, const void* q, i
                                  int32_t out_type, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
- * pced_logits_process -- what a request asks of its logits (or
- * log-probabilities) before a token is chosen: all R rows of a query (its
- * experts and the amateur) are processed alike, as they share one history.
+ * pced_logits_process -- what a request asks of its logits before they are
+ * normalised: all R rows of a query (its experts and the amateur) are processed
+ * alike, as they share one history.  The repetition penalty asks for a logit's
+ * sign, so the rows of pced_lm_head_logprobs are to be made logits again first:
+ * logprobs[s][v] + lse[s].  Penalties, biases and masks change the rows' sums, so
+ * a log-softmax of the caller's own has to follow before pced_contrastive_select
+ * (which compares experts by their log-probabilities) and pced_adacad_beta (which
+ * takes distributions).
  *   x, y         fp32 rows of V entries, row i at i * stride elements, row
  *                b*R + j belongs to query b; y may be x, and must not overlap
  *                it otherwise

@@ -437,11 +437,11 @@ def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=N
 
 def logits_process(logits, rows_per_query: int, history=None, history_len=None, penalties=None, bias_ids=None,
                    bias=None, mask=None, mask_row=None, out=None, status=None, stream=None):
-    """pced_logits_process: fp32 [B * rows_per_query, V] (rows may be strided) with the penalties of repeated tokens
-    (history int32 [B, n], history_len int32 [B], penalties fp32 [B, 3]: repetition, frequency, presence), biases
-    (bias_ids int32 and bias fp32 [B, n]) and masks (int32 words [n_masks, ceil(V / 32)], bit set: allowed; mask_row
-    int32 [B], -1: none) applied.  out: another buffer of that shape and stride, or logits itself (in place);
-    returned."""
+    """pced_logits_process: logits fp32 [B * rows_per_query, V] (rows may be strided) with the penalties of repeated
+    tokens (history int32 [B, n], history_len int32 [B], penalties fp32 [B, 3]: repetition, frequency, presence),
+    biases (bias_ids int32 and bias fp32 [B, n]) and masks (int32 words [n_masks, ceil(V / 32)], bit set: allowed;
+    mask_row int32 [B], -1: none) applied; normalise them afterwards.  out: another buffer of that shape and stride,
+    or logits itself (in place); returned."""
     if out is None:
         rows, V = logits.shape
         out = _empty((rows, logits.stride(0) if rows > 1 else V), torch.float32, logits.device, stream)[:, :V]
