@@ -318,8 +318,12 @@ def _is(t, dtype, shape):
     return t.dtype == dtype and t.shape == shape and t.is_contiguous()
 
 
-def _handle(stream):
-    return None if stream is None else stream.cuda_stream
+def _handle(stream, gpu):
+    """The raw handle of a stream of device `gpu` (None: the current stream)."""
+    if stream is None:
+        return None
+    _require(getattr(stream, "device_index", gpu) == gpu, "the stream is another device's than the tensors")
+    return stream.cuda_stream
 
 
 class PagedCache:
@@ -332,7 +336,8 @@ class PagedCache:
     ``key_step``       fp32 [Hkv]: the blocks' key summaries, for block_select (optional)
 
     k and v may be None where only block_select is called (block_rows is then needed).  The tensors are held,
-    and their addresses taken once: change their contents, not their storage."""
+    and their addresses taken once: change their contents, not their storage.  They lie on one CUDA device, which is
+    the current one when the calls are made."""
 
     def __init__(self, k, v, block_table, seq_len, *, block_rows=None, summary=None, key_step=None):
         _require(k is not None or (summary is not None and block_rows is not None),
@@ -384,7 +389,7 @@ def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=N
     if q_out is None and q is not None:
         q_out = _empty((q.shape[0], q.shape[1], cache.D), torch.bfloat16, q.device, stream)
     rc = (_calls or _native()).kv_append(cache.at, cache.gpu, q, k, v, rope, tok_start, positions, q_out, status,
-                                         _handle(stream))
+                                         _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_kv_append")
     return q_out
@@ -392,7 +397,7 @@ def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=N
 
 def block_summaries(cache: PagedCache, status=None, stream=None):
     """pced_block_summaries: cache.summary from the cached keys of all live blocks; returns it."""
-    rc = (_calls or _native()).block_summaries(cache.at, cache.gpu, status, _handle(stream))
+    rc = (_calls or _native()).block_summaries(cache.at, cache.gpu, status, _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_block_summaries")
     return cache.summary
@@ -404,7 +409,8 @@ def block_select(cache: PagedCache, q, n_sel: int, n_first: int = 1, n_last: int
     (-1 after the last): the first n_first, the last n_last and those with the highest scores."""
     if sel is None:
         sel = _empty((cache.S, cache.Hkv, n_sel), torch.int32, q.device, stream)
-    rc = (_calls or _native()).block_select(cache.at, cache.gpu, q, n_sel, n_first, n_last, sel, status, _handle(stream))
+    rc = (_calls or _native()).block_select(cache.at, cache.gpu, q, n_sel, n_first, n_last, sel, status,
+                                            _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_block_select")
     return sel
@@ -429,7 +435,7 @@ def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=N
             ws.zero_()
     rc = (_calls or _native()).paged_attention(cache.at, cache.gpu, q, sel, total_rows,
                                                1.0 / math.sqrt(cache.D) if scale is None else scale, out, lse, ws,
-                                               _handle(stream))
+                                               _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_paged_attention")
     return out
@@ -446,7 +452,8 @@ def logits_process(logits, rows_per_query: int, history=None, history_len=None, 
         rows, V = logits.shape
         out = _empty((rows, logits.stride(0) if rows > 1 else V), torch.float32, logits.device, stream)[:, :V]
     rc = (_calls or _native()).logits_process(logits, rows_per_query, history, history_len, penalties, bias_ids, bias,
-                                              mask, mask_row, out, status, _handle(stream))
+                                              mask, mask_row, out, status,
+                                              None if stream is None else _handle(stream, logits.get_device()))
     if rc:
         _check(rc, "pced_logits_process")
     return out

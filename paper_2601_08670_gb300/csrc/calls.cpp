@@ -4,6 +4,7 @@
 // Python, beside 3 us for the call itself; a call that a program makes for every
 // layer and token is mostly that.  No arithmetic is done here.
 #include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -66,15 +67,19 @@ int64_t token_stride(const at::Tensor* t, int64_t T, int64_t heads, int64_t D, c
     return T > 1 ? t->stride(0) : t->size(1) * D;
   throw Refused(what);
 }
+// all on this device, which is the current one: the library launches there
 void on_gpu(std::initializer_list<const at::Tensor*> all, int device) {
   for (const at::Tensor* t : all)
     require(!t || (t->is_cuda() && t->get_device() == device), "tensors lie on the cache's (the logits') CUDA device");
+  require(c10::cuda::current_device() == device, "the tensors' device is not the current one");
 }
 
 // the raw stream of an integer handle, or the current one for None
 void* stream_of(PyObject* o) {
-  if (o != Py_None) return PyLong_AsVoidPtr(o);
-  return (void*)c10::cuda::getCurrentCUDAStream().stream();
+  if (o == Py_None) return (void*)c10::cuda::getCurrentCUDAStream().stream();
+  void* s = PyLong_AsVoidPtr(o);
+  if (!s && PyErr_Occurred()) throw Refused("");
+  return s;
 }
 struct Cache {  // a PagedCache: the address of its struct, its device (-1: not a CUDA device)
   const pced_paged_cache* c;
