@@ -336,8 +336,23 @@ class PagedCache:
     ``key_step``       fp32 [Hkv]: the blocks' key summaries, for block_select (optional)
 
     k and v may be None where only block_select is called (block_rows is then needed).  The tensors are held,
-    and their addresses taken once: change their contents, not their storage.  They lie on one CUDA device, which is
+    and their addresses taken once: change their contents, not their storage (the fields take no other tensor; for
+    one, make another PagedCache).  They lie on one CUDA device, which is
     the current one when the calls are made."""
+
+    _TAKEN = frozenset(["k", "v", "block_table", "seq_len", "summary", "key_step", "num_blocks", "Hkv", "block_rows",
+                        "D", "S", "max_blocks"])
+
+    def __setattr__(self, name, value):
+        # (`cache.seq_len += 1` works in place and puts the same tensor back)
+        if name in self._TAKEN and self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name}: its address or size has been taken; make another PagedCache")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        if name in self._TAKEN:
+            raise AttributeError(f"{name}: its address or size has been taken")
+        super().__delattr__(name)
 
     def __init__(self, k, v, block_table, seq_len, *, block_rows=None, summary=None, key_step=None):
         _require(k is not None or (summary is not None and block_rows is not None),
