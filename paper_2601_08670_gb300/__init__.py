@@ -319,9 +319,7 @@ def _is(t, dtype, shape):
 
 
 def _handle(stream, gpu):
-    """The raw handle of a stream of device `gpu` (None: the current stream)."""
-    if stream is None:
-        return None
+    """The raw handle of a stream of device `gpu`."""
     _require(getattr(stream, "device_index", gpu) == gpu, "the stream is another device's than the tensors")
     return stream.cuda_stream
 
@@ -404,7 +402,7 @@ def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=N
     if q_out is None and q is not None:
         q_out = _empty((q.shape[0], q.shape[1], cache.D), torch.bfloat16, q.device, stream)
     rc = (_calls or _native()).kv_append(cache.at, cache.gpu, q, k, v, rope, tok_start, positions, q_out, status,
-                                         _handle(stream, cache.gpu))
+                                         None if stream is None else _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_kv_append")
     return q_out
@@ -412,7 +410,8 @@ def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=N
 
 def block_summaries(cache: PagedCache, status=None, stream=None):
     """pced_block_summaries: cache.summary from the cached keys of all live blocks; returns it."""
-    rc = (_calls or _native()).block_summaries(cache.at, cache.gpu, status, _handle(stream, cache.gpu))
+    rc = (_calls or _native()).block_summaries(cache.at, cache.gpu, status,
+                                               None if stream is None else _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_block_summaries")
     return cache.summary
@@ -425,7 +424,7 @@ def block_select(cache: PagedCache, q, n_sel: int, n_first: int = 1, n_last: int
     if sel is None:
         sel = _empty((cache.S, cache.Hkv, n_sel), torch.int32, q.device, stream)
     rc = (_calls or _native()).block_select(cache.at, cache.gpu, q, n_sel, n_first, n_last, sel, status,
-                                            _handle(stream, cache.gpu))
+                                            None if stream is None else _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_block_select")
     return sel
@@ -450,7 +449,7 @@ def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=N
             ws.zero_()
     rc = (_calls or _native()).paged_attention(cache.at, cache.gpu, q, sel, total_rows,
                                                1.0 / math.sqrt(cache.D) if scale is None else scale, out, lse, ws,
-                                               _handle(stream, cache.gpu))
+                                               None if stream is None else _handle(stream, cache.gpu))
     if rc:
         _check(rc, "pced_paged_attention")
     return out

@@ -67,18 +67,24 @@ int64_t token_stride(const at::Tensor* t, int64_t T, int64_t heads, int64_t D, c
     return T > 1 ? t->stride(0) : t->size(1) * D;
   throw Refused(what);
 }
-// all on this device, which is the current one: the library launches there
 void on_gpu(std::initializer_list<const at::Tensor*> all, int device) {
   for (const at::Tensor* t : all)
     require(!t || (t->is_cuda() && t->get_device() == device), "tensors lie on the cache's (the logits') CUDA device");
-  require(c10::cuda::current_device() == device, "the tensors' device is not the current one");
 }
 
-// the raw stream of an integer handle, or the current one for None
-void* stream_of(PyObject* o) {
-  if (o == Py_None) return (void*)c10::cuda::getCurrentCUDAStream().stream();
+// The raw stream of an integer handle, or the current one for None.  The tensors'
+// device has to be the current one, where the library launches (the current stream
+// knows it: asked for apart it is 5 % of a small call).
+void* stream_of(PyObject* o, int device) {
+  const char* other = "the tensors' device is not the current one";
+  if (o == Py_None) {
+    const c10::cuda::CUDAStream s = c10::cuda::getCurrentCUDAStream();
+    require(s.device_index() == device, other);
+    return (void*)s.stream();
+  }
   void* s = PyLong_AsVoidPtr(o);
   if (!s && PyErr_Occurred()) throw Refused("");
+  require(c10::cuda::current_device() == device, other);
   return s;
 }
 struct Cache {  // a PagedCache: the address of its struct, its device (-1: not a CUDA device)
@@ -129,7 +135,7 @@ pced_status kv_append(PyObject* const* a) {
   require(T <= INT32_MAX && rows <= INT32_MAX, "T, rows: below 2^31");
   cache.on_gpu();
   on_gpu({q, k, v, rope, start, pos, out, status}, cache.device);
-  void* s = stream_of(a[10]);
+  void* s = stream_of(a[10], cache.device);
   return without_gil([&] {
     return pced_kv_append(cache.c, address(q), qs, address(k), ks, address(v), vs, address(out), (int32_t)Hq,
                           (const int32_t*)address(start), (int32_t)T, (const float*)address(rope), (int32_t)rows,
@@ -144,7 +150,7 @@ pced_status block_summaries(PyObject* const* a) {
   check_status(status);
   cache.on_gpu();
   on_gpu({status}, cache.device);
-  void* s = stream_of(a[3]);
+  void* s = stream_of(a[3], cache.device);
   return without_gil([&] { return pced_block_summaries(cache.c, (int32_t*)address(status), s); });
 }
 
@@ -160,7 +166,7 @@ pced_status block_select(PyObject* const* a) {
   check_status(status);
   cache.on_gpu();
   on_gpu({q, sel, status}, cache.device);
-  void* s = stream_of(a[8]);
+  void* s = stream_of(a[8], cache.device);
   return without_gil([&] {
     return pced_block_select(cache.c, address(q), qs, (int32_t)q->size(1), n_sel, n_first, n_last,
                              (int32_t*)address(sel), (int32_t*)address(status), s);
@@ -192,7 +198,7 @@ pced_status paged_attention(PyObject* const* a) {
   require(n_sel <= INT32_MAX, "n_sel: below 2^31");
   cache.on_gpu();
   on_gpu({q, sel, out, lse, ws}, cache.device);
-  void* s = stream_of(a[9]);
+  void* s = stream_of(a[9], cache.device);
   return without_gil([&] {
     return pced_paged_attention(cache.c, address(q), qs, (int32_t)Hq, (const int32_t*)address(sel), (int32_t)n_sel,
                                 total_rows, (float)scale, address(out), f32 ? PCED_OUT_F32 : PCED_OUT_BF16,
@@ -247,7 +253,7 @@ pced_status logits_process(PyObject* const* a) {
   for (const int64_t n : {B, R, V, n_hist, n_bias, n_masks, words}) require(n <= INT32_MAX, "sizes: below 2^31");
   require(x->is_cuda(), "logits: on a CUDA device");
   on_gpu({x, hist, len, pen, ids, bias, mask, row, out, status}, x->get_device());
-  void* s = stream_of(a[11]);
+  void* s = stream_of(a[11], x->get_device());
   return without_gil([&] {
     return pced_logits_process((const float*)address(x), (float*)address(out), stride, (int32_t)B, (int32_t)R,
                                (int32_t)V, (const int32_t*)address(hist), (int32_t)n_hist,
