@@ -43,13 +43,11 @@ struct AppendItem {
 // New rows of sequence s: {first token, count, live rows}; count 0 where the
 // counts do not fit (flagged).  falls: its starts fall.
 __device__ __forceinline__ int3 new_rows(const AppendArgs& a, int s, bool& falls) {
-  bool fits;
-  const int n = paged_len(a.c, s, a.status, fits);
-  const int t0 = a.tok_start[s], t1 = a.tok_start[s + 1];
+  const int n = a.c.seq_len[s], t0 = a.tok_start[s], t1 = a.tok_start[s + 1];
   falls = t1 < t0;
-  if (!fits || t0 < 0 || t1 < t0 || t1 > a.T || t1 - t0 > n) {
+  if (n < 0 || n > a.c.max_blocks * a.c.block_rows || t0 < 0 || t1 < t0 || t1 > a.T || t1 - t0 > n) {
     dev_flag(a.status, PCED_DEV_BAD_LENGTH);
-    return make_int3(0, 0, n);
+    return make_int3(0, 0, 0);
   }
   return make_int3(t0, t1 - t0, n);
 }
@@ -84,16 +82,18 @@ __device__ __forceinline__ AppendItem find_item(const AppendArgs& a, int want) {
     const int v = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += v;
   }
-  fall = __reduce_min_sync(0xffffffffu, fall);
-  if (lane == 31) wsum[warp] = incl, wfall[warp] = fall;
+  if (lane == 31) wsum[warp] = incl;
   if (tid == 0) it.s = -1;
-  __syncthreads();
+  if (__syncthreads_or(fall != INT32_MAX)) {
+    fall = __reduce_min_sync(0xffffffffu, fall);
+    if (lane == 0) wfall[warp] = fall;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < APP_THREADS / 32; ++w) fall = min(fall, wfall[w]);
+  }
   int at = incl - own;
 #pragma unroll
-  for (int w = 0; w < APP_THREADS / 32; ++w) {
-    at += w < warp ? wsum[w] : 0;
-    fall = min(fall, wfall[w]);
-  }
+  for (int w = 0; w < APP_THREADS / 32; ++w) at += w < warp ? wsum[w] : 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     if (want >= at && want < at + nb[i] && s0 + i < fall) {
