@@ -487,7 +487,8 @@ pced_status pced_kv_append(const pced_paged_cache* cache, const void* q, int64_t
  * pced_block_summaries -- summaries of all live blocks of the sequences, for
  * caches that were built elsewhere (documents encoded offline); the rows past
  * a sequence's last do not count.  Blocks without live rows keep theirs.  A block
- * of several sequences has to be as long in each.
+ * of several sequences has to be as long in each.  The launch has CTAs for every
+ * entry of the table, so a table much wider than the sequences costs time.
  * ------------------------------------------------------------------------ */
 pced_status pced_block_summaries(const pced_paged_cache* cache, int32_t* status, void* stream);
 
@@ -499,7 +500,10 @@ pced_status pced_block_summaries(const pced_paged_cache* cache, int32_t* status,
  *   P_d = sum max(q_gd, 0),  N_d = sum min(q_gd, 0)   (fp32),
  *   m = max_d max(P_d, -N_d),  p = rint(P * (127 / m)),  n = rint(N * (127 / m)),
  *   score(j) = sum_d p_d max_jd + n_d min_jd,
- * an upper bound, in steps, of the group's summed q.k over the block.  p, n and
+ * an estimate, in steps, of the largest that the group's summed q.k can be over
+ * the block.  It is no bound of it: p and n are rounded to nearest (off by up to
+ * half a step in each channel, so that a channel below half a step of the largest
+ * drops out), and a summary whose keys were clipped understates them.  p, n and
  * the summaries are whole numbers, so a choice depends on no order of sums.
  * Ties go to the lowest block.  Where m or 127 / m is not finite all scores are 0.
  *   q    bf16 [S][Hq][D], sequence s at s * q_stride elements (16-byte
@@ -555,12 +559,14 @@ pced_status pced_paged_attention(const pced_paged_cache* cache, const void* q, i
  *                b*R + j belongs to query b; y may be x, and must not overlap
  *                it otherwise
  *   history      int32 [B][history_stride]: query b's tokens are its first
- *                history_len[b] (device int32 [B]) entries; -1 counts as none.
- *                NULL: no penalties
+ *                history_len[b] (device int32 [B]) entries; -1 counts as none
  *   penalties    fp32 [B][3] (device): repetition t > 0, frequency f, presence p.
  *                A token that is in the history c > 0 times:
  *                  x <- (x > 0 ? x / t : x * t) - (c f + p)
- *                NULL: none
+ *                history, history_len and penalties go together; all three NULL:
+ *                no penalties.  One history serves all of them: where t counts
+ *                other tokens than f and p do (the prompt's, say), two calls do
+ *                it, first with f = p = 0, then with t = 1
  *   bias_ids     int32 [B][n_bias], bias fp32 [B][n_bias] (device): added to the
  *                token's entry; -1: none; of a token named twice the last
  *                counts.  NULL (n_bias = 0): none
@@ -571,7 +577,8 @@ pced_status pced_paged_attention(const pced_paged_cache* cache, const void* q, i
  *                mask b for query b.  Another number sets PCED_DEV_BAD_INDEX
  *                and masks nothing
  *   status       device int32 word, may be NULL
- * In this order, each operation rounded to fp32.  A token outside [0, V) sets
+ * In this order, each operation rounded to fp32.  B, R <= 65535, V <= 65535*2048,
+ * stride >= V.  A token outside [0, V) sets
  * PCED_DEV_BAD_TOKEN and is left out; a history_len outside
  * [0, history_stride] sets PCED_DEV_BAD_LENGTH and is clipped.
  * pced_contrastive_select never chooses an entry that is -inf in the expert's

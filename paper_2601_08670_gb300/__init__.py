@@ -335,8 +335,7 @@ class PagedCache:
 
     k and v may be None where only block_select is called (block_rows is then needed).  The tensors are held,
     and their addresses taken once: change their contents, not their storage (the fields take no other tensor; for
-    one, make another PagedCache).  They lie on one CUDA device, which is
-    the current one when the calls are made."""
+    one, make another PagedCache).  They lie on one CUDA device, which is the current one when the calls are made."""
 
     _TAKEN = frozenset(["k", "v", "block_table", "seq_len", "summary", "key_step", "num_blocks", "Hkv", "block_rows",
                         "D", "S", "max_blocks"])
