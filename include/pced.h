@@ -60,6 +60,7 @@ typedef enum pced_status {
 #define PCED_DEV_BAD_BLOCK 0x20u  /* paged caches: a needed block-table entry is missing or outside the pool */
 #define PCED_DEV_BOUNDS 0x40u     /* bounds-checked build only: an index outside its buffer (the access was skipped) */
 #define PCED_DEV_BAD_INDEX 0x80u  /* a position outside the rotation table, or a mask number outside the masks */
+#define PCED_DEV_BAD_PARAM 0x100u /* a row's parameter outside its range (pced_sample) */
 
 /* Static description of a status code (host). */
 const char* pced_status_string(int32_t status);
@@ -589,6 +590,91 @@ pced_status pced_logits_process(const float* x, float* y, int64_t stride, int32_
                                 const float* penalties, const int32_t* bias_ids, const float* bias, int32_t n_bias,
                                 const uint32_t* mask, int32_t n_masks, int32_t mask_words, const int32_t* mask_row,
                                 int32_t* status, void* stream);
+
+/* ========================================================================
+ * Paged caches in 8 bits: half the memory, and half the bytes of a step.
+ *
+ * pced_paged_cache8 is a pced_paged_cache whose k and v are e4m3 numbers (a
+ * byte each, the layout otherwise the same), and
+ *   scale        fp32 [num_blocks][Hkv][2] (8-byte aligned): what a block's
+ *                numbers are multiples of, the keys' (0) and the values' (1)
+ * pced_kv_append8 writes powers of two there, from 2^-100 on; a cache of the
+ * caller's own making may hold any finite scales above 0.  pages alone serves
+ * pced_block_select, which reads the summaries; pced_block_summaries, which reads
+ * bf16 keys, must not be given it.
+ * ======================================================================== */
+typedef struct pced_paged_cache8 {
+  pced_paged_cache pages;
+  float* scale;
+} pced_paged_cache8;
+
+/* ------------------------------------------------------------------------
+ * pced_kv_append8 -- pced_kv_append into an 8-bit cache; arguments and device
+ * conditions are its.  Of each block, kv-head and kind (keys, values) that
+ * gets new rows, with a the largest of their absolute values (those that are
+ * not finite apart) and n the smallest 2^e, e >= -100, with a <= 448 n:
+ *   the block's first row is new: s = n;
+ *   else s = max(s0, n), and where that is not s0 the rows that the block holds
+ *   before the new ones are moved: b <- e4m3(b * (s0 / s));
+ * the new rows are e4m3(x * (1 / s)), rounded to nearest even from the rotated
+ * fp32 keys (from the bf16 values); what is not finite becomes not-a-number.
+ * Quotients and products are rounded to fp32.  With powers of two a move loses
+ * what falls below e4m3's smallest numbers, and nothing else.  Rows appended one
+ * by one and at once can differ by that, and by the scale that the block had when
+ * they came.
+ * The summaries are of the rotated fp32 keys.
+ * ------------------------------------------------------------------------ */
+pced_status pced_kv_append8(const pced_paged_cache8* cache, const void* q, int64_t q_stride, const void* k,
+                            int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int32_t Hq,
+                            const int32_t* tok_start, int32_t T, const float* rope, int32_t rope_rows,
+                            const int32_t* positions, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------
+ * pced_paged_attention8 -- pced_paged_attention over an 8-bit cache, of the
+ * numbers that the bytes stand for (times their scale); arguments, conditions and
+ * the workspace (pced_paged_attention_workspace_size) are its.  Queries are not
+ * rounded, probabilities are held to 23 bits, sums in fp32.
+ * ------------------------------------------------------------------------ */
+pced_status pced_paged_attention8(const pced_paged_cache8* cache, const void* q, int64_t q_stride, int32_t Hq,
+                                  const int32_t* sel, int32_t n_sel, int64_t total_rows, float scale, void* out,
+                                  int32_t out_type, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * pced_sample -- a token for every row of logits (or log-probabilities) from a
+ * random number of the caller's: for programs that draw where
+ * pced_contrastive_select takes the best.
+ *   x            rows of V logits, fp32 (PCED_IN_F32) or bf16 (PCED_IN_BF16),
+ *                row i at i * stride elements, of the type's own alignment;
+ *                what is not a number counts as -inf
+ *   u            fp32 [rows], in [0, 1]
+ *   temperature  fp32 [rows], t >= 0; NULL: 1
+ *   top_k        int32 [rows]; k <= 0 or >= V: no cut; NULL: none
+ *   top_p        fp32 [rows]; p >= 1: no cut; NULL: none
+ *   min_p        fp32 [rows]; <= 0: no cut; NULL: none
+ *   token        int32 [rows]
+ *   logprob      fp32 [rows], may be NULL: the token's log-probability under the
+ *                distribution that it was drawn from, cuts included
+ *   status       device int32 word, may be NULL
+ * With m the row's largest logit and w_v = exp((x_v - m) / t), the tokens
+ * ordered by logit, the lower one first where logits are equal: the first k
+ * are kept; of these the shortest first part that holds at least p of their
+ * weight; of these those with w_v >= min_p.  The largest is always kept.  The token is
+ * the first kept one, in the order of the vocabulary, with
+ * sum_{v' <= v} w_v' > u sum w.  t = 0, k = 1, p <= 0 and min_p > 1 give the
+ * first of the largest (logprob 0).  Logits of +inf share everything equally.
+ * Weights are whole numbers of 2^-44 of the largest, exact to about 2^-32 of
+ * themselves (a smaller one is never drawn), and added as such: the choice
+ * depends on no order of sums and differs from that of exact sums in about one
+ * row of a million.  Temperatures above 1e30 count as infinite.
+ * A row whose logits are all -inf has token -1 and logprob -inf; so has one
+ * with a parameter that is not a number, t < 0 or u outside [0, 1], which sets
+ * PCED_DEV_BAD_PARAM.  V <= 393216.
+ * ------------------------------------------------------------------------ */
+#define PCED_IN_F32 0
+#define PCED_IN_BF16 1
+pced_status pced_sample(const void* x, int32_t type, int64_t stride, int32_t rows, int32_t V, const float* u,
+                        const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                        int32_t* token, float* logprob, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -29,6 +29,7 @@ PCED_DEV_STEP_LIMIT = 0x10
 PCED_DEV_BAD_BLOCK = 0x20
 PCED_DEV_BOUNDS = 0x40
 PCED_DEV_BAD_INDEX = 0x80
+PCED_DEV_BAD_PARAM = 0x100
 
 
 class PcedError(RuntimeError):
@@ -65,6 +66,10 @@ class PagedCacheStruct(ctypes.Structure):
                 ("key_step", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
                 ("num_blocks", ctypes.c_int32), ("block_rows", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
                 ("S", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32)]
+
+
+class PagedCache8Struct(ctypes.Structure):
+    _fields_ = [("pages", PagedCacheStruct), ("scale", ctypes.c_void_p)]
 
 
 _lib = None
@@ -131,6 +136,13 @@ def lib(path: str = LIB_PATH):
         L.pced_paged_attention.restype = I32
         L.pced_logits_process.argtypes = [P, P, I64, I32, I32, I32, P, I32, P, P, P, P, I32, P, I32, I32, P, P, P]
         L.pced_logits_process.restype = I32
+        C8 = ctypes.POINTER(PagedCache8Struct)
+        L.pced_kv_append8.argtypes = [C8, *L.pced_kv_append.argtypes[1:]]
+        L.pced_kv_append8.restype = I32
+        L.pced_paged_attention8.argtypes = [C8, *L.pced_paged_attention.argtypes[1:]]
+        L.pced_paged_attention8.restype = I32
+        L.pced_sample.argtypes = [P, I32, I64, I32, I32, P, P, P, P, P, P, P, P, P]
+        L.pced_sample.restype = I32
         _lib = L
     return _lib
 
@@ -337,8 +349,10 @@ class PagedCache:
     and their addresses taken once: change their contents, not their storage (the fields take no other tensor; for
     one, make another PagedCache).  They lie on one CUDA device, which is the current one when the calls are made."""
 
-    _TAKEN = frozenset(["k", "v", "block_table", "seq_len", "summary", "key_step", "num_blocks", "Hkv", "block_rows",
-                        "D", "S", "max_blocks"])
+    _TAKEN = frozenset(["k", "v", "scale", "block_table", "seq_len", "summary", "key_step", "num_blocks", "Hkv",
+                        "block_rows", "D", "S", "max_blocks"])
+    _NUMBERS, _NAME = torch.bfloat16, "bf16"
+    eight = False  # whether k and v are 8-bit numbers with scales
 
     def __setattr__(self, name, value):
         # (`cache.seq_len += 1` works in place and puts the same tensor back)
@@ -362,8 +376,8 @@ class PagedCache:
             _require(summary.dim() == 4, "summary: [num_blocks, Hkv, 2, D]")
             nb, Hkv, P, D = summary.shape[0], summary.shape[1], int(block_rows), summary.shape[3]
         for name, t in (("k", k), ("v", v)):
-            _require(t is None or _is(t, torch.bfloat16, (nb, Hkv, P, D)),
-                     f"{name}: contiguous bf16 [num_blocks, Hkv, block_rows, D]")
+            _require(t is None or _is(t, self._NUMBERS, (nb, Hkv, P, D)),
+                     f"{name}: contiguous {self._NAME} [num_blocks, Hkv, block_rows, D]")
         _require(summary is None or _is(summary, torch.int8, (nb, Hkv, 2, D)),
                  "summary: contiguous int8 [num_blocks, Hkv, 2, D]")
         _require(key_step is None or _is(key_step, torch.float32, (Hkv,)), "key_step: fp32 [Hkv]")
@@ -384,6 +398,32 @@ class PagedCache:
         self.gpu = self.device.index if self.device.type == "cuda" else -1
 
 
+class PagedCache8(PagedCache):
+    """One layer's paged cache in 8 bits (pced_paged_cache8 in pced.h), for the same calls as a PagedCache:
+
+    ``k``, ``v``       e4m3 (torch.float8_e4m3fn) [num_blocks, Hkv, block_rows, D]
+    ``scale``          fp32 [num_blocks, Hkv, 2]: what a block's numbers are multiples of, keys' and values'
+    and the other tensors of a PagedCache.
+
+    kv_append writes numbers and scales (rows of another cache become bytes by appending them), paged_attention reads
+    them, block_select reads the summaries, which kv_append keeps; block_summaries reads bf16 keys and takes a PagedCache
+    alone."""
+
+    _NUMBERS, _NAME = torch.float8_e4m3fn, "e4m3"
+    eight = True
+
+    def __init__(self, k, v, scale, block_table, seq_len, *, summary=None, key_step=None):
+        _require(k is not None and v is not None and scale is not None, "k, v and scale are needed")
+        super().__init__(k, v, block_table, seq_len, summary=summary, key_step=key_step)
+        _require(_is(scale, torch.float32, (self.num_blocks, self.Hkv, 2)),
+                 "scale: contiguous fp32 [num_blocks, Hkv, 2]")
+        _require(scale.device == self.device, "a cache's tensors lie on one device")
+        self.scale = scale
+        self.struct8 = PagedCache8Struct(self.struct, _ptr(scale))
+        self.struct = self.struct8.pages
+        self.at = ctypes.addressof(self.struct8)
+
+
 def rope_table(theta: float, D: int, rows: int, device="cuda") -> torch.Tensor:
     """Rotation table of kv_append, fp32 [rows, D]: cosines, then sines, of the
     angles fp32(p * fp32(theta^(-2f/D))), which pced_step rotates by."""
@@ -394,21 +434,24 @@ def rope_table(theta: float, D: int, rows: int, device="cuda") -> torch.Tensor:
 
 def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=None, q_out=None, status=None,
               stream=None):
-    """pced_kv_append: k, v bf16 [T, Hkv, D] into the last rows of the sequences, q bf16 [T, Hq, D] (or None)
+    """pced_kv_append (pced_kv_append8 for a PagedCache8): k, v bf16 [T, Hkv, D] into the last rows of the sequences, q bf16 [T, Hq, D] (or None)
     rotated into q_out, which is returned.  The parts of one projection's output need no copies (strides between
     tokens).  rope: fp32 [rows, D] (rope_table), None: no rotation; tok_start: int32 [S + 1], None: one token per
     sequence; positions: int32 [T], None: the rows themselves.  Device conditions go to the int32 tensor status."""
     if q_out is None and q is not None:
         q_out = _empty((q.shape[0], q.shape[1], cache.D), torch.bfloat16, q.device, stream)
-    rc = (_calls or _native()).kv_append(cache.at, cache.gpu, q, k, v, rope, tok_start, positions, q_out, status,
-                                         None if stream is None else _handle(stream, cache.gpu))
+    native = _calls or _native()
+    rc = (native.kv_append8 if cache.eight else native.kv_append)(
+        cache.at, cache.gpu, q, k, v, rope, tok_start, positions, q_out, status,
+        None if stream is None else _handle(stream, cache.gpu))
     if rc:
-        _check(rc, "pced_kv_append")
+        _check(rc, "pced_kv_append8" if cache.eight else "pced_kv_append")
     return q_out
 
 
 def block_summaries(cache: PagedCache, status=None, stream=None):
     """pced_block_summaries: cache.summary from the cached keys of all live blocks; returns it."""
+    _require(not cache.eight, "block_summaries reads bf16 keys; kv_append keeps the summaries of a PagedCache8")
     rc = (_calls or _native()).block_summaries(cache.at, cache.gpu, status,
                                                None if stream is None else _handle(stream, cache.gpu))
     if rc:
@@ -435,7 +478,7 @@ def paged_attention_workspace_size(S, Hq, Hkv, D) -> int:
 
 def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=None, out=None, lse=None, ws=None,
                     stream=None):
-    """pced_paged_attention: q bf16 [S, Hq, D] over the cache, or over the blocks sel int32 [S, Hkv, n_sel]; returns
+    """pced_paged_attention (pced_paged_attention8 for a PagedCache8): q bf16 [S, Hq, D] over the cache, or over the blocks sel int32 [S, Hkv, n_sel]; returns
     out [S, Hq, D], fp32 unless a bf16 `out` is passed.  lse: fp32 [S, Hq] that receives the log of the softmax's sum.
     total_rows: upper bound of the rows attended to (of one kv-head, over all sequences), 0: unknown.  A workspace of
     the caller's own is zeroed before its first use (workspace())."""
@@ -446,11 +489,12 @@ def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=N
                     q.device, stream)
         with torch.cuda.stream(stream):  # (None: the current one)
             ws.zero_()
-    rc = (_calls or _native()).paged_attention(cache.at, cache.gpu, q, sel, total_rows,
-                                               1.0 / math.sqrt(cache.D) if scale is None else scale, out, lse, ws,
-                                               None if stream is None else _handle(stream, cache.gpu))
+    native = _calls or _native()
+    rc = (native.paged_attention8 if cache.eight else native.paged_attention)(
+        cache.at, cache.gpu, q, sel, total_rows, 1.0 / math.sqrt(cache.D) if scale is None else scale, out, lse, ws,
+        None if stream is None else _handle(stream, cache.gpu))
     if rc:
-        _check(rc, "pced_paged_attention")
+        _check(rc, "pced_paged_attention8" if cache.eight else "pced_paged_attention")
     return out
 
 
@@ -470,6 +514,21 @@ def logits_process(logits, rows_per_query: int, history=None, history_len=None, 
     if rc:
         _check(rc, "pced_logits_process")
     return out
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, status=None,
+           stream=None):
+    """pced_sample: int32 [rows], a token for every row of logits fp32 or bf16 [rows, V] (rows may be strided), drawn by
+    u fp32 [rows] in [0, 1].  temperature, top_p, min_p fp32 [rows] and top_k int32 [rows]: each row's own (None: 1,
+    and no cut).  logprob: fp32 [rows] that receives the tokens' log-probabilities under what they were drawn from.  A
+    row without a token that could be drawn gets -1."""
+    if token is None:
+        token = _empty((logits.shape[0],), torch.int32, logits.device, stream)
+    rc = (_calls or _native()).sample(logits, u, temperature, top_k, top_p, min_p, token, logprob, status,
+                                      None if stream is None else _handle(stream, logits.get_device()))
+    if rc:
+        _check(rc, "pced_sample")
+    return token
 
 
 def dims(B, N, L, Hq, Hkv, D, V) -> Dims:

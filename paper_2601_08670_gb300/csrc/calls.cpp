@@ -87,11 +87,14 @@ void* stream_of(PyObject* o, int device) {
   require(c10::cuda::current_device() == device, other);
   return s;
 }
-struct Cache {  // a PagedCache: the address of its struct, its device (-1: not a CUDA device)
+// a PagedCache: the address of its struct (of a PagedCache8: of the larger one that begins
+// with it), its device (-1: not a CUDA device)
+struct Cache {
   const pced_paged_cache* c;
   int device;
   Cache(PyObject* addr, PyObject* dev)
       : c((const pced_paged_cache*)PyLong_AsVoidPtr(addr)), device((int)number(dev)) {}
+  const pced_paged_cache8* eight() const { return (const pced_paged_cache8*)c; }
   void on_gpu() const { require(device >= 0, "the cache's tensors lie on a CUDA device"); }
 };
 
@@ -103,6 +106,7 @@ pced_status without_gil(F f) {
 }
 
 // (cache, device, q, k, v, rope, tok_start, positions, q_out, status, stream)
+template <bool EIGHT>
 pced_status kv_append(PyObject* const* a) {
   const Cache cache(a[0], a[1]);
   const pced_paged_cache& c = *cache.c;
@@ -137,9 +141,12 @@ pced_status kv_append(PyObject* const* a) {
   on_gpu({q, k, v, rope, start, pos, out, status}, cache.device);
   void* s = stream_of(a[10], cache.device);
   return without_gil([&] {
-    return pced_kv_append(cache.c, address(q), qs, address(k), ks, address(v), vs, address(out), (int32_t)Hq,
-                          (const int32_t*)address(start), (int32_t)T, (const float*)address(rope), (int32_t)rows,
-                          (const int32_t*)address(pos), (int32_t*)address(status), s);
+    const auto call = [&](auto f, auto c) {
+      return f(c, address(q), qs, address(k), ks, address(v), vs, address(out), (int32_t)Hq,
+               (const int32_t*)address(start), (int32_t)T, (const float*)address(rope), (int32_t)rows,
+               (const int32_t*)address(pos), (int32_t*)address(status), s);
+    };
+    return EIGHT ? call(pced_kv_append8, cache.eight()) : call(pced_kv_append, cache.c);
   });
 }
 
@@ -174,6 +181,7 @@ pced_status block_select(PyObject* const* a) {
 }
 
 // (cache, device, q, sel, total_rows, scale, out, lse, ws, stream)
+template <bool EIGHT>
 pced_status paged_attention(PyObject* const* a) {
   const Cache cache(a[0], a[1]);
   const pced_paged_cache& c = *cache.c;
@@ -200,9 +208,12 @@ pced_status paged_attention(PyObject* const* a) {
   on_gpu({q, sel, out, lse, ws}, cache.device);
   void* s = stream_of(a[9], cache.device);
   return without_gil([&] {
-    return pced_paged_attention(cache.c, address(q), qs, (int32_t)Hq, (const int32_t*)address(sel), (int32_t)n_sel,
-                                total_rows, (float)scale, address(out), f32 ? PCED_OUT_F32 : PCED_OUT_BF16,
-                                (float*)address(lse), address(ws), (size_t)ws->numel(), s);
+    const auto call = [&](auto f, auto c) {
+      return f(c, address(q), qs, (int32_t)Hq, (const int32_t*)address(sel), (int32_t)n_sel, total_rows, (float)scale,
+               address(out), f32 ? PCED_OUT_F32 : PCED_OUT_BF16, (float*)address(lse), address(ws),
+               (size_t)ws->numel(), s);
+    };
+    return EIGHT ? call(pced_paged_attention8, cache.eight()) : call(pced_paged_attention, cache.c);
   });
 }
 
@@ -264,6 +275,37 @@ pced_status logits_process(PyObject* const* a) {
   });
 }
 
+// (logits, u, temperature, top_k, top_p, min_p, token, logprob, status, stream)
+pced_status sample(PyObject* const* a) {
+  const at::Tensor *x = tensor(a[0], "logits"), *u = tensor(a[1], "u"), *t = tensor(a[2], "temperature"),
+                   *k = tensor(a[3], "top_k"), *p = tensor(a[4], "top_p"), *low = tensor(a[5], "min_p"),
+                   *token = tensor(a[6], "token"), *logprob = tensor(a[7], "logprob"), *status = tensor(a[8], "status");
+  require(x && (x->scalar_type() == at::kFloat || x->scalar_type() == at::kBFloat16) && x->dim() == 2 &&
+              (x->stride(1) == 1 || x->size(1) == 1),
+          "logits: fp32 or bf16 [rows, V]");
+  const int64_t rows = x->size(0), V = x->size(1), stride = rows > 1 ? x->stride(0) : V;
+  require(V > 0, "logits: no tokens");
+  require(u && token, "u, token: tensors");
+  check(u, at::kFloat, {rows}, "u: fp32 [rows]");
+  check(t, at::kFloat, {rows}, "temperature: fp32 [rows]");
+  check(k, at::kInt, {rows}, "top_k: int32 [rows]");
+  check(p, at::kFloat, {rows}, "top_p: fp32 [rows]");
+  check(low, at::kFloat, {rows}, "min_p: fp32 [rows]");
+  check(token, at::kInt, {rows}, "token: int32 [rows]");
+  check(logprob, at::kFloat, {rows}, "logprob: fp32 [rows]");
+  check_status(status);
+  require(rows <= INT32_MAX && V <= INT32_MAX, "sizes: below 2^31");
+  require(x->is_cuda(), "logits: on a CUDA device");
+  on_gpu({x, u, t, k, p, low, token, logprob, status}, x->get_device());
+  void* s = stream_of(a[9], x->get_device());
+  return without_gil([&] {
+    return pced_sample(address(x), x->scalar_type() == at::kFloat ? PCED_IN_F32 : PCED_IN_BF16, stride, (int32_t)rows,
+                       (int32_t)V, (const float*)address(u), (const float*)address(t), (const int32_t*)address(k),
+                       (const float*)address(p), (const float*)address(low), (int32_t*)address(token),
+                       (float*)address(logprob), (int32_t*)address(status), s);
+  });
+}
+
 // A call's status as a Python number; no C++ exception leaves it.
 template <pced_status (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -286,11 +328,14 @@ PyMethodDef method(const char* name) {
   return {name, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<kv_append, 11>("kv_append"),
+PyMethodDef methods[] = {method<kv_append<false>, 11>("kv_append"),
+                         method<kv_append<true>, 11>("kv_append8"),
                          method<block_summaries, 4>("block_summaries"),
                          method<block_select, 9>("block_select"),
-                         method<paged_attention, 10>("paged_attention"),
+                         method<paged_attention<false>, 10>("paged_attention"),
+                         method<paged_attention<true>, 10>("paged_attention8"),
                          method<logits_process, 12>("logits_process"),
+                         method<sample, 10>("sample"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "pced_calls", nullptr, -1, methods};
 

@@ -124,6 +124,24 @@ pced_status make_tmap_kv_part(CUtensorMap* map, const void* base, uint64_t rows,
   return PCED_OK;
 }
 
+pced_status make_tmap_bytes(CUtensorMap* map, const void* base, uint64_t rows, uint32_t D, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return fail(PCED_ERR_CUDA, "cuTensorMapEncodeTiled unavailable");
+  if ((D != 64 && D != 128) || box_rows < 1 || box_rows > 256 || rows < 1 || rows > (1ull << 32) ||
+      ((uintptr_t)base & 15u))
+    return fail(PCED_ERR_INVALID_ARG, "kv tensor map: unsupported geometry");
+  const cuuint64_t dims[3] = {D, rows, 1};
+  const cuuint64_t strides[2] = {D, (cuuint64_t)D * rows};
+  const cuuint32_t box[3] = {D, box_rows, 1};
+  const cuuint32_t es[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, es,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(PCED_ERR_CUDA, "cuTensorMapEncodeTiled (8-bit kv tile) failed (%d)", (int)r);
+  return PCED_OK;
+}
+
 }  // namespace pced_host
 
 extern "C" const char* pced_status_string(int32_t status) {

@@ -86,6 +86,9 @@ pced_status check_paged_heads(const pced_paged_cache* c, int32_t Hq, const char*
 // host.cu: make_tmap_kv with `blocks` of the D / 64 column blocks in a copy
 pced_status make_tmap_kv_part(CUtensorMap* map, const void* base, uint64_t rows, uint32_t D, uint32_t box_rows,
                               uint32_t blocks);
+// ... over a pool of `rows` rows of D bytes, box_rows whole rows in a copy, swizzled
+// over D bytes (16-byte part c of row r lies at c ^ (r & 7), for D = 64 at c ^ (r >> 1 & 3))
+pced_status make_tmap_bytes(CUtensorMap* map, const void* base, uint64_t rows, uint32_t D, uint32_t box_rows);
 // more than 48 KB of dynamic shared memory for a kernel: asked for once per device
 template <typename K>
 inline cudaError_t allow_smem(K kernel, size_t bytes, bool (&done)[64]) {
