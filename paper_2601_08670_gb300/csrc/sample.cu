@@ -6,16 +6,17 @@
 // p of their weight, those of weight min_p or more.  The token is the first kept one, in
 // the order of the vocabulary, up to which the kept weights sum to more than u of all.
 //
-// A sum over a vocabulary decides at which token u falls, so it must not depend on its
-// order, and its error counts 150,000 times (every border of two tokens is a place to be
-// wrong): with weights of 24 bits, one row in some thousands gets another token than in 64
-// bits.  So weights are whole numbers of 2^-44, exact to about 2^-32 of themselves (see
-// Weight), and summed as such.
+// A sum over a vocabulary decides at which token u falls, and its error counts 150,000
+// times (every border of two tokens is a place to be wrong): with weights of 24 bits one row
+// in some thousands gets another token than in 64 bits.  So weights are exact to about
+// 2^-32 of themselves, and are added without further loss (see Sum).
 //
 // A cluster of CTAs holds a row in shared memory, read once.  A cut is found by counting
-// (or weighing) the tokens in 1024 equal ranges of x below m, then the border range's
-// tokens one by one if they are few, else in 1024 equal ranges of their (logit, token)
-// pairs, as 64-bit numbers, again and again: pairs are distinct, so that ends.
+// the tokens in equal ranges of x below m.  For the top k the range that brings the count to
+// k is then ranked token by token; for the top p the counts bound the weights, so
+// that a few ranges are left, whose tokens are weighed in finer ones, of which one is ranked.
+// Ranges with too many tokens (of equal logits, say) are split by (logit, token) pairs as
+// 64-bit numbers, again and again: pairs are distinct, so that ends.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -40,413 +41,930 @@ struct SampleArgs {
 
 constexpr int SMP_THREADS = 512;
 constexpr int SMP_WARPS = SMP_THREADS / 32;
-constexpr int SMP_BINS = 1024;
-constexpr int SMP_FEW = 512;          // tokens of a border range that are ranked one by one
-constexpr int SMP_EACH = 8;           // tokens of a lane in a tile
-constexpr int SMP_TILE = 32 * SMP_EACH;
-constexpr int SMP_MAX_V = 393216;     // a cluster's shared memory (and 2^44 V < 2^63)
+constexpr int SMP_BINS = 1024;        // ranges
+constexpr int SMP_FEW = 512;          // tokens of a range that are ranked one by one
+constexpr int SMP_EACH = 16;          // tokens of a lane in a group, whose weight is kept
+constexpr int SMP_GROUP = 32 * SMP_EACH;
+constexpr int SMP_FINE = 256;         // ranges that a cluster weighs (what its CTAs read of one another is slow)
+constexpr int SMP_LIST = 1536;        // tokens of a CTA that are worth a list
+constexpr int SMP_SOLO = 4096;        // ... of a row that one CTA goes on with alone
+constexpr int SMP_MAX_V = 393216;     // (what a cluster's shared memory holds)
 constexpr int SMP_MAX_BYTES = 192 * 1024;  // of a CTA's part of a row
-constexpr int SMP_MAX_TILES = SMP_MAX_BYTES / 2 / SMP_TILE;
-constexpr float SMP_LEAST = -45.f;    // log2 of weights that are nothing in steps of 2^-44
-constexpr uint64_t SMP_ONE = (uint64_t)1 << 44;
+constexpr int SMP_MAX_GROUPS = SMP_MAX_BYTES / 2 / SMP_GROUP + 1;
+constexpr int SMP_UNIT = 42;          // weights are counted in steps of 2^-42
+constexpr float SMP_ALIVE = 44.f;     // -log2 of weights that no cut asks about
+constexpr float SMP_LOWEST = 100.f;   // ... and that are nothing
 
-// 2^(j / 32) in steps of 2^-31
-__device__ const uint32_t kExp2Table[32] = {
-    2147483648u, 2194507417u, 2242560872u, 2291666561u, 2341847524u, 2393127307u, 2445529972u, 2499080105u,
-    2553802834u, 2609723834u, 2666869345u, 2725266179u, 2784941738u, 2845924021u, 2908241642u, 2971923842u,
-    3037000500u, 3103502151u, 3171459999u, 3240905930u, 3311872529u, 3384393094u, 3458501653u, 3534232978u,
-    3611622603u, 3690706840u, 3771522796u, 3854108391u, 3938502376u, 4024744348u, 4112874773u, 4202935003u};
+// {2^(j / 32) as fp32, what it is short of, relative}
+struct Exp2Entry {
+  uint32_t bits;
+  float rest;
+};
+__device__ const Exp2Entry kExp2Table[32] = {
+    {0x3F800000u, 0.f}, {0x3F82CD87u, -4.70845762e-08f}, {0x3F85AAC3u, 4.62854715e-08f}, {0x3F88980Fu, -5.56042252e-08f},
+    {0x3F8B95C2u, -1.19921575e-08f}, {0x3F8EA43Au, -4.87760623e-08f}, {0x3F91C3D3u, 4.72978243e-08f}, {0x3F94F4F0u, -3.48144269e-08f},
+    {0x3F9837F0u, 3.19341815e-08f}, {0x3F9B8D3Au, -2.68866653e-08f}, {0x3F9EF532u, 3.62105723e-08f}, {0x3FA27043u, 1.11842102e-09f},
+    {0x3FA5FED7u, -3.09907193e-08f}, {0x3FA9A15Bu, -2.63830096e-08f}, {0x3FAD583Fu, -7.47521334e-09f}, {0x3FB123F6u, -4.24563567e-08f},
+    {0x3FB504F3u, 1.71142709e-08f}, {0x3FB8FBAFu, 2.30019666e-08f}, {0x3FBD08A4u, -3.04768335e-08f}, {0x3FC12C4Du, -1.65385377e-08f},
+    {0x3FC5672Au, 5.23333421e-09f}, {0x3FC9B9BEu, -3.5920646e-08f}, {0x3FCE248Cu, 6.10759177e-09f}, {0x3FD2A81Eu, -3.11405444e-08f},
+    {0x3FD744FDu, -1.47196051e-08f}, {0x3FDBFBB8u, -2.82181016e-08f}, {0x3FE0CCDFu, -5.25879518e-09f}, {0x3FE5B907u, -6.36038733e-09f},
+    {0x3FEAC0C7u, -6.12825968e-09f}, {0x3FEFE4BAu, -2.48804088e-08f}, {0x3FF5257Du, 5.14060927e-09f}, {0x3FFA83B3u, -8.69726691e-09f}};
 
-// Weights of a row's logits.  y = (x - m) log2(e) / t is held in two fp32 numbers (x - m
-// exactly, by the two-sum; the factor in two parts): y = q / 32 + r, q whole, |r| <= 1/64.
-// 2^(q / 32) comes from the table, 2^r - 1 from its series to r^4 (the next term is below
-// 2^-39), both in whole steps of 2^-31, so that their product is one of two 32-bit numbers.
+// What a row's weights are made with.  y = x log2(e) / t, from a factor in two parts, is
+// p + low, p rounded to q / 32 + r, q whole; w = 2^(y - N), N the ceiling of the largest
+// y (so the largest weight lies in (1/2, 1]).  2^(q / 32 - N) comes from a table that the
+// row's CTA makes (16 copies side by side, so that a warp's lanes do not meet on banks),
+// 2^r - 1 from its series to r^4, of which the rest is below 2^-36 of it.
 struct Weight {
-  float m, ch, cl;  // ch + cl = log2(e) / t
-  uint32_t table;   // entry `lane`
-  __device__ __forceinline__ void set(float m_, float t, int lane) {
-    m = m_;
-    ch = cl = 0.f;
-    if (t < 1e30f) {  // (above, all weights are the same)
-      const float lh = 1.44269502f, ll = 1.92596303e-08f;
-      ch = __fdiv_rn(lh, t);
-      cl = __fdiv_rn(fmaf(-ch, t, lh) + ll, t);
-    }
-    table = kExp2Table[lane];
-  }
-  // whether a weight can be more than nothing
-  __device__ __forceinline__ bool some(float x) const { return x == m || (x - m) * ch > SMP_LEAST; }
-  // All lanes of a warp.
-  __device__ __forceinline__ uint64_t of(float x) const {
-    const float s = __fsub_rn(x, m), b = __fsub_rn(s, x);
-    const float e = __fadd_rn(__fsub_rn(x, __fsub_rn(s, b)), __fsub_rn(-m, b));
-    const float p = __fmul_rn(s, ch);
-    const float low = fmaf(e, ch, fmaf(s, cl, fmaf(s, ch, -p)));
-    constexpr float MAGIC = 393216.f;  // 1.5 2^18: sums with it are rounded to 32nds
+  float ch, cl;            // ch + cl = log2(e) / t
+  float floor;             // logits are taken as this at least: 2^-SMP_LOWEST
+  const float2* table;     // this lane's copy
+  // a (1 + g): the weight
+  __device__ __forceinline__ void of(float x, float& a, float& g) const {
+    constexpr float MAGIC = 393216.f;  // 1.5 2^18: sums with it are rounded to 32nds; its low bits are 0
+    x = fmaxf(x, floor);               // (also of what is not a number)
+    const float p = __fmul_rn(x, ch);
+    const float low = fmaf(x, cl, fmaf(x, ch, -p));
     const float shifted = __fadd_rn(p, MAGIC);
     const float r = __fadd_rn(__fsub_rn(p, __fsub_rn(shifted, MAGIC)), low);
-    const int q = __float_as_int(shifted) - __float_as_int(MAGIC);
-    const float g = r * fmaf(r, fmaf(r, fmaf(r, 20654774.98f, 119194165.75f), 515882495.51f), 1488522235.91f);
-    const uint32_t f = 0x80000000u + (uint32_t)__float2int_rn(g);
-    const uint32_t t = __shfl_sync(0xffffffffu, table, q & 31);
-    const uint64_t w = (uint64_t)t * f >> ((18 - (q >> 5)) & 63);
-    return x == m ? SMP_ONE : p > SMP_LEAST ? w : 0;
+    const uint32_t q = __float_as_uint(shifted);
+    const float2 e = *reinterpret_cast<const float2*>(reinterpret_cast<const char*>(table) + (q << 7 & 0xF80u));
+    a = __uint_as_float(__float_as_uint(e.x) + (q << 18));  // (the entries make up for what q's low bits add)
+    g = fmaf(r, fmaf(r, fmaf(r, fmaf(r, 9.61812911e-3f, 5.55041087e-2f), 2.40226507e-1f), 6.93147181e-1f), e.y);
   }
 };
 
-// Order of (logit, token) pairs: larger logits first, then lower tokens
-__device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t b = __float_as_uint(x);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ uint64_t pair_of(float x, int v) { return (uint64_t)order_key(x) << 32 | (uint32_t)~v; }
-
-__device__ __forceinline__ float load_logit(const float* p) { return *p; }
-__device__ __forceinline__ float load_logit(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-
-__device__ __forceinline__ uint64_t warp_sum64(uint64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// The first range that brings the sum to the target, and what lies before it.
-struct Border {
-  uint32_t found, bin, count, n;  // count: tokens before it, n: in it
-  uint64_t mass;                  // weight before it
+// A sum of weights, at most SMP_EACH of them: what fits the grid of 2^-18 that numbers from
+// 32 to 64 have is added exactly, the rest, below 2^-19 each, beside it.
+struct Sum {
+  float high = 32.f, low = 0.f;
+  __device__ __forceinline__ void add(float a, float g) {
+    const float h1 = __fadd_rn(high, a);
+    low += __fsub_rn(a, __fsub_rn(h1, high));
+    const float h2 = fmaf(a, g, h1);
+    low += fmaf(a, g, -__fsub_rn(h2, h1));
+    high = h2;
+  }
+  // in whole steps of 2^-SMP_UNIT: high part of 2^-18, low part from 0 to 2^24 - 1
+  __device__ __forceinline__ void parts(int& h, int& l) const {
+    h = __float_as_int(high) - __float_as_int(32.f);
+    l = __float2int_rn(low * (float)((uint64_t)1 << SMP_UNIT));
+    h += l >> 24;
+    l &= 0xFFFFFF;
+  }
+  __device__ __forceinline__ uint64_t steps() const {
+    int h, l;
+    parts(h, l);
+    return (uint64_t)(((int64_t)h << 24) + l);
+  }
+  __device__ __forceinline__ uint64_t warp_steps() const {
+    int h, l;
+    parts(h, l);
+    h = __reduce_add_sync(0xffffffffu, h);
+    l = __reduce_add_sync(0xffffffffu, l);
+    return (uint64_t)(((int64_t)h << 24) + l);
+  }
 };
+static_assert(SMP_UNIT == 42, "18 + 24");
+static_assert(SMP_BINS == 4 * SMP_FINE, "see keep_share");
 
-struct SampleShared {
-  uint32_t hist[4][SMP_BINS];  // tokens of a range; their weights' 15-bit parts
-  uint64_t cand[SMP_FEW], cand_w[SMP_FEW];
-  uint64_t tile_mass[SMP_MAX_TILES];
-  uint32_t n_cand;
-  uint32_t wcount[SMP_WARPS];
-  uint64_t wmass[SMP_WARPS], wmin[SMP_WARPS], wmax[SMP_WARPS];
-  float fmax[SMP_WARPS], fmin[SMP_WARPS];
-  // what the cluster's CTAs tell one another: two of each, by turns, with a barrier of
-  // the cluster between a write and its reads, so that the next write to one comes after them
-  struct Told {
-    float mx, mn;
-    uint32_t count;
-    uint64_t mass, lo, hi, cut;
-    Border border;
-  } told[2];
-  uint64_t target, seek;
-  float threshold;
+// Order of (logit, token) pairs: larger logits first, then lower tokens
+__device__ __forceinline__ uint64_t pair_of(float x, int token) {
+  const uint32_t b = __float_as_uint(x + 0.f);  // (-0 is 0)
+  return (uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~token;
+}
+// The last kept pair: x, then token.
+struct Cut {
+  float x = -INFINITY;
+  int token = INT32_MAX;
+  __device__ __forceinline__ bool keeps(float v, int t) const { return v > x || (v == x && t <= token); }
+  __device__ __forceinline__ void set(uint64_t pair) {
+    const uint32_t k = (uint32_t)(pair >> 32);
+    x = __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+    token = (int)~(uint32_t)pair;
+  }
 };
 
 template <typename T>
+struct Words;  // 16 bytes of logits
+template <>
+struct Words<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void split(uint4 v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ float to(float x) { return x; }
+};
+template <>
+struct Words<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void split(uint4 v, float (&x)[8]) {
+    x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
+    x[4] = bf16_lo(v.z), x[5] = bf16_hi(v.z), x[6] = bf16_lo(v.w), x[7] = bf16_hi(v.w);
+  }
+  static __device__ __forceinline__ __nv_bfloat16 to(float x) { return __float2bfloat16_rn(x); }
+};
+
+// Equal ranges of x, in sixteenths: the float `magic` + 16ths has them in its low bits.
+struct Ranges {
+  static constexpr float MAGIC = 524288.f;  // 2^19
+  float top, per;                           // the first one's upper end; ranges of a unit of x
+  __device__ __forceinline__ void set(float top_, float width) {  // SMP_BINS - 4 ranges from top down
+    top = top_;
+    per = (float)(SMP_BINS - 4) / width;
+  }
+  // a number that all of the ranges up to `bin` are above
+  __device__ __forceinline__ float below(int bin) const {
+    return bin >= SMP_BINS - 4 ? -INFINITY : top - ((float)bin + 1.25f) / per;
+  }
+  __device__ __forceinline__ int sixteenths(float x) const {
+    return __float_as_int(fmaf(top - x, per, MAGIC + 1.f / 16)) - __float_as_int(MAGIC);
+  }
+};
+
+// The first range that brings the sum to the target, and what lies before it.
+struct Border {
+  bool found;
+  uint32_t bin, n;  // n: tokens in it
+  uint64_t before;
+};
+
+struct SampleShared {
+  float2 table[32][16];
+  uint32_t count[SMP_BINS / 2];  // tokens of a range, 16 bits each
+  uint32_t weight[3][SMP_BINS];  // their weights, 15 bits each
+  uint64_t cand[SMP_FEW];
+  uint64_t group[SMP_MAX_GROUPS];  // kept weight (on its way in two numbers, 21 bits in the first)
+  uint16_t list[SMP_LIST];       // places of the tokens that matter
+  uint32_t n_list, n_cand;
+  int at[2];
+  uint64_t wscan[SMP_WARPS];
+  uint32_t wkept[SMP_WARPS];
+  float2 fscan[SMP_WARPS];
+  Border border;
+  float threshold;
+  double below;  // of a min_p: t log(p)
+  uint64_t cut;
+  // what the cluster's warps tell one another: two of each, by turns, with a barrier of the
+  // cluster between a write and its reads, so that the next write to one comes after them
+  struct alignas(16) Told {
+    int mx[SMP_WARPS], mn[SMP_WARPS];
+    uint64_t sum[SMP_WARPS], lo[SMP_WARPS], hi[SMP_WARPS];
+    uint32_t count;
+  } told[2];
+
+  // When a range is ranked the histograms are free: this CTA's candidates and their weights,
+  // all the cluster's and theirs.
+  __device__ __forceinline__ uint64_t* candidates(int which) { return which ? reinterpret_cast<uint64_t*>(weight[which - 1]) : cand; }
+};
+static_assert(SMP_BINS * 4 >= SMP_FEW * 8, "room for the candidates");
+
+// floats as whole numbers of the same order
+__device__ __forceinline__ int ordered(float x) {
+  const int b = __float_as_int(x);
+  return b >= 0 ? b : b ^ 0x7FFFFFFF;
+}
+__device__ __forceinline__ float from_ordered(int b) { return __int_as_float(b >= 0 ? b : b ^ 0x7FFFFFFF); }
+
+template <typename T>
 struct Row {
+  static constexpr int W = Words<T>::N, TILES = SMP_EACH / W;  // logits of 16 bytes; 16 bytes of a lane in a group
   const SampleArgs& a;
   SampleShared& s;
   cg::cluster_group cluster;
-  const T* data;  // this CTA's part of the row
-  int first, n;   // its first token, their number
+  uint4* data;                         // this CTA's part of the row, from 16 bytes of the row on, -inf around it
+  int first, groups;                   // token of its first place
   int ctas, rank, tid, lane, warp, turn;
+  float mx, mn;                        // of the row
   Weight w;
-  uint64_t cut;  // pairs below it are not kept
+  float ym;                            // log2 of the largest weight
+  float alive;                         // smaller logits have weights that no cut asks about
+  Ranges coarse;
+  float log2_range;                    // log2 of weights at a range's ends, the difference
+  Cut cut;
+  float low;                           // smaller logits are not kept
+  bool listed;                         // the others' places are in the list (each CTA's own matter, as is `low`)
+  int solo;                            // > 0: so many tokens are left, and this CTA, which has them, alone
+  bool gone;                           // ... another CTA
 
-  __device__ __forceinline__ SampleShared::Told& mine() { return s.told[turn & 1]; }
-  __device__ __forceinline__ const SampleShared::Told& theirs(int r) { return cluster.map_shared_rank(&s, r)->told[turn & 1]; }
-  // all have told; read with theirs(), then call next()
-  __device__ __forceinline__ void meet() { cluster.sync(); }
-  __device__ __forceinline__ void next() { ++turn; }
-
-  __device__ __forceinline__ float logit(int i) const {  // (-0 is 0, what is not a number: -inf)
-    return i < n ? fmaxf(load_logit(data + i), -INFINITY) + 0.f : -INFINITY;
+  __device__ __forceinline__ typename SampleShared::Told& mine() { return s.told[turn & 1]; }
+  __device__ __forceinline__ const typename SampleShared::Told& theirs(int r) {
+    return cluster.map_shared_rank(&s, r)->told[turn & 1];
   }
-  // f(token of the part, logit) for all lanes and tiles; tokens past the end are -inf
+  __device__ __forceinline__ float at(int place) const { return (float)reinterpret_cast<const T*>(data)[place]; }
+
+  // f(e, logit, place) for the SMP_EACH places of a lane in group g
   template <typename F>
-  __device__ __forceinline__ void each_tile(F f) {
-    for (int t = warp; t * SMP_TILE < n; t += SMP_WARPS) f(t);
-  }
-  __device__ __forceinline__ bool keeps(float x, int i) const { return w.some(x) && pair_of(x, first + i) >= cut; }
-
-  // Weight of all kept tokens, tile by tile into tile_mass; the CTA's sum to all threads.
-  __device__ __forceinline__ uint64_t weigh() {
-    uint64_t sum = 0;
-    each_tile([&](int t) {
-      uint64_t mass = 0;
+  __device__ __forceinline__ void each_of(int g, F f) const {
 #pragma unroll
-      for (int e = 0; e < SMP_EACH; ++e) {
-        const int i = t * SMP_TILE + e * 32 + lane;
-        const float x = logit(i);
-        const bool k = keeps(x, i);
-        if (cut == 0 || __any_sync(0xffffffffu, k)) {
-          const uint64_t v = w.of(x);
-          mass += k ? v : 0;
+    for (int t = 0; t < TILES; ++t) {
+      const int v = (g * TILES + t) * 32 + lane;
+      float x[W];
+      Words<T>::split(data[v], x);
+#pragma unroll
+      for (int e = 0; e < W; ++e) f(t * W + e, x[e], v * W + e);
+    }
+  }
+  // A barrier of the CTAs that still work on the row.
+  __device__ __forceinline__ void meet() {
+    if (solo) __syncthreads();
+    else cluster.sync();
+  }
+  // f(logit, token) for the tokens that `low` leaves
+  template <typename F>
+  __device__ __forceinline__ void each_left(F f) const {
+    if (listed) {
+      const int n = solo ? solo : (int)s.n_list;
+      const float2* left = reinterpret_cast<const float2*>(data);
+      for (int i = tid; i < n; i += SMP_THREADS) {
+        if (solo) {
+          f(left[i].x, __float_as_int(left[i].y));
+        } else {
+          const int place = s.list[i];
+          f(at(place), first + place);
         }
       }
-      mass = warp_sum64(mass);
-      if (lane == 0) s.tile_mass[t] = mass;
-      sum += mass;
-    });
-    __syncthreads();
-    if (lane == 0) s.wmass[warp] = sum;
-    __syncthreads();
-    sum = 0;
-    for (int i = 0; i < SMP_WARPS; ++i) sum += s.wmass[i];
-    return sum;
-  }
-
-  // Border of the histogram, which the cluster's CTAs bring together, a part of the
-  // ranges each; `share` > 0: the target is that share of the weight, at least 1.
-  __device__ __forceinline__ Border border(bool by_mass, uint64_t target, double share) {
-    meet();  // all histograms are complete
-    const int slice = SMP_BINS / ctas, each = (slice + SMP_THREADS - 1) / SMP_THREADS;  // of a CTA, of a thread
-    const int b0 = rank * slice + tid * each, mine_n = tid * each < slice ? each : 0;
-    uint32_t count[2] = {0, 0};
-    uint64_t mass[2] = {0, 0};
-    uint32_t c = 0;
-    uint64_t ms = 0;
-    for (int j = 0; j < mine_n; ++j) {
-      for (int r = 0; r < ctas; ++r) {
-        const SampleShared& o = *cluster.map_shared_rank(&s, r);
-        count[j] += o.hist[0][b0 + j];
-        if (by_mass)
-          mass[j] += o.hist[1][b0 + j] + ((uint64_t)o.hist[2][b0 + j] << 15) + ((uint64_t)o.hist[3][b0 + j] << 30);
-      }
-      c += count[j];
-      ms += mass[j];
+      return;
     }
-    // sums up to this thread
-    uint32_t ci = c;
-    uint64_t mi = ms;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, ci, o);
-      const uint64_t y = __shfl_up_sync(0xffffffffu, mi, o);
-      if (lane >= o) ci += x, mi += y;
-    }
-    __syncthreads();
-    if (lane == 31) s.wcount[warp] = ci, s.wmass[warp] = mi;
-    __syncthreads();
-    for (int i = 0; i < warp; ++i) ci += s.wcount[i], mi += s.wmass[i];
-    if (tid == SMP_THREADS - 1) mine().count = ci, mine().mass = mi;
-    meet();
-    uint64_t all = 0;
-    uint32_t before_c = 0;
-    uint64_t before_m = 0;
-    for (int r = 0; r < ctas; ++r) {
-      all += theirs(r).mass;
-      if (r < rank) before_c += theirs(r).count, before_m += theirs(r).mass;
-    }
-    next();
-    if (share > 0) {
-      const double want = ceil(share * (double)all);
-      target = want < 1.0 ? 1 : (uint64_t)want;
-    }
-    if (tid == 0) mine().border.found = 0;
-    __syncthreads();
-    uint32_t at_c = before_c + ci - c;
-    uint64_t at_m = before_m + mi - ms;
-    for (int j = 0; j < mine_n; ++j) {
-      const uint64_t from = by_mass ? at_m : at_c, to = from + (by_mass ? mass[j] : count[j]);
-      if (from < target && to >= target) {
-        Border b;
-        b.found = 1, b.bin = b0 + j, b.count = at_c, b.n = count[j], b.mass = at_m;
-        mine().border = b;
-      }
-      at_c += count[j], at_m += mass[j];
-    }
-    s.target = target;
-    meet();
-    Border b;
-    b.found = 0;
-    for (int r = 0; r < ctas; ++r)
-      if (theirs(r).border.found) b = theirs(r).border;
-    next();
-    return b;
-  }
-
-  // Cuts off what lies behind the first `target` tokens (by_mass: behind the first that
-  // hold `share` of the kept weight).
-  __device__ __forceinline__ void search(bool by_mass, uint64_t target, double share, float per_range) {
-    uint64_t lo = cut, hi = ~0ull;
-    int shift = -1;  // -1: equal ranges of x
-    for (int level = 0; level < 10; ++level) {
-      const auto range_of = [&](float x, uint64_t pair) -> int {
-        if (shift >= 0) return (int)((hi - pair) >> shift);
-        return x == w.m ? 0 : (int)fminf((w.m - x) * per_range, (float)(SMP_BINS - 1));
-      };
-      __syncthreads();
-      for (int i = tid; i < 4 * SMP_BINS; i += SMP_THREADS) s.hist[0][i] = 0;
-      if (tid == 0) s.n_cand = 0;
-      __syncthreads();
-      each_tile([&](int t) {
-#pragma unroll
-        for (int e = 0; e < SMP_EACH; ++e) {
-          const int i = t * SMP_TILE + e * 32 + lane;
-          const float x = logit(i);
-          const uint64_t pair = pair_of(x, first + i);
-          const bool in = w.some(x) && pair >= lo && pair <= hi;
-          if (!__any_sync(0xffffffffu, in)) continue;
-          const int b = in ? range_of(x, pair) : 0;
-          if (in) atomicAdd(&s.hist[0][b], 1u);
-          if (by_mass) {
-            const uint64_t v = w.of(x);
-            if (in) {
-              atomicAdd(&s.hist[1][b], (uint32_t)v & 0x7FFFu);
-              atomicAdd(&s.hist[2][b], (uint32_t)(v >> 15) & 0x7FFFu);
-              atomicAdd(&s.hist[3][b], (uint32_t)(v >> 30));
-            }
-          }
-        }
-      });
-      const Border b = border(by_mass, target, share);
-      if (!b.found) return;  // all are kept
-      // the next level counts from what lies before this range on
-      target = s.target - (by_mass ? b.mass : b.count);
-      share = 0.0;
-      const bool few = b.n <= SMP_FEW;
-      uint64_t least = ~0ull, most = 0;
-      if (few || shift < 0) {
-        each_tile([&](int t) {
-#pragma unroll
-          for (int e = 0; e < SMP_EACH; ++e) {
-            const int i = t * SMP_TILE + e * 32 + lane;
-            const float x = logit(i);
-            const uint64_t pair = pair_of(x, first + i);
-            const bool in = w.some(x) && pair >= lo && pair <= hi && range_of(x, pair) == (int)b.bin;
-            if (!__any_sync(0xffffffffu, in)) continue;
-            const uint64_t v = by_mass && few ? w.of(x) : 0;
-            if (!in) continue;
-            least = min(least, pair), most = max(most, pair);
-            if (few) {
-              const uint32_t at = atomicAdd(&s.n_cand, 1u);
-              s.cand[at] = pair, s.cand_w[at] = v;
-            }
-          }
+    for (int g = warp; g < groups; g += SMP_WARPS) {
+      uint32_t take = 0;
+      each_of(g, [&](int e, float x, int) { take |= (uint32_t)(x >= low) << e; });
+      if (__any_sync(0xffffffffu, take))
+        each_of(g, [&](int e, float x, int place) {
+          if (take >> e & 1u) f(x, first + place);
         });
+    }
+  }
+  // Where few tokens are left, CTA 0 takes them all (logit, token) and goes on alone: a barrier of
+  // a cluster takes half a microsecond, and what its CTAs read of one another 10 bytes a clock.
+  __device__ __forceinline__ void try_solo() {
+    if (ctas == 1) return;
+    if (tid == 0) mine().count = listed ? s.n_list : SMP_SOLO + 1;
+    cluster.sync();
+    const int n = lane < ctas ? (int)theirs(lane).count : 0;
+    ++turn;
+    int to = n;
+#pragma unroll
+    for (int o = 1; o < ROW_CLUSTER; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, to, o);
+      if (lane >= o) to += y;
+    }
+    const int total = __shfl_sync(0xffffffffu, to, ROW_CLUSTER - 1);
+    if (total > SMP_SOLO || total * 8 > a.per * (int)sizeof(T)) return;
+    gone = rank != 0;
+    if (rank == 0) {
+      // (its own first, as the others' come where its part of the row was)
+      const int own = __shfl_sync(0xffffffffu, n, 0);
+      float2 x[SMP_LIST / SMP_THREADS];
+#pragma unroll
+      for (int j = 0; j < SMP_LIST / SMP_THREADS; ++j) {
+        const int i = tid + j * SMP_THREADS;
+        if (i < own) x[j] = make_float2(at(s.list[i]), __int_as_float(first + s.list[i]));
       }
-      if (few) {
-        rank_few(by_mass, target);
+      __syncthreads();
+      float2* left = reinterpret_cast<float2*>(data);
+#pragma unroll
+      for (int j = 0; j < SMP_LIST / SMP_THREADS; ++j) {
+        const int i = tid + j * SMP_THREADS;
+        if (i < own) left[i] = x[j];
+      }
+      // two warps for each CTA
+      const int r = warp / 2, their_n = __shfl_sync(0xffffffffu, n, r), base = __shfl_sync(0xffffffffu, to, r) - their_n;
+      if (r > 0 && r < ctas) {
+        const SampleShared& o = *cluster.map_shared_rank(&s, r);
+        const T* part = reinterpret_cast<const T*>(cluster.map_shared_rank(data, r));
+        const int64_t from = (int64_t)r * a.per;
+        const T* src = (const T*)a.x + (int64_t)(blockIdx.x / ctas) * a.stride + from;
+        const int phase = (int)((uintptr_t)src / sizeof(T) % W);
+        for (int i = tid & 63; i < their_n; i += 64) {
+          const int place = o.list[i];
+          left[base + i] = make_float2((float)part[place], __int_as_float((int)from - phase + place));
+        }
+      }
+    }
+    cluster.sync();  // (CTA 0 has read the others' memory)
+    if (rank == 0) {
+      ctas = 1;
+      solo = total;
+    }
+  }
+  // The places of the tokens from `low_` on, where they are few enough.
+  __device__ __forceinline__ void list(float low_) {
+    low = low_;
+    listed = false;
+    __syncthreads();
+    if (tid == 0) s.n_list = 0;
+    __syncthreads();
+    for (int g = warp; g < groups; g += SMP_WARPS) {
+      uint32_t take = 0;
+      each_of(g, [&](int e, float x, int) { take |= (uint32_t)(x >= low) << e; });
+      if (!__any_sync(0xffffffffu, take)) continue;
+      const int n = __popc(take);
+      int to = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, to, o);
+        if (lane >= o) to += y;
+      }
+      int base = 0;
+      if (lane == 31) base = (int)atomicAdd(&s.n_list, (uint32_t)to);
+      base = __shfl_sync(0xffffffffu, base, 31) + to - n;
+      each_of(g, [&](int e, float, int place) {
+        if ((take >> e & 1u) && base < SMP_LIST) s.list[base] = (uint16_t)place;
+        base += take >> e & 1u;
+      });
+    }
+    __syncthreads();
+    listed = s.n_list <= SMP_LIST;
+  }
+
+  // m, N and the table for temperature t.  Where |m| / t is very large, the logits are first
+  // made differences from m: those that count lie so near to it that they are exact.  (A row
+  // with +inf becomes 0 at those and -inf elsewhere.)  inverse: 1 / w.ch, entry: of the table
+  __device__ __forceinline__ void set_weights(float inverse, Exp2Entry entry) {
+    if (!(fabsf(mx) * w.ch <= 8192.f)) {
+      __syncthreads();
+      T* p = reinterpret_cast<T*>(data);
+      for (int i = tid; i < groups * SMP_GROUP; i += SMP_THREADS) {
+        const float x = (float)p[i];
+        p[i] = Words<T>::to(mx == INFINITY ? (x == mx ? 0.f : -INFINITY) : x - mx);
+      }
+      thread_max = (float)Words<T>::to(mx == INFINITY ? (thread_max == mx ? 0.f : -INFINITY) : thread_max - mx);
+      mn = mx == INFINITY ? 0.f : fmaxf(mn - mx, -3e38f);
+      mx = 0.f;
+    }
+    const float y = __fmul_rn(mx, w.ch), top = ceilf(y);
+    ym = (y - top) + fmaf(mx, w.cl, fmaf(mx, w.ch, -y));
+    w.floor = (top - SMP_LOWEST) * inverse;
+    alive = (top - SMP_ALIVE) * inverse;
+    low = alive;
+    listed = gone = false;
+    solo = 0;
+    w.table = &s.table[0][lane & 15];
+    const uint32_t j = tid / 16;
+    s.table[j][tid % 16] =
+        make_float2(__uint_as_float(entry.bits - (j << 18) - ((uint32_t)(int)top << 23)), entry.rest);
+    const float width = fminf((SMP_ALIVE + 1.f) * inverse, fmaxf(mx - mn, 1e-30f));
+    coarse.set(mx, width);
+    log2_range = w.ch * width * (1.f / (SMP_BINS - 4));
+    __syncthreads();
+  }
+
+  // The cluster's sum of the warps' sums, of the CTAs before this one, and this one's.
+  struct Sums {
+    uint64_t all, before, own;
+  };
+  __device__ __forceinline__ Sums sum_up(uint64_t v) {
+    if (lane == 0) mine().sum[warp] = v;
+    meet();
+    // a CTA's sixteen by four lanes
+    const int r = lane >> 2;
+    uint64_t of_cta = 0;
+    if (r < ctas) {
+      const uint64_t* q = theirs(r).sum + (lane & 3) * (SMP_WARPS / 4);
+      const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(q), y = *reinterpret_cast<const ulonglong2*>(q + 2);
+      of_cta = x.x + x.y + y.x + y.y;
+    }
+    of_cta += __shfl_xor_sync(0xffffffffu, of_cta, 1);
+    of_cta += __shfl_xor_sync(0xffffffffu, of_cta, 2);
+    Sums z;
+    z.own = __shfl_sync(0xffffffffu, of_cta, 4 * rank);
+    z.all = of_cta, z.before = r < rank ? of_cta : 0;
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      z.all += __shfl_xor_sync(0xffffffffu, z.all, o);
+      z.before += __shfl_xor_sync(0xffffffffu, z.before, o);
+    }
+    ++turn;
+    return z;
+  }
+
+  // Weight of all tokens; the coarse ranges' numbers of them too.
+  template <bool COUNT>
+  __device__ __forceinline__ Sums weigh_all() {
+    uint64_t total = 0;
+    for (int g = warp; g < groups; g += SMP_WARPS) {
+      Sum sum;
+      each_of(g, [&](int, float x, int) {
+        float b, c;
+        w.of(x, b, c);
+        sum.add(b, c);
+        if (COUNT && x >= alive) count_in(coarse_of(x));
+      });
+      const uint64_t v = sum.warp_steps();
+      if (lane == 0) s.group[g] = v;
+      total += v;
+    }
+    return sum_up(total);
+  }
+  // ... of the kept ones among those that `low` leaves; GROUPS: by groups too
+  template <bool COUNT, bool GROUPS>
+  __device__ __forceinline__ Sums weigh_kept() {
+    __syncthreads();
+    if (GROUPS) {
+      for (int g = tid; g < groups; g += SMP_THREADS) s.group[g] = 0;
+      __syncthreads();
+    }
+    uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
+    uint64_t total = 0;
+    each_left([&](float x, int token) {
+      if (!cut.keeps(x, token)) return;
+      const uint64_t v = steps_of(x);
+      if (GROUPS) {
+        const int g = (token - first) / SMP_GROUP;
+        atomicAdd(part + 2 * g, (uint32_t)v & 0x1FFFFFu);
+        atomicAdd(part + 2 * g + 1, (uint32_t)(v >> 21));
+      } else {
+        total += v;
+      }
+      if (COUNT) count_in(coarse_of(x));
+    });
+    if (GROUPS) {
+      __syncthreads();
+      for (int g = tid; g < groups; g += SMP_THREADS) {
+        const uint64_t v = part[2 * g] + ((uint64_t)part[2 * g + 1] << 21);
+        s.group[g] = v;
+        total += v;
+      }
+    }
+    return sum_up(warp_sum64(total));
+  }
+  __device__ __forceinline__ int coarse_of(float x) const { return min(coarse.sixteenths(x) >> 4, SMP_BINS - 1); }
+  __device__ __forceinline__ void count_in(int bin) { atomicAdd(&s.count[bin >> 1], 1u << (16 * (bin & 1))); }
+  static __device__ __forceinline__ uint64_t warp_sum64(uint64_t v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  }
+
+  // Two ranges' tokens (and weights) of the cluster, each thread its own.
+  template <bool MASS>
+  __device__ __forceinline__ void gather_ranges(uint32_t (&n)[2], uint64_t (&m)[2]) {
+    static_assert(SMP_BINS == 2 * SMP_THREADS && ROW_CLUSTER == 8, "two ranges a thread");
+    n[0] = n[1] = 0;
+    m[0] = m[1] = 0;
+    if (MASS && !solo && 2 * tid >= SMP_FINE) return;
+    constexpr int BATCH = MASS ? 2 : 8;  // CTAs whose loads are in flight
+#pragma unroll
+    for (int r0 = 0; r0 < ROW_CLUSTER; r0 += BATCH) {
+      if (r0 >= ctas) break;
+      uint32_t c[BATCH];
+      uint2 b[BATCH][3];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        c[k] = 0;
+        if (r0 + k >= ctas) continue;
+        const SampleShared& o = *cluster.map_shared_rank(&s, r0 + k);
+        c[k] = o.count[tid];
+        if (MASS)
+#pragma unroll
+          for (int i = 0; i < 3; ++i) b[k][i] = *reinterpret_cast<const uint2*>(&o.weight[i][2 * tid]);
+      }
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        n[0] += c[k] & 0xFFFFu, n[1] += c[k] >> 16;
+        if (r0 + k >= ctas || !MASS) continue;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) m[0] += (uint64_t)b[k][i].x << (15 * i), m[1] += (uint64_t)b[k][i].y << (15 * i);
+      }
+    }
+  }
+  // The first range that brings the sum of the tokens' number (MASS: weight) to the target,
+  // after a barrier: all histograms are complete.  One follows here: all have read them.
+  template <bool MASS>
+  __device__ __forceinline__ Border find_border(uint64_t target) {
+    uint32_t n[2];
+    uint64_t m[2];
+    gather_ranges<MASS>(n, m);
+    if (!MASS) m[0] = n[0], m[1] = n[1];
+    uint64_t to = prefix(m[0] + m[1]);
+    __syncthreads();
+    if (lane == 31) s.wscan[warp] = to;
+    if (tid == 0) s.border.found = false;
+    __syncthreads();
+    const uint64_t ahead = lane < warp ? s.wscan[lane] : 0;  // (warp < 16)
+    to += warp_sum64(ahead);
+    uint64_t from = to - m[0] - m[1];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (from < target && from + m[j] >= target) {
+        s.border.found = true, s.border.bin = 2 * tid + j, s.border.n = n[j], s.border.before = from;
+      }
+      from += m[j];
+    }
+    meet();
+    return s.border;
+  }
+
+  __device__ __forceinline__ void clear_ranges(bool mass) {
+    __syncthreads();
+    s.count[tid] = 0;
+    if (mass)
+      for (int i = tid; i < SMP_BINS; i += SMP_THREADS) s.weight[0][i] = s.weight[1][i] = s.weight[2][i] = 0;
+    __syncthreads();
+  }
+  __device__ __forceinline__ uint64_t steps_of(float x) const {
+    Sum one;
+    float b, c;
+    w.of(x, b, c);
+    one.add(b, c);
+    return one.steps();
+  }
+  __device__ __forceinline__ void add_to_range(int bin, uint64_t v) {
+    count_in(bin);
+    atomicAdd(&s.weight[0][bin], (uint32_t)v & 0x7FFFu);
+    atomicAdd(&s.weight[1][bin], (uint32_t)(v >> 15) & 0x7FFFu);
+    atomicAdd(&s.weight[2][bin], (uint32_t)(v >> 30));
+  }
+
+  // The cut among the tokens in(x, token), `n` of the cluster: the one that brings the sum
+  // of their number (MASS: weight) to the target.
+  template <bool MASS, typename F>
+  __device__ __forceinline__ void cut_among(uint32_t n, uint64_t target, F in) {
+    if (n <= SMP_FEW) {
+      rank_few<MASS>(target, in);
+      return;
+    }
+    uint64_t lo = ~(uint64_t)0, hi = 0;
+    each_left([&](float x, int token) {
+      if (in(x, token)) {
+        const uint64_t p = pair_of(x, token);
+        lo = min(lo, p), hi = max(hi, p);
+      }
+    });
+    warp_bounds(lo, hi);
+    if (lane == 0) mine().lo[warp] = lo, mine().hi[warp] = hi;
+    meet();
+    lo = ~(uint64_t)0, hi = 0;
+    for (int i = lane; i < ctas * SMP_WARPS; i += 32) {
+      const auto& o = theirs(i / SMP_WARPS);
+      lo = min(lo, o.lo[i % SMP_WARPS]), hi = max(hi, o.hi[i % SMP_WARPS]);
+    }
+    warp_bounds(lo, hi);
+    ++turn;
+    for (int level = 0; level < 9; ++level) {  // (each takes eight bits or more off 64)
+      const int shift = max(0, (MASS && !solo ? 56 : 54) - __clzll((long long)(hi - lo)));
+      const auto inside = [&](float x, int token) {
+        const uint64_t p = pair_of(x, token);
+        return p >= lo && p <= hi;
+      };
+      clear_ranges(true);
+      each_left([&](float x, int token) {
+        if (!inside(x, token)) return;
+        add_to_range((int)((hi - pair_of(x, token)) >> shift), MASS ? steps_of(x) : 0);
+      });
+      meet();
+      const Border b = find_border<MASS>(target);
+      if (!b.found) {  // (weights that rounding makes a step too small: to the end of these)
+        cut.set(lo);
         return;
       }
-      if (shift < 0) {  // the pairs that the range holds
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
-          most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-        }
-        if (lane == 0) s.wmin[warp] = least, s.wmax[warp] = most;
-        __syncthreads();
-        if (tid == 0) {
-          for (int i = 1; i < SMP_WARPS; ++i) least = min(least, s.wmin[i]), most = max(most, s.wmax[i]);
-          mine().lo = least, mine().hi = most;
-        }
-        meet();
-        lo = ~0ull, hi = 0;
-        for (int r = 0; r < ctas; ++r) lo = min(lo, theirs(r).lo), hi = max(hi, theirs(r).hi);
-        next();
-      } else {
-        const uint64_t top = hi - ((uint64_t)b.bin << shift);
-        const uint64_t bottom = top - (((uint64_t)1 << shift) - 1);
-        lo = bottom > lo ? bottom : lo;
-        hi = top;
+      target -= b.before;
+      hi -= (uint64_t)b.bin << shift;
+      const uint64_t bottom = hi - (((uint64_t)1 << shift) - 1);
+      lo = bottom > lo ? bottom : lo;
+      if (b.n <= SMP_FEW) {
+        rank_few<MASS>(target, inside);
+        return;
       }
-      shift = max(0, 64 - __clzll((long long)(hi - lo)) - 10);
+    }
+  }
+  static __device__ __forceinline__ void warp_bounds(uint64_t& lo, uint64_t& hi) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
   }
 
-  // The cluster's candidates, at most SMP_FEW, ranked by CTA 0: the cut is the one that
-  // brings the sum to the target.
-  __device__ __forceinline__ void rank_few(bool by_mass, uint64_t target) {
+  // ... which every CTA ranks for itself
+  template <bool MASS, typename F>
+  __device__ __forceinline__ void rank_few(uint64_t target, F in) {
+    __syncthreads();
+    if (tid == 0) s.n_cand = 0, s.cut = 0;
+    __syncthreads();
+    each_left([&](float x, int token) {
+      if (!in(x, token)) return;
+      const uint32_t i = atomicAdd(&s.n_cand, 1u);
+      if (PCED_IN_BOUNDS(i < SMP_FEW, a.status))
+        s.candidates(0)[i] = pair_of(x, token), s.candidates(1)[i] = MASS ? steps_of(x) : 1;
+    });
+    cut.set(rank_candidates(target));
+  }
+  // Of the cluster's candidates the one that brings the sum of their weights to the target.
+  __device__ __forceinline__ uint64_t rank_candidates(uint64_t target) {
     __syncthreads();
     if (tid == 0) mine().count = s.n_cand;
     meet();
-    if (rank == 0) {
-      int total = s.n_cand;
-      for (int r = 1; r < ctas; ++r) {
-        const SampleShared& o = *cluster.map_shared_rank(&s, r);
-        const int k = theirs(r).count;
-        for (int i = tid; i < k; i += SMP_THREADS)
-          if (PCED_IN_BOUNDS(total + i < SMP_FEW, a.status)) s.cand[total + i] = o.cand[i], s.cand_w[total + i] = o.cand_w[i];
-        total += k;
-      }
-      if (tid == 0) mine().cut = cut;
-      __syncthreads();
-      if (tid < total) {
-        const uint64_t own = s.cand[tid], ow = by_mass ? s.cand_w[tid] : 1;
-        uint64_t before = 0;
-        for (int i = 0; i < total; ++i)
-          if (s.cand[i] > own) before += by_mass ? s.cand_w[i] : 1;
-        if (before < target && before + ow >= target) mine().cut = own;
-      }
-      __syncthreads();
+    // the candidates of all CTAs, two warps for each
+    uint64_t *pairs = s.candidates(2), *weights = s.candidates(3);
+    const int their_n = lane < ctas ? (int)theirs(lane).count : 0;
+    int to = their_n;
+#pragma unroll
+    for (int o = 1; o < ROW_CLUSTER; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, to, o);
+      if (lane >= o) to += y;
     }
-    next();
-    if (rank == 0 && tid == 0) mine().cut = s.told[(turn - 1) & 1].cut;
-    meet();
-    cut = theirs(0).cut;
-    next();
+    const int total = __shfl_sync(0xffffffffu, to, ROW_CLUSTER - 1);
+    const int r = warp / 2, n = __shfl_sync(0xffffffffu, their_n, r), base = __shfl_sync(0xffffffffu, to, r) - n;
+    if (r < ctas) {
+      SampleShared& o = *cluster.map_shared_rank(&s, r);
+      for (int i = tid & 63; i < n; i += 64)
+        if (PCED_IN_BOUNDS(base + i < SMP_FEW, a.status))
+          pairs[base + i] = o.candidates(0)[i], weights[base + i] = o.candidates(1)[i];
+    }
+    ++turn;
+    __syncthreads();
+    if (tid < total) {
+      const uint64_t own = pairs[tid], ow = weights[tid];
+      uint64_t before = 0, last = ~(uint64_t)0;
+#pragma unroll 4
+      for (int i = 0; i < total; ++i) {
+        if (pairs[i] > own) before += weights[i];
+        last = min(last, pairs[i]);
+      }
+      // (the last one also where rounding left the sum a step short)
+      if (before < target && (before + ow >= target || own == last)) s.cut = own;
+    }
+    __syncthreads();
+    return s.cut;
   }
+
+  // The first k tokens.
+  __device__ __forceinline__ void keep_top(int k) {
+    // At least k tokens lie from the k-th of the threads' largest logits on, so where k is below
+    // the threads' number, the ranges of those tell where to look.
+    if (k <= SMP_THREADS * ctas / 2) {
+      clear_ranges(false);
+      if (thread_max >= alive) count_in(coarse_of(thread_max));
+      meet();
+      const Border b = find_border<false>((uint64_t)k);
+      if (b.found) {
+        list(fmaxf(alive, coarse.below((int)b.bin)));
+        try_solo();
+        if (gone) return;
+      }
+    }
+    if (solo && solo <= SMP_FEW) {
+      if (solo > k) rank_few<false>((uint64_t)k, [](float, int) { return true; });
+      return;
+    }
+    clear_ranges(false);
+    each_left([&](float x, int) { count_in(coarse_of(x)); });
+    meet();
+    const Border b = find_border<false>((uint64_t)k);
+    if (!b.found) return;  // there are no more than k
+    if (!listed) list(fmaxf(alive, coarse.below((int)b.bin)));
+    cut_among<false>(b.n, k - b.before, [&](float x, int) { return coarse_of(x) == (int)b.bin; });
+  }
+
+  // The shortest first part of the kept tokens that holds `share` of their weight.
+  __device__ __forceinline__ void keep_share(double share) {
+    if (cut.x != -INFINITY) meet();  // (all have read the candidates of the top k, which lie in the ranges)
+    clear_ranges(true);
+    const uint64_t all = (cut.x == -INFINITY && !solo ? weigh_all<true>() : weigh_kept<true, false>()).all;
+    const double want = ceil(share * (double)all);
+    const uint64_t target = want < 1.0 ? 1 : (uint64_t)want;
+    // ranges that can hold the border: a range's weight lies between its number times the weights at its ends
+    const float goal = (float)want * (float)(1.0 / (double)((uint64_t)1 << SMP_UNIT));
+    int b_lo, b_hi;
+    {
+      uint32_t n[2];
+      uint64_t m[2];
+      gather_ranges<false>(n, m);
+      float up[2], down[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float b = (float)(2 * tid + j);
+        up[j] = n[j] * exp2f(ym - (b - 0.125f) * log2_range);
+        down[j] = n[j] * exp2f(ym - (b + 1.125f) * log2_range);
+      }
+      float tu = up[0] + up[1], td = down[0] + down[1];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const float y = __shfl_up_sync(0xffffffffu, tu, o), z = __shfl_up_sync(0xffffffffu, td, o);
+        if (lane >= o) tu += y, td += z;
+      }
+      __syncthreads();
+      if (lane == 31) s.fscan[warp] = make_float2(tu, td);
+      if (tid == 0) s.at[0] = s.at[1] = SMP_BINS;
+      __syncthreads();
+      const float2 ahead = lane < warp ? s.fscan[lane] : make_float2(0.f, 0.f);
+      tu += warp_sum(ahead.x), td += warp_sum(ahead.y);
+      // (sums in fp32 are off by less than 2^-14 of themselves)
+      constexpr float MORE = 1.f + 1.f / 8192, LESS = 1.f - 1.f / 8192;
+      if (tu * MORE >= goal) atomicMin(&s.at[0], (tu - up[1]) * MORE >= goal ? 2 * tid : 2 * tid + 1);
+      if (td * LESS >= goal) atomicMin(&s.at[1], (td - down[1]) * LESS >= goal ? 2 * tid : 2 * tid + 1);
+      __syncthreads();
+      b_lo = s.at[0], b_hi = min(s.at[1], SMP_BINS - 1);
+    }
+    meet();  // (all have read the ranges)
+    if (b_lo == SMP_BINS) return;  // all are kept
+    const float least = fmaxf(alive, coarse.below(b_hi));
+    if (!solo) {
+      if (!listed) list(least);
+      try_solo();
+      if (gone) return;
+    }
+    // weight before them, and theirs, in finer ranges
+    const int bins = solo ? SMP_BINS : SMP_FINE;
+    const int from = 16 * b_lo, to = b_hi == SMP_BINS - 1 ? INT32_MAX : 16 * (b_hi + 1);
+    Ranges fine;  // (a quarter of them where the cluster weighs)
+    fine.set(fminf(mx, mx - ((float)b_lo - 0.25f) / coarse.per),
+             fmaxf((float)(min(b_hi, SMP_BINS - 4) - b_lo) + 1.5f, 1.f) / coarse.per);
+    const Cut old = cut;
+    const auto inside = [&](float x, int token) {
+      const int v = coarse.sixteenths(x);
+      return v >= from && v < to && old.keeps(x, token);
+    };
+    const int fine_shift = solo ? 4 : 6;
+    const auto bin_of = [&](float x) { return min(max(fine.sixteenths(x), 0) >> fine_shift, bins - 1); };
+    clear_ranges(true);
+    uint64_t above = 0;
+    each_left([&](float x, int token) {
+      const int v = coarse.sixteenths(x);
+      if (v >= to || !old.keeps(x, token)) return;
+      const uint64_t m = steps_of(x);
+      if (v < from) above += m;
+      else add_to_range(bin_of(x), m);
+    });
+    above = sum_up(warp_sum64(above)).all;
+    const uint64_t rest = target > above ? target - above : 1;
+    const Border b = find_border<true>(rest);
+    if (!b.found) {  // (weights that rounding makes a step too small: to the end of these)
+      if (cut.x < least) cut.x = least, cut.token = INT32_MAX;
+      return;
+    }
+    cut_among<true>(b.n, rest - b.before, [&](float x, int token) { return inside(x, token) && bin_of(x) == (int)b.bin; });
+  }
+
+  // Tokens from m + `below` on.
+  __device__ __forceinline__ void keep_from(const double& below) {
+    __syncthreads();
+    if (tid == 0) s.threshold = __double2float_ru((double)mx + below);
+    __syncthreads();
+    const float x = s.threshold;
+    if (x > cut.x) {
+      cut.x = x, cut.token = INT32_MAX;
+      if (!solo) {
+        if (!listed && x > low) list(x);
+        try_solo();
+      }
+    }
+  }
+
+  // The token of this CTA's part up to which the kept weights sum to more than `left`, by groups.
+  __device__ __forceinline__ void draw(uint64_t left, int64_t row, float t, uint64_t total) {
+    // its group: each lane some of them in a row
+    const int each = (groups + 31) / 32;
+    uint64_t sum = 0;
+    for (int i = lane * each; i < min(groups, (lane + 1) * each); ++i) sum += s.group[i];
+    uint64_t to = prefix(sum);
+    const int who = __ffs(__ballot_sync(0xffffffffu, to > left)) - 1;
+    left -= __shfl_sync(0xffffffffu, to - sum, who);
+    int g = who * each;
+    while (left >= s.group[g]) left -= s.group[g++];
+    // a thread for each of its tokens
+    static_assert(SMP_GROUP == SMP_THREADS, "a thread for each token of a group");
+    const int token = first + g * SMP_GROUP + tid;
+    const float x = at(g * SMP_GROUP + tid);
+    const bool keep = x >= low && cut.keeps(x, token);
+    const uint64_t m = keep ? steps_of(x) : 0;
+    to = prefix(m);
+    if (lane == 31) s.wscan[warp] = to;
+    const uint32_t kept = __ballot_sync(0xffffffffu, keep);
+    if (lane == 0) s.wkept[warp] = kept;
+    __syncthreads();
+    to += warp_sum64(lane < warp ? s.wscan[lane] : 0);
+    const bool mine_ = keep && to > left && to - m <= left;
+    // (where rounding left the tokens' sum short of the group's: the last kept one)
+    const bool in_later_warps = __any_sync(0xffffffffu, lane > warp && lane < SMP_WARPS && s.wkept[lane & (SMP_WARPS - 1)]);
+    const bool last = !__syncthreads_or(mine_) && keep && !in_later_warps && !(kept >> lane >> 1);
+    if (mine_ || last) write(x, token, row, t, total);
+  }
+  // ... of the tokens that are left to this CTA: by ranges of tokens, then one by one
+  __device__ __forceinline__ void draw_solo(uint64_t left, int64_t row, float t, uint64_t total) {
+    const int shift = max(0, 22 - __clz(a.V));  // at most SMP_BINS ranges of at most SMP_FEW tokens
+    static_assert(SMP_BINS == 1 << 10 && SMP_MAX_V <= SMP_BINS * SMP_FEW, "see there");
+    clear_ranges(true);
+    if (tid == 0) s.n_cand = 0, s.cut = 0;
+    each_left([&](float x, int token) {
+      if (cut.keeps(x, token)) add_to_range(token >> shift, steps_of(x));
+    });
+    __syncthreads();
+    const Border b = find_border<true>(left + 1);
+    const int bin = b.bin;
+    each_left([&](float x, int token) {
+      if (token >> shift != bin || !cut.keeps(x, token)) return;
+      const uint32_t i = atomicAdd(&s.n_cand, 1u);
+      if (PCED_IN_BOUNDS(i < SMP_FEW, a.status))
+        s.candidates(0)[i] = (uint32_t)~token, s.candidates(1)[i] = steps_of(x);
+    });
+    const int token_drawn = (int)~(uint32_t)rank_candidates(left + 1 - b.before);
+    each_left([&](float x, int token) {
+      if (token == token_drawn) write(x, token, row, t, total);
+    });
+  }
+  __device__ __forceinline__ void write(float x, int token, int64_t row, float t, uint64_t total) const {
+    a.token[row] = token;
+    if (a.logprob) {
+      // the largest weight is 2^ym of 2^SMP_UNIT steps; 32 bits serve a logarithm's own rounding
+      const float all = (float)total;
+      const float rest = (float)((int64_t)(total - (uint64_t)all)) / all;
+      const float log_all = logf(all * (1.f / (float)((uint64_t)1 << SMP_UNIT))) + rest;
+      a.logprob[row] = (mx == x ? 0.f : (x - mx) / t) - (log_all - ym * 0.693147181f);
+    }
+  }
+  __device__ __forceinline__ uint64_t prefix(uint64_t v) const {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    return v;
+  }
+  float thread_max;  // the largest logit that this thread loaded
 };
 
 template <typename T>
 __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  __shared__ SampleShared s;
+  __shared__ __align__(16) SampleShared s;
   cg::cluster_group cluster = cg::this_cluster();
+  constexpr int W = Words<T>::N;
   const int ctas = cluster.num_blocks(), rank = cluster.block_rank(), tid = threadIdx.x;
   const int64_t row = blockIdx.x / ctas;
-  Row<T> R = {a, s, cluster, nullptr, rank * a.per, 0, ctas, rank, tid, tid & 31, tid >> 5, 0, {}, 0};
-  R.n = max(0, min(a.per, a.V - R.first));
+  const int start = rank * a.per, n = max(0, min(a.per, a.V - start));  // this CTA's tokens
+  const T* src = (const T*)a.x + row * a.stride + start;
+  const int phase = (int)((uintptr_t)src / sizeof(T) % W);  // the row's offset in 16 bytes, kept in shared memory
+  const int groups = (phase + n + SMP_GROUP - 1) / SMP_GROUP;
+  Row<T> R = {a, s, cluster, reinterpret_cast<uint4*>(smem_raw), start - phase, groups, ctas, rank, tid, tid & 31, tid >> 5, 0};
+  const Exp2Entry entry = kExp2Table[tid / 16];
   pdl_wait();
-  // ---- the row into shared memory, at the offset in 16 bytes that it has in memory
-  const T* src = (const T*)a.x + row * a.stride + R.first;
-  constexpr int W = 16 / sizeof(T);
-  const int phase = (int)((uintptr_t)src / sizeof(T) % W);
+  // ---- what the row asks for
+  const float t = a.temperature ? a.temperature[row] : 1.f, u = a.u[row];
+  const float p = a.top_p ? a.top_p[row] : 1.f, least = a.min_p ? a.min_p[row] : 0.f;
+  const int k = a.top_k ? a.top_k[row] : 0;
+  // ---- the row, its largest and smallest logit
   T* data = reinterpret_cast<T*>(smem_raw) + phase;
-  R.data = data;
   float mx = -INFINITY, mn = INFINITY;
   const auto take = [&](float x) {
     mx = fmaxf(mx, x);
     mn = x > -INFINITY ? fminf(mn, x) : mn;
   };
-  const int head = min(R.n, (W - phase) % W), words = (R.n - head) / W;
   {
+    const int head = min(n, (W - phase) % W), words = (n - head) / W;
     const uint4* from = reinterpret_cast<const uint4*>(src + head);
     uint4* to = reinterpret_cast<uint4*>(data + head);
     constexpr int BATCH = 8;
     for (int i0 = tid; i0 < words; i0 += BATCH * SMP_THREADS) {
       uint4 v[BATCH];
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k)
-        if (i0 + k * SMP_THREADS < words) v[k] = from[i0 + k * SMP_THREADS];
+      for (int j = 0; j < BATCH; ++j)
+        if (i0 + j * SMP_THREADS < words) v[j] = from[i0 + j * SMP_THREADS];
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k) {
-        if (i0 + k * SMP_THREADS >= words) break;
-        to[i0 + k * SMP_THREADS] = v[k];
-        const T* p = reinterpret_cast<const T*>(&v[k]);
+      for (int j = 0; j < BATCH; ++j) {
+        if (i0 + j * SMP_THREADS >= words) break;
+        to[i0 + j * SMP_THREADS] = v[j];
+        float x[W];
+        Words<T>::split(v[j], x);
 #pragma unroll
-        for (int e = 0; e < W; ++e) take(load_logit(p + e));
+        for (int e = 0; e < W; ++e) take(x[e]);
       }
     }
-    const int edges = head + (R.n - head) % W;
+    const int edges = head + (n - head) % W;
     for (int i = tid; i < edges; i += SMP_THREADS) {
       const int at = i < head ? i : head + words * W + i - head;
       data[at] = src[at];
-      take(load_logit(src + at));
+      take((float)src[at]);
     }
+    // (what is around it)
+    for (int i = tid; i < phase; i += SMP_THREADS) data[i - phase] = Words<T>::to(-INFINITY);
+    for (int i = n + tid; i < groups * SMP_GROUP - phase; i += SMP_THREADS) data[i] = Words<T>::to(-INFINITY);
   }
-  // ---- its largest and smallest logit
-  mx = warp_max(mx), mn = -warp_max(-mn);
-  if (R.lane == 0) s.fmax[R.warp] = mx, s.fmin[R.warp] = mn;
-  __syncthreads();
-  if (tid == 0) {
-    for (int i = 1; i < SMP_WARPS; ++i) mx = fmaxf(mx, s.fmax[i]), mn = fminf(mn, s.fmin[i]);
-    R.mine().mx = mx, R.mine().mn = mn;
+  // (the reciprocals come while the last loads are on their way)
+  const float held = fminf(fmaxf(t, 1e-37f), 1e30f), lh = 1.44269502f, ll = 1.92596303e-08f;
+  R.w.ch = __fdiv_rn(lh, held);
+  R.w.cl = __fdiv_rn(fmaf(-R.w.ch, held, lh) + ll, held);
+  const float inverse = held * 0.693147181f;
+  R.thread_max = mx + 0.f;
+  {
+    const int hi = __reduce_max_sync(0xffffffffu, ordered(mx + 0.f)), lo = __reduce_min_sync(0xffffffffu, ordered(mn + 0.f));
+    if (R.lane == 0) R.mine().mx[R.warp] = hi, R.mine().mn[R.warp] = lo;
+    cluster.barrier_arrive();
+    if (tid == SMP_THREADS - 1 && least > 0.f) s.below = (double)t * log((double)least);  // (takes a microsecond)
+    __syncwarp();
+    cluster.barrier_wait();
+    const int r = R.lane >> 2;  // a CTA's sixteen by four lanes
+    int4 x = make_int4(INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN), y = make_int4(INT32_MAX, INT32_MAX, INT32_MAX, INT32_MAX);
+    if (r < ctas) {
+      x = *reinterpret_cast<const int4*>(R.theirs(r).mx + 4 * (R.lane & 3));
+      y = *reinterpret_cast<const int4*>(R.theirs(r).mn + 4 * (R.lane & 3));
+    }
+    R.mx = mx = from_ordered(__reduce_max_sync(0xffffffffu, max(max(x.x, x.y), max(x.z, x.w))));
+    R.mn = mn = from_ordered(__reduce_min_sync(0xffffffffu, min(min(y.x, y.y), min(y.z, y.w))));
+    ++R.turn;
   }
-  R.meet();
-  for (int r = 0; r < ctas; ++r) mx = fmaxf(mx, R.theirs(r).mx), mn = fminf(mn, R.theirs(r).mn);
-  R.next();
-  mx += 0.f;
-  // ---- what the row asks for
-  const float t = a.temperature ? a.temperature[row] : 1.f, u = a.u[row];
-  const float p = a.top_p ? a.top_p[row] : 1.f, least = a.min_p ? a.min_p[row] : 0.f;
-  const int k = a.top_k ? a.top_k[row] : 0;
   const bool bad = !(t >= 0.f) || !(u >= 0.f && u <= 1.f) || p != p || least != least;
   if (bad || mx == -INFINITY) {  // a request out of range, or a row without a token
     if (rank == 0 && tid == 0) {
@@ -459,92 +977,39 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
   }
   if (t == 0.f || k == 1 || p <= 0.f || least > 1.f) {  // the first of the largest
     uint32_t at = UINT32_MAX;
-    for (int i = tid; i < R.n; i += SMP_THREADS)
-      if (R.logit(i) == mx) at = min(at, (uint32_t)i);
+    for (int g = R.warp; g < groups; g += SMP_WARPS)
+      R.each_of(g, [&](int, float x, int place) { at = x == mx ? min(at, (uint32_t)(R.first + place)) : at; });
     at = __reduce_min_sync(0xffffffffu, at);
-    if (R.lane == 0) s.wcount[R.warp] = at;
-    __syncthreads();
-    if (tid == 0) {
-      for (int i = 1; i < SMP_WARPS; ++i) at = min(at, s.wcount[i]);
-      R.mine().count = at == UINT32_MAX ? at : R.first + at;
-    }
-    R.meet();
-    if (rank == 0 && tid == 0) {
-      for (int r = 0; r < ctas; ++r) at = min(r == 0 ? UINT32_MAX : at, R.theirs(r).count);
-      a.token[row] = (int32_t)at;
-      if (a.logprob) a.logprob[row] = 0.f;
+    if (R.lane == 0) R.mine().sum[R.warp] = at;
+    cluster.sync();
+    if (rank == 0 && R.warp == 0) {
+      for (int i = R.lane; i < ctas * SMP_WARPS; i += 32) at = min(at, (uint32_t)R.theirs(i / SMP_WARPS).sum[i % SMP_WARPS]);
+      at = __reduce_min_sync(0xffffffffu, at);
+      if (R.lane == 0) {
+        a.token[row] = (int32_t)at;
+        if (a.logprob) a.logprob[row] = 0.f;
+      }
     }
     cluster.sync();
     return;
   }
-  R.w.set(mx, t, R.lane);
+  R.set_weights(inverse, entry);
   // ---- cuts
-  const float per_range = (float)(SMP_BINS - 1) / fminf(32.f * t, mx - mn);
-  if (k > 1 && k < a.V) R.search(false, (uint64_t)k, 0.0, per_range);
-  if (p < 1.f) R.search(true, 0, (double)p, per_range);
-  if (least > 0.f) {
-    if (tid == 0)
-      s.threshold = __double2float_ru((double)mx + (double)t * log((double)least));
-    __syncthreads();
-    const uint64_t from = (uint64_t)order_key(s.threshold + 0.f) << 32;
-    R.cut = from > R.cut ? from : R.cut;
+  if (k > 1 && k < a.V) R.keep_top(k);
+  if (!R.gone && p < 1.f) R.keep_share((double)p);
+  if (!R.gone && least > 0.f) R.keep_from(s.below);
+  if (R.gone) return;
+  // ---- the kept weights, and where u falls (both factors are exact)
+  const auto seek = [&](uint64_t total) { return min((uint64_t)((double)u * (double)total), total - 1); };
+  if (R.solo) {
+    const uint64_t total = R.template weigh_kept<false, false>().all;
+    R.draw_solo(seek(total), row, t, total);
+    return;
   }
-  // ---- the kept weights, and where u falls
-  const uint64_t own = R.weigh();
-  if (tid == 0) R.mine().mass = own;
-  R.meet();
-  uint64_t total = 0, before = 0;
-  for (int r = 0; r < ctas; ++r) {
-    const uint64_t m = R.theirs(r).mass;
-    total += m;
-    if (r < rank) before += m;
-  }
-  R.next();
-  if (R.warp == 0) {
-    // (both factors are exact, and total is below 2^63)
-    const uint64_t seek = min((uint64_t)((double)u * (double)total), total - 1);
-    if (seek >= before && seek < before + own) {
-      uint64_t left = seek - before;
-      // its tile: each lane some of them in a row
-      const int tiles = (R.n + SMP_TILE - 1) / SMP_TILE, each = (tiles + 31) / 32;
-      uint64_t sum = 0;
-      for (int i = R.lane * each; i < min(tiles, (R.lane + 1) * each); ++i) sum += s.tile_mass[i];
-      uint64_t to = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t y = __shfl_up_sync(0xffffffffu, to, o);
-        if (R.lane >= o) to += y;
-      }
-      const int who = __ffs(__ballot_sync(0xffffffffu, to > left)) - 1;
-      left -= __shfl_sync(0xffffffffu, to - sum, who);
-      int tile = who * each;
-      while (left >= s.tile_mass[tile]) left -= s.tile_mass[tile++];
-      // its token: 32 at a time
-      for (int e = 0; e < SMP_EACH; ++e) {
-        const int i = tile * SMP_TILE + e * 32 + R.lane;
-        const float x = R.logit(i);
-        const uint64_t v = R.w.of(x);
-        uint64_t run = R.keeps(x, i) ? v : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint64_t y = __shfl_up_sync(0xffffffffu, run, o);
-          if (R.lane >= o) run += y;
-        }
-        const uint32_t past = __ballot_sync(0xffffffffu, run > left);
-        if (past) {
-          if (R.lane == __ffs(past) - 1) {
-            a.token[row] = R.first + i;
-            if (a.logprob) {
-              const double z = x == mx ? 0.0 : ((double)x - (double)mx) / (double)t;
-              a.logprob[row] = (float)(z - log((double)total * (1.0 / (double)SMP_ONE)));
-            }
-          }
-          break;
-        }
-        left -= __shfl_sync(0xffffffffu, run, 31);
-      }
-    }
-  }
+  const typename Row<T>::Sums sums =
+      R.cut.x == -INFINITY ? R.template weigh_all<false>() : R.template weigh_kept<false, true>();
+  const uint64_t left = seek(sums.all);
+  if (left >= sums.before && left < sums.before + sums.own) R.draw(left - sums.before, row, t, sums.all);
   cluster.sync();  // (a CTA's memory stays until the others have read it)
 }
 
@@ -557,7 +1022,8 @@ template <typename T>
 static cudaError_t launch_sample(SampleArgs a, int32_t rows, cudaStream_t stream) {
   static bool done[64];
   const auto kernel = sample_kernel<T>;
-  cudaError_t e = allow_smem(kernel, SMP_MAX_BYTES + 16, done);
+  constexpr size_t AROUND = (SMP_GROUP + Words<T>::N) * sizeof(T);  // places before and behind a part
+  cudaError_t e = allow_smem(kernel, SMP_MAX_BYTES + AROUND, done);
   if (e != cudaSuccess) return e;
   const auto part = [&](int ctas) { return ((int64_t)a.V + ctas - 1) / ctas; };
   int ctas = 1;
@@ -567,7 +1033,7 @@ static cudaError_t launch_sample(SampleArgs a, int32_t rows, cudaStream_t stream
   while (ctas < ROW_CLUSTER && (part(ctas) > HALF || (2 * ctas * (int64_t)rows <= 2 * num_sms() && part(ctas) > FEW)))
     ctas *= 2;
   a.per = (int32_t)part(ctas);
-  const size_t smem = align_up((size_t)a.per * sizeof(T) + 16, 16);
+  const size_t smem = align_up((size_t)a.per * sizeof(T) + AROUND, 16);
   return launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, smem, stream, true, a);
 }
 
