@@ -11,12 +11,14 @@
 // in some thousands gets another token than in 64 bits.  So weights are exact to about
 // 2^-32 of themselves, and are added without further loss (see Sum).
 //
-// A cluster of CTAs holds a row in shared memory, read once.  A cut is found by counting
-// the tokens in equal ranges of x below m.  For the top k the range that brings the count to
-// k is then ranked token by token; for the top p the counts bound the weights, so
-// that a few ranges are left, whose tokens are weighed in finer ones, of which one is ranked.
-// Ranges with too many tokens (of equal logits, say) are split by (logit, token) pairs as
-// 64-bit numbers, again and again: pairs are distinct, so that ends.
+// A cluster of CTAs (one, where there are many rows) reads a row up to four times, from L2
+// after the first: for its largest logit, for its weights, for the list of the tokens that a
+// cut can leave.  A cut is found by counting the tokens in equal ranges of x below m.  For the
+// top k the range that brings the count to k is then ranked token by token; for the top p
+// the counts bound the weights, so that a few ranges are left, whose tokens are weighed in
+// finer ones, of which one is ranked.  Ranges with too many tokens (of equal logits, say) are
+// split by (logit, token) pairs as 64-bit numbers, again and again: pairs are distinct, so
+// that ends.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -28,7 +30,8 @@ namespace cg = cooperative_groups;
 struct SampleArgs {
   const void* x;
   int64_t stride;
-  int32_t V, per;  // tokens; of a CTA of the row's cluster
+  int32_t V, per;    // tokens; of a CTA of the row's cluster
+  int32_t list_cap;  // tokens that a CTA's list takes
   const float* u;
   const float* temperature;
   const int32_t* top_k;
@@ -46,11 +49,10 @@ constexpr int SMP_FEW = 512;          // tokens of a range that are ranked one b
 constexpr int SMP_EACH = 16;          // tokens of a lane in a group, whose weight is kept
 constexpr int SMP_GROUP = 32 * SMP_EACH;
 constexpr int SMP_FINE = 256;         // ranges that a cluster weighs (what its CTAs read of one another is slow)
-constexpr int SMP_LIST = 1536;        // tokens of a CTA that are worth a list
-constexpr int SMP_SOLO = 4096;        // ... of a row that one CTA goes on with alone
-constexpr int SMP_MAX_V = 393216;     // (what a cluster's shared memory holds)
-constexpr int SMP_MAX_BYTES = 192 * 1024;  // of a CTA's part of a row
-constexpr int SMP_MAX_GROUPS = SMP_MAX_BYTES / 2 / SMP_GROUP + 1;
+constexpr int SMP_LIST = 9216;        // tokens that a CTA's list takes (two CTAs an SM)
+constexpr int SMP_SOLO = 4096;        // tokens of a row that one CTA goes on with alone
+constexpr int SMP_MAX_V = 393216;     // (sets the groups)
+constexpr int SMP_MAX_GROUPS = SMP_MAX_V / SMP_GROUP + 1;
 constexpr int SMP_UNIT = 42;          // weights are counted in steps of 2^-42
 constexpr float SMP_ALIVE = 44.f;     // -log2 of weights that no cut asks about
 constexpr float SMP_LOWEST = 100.f;   // ... and that are nothing
@@ -153,7 +155,6 @@ struct Words<float> {
   static __device__ __forceinline__ void split(uint4 v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
   }
-  static __device__ __forceinline__ float to(float x) { return x; }
 };
 template <>
 struct Words<__nv_bfloat16> {
@@ -162,12 +163,11 @@ struct Words<__nv_bfloat16> {
     x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
     x[4] = bf16_lo(v.z), x[5] = bf16_hi(v.z), x[6] = bf16_lo(v.w), x[7] = bf16_hi(v.w);
   }
-  static __device__ __forceinline__ __nv_bfloat16 to(float x) { return __float2bfloat16_rn(x); }
 };
 
-// Equal ranges of x, in sixteenths: the float `magic` + 16ths has them in its low bits.
+// Equal ranges of x, in 64ths: the float MAGIC + 64ths has them in its low bits.
 struct Ranges {
-  static constexpr float MAGIC = 524288.f;  // 2^19
+  static constexpr float MAGIC = 131072.f;  // 2^17
   float top, per;                           // the first one's upper end; ranges of a unit of x
   __device__ __forceinline__ void set(float top_, float width) {  // SMP_BINS - 4 ranges from top down
     top = top_;
@@ -177,8 +177,9 @@ struct Ranges {
   __device__ __forceinline__ float below(int bin) const {
     return bin >= SMP_BINS - 4 ? -INFINITY : top - ((float)bin + 1.25f) / per;
   }
-  __device__ __forceinline__ int sixteenths(float x) const {
-    return __float_as_int(fmaf(top - x, per, MAGIC + 1.f / 16)) - __float_as_int(MAGIC);
+  // (1 + 64 (top - x) per, rounded)
+  __device__ __forceinline__ int place(float x) const {
+    return __float_as_int(fmaf(top - x, per, MAGIC + 1.f / 64)) - __float_as_int(MAGIC);
   }
 };
 
@@ -191,13 +192,13 @@ struct Border {
 
 struct SampleShared {
   float2 table[32][16];
-  uint32_t count[SMP_BINS / 2];  // tokens of a range, 16 bits each
+  uint32_t count[SMP_BINS];      // tokens of a range (16 bits each where a part has no more)
   uint32_t weight[3][SMP_BINS];  // their weights, 15 bits each
   uint64_t cand[SMP_FEW];
   uint64_t group[SMP_MAX_GROUPS];  // kept weight (on its way in two numbers, 21 bits in the first)
-  uint16_t list[SMP_LIST];       // places of the tokens that matter
+  float2 queue[SMP_WARPS][64];     // tokens on their way to a whole warp
   uint32_t n_list, n_cand;
-  int at[2];
+  int at[5];
   uint64_t wscan[SMP_WARPS];
   uint32_t wkept[SMP_WARPS];
   float2 fscan[SMP_WARPS];
@@ -232,12 +233,16 @@ struct Row {
   const SampleArgs& a;
   SampleShared& s;
   cg::cluster_group cluster;
-  uint4* data;                         // this CTA's part of the row, from 16 bytes of the row on, -inf around it
-  int first, groups;                   // token of its first place
+  const uint4* data;                   // this CTA's part of the row, from an address of 16 bytes on
+  float2* left;                        // the list: (logit, token)
+  int phase, n;                        // the part's places are phase ... phase + n - 1
+  int first, groups;                   // token of place 0
   int ctas, rank, tid, lane, warp, turn;
   float mx, mn;                        // of the row
   Weight w;
-  float ym;                            // log2 of the largest weight
+  float origin;                        // see moved()
+  bool back;                           // see each_group()
+  float whole, ym;                     // N; log2 of the largest weight
   float alive;                         // smaller logits have weights that no cut asks about
   Ranges coarse;
   float log2_range;                    // log2 of weights at a range's ends, the difference
@@ -246,101 +251,127 @@ struct Row {
   bool listed;                         // the others' places are in the list (each CTA's own matter, as is `low`)
   int solo;                            // > 0: so many tokens are left, and this CTA, which has them, alone
   bool gone;                           // ... another CTA
+  bool grouped;                        // the groups' kept weight is known; the list has a part of the tokens only
 
   __device__ __forceinline__ typename SampleShared::Told& mine() { return s.told[turn & 1]; }
   __device__ __forceinline__ const typename SampleShared::Told& theirs(int r) {
     return cluster.map_shared_rank(&s, r)->told[turn & 1];
   }
-  __device__ __forceinline__ float at(int place) const { return (float)reinterpret_cast<const T*>(data)[place]; }
-
-  // f(e, logit, place) for the SMP_EACH places of a lane in group g
+  // A logit as it counts.  Where |m| / t is very large, logits are taken as differences from m:
+  // those that count lie so near to it that they are exact.  (A row with +inf is 0 there
+  // and -inf elsewhere.)
+  __device__ __forceinline__ float moved(float x) const {
+    if (origin != 0.f) x = origin == INFINITY ? (x == origin ? 0.f : -INFINITY) : x - origin;
+    return x;
+  }
+  __device__ __forceinline__ float at(int place) const {
+    if (place < phase || place >= phase + n) return -INFINITY;
+    return moved((float)reinterpret_cast<const T*>(data)[place]);
+  }
+  // f(e, logit, place) for the SMP_EACH places of a lane in group g (-inf around the part)
   template <typename F>
   __device__ __forceinline__ void each_of(int g, F f) const {
+    float x[TILES][W];
+    const int v0 = g * TILES * 32 + lane;
+    if (g * SMP_GROUP >= phase && (g + 1) * SMP_GROUP <= phase + n) {
+      uint4 w[TILES];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      const int v = (g * TILES + t) * 32 + lane;
-      float x[W];
-      Words<T>::split(data[v], x);
+      for (int t = 0; t < TILES; ++t) w[t] = data[v0 + t * 32];
 #pragma unroll
-      for (int e = 0; e < W; ++e) f(t * W + e, x[e], v * W + e);
+      for (int t = 0; t < TILES; ++t) Words<T>::split(w[t], x[t]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const int place = (v0 + t * 32) * W;
+        if (place >= phase && place + W <= phase + n) {
+          Words<T>::split(data[v0 + t * 32], x[t]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < W; ++e)
+            x[t][e] = place + e >= phase && place + e < phase + n ? (float)reinterpret_cast<const T*>(data)[place + e] : -INFINITY;
+        }
+      }
     }
+    if (origin != 0.f) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < W; ++e) x[t][e] = moved(x[t][e]);
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int e = 0; e < W; ++e) f(t * W + e, x[t][e], (v0 + t * 32) * W + e);
+  }
+  // f(group) for the warp's groups, every time the other way round: what was read last is
+  // what L2 still has
+  template <typename F>
+  __device__ __forceinline__ void each_group(F f) {
+    back = !back;
+    for (int i = warp; i < groups; i += SMP_WARPS) f(back ? groups - 1 - i : i);
   }
   // A barrier of the CTAs that still work on the row.
   __device__ __forceinline__ void meet() {
     if (solo) __syncthreads();
     else cluster.sync();
   }
-  // f(logit, token) for the tokens that `low` leaves
+  // f(logit, token) for the tokens that `low` leaves, a lane each
   template <typename F>
-  __device__ __forceinline__ void each_left(F f) const {
+  __device__ __forceinline__ void each_left(F f) {
     if (listed) {
-      const int n = solo ? solo : (int)s.n_list;
-      const float2* left = reinterpret_cast<const float2*>(data);
-      for (int i = tid; i < n; i += SMP_THREADS) {
-        if (solo) {
-          f(left[i].x, __float_as_int(left[i].y));
-        } else {
-          const int place = s.list[i];
-          f(at(place), first + place);
-        }
-      }
+      const int k = solo ? solo : (int)s.n_list;
+      for (int i = tid; i < k; i += SMP_THREADS) f(left[i].x, __float_as_int(left[i].y));
       return;
     }
-    for (int g = warp; g < groups; g += SMP_WARPS) {
+    float2* const q = s.queue[warp];
+    int held = 0;
+    each_group([&](int g) {
       uint32_t take = 0;
       each_of(g, [&](int e, float x, int) { take |= (uint32_t)(x >= low) << e; });
-      if (__any_sync(0xffffffffu, take))
-        each_of(g, [&](int e, float x, int place) {
-          if (take >> e & 1u) f(x, first + place);
-        });
-    }
+      if (!__any_sync(0xffffffffu, take)) return;
+      each_of(g, [&](int e, float x, int place) {
+        const bool k = take >> e & 1u;
+        const uint32_t who = __ballot_sync(0xffffffffu, k);
+        if (!who) return;
+        if (k) q[held + __popc(who & ((1u << lane) - 1))] = make_float2(x, __int_as_float(first + place));
+        held += __popc(who);
+        if (held < 32) return;
+        held -= 32;  // (the last ones first)
+        __syncwarp();
+        const float2 y = q[held + lane];
+        __syncwarp();
+        f(y.x, __float_as_int(y.y));
+      });
+    });
+    __syncwarp();
+    if (lane < held) f(q[lane].x, __float_as_int(q[lane].y));
+    __syncwarp();
   }
   // Where few tokens are left, CTA 0 takes them all (logit, token) and goes on alone: a barrier of
   // a cluster takes half a microsecond, and what its CTAs read of one another 10 bytes a clock.
   __device__ __forceinline__ void try_solo() {
-    if (ctas == 1) return;
+    if (ctas == 1) {
+      if (listed) solo = s.n_list;
+      return;
+    }
     if (tid == 0) mine().count = listed ? s.n_list : SMP_SOLO + 1;
     cluster.sync();
-    const int n = lane < ctas ? (int)theirs(lane).count : 0;
+    const int k = lane < ctas ? (int)theirs(lane).count : 0;
     ++turn;
-    int to = n;
+    int to = k;
 #pragma unroll
     for (int o = 1; o < ROW_CLUSTER; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, to, o);
       if (lane >= o) to += y;
     }
     const int total = __shfl_sync(0xffffffffu, to, ROW_CLUSTER - 1);
-    if (total > SMP_SOLO || total * 8 > a.per * (int)sizeof(T)) return;
+    if (total > SMP_SOLO || total > a.list_cap) return;
     gone = rank != 0;
-    if (rank == 0) {
-      // (its own first, as the others' come where its part of the row was)
-      const int own = __shfl_sync(0xffffffffu, n, 0);
-      float2 x[SMP_LIST / SMP_THREADS];
-#pragma unroll
-      for (int j = 0; j < SMP_LIST / SMP_THREADS; ++j) {
-        const int i = tid + j * SMP_THREADS;
-        if (i < own) x[j] = make_float2(at(s.list[i]), __int_as_float(first + s.list[i]));
-      }
-      __syncthreads();
-      float2* left = reinterpret_cast<float2*>(data);
-#pragma unroll
-      for (int j = 0; j < SMP_LIST / SMP_THREADS; ++j) {
-        const int i = tid + j * SMP_THREADS;
-        if (i < own) left[i] = x[j];
-      }
-      // two warps for each CTA
-      const int r = warp / 2, their_n = __shfl_sync(0xffffffffu, n, r), base = __shfl_sync(0xffffffffu, to, r) - their_n;
-      if (r > 0 && r < ctas) {
-        const SampleShared& o = *cluster.map_shared_rank(&s, r);
-        const T* part = reinterpret_cast<const T*>(cluster.map_shared_rank(data, r));
-        const int64_t from = (int64_t)r * a.per;
-        const T* src = (const T*)a.x + (int64_t)(blockIdx.x / ctas) * a.stride + from;
-        const int phase = (int)((uintptr_t)src / sizeof(T) % W);
-        for (int i = tid & 63; i < their_n; i += 64) {
-          const int place = o.list[i];
-          left[base + i] = make_float2((float)part[place], __int_as_float((int)from - phase + place));
-        }
-      }
+    // two warps for each CTA
+    const int r = warp / 2, their_n = __shfl_sync(0xffffffffu, k, r), base = __shfl_sync(0xffffffffu, to, r) - their_n;
+    if (rank == 0 && r > 0 && r < ctas) {
+      const float2* theirs_ = cluster.map_shared_rank(left, r);
+      for (int i = tid & 63; i < their_n; i += 64) left[base + i] = theirs_[i];
     }
     cluster.sync();  // (CTA 0 has read the others' memory)
     if (rank == 0) {
@@ -348,19 +379,19 @@ struct Row {
       solo = total;
     }
   }
-  // The places of the tokens from `low_` on, where they are few enough.
+  // The list of the tokens from `low_` on, where they are few enough.
   __device__ __forceinline__ void list(float low_) {
     low = low_;
     listed = false;
     __syncthreads();
     if (tid == 0) s.n_list = 0;
     __syncthreads();
-    for (int g = warp; g < groups; g += SMP_WARPS) {
+    each_group([&](int g) {
       uint32_t take = 0;
       each_of(g, [&](int e, float x, int) { take |= (uint32_t)(x >= low) << e; });
-      if (!__any_sync(0xffffffffu, take)) continue;
-      const int n = __popc(take);
-      int to = n;
+      if (!__any_sync(0xffffffffu, take)) return;
+      const int k = __popc(take);
+      int to = k;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, to, o);
@@ -368,28 +399,21 @@ struct Row {
       }
       int base = 0;
       if (lane == 31) base = (int)atomicAdd(&s.n_list, (uint32_t)to);
-      base = __shfl_sync(0xffffffffu, base, 31) + to - n;
-      each_of(g, [&](int e, float, int place) {
-        if ((take >> e & 1u) && base < SMP_LIST) s.list[base] = (uint16_t)place;
+      base = __shfl_sync(0xffffffffu, base, 31) + to - k;
+      each_of(g, [&](int e, float x, int place) {
+        if ((take >> e & 1u) && base < a.list_cap) left[base] = make_float2(x, __int_as_float(first + place));
         base += take >> e & 1u;
       });
-    }
+    });
     __syncthreads();
-    listed = s.n_list <= SMP_LIST;
+    listed = s.n_list <= a.list_cap;
   }
 
-  // m, N and the table for temperature t.  Where |m| / t is very large, the logits are first
-  // made differences from m: those that count lie so near to it that they are exact.  (A row
-  // with +inf becomes 0 at those and -inf elsewhere.)  inverse: 1 / w.ch, entry: of the table
+  // m, N and the table for temperature t (inverse: 1 / w.ch, entry: of the table)
   __device__ __forceinline__ void set_weights(float inverse, Exp2Entry entry) {
     if (!(fabsf(mx) * w.ch <= 8192.f)) {
-      __syncthreads();
-      T* p = reinterpret_cast<T*>(data);
-      for (int i = tid; i < groups * SMP_GROUP; i += SMP_THREADS) {
-        const float x = (float)p[i];
-        p[i] = Words<T>::to(mx == INFINITY ? (x == mx ? 0.f : -INFINITY) : x - mx);
-      }
-      thread_max = (float)Words<T>::to(mx == INFINITY ? (thread_max == mx ? 0.f : -INFINITY) : thread_max - mx);
+      origin = mx;
+      thread_max = moved(thread_max);
       mn = mx == INFINITY ? 0.f : fmaxf(mn - mx, -3e38f);
       mx = 0.f;
     }
@@ -398,7 +422,7 @@ struct Row {
     w.floor = (top - SMP_LOWEST) * inverse;
     alive = (top - SMP_ALIVE) * inverse;
     low = alive;
-    listed = gone = false;
+    listed = gone = grouped = false;
     solo = 0;
     w.table = &s.table[0][lane & 15];
     const uint32_t j = tid / 16;
@@ -407,6 +431,7 @@ struct Row {
     const float width = fminf((SMP_ALIVE + 1.f) * inverse, fmaxf(mx - mn, 1e-30f));
     coarse.set(mx, width);
     log2_range = w.ch * width * (1.f / (SMP_BINS - 4));
+    whole = top;
     __syncthreads();
   }
 
@@ -439,93 +464,123 @@ struct Row {
     return z;
   }
 
-  // Weight of all tokens; the coarse ranges' numbers of them too.
+  // Weight of all tokens; COUNT: those from `from` on in the coarse ranges too
   template <bool COUNT>
-  __device__ __forceinline__ Sums weigh_all() {
+  __device__ __forceinline__ Sums weigh_all(float from) {
     uint64_t total = 0;
-    for (int g = warp; g < groups; g += SMP_WARPS) {
+    each_group([&](int g) {
       Sum sum;
       each_of(g, [&](int, float x, int) {
         float b, c;
         w.of(x, b, c);
         sum.add(b, c);
-        if (COUNT && x >= alive) count_in(coarse_of(x));
+        if (COUNT && x >= from) count_place(x);
       });
       const uint64_t v = sum.warp_steps();
       if (lane == 0) s.group[g] = v;
       total += v;
-    }
+    });
     return sum_up(total);
   }
-  // ... of the kept ones among those that `low` leaves; GROUPS: by groups too
-  template <bool COUNT, bool GROUPS>
+  // ... of the kept ones among those that `low` leaves; COUNT: all of them in the coarse ranges too
+  template <bool COUNT>
   __device__ __forceinline__ Sums weigh_kept() {
     __syncthreads();
-    if (GROUPS) {
-      for (int g = tid; g < groups; g += SMP_THREADS) s.group[g] = 0;
-      __syncthreads();
-    }
-    uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
     uint64_t total = 0;
     each_left([&](float x, int token) {
       if (!cut.keeps(x, token)) return;
-      const uint64_t v = steps_of(x);
-      if (GROUPS) {
+      total += steps_of(x);
+      if (COUNT) count_place(x);
+    });
+    return sum_up(warp_sum64(total));
+  }
+  // ... by groups
+  __device__ __forceinline__ Sums weigh_groups() {
+    uint64_t total = 0;
+    __syncthreads();
+    if (listed) {
+      for (int g = tid; g < groups; g += SMP_THREADS) s.group[g] = 0;
+      __syncthreads();
+      uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
+      each_left([&](float x, int token) {
+        if (!cut.keeps(x, token)) return;
+        const uint64_t v = steps_of(x);
         const int g = (token - first) / SMP_GROUP;
         atomicAdd(part + 2 * g, (uint32_t)v & 0x1FFFFFu);
         atomicAdd(part + 2 * g + 1, (uint32_t)(v >> 21));
-      } else {
-        total += v;
-      }
-      if (COUNT) count_in(coarse_of(x));
-    });
-    if (GROUPS) {
+      });
       __syncthreads();
       for (int g = tid; g < groups; g += SMP_THREADS) {
         const uint64_t v = part[2 * g] + ((uint64_t)part[2 * g + 1] << 21);
         s.group[g] = v;
         total += v;
       }
+      total = warp_sum64(total);
+    } else {
+      each_group([&](int g) {
+        Sum sum;
+        bool some = false;
+        each_of(g, [&](int, float x, int place) {
+          const bool k = x >= low && cut.keeps(x, first + place);
+          if (!__any_sync(0xffffffffu, k)) return;
+          some = true;
+          float b, c;
+          w.of(x, b, c);
+          sum.add(k ? b : 0.f, c);
+        });
+        const uint64_t v = some ? sum.warp_steps() : 0;
+        if (lane == 0) s.group[g] = v;
+        total += v;
+      });
     }
-    return sum_up(warp_sum64(total));
+    return sum_up(total);
   }
-  __device__ __forceinline__ int coarse_of(float x) const { return min(coarse.sixteenths(x) >> 4, SMP_BINS - 1); }
-  __device__ __forceinline__ void count_in(int bin) { atomicAdd(&s.count[bin >> 1], 1u << (16 * (bin & 1))); }
+  __device__ __forceinline__ int coarse_of(float x) const { return min(coarse.place(x) >> 6, SMP_BINS - 1); }
+  // ... with its place in the range
+  __device__ __forceinline__ void count_place(float x) {
+    const int v = coarse.place(x), bin = min(v >> 6, SMP_BINS - 1);
+    count_in(bin);
+    atomicAdd(&s.weight[0][bin], (uint32_t)v & 63u);
+  }
+  __device__ __forceinline__ bool wide() const { return a.per > 0xFFFF; }
+  __device__ __forceinline__ void count_in(int bin) {
+    if (wide()) atomicAdd(&s.count[bin], 1u);
+    else atomicAdd(&s.count[bin >> 1], 1u << (16 * (bin & 1)));
+  }
   static __device__ __forceinline__ uint64_t warp_sum64(uint64_t v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   }
 
-  // Two ranges' tokens (and weights) of the cluster, each thread its own.
-  template <bool MASS>
+  // Two ranges' tokens of the cluster, each thread its own; PARTS 3: and weights, 1: and the sum of their places.
+  template <int PARTS>
   __device__ __forceinline__ void gather_ranges(uint32_t (&n)[2], uint64_t (&m)[2]) {
     static_assert(SMP_BINS == 2 * SMP_THREADS && ROW_CLUSTER == 8, "two ranges a thread");
     n[0] = n[1] = 0;
     m[0] = m[1] = 0;
-    if (MASS && !solo && 2 * tid >= SMP_FINE) return;
-    constexpr int BATCH = MASS ? 2 : 8;  // CTAs whose loads are in flight
+    if (PARTS == 3 && !solo && 2 * tid >= SMP_FINE) return;
+    constexpr int BATCH = PARTS == 3 ? 2 : 4;  // CTAs whose loads are in flight
 #pragma unroll
     for (int r0 = 0; r0 < ROW_CLUSTER; r0 += BATCH) {
       if (r0 >= ctas) break;
-      uint32_t c[BATCH];
-      uint2 b[BATCH][3];
+      uint2 c[BATCH], b[BATCH][PARTS + 1];
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
-        c[k] = 0;
+        c[k] = make_uint2(0, 0);
         if (r0 + k >= ctas) continue;
         const SampleShared& o = *cluster.map_shared_rank(&s, r0 + k);
-        c[k] = o.count[tid];
-        if (MASS)
+        if (wide()) c[k] = *reinterpret_cast<const uint2*>(&o.count[2 * tid]);
+        else c[k].x = o.count[tid], c[k].y = c[k].x >> 16, c[k].x &= 0xFFFFu;
 #pragma unroll
-          for (int i = 0; i < 3; ++i) b[k][i] = *reinterpret_cast<const uint2*>(&o.weight[i][2 * tid]);
+          for (int i = 0; i < PARTS; ++i) b[k][i] = *reinterpret_cast<const uint2*>(&o.weight[i][2 * tid]);
       }
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
-        n[0] += c[k] & 0xFFFFu, n[1] += c[k] >> 16;
-        if (r0 + k >= ctas || !MASS) continue;
+        n[0] += c[k].x, n[1] += c[k].y;
+        if (r0 + k >= ctas) continue;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) m[0] += (uint64_t)b[k][i].x << (15 * i), m[1] += (uint64_t)b[k][i].y << (15 * i);
+        for (int i = 0; i < PARTS; ++i) m[0] += (uint64_t)b[k][i].x << (15 * i), m[1] += (uint64_t)b[k][i].y << (15 * i);
       }
     }
   }
@@ -535,7 +590,7 @@ struct Row {
   __device__ __forceinline__ Border find_border(uint64_t target) {
     uint32_t n[2];
     uint64_t m[2];
-    gather_ranges<MASS>(n, m);
+    gather_ranges<MASS ? 3 : 0>(n, m);
     if (!MASS) m[0] = n[0], m[1] = n[1];
     uint64_t to = prefix(m[0] + m[1]);
     __syncthreads();
@@ -558,9 +613,10 @@ struct Row {
 
   __device__ __forceinline__ void clear_ranges(bool mass) {
     __syncthreads();
-    s.count[tid] = 0;
-    if (mass)
-      for (int i = tid; i < SMP_BINS; i += SMP_THREADS) s.weight[0][i] = s.weight[1][i] = s.weight[2][i] = 0;
+    for (int i = tid; i < SMP_BINS; i += SMP_THREADS) {
+      s.count[i] = 0;
+      if (mass) s.weight[0][i] = s.weight[1][i] = s.weight[2][i] = 0;
+    }
     __syncthreads();
   }
   __device__ __forceinline__ uint64_t steps_of(float x) const {
@@ -692,11 +748,20 @@ struct Row {
 
   // The first k tokens.
   __device__ __forceinline__ void keep_top(int k) {
-    // At least k tokens lie from the k-th of the threads' largest logits on, so where k is below
-    // the threads' number, the ranges of those tell where to look.
-    if (k <= SMP_THREADS * ctas / 2) {
+    // At least k tokens lie from the k-th of the threads' largest logits on, or of those of the
+    // lanes in each group, so where k is below their number, their ranges tell where to look.
+    const bool few = k <= SMP_THREADS * ctas / 2;
+    if (few || k <= a.V / SMP_EACH / 2) {
       clear_ranges(false);
-      if (thread_max >= alive) count_in(coarse_of(thread_max));
+      if (few) {
+        if (thread_max >= alive) count_in(coarse_of(thread_max));
+      } else {
+        each_group([&](int g) {
+          float top = -INFINITY;
+          each_of(g, [&](int, float x, int) { top = fmaxf(top, x); });
+          if (top >= alive) count_in(coarse_of(top));
+        });
+      }
       meet();
       const Border b = find_border<false>((uint64_t)k);
       if (b.found) {
@@ -722,80 +787,198 @@ struct Row {
   __device__ __forceinline__ void keep_share(double share) {
     if (cut.x != -INFINITY) meet();  // (all have read the candidates of the top k, which lie in the ranges)
     clear_ranges(true);
-    const uint64_t all = (cut.x == -INFINITY && !solo ? weigh_all<true>() : weigh_kept<true, false>()).all;
+    constexpr float UNIT = 1.f / (float)((uint64_t)1 << SMP_UNIT);
+    uint64_t all;
+    float counted = alive, missed = 0.f;  // smaller ones are not counted; bound of their weight
+    if (cut.x == -INFINITY && !solo) {
+      // Tokens of weight c weigh V c at most, so those of c = (1 - p) / 4 of all / V have no part in
+      // the border; all is more than the threads' largest together.
+      float b, c;
+      w.of(thread_max, b, c);
+      const float some = (float)sum_up(warp_sum64((uint64_t)(b * (float)((uint64_t)1 << SMP_UNIT)))).all * UNIT;
+      missed = 0.25f * (1.f - (float)share) * some;
+      counted = fmaxf(alive, (whole + log2f(missed / (float)a.V)) / w.ch);
+      all = weigh_all<true>(counted).all;
+    } else {
+      all = weigh_kept<true>().all;
+    }
     const double want = ceil(share * (double)all);
     const uint64_t target = want < 1.0 ? 1 : (uint64_t)want;
-    // ranges that can hold the border: a range's weight lies between its number times the weights at its ends
-    const float goal = (float)want * (float)(1.0 / (double)((uint64_t)1 << SMP_UNIT));
-    int b_lo, b_hi;
-    {
-      uint32_t n[2];
-      uint64_t m[2];
-      gather_ranges<false>(n, m);
-      float up[2], down[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float b = (float)(2 * tid + j);
-        up[j] = n[j] * exp2f(ym - (b - 0.125f) * log2_range);
-        down[j] = n[j] * exp2f(ym - (b + 1.125f) * log2_range);
-      }
-      float tu = up[0] + up[1], td = down[0] + down[1];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const float y = __shfl_up_sync(0xffffffffu, tu, o), z = __shfl_up_sync(0xffffffffu, td, o);
-        if (lane >= o) tu += y, td += z;
-      }
-      __syncthreads();
-      if (lane == 31) s.fscan[warp] = make_float2(tu, td);
-      if (tid == 0) s.at[0] = s.at[1] = SMP_BINS;
-      __syncthreads();
-      const float2 ahead = lane < warp ? s.fscan[lane] : make_float2(0.f, 0.f);
-      tu += warp_sum(ahead.x), td += warp_sum(ahead.y);
-      // (sums in fp32 are off by less than 2^-14 of themselves)
-      constexpr float MORE = 1.f + 1.f / 8192, LESS = 1.f - 1.f / 8192;
-      if (tu * MORE >= goal) atomicMin(&s.at[0], (tu - up[1]) * MORE >= goal ? 2 * tid : 2 * tid + 1);
-      if (td * LESS >= goal) atomicMin(&s.at[1], (td - down[1]) * LESS >= goal ? 2 * tid : 2 * tid + 1);
-      __syncthreads();
-      b_lo = s.at[0], b_hi = min(s.at[1], SMP_BINS - 1);
-    }
-    meet();  // (all have read the ranges)
-    if (b_lo == SMP_BINS) return;  // all are kept
-    const float least = fmaxf(alive, coarse.below(b_hi));
-    if (!solo) {
-      if (!listed) list(least);
+    const Window win = window((float)all * UNIT, (float)want * UNIT, missed);
+    if (win.lo == SMP_BINS) return;  // all are kept
+    const float least = fmaxf(counted, coarse.below(win.hi));
+    if (!solo && win.through <= SMP_SOLO) {
+      listed = false;
+      list(least);
       try_solo();
       if (gone) return;
     }
-    // weight before them, and theirs, in finer ranges
-    const int bins = solo ? SMP_BINS : SMP_FINE;
-    const int from = 16 * b_lo, to = b_hi == SMP_BINS - 1 ? INT32_MAX : 16 * (b_hi + 1);
-    Ranges fine;  // (a quarter of them where the cluster weighs)
-    fine.set(fminf(mx, mx - ((float)b_lo - 0.25f) / coarse.per),
-             fmaxf((float)(min(b_hi, SMP_BINS - 4) - b_lo) + 1.5f, 1.f) / coarse.per);
+    const int from = 64 * win.lo, to = win.hi == SMP_BINS - 1 ? INT32_MAX : 64 * (win.hi + 1);
     const Cut old = cut;
     const auto inside = [&](float x, int token) {
-      const int v = coarse.sixteenths(x);
-      return v >= from && v < to && old.keeps(x, token);
+      const int v = coarse.place(x);
+      return x >= least && v >= from && v < to && old.keeps(x, token);
     };
-    const int fine_shift = solo ? 4 : 6;
-    const auto bin_of = [&](float x) { return min(max(fine.sixteenths(x), 0) >> fine_shift, bins - 1); };
-    clear_ranges(true);
     uint64_t above = 0;
-    each_left([&](float x, int token) {
-      const int v = coarse.sixteenths(x);
-      if (v >= to || !old.keeps(x, token)) return;
-      const uint64_t m = steps_of(x);
-      if (v < from) above += m;
-      else add_to_range(bin_of(x), m);
-    });
-    above = sum_up(warp_sum64(above)).all;
-    const uint64_t rest = target > above ? target - above : 1;
-    const Border b = find_border<true>(rest);
-    if (!b.found) {  // (weights that rounding makes a step too small: to the end of these)
-      if (cut.x < least) cut.x = least, cut.token = INT32_MAX;
-      return;
+    if (solo) {
+      each_left([&](float x, int token) {
+        if (coarse.place(x) < from && old.keeps(x, token)) above += steps_of(x);
+      });
+      above = sum_up(warp_sum64(above)).all;
+    } else {
+      above = group_and_list(least, from, to, 32 * (int64_t)win.before > a.V);
     }
-    cut_among<true>(b.n, rest - b.before, [&](float x, int token) { return inside(x, token) && bin_of(x) == (int)b.bin; });
+    uint64_t rest = target > above ? target - above : 1;
+    if (win.inside <= SMP_FEW) {
+      rank_few<true>(rest, inside);
+    } else {
+      // the window's weight in finer ranges (a quarter of them where the cluster weighs)
+      Ranges fine;
+      fine.set(fminf(mx, mx - ((float)win.lo - 0.25f) / coarse.per),
+               fmaxf((float)(min(win.hi, SMP_BINS - 4) - win.lo) + 1.5f, 1.f) / coarse.per);
+      const int shift = solo ? 6 : 8, bins = solo ? SMP_BINS : SMP_FINE;
+      const auto bin_of = [&](float x) { return min(max(fine.place(x), 0) >> shift, bins - 1); };
+      clear_ranges(true);
+      each_left([&](float x, int token) {
+        if (inside(x, token)) add_to_range(bin_of(x), steps_of(x));
+      });
+      meet();
+      const Border b = find_border<true>(rest);
+      if (!b.found) {  // (weights that rounding makes a step too small: to the end of these)
+        if (cut.x < least) cut.x = least, cut.token = INT32_MAX;
+      } else {
+        cut_among<true>(b.n, rest - b.before, [&](float x, int token) { return inside(x, token) && bin_of(x) == (int)b.bin; });
+      }
+    }
+    if (!solo) {  // the groups' weight with what is kept of the window
+      __syncthreads();
+      each_left([&](float x, int token) {
+        if (inside(x, token) && cut.keeps(x, token))
+          atomicAdd((unsigned long long*)&s.group[(token - first) / SMP_GROUP], (unsigned long long)steps_of(x));
+      });
+      grouped = true;
+    }
+  }
+  // Ranges that can hold the border: a range's tokens weigh as many times the weight at their
+  // mean place, by what their places are rounded (a 128th of a range) more or less, and by the
+  // spread of a range more (2^-13 of it).  Summed from the first range on, and from the last
+  // one back, where `missed` comes on top, from the weight of all.
+  struct Window {
+    int lo, hi;                        // lo = SMP_BINS: no range
+    uint32_t before, inside, through;  // tokens before them, in them, in all up to one behind them
+  };
+  __device__ __forceinline__ Window window(float all, float goal, float missed) {
+    uint32_t n[2];
+    uint64_t places[2];
+    gather_ranges<1>(n, places);
+    const float off = log2_range * (1.f / 120.f);  // (a 128th, and the roundings of a place)
+    float up[2], down[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float mean = n[j] ? ((float)places[j] / (float)n[j] - 1.f) * (1.f / 64) : 0.f;
+      const float y = ym - ((float)(2 * tid + j) + mean) * log2_range;
+      up[j] = (float)n[j] * exp2f(y + off) * (1.f + 1.f / 4096);
+      down[j] = (float)n[j] * exp2f(y - off);
+    }
+    float tu = up[0] + up[1], td = down[0] + down[1];
+    uint32_t tn = n[0] + n[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float y = __shfl_up_sync(0xffffffffu, tu, o), z = __shfl_up_sync(0xffffffffu, td, o);
+      const uint32_t c = __shfl_up_sync(0xffffffffu, tn, o);
+      if (lane >= o) tu += y, td += z, tn += c;
+    }
+    __syncthreads();
+    if (lane == 31) s.fscan[warp] = make_float2(tu, td), s.wkept[warp] = tn;
+    if (tid == 0) s.at[0] = s.at[1] = SMP_BINS, s.at[2] = s.at[3] = s.at[4] = 0;
+    __syncthreads();
+    float all_up = 0.f, all_down = 0.f;
+    for (int i = 0; i < SMP_WARPS; ++i) {
+      const float2 o = s.fscan[i];
+      if (i < warp) tu += o.x, td += o.y, tn += s.wkept[i];
+      all_up += o.x, all_down += o.y;
+    }
+    const float slack = all * (1.f / (1 << 18));  // (sums in fp32)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float u = j ? tu : tu - up[1], d = j ? td : td - down[1];  // up to range 2 tid + j
+      if (fminf(u, all - (all_down - d)) + slack >= goal) atomicMin(&s.at[0], 2 * tid + j);
+      if (fmaxf(d, all - (all_up - u) - missed) - slack >= goal) atomicMin(&s.at[1], 2 * tid + j);
+    }
+    __syncthreads();
+    Window z;
+    z.lo = s.at[0], z.hi = min(s.at[1], SMP_BINS - 1);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int b = 2 * tid + j;
+      const uint32_t c = j ? tn : tn - n[1];  // tokens up to range b
+      if (b == z.lo - 1) s.at[2] = c;
+      if (b == z.hi) s.at[3] = c;
+      if (b == min(z.hi + 1, SMP_BINS - 1)) s.at[4] = c;
+    }
+    meet();  // (all have read the ranges)
+    z.before = s.at[2], z.inside = s.at[3] - s.at[2], z.through = s.at[4];
+    return z;
+  }
+  // Weight by groups of the kept tokens before place `from`; the list of those up to `to`.
+  __device__ __forceinline__ uint64_t group_and_list(float least, int from, int to, bool dense) {
+    low = least;
+    listed = false;
+    __syncthreads();
+    if (tid == 0) s.n_list = 0;
+    for (int g = tid; g < groups; g += SMP_THREADS) s.group[g] = 0;
+    __syncthreads();
+    uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
+    uint64_t total = 0;
+    const auto put = [&](float x, int token) {
+      const uint32_t i = atomicAdd(&s.n_list, 1u);
+      if (i < (uint32_t)a.list_cap) left[i] = make_float2(x, __int_as_float(token));
+    };
+    if (dense) {
+      each_group([&](int g) {
+        Sum sum;
+        each_of(g, [&](int, float x, int place) {
+          const int v = coarse.place(x);
+          const bool k = x >= low && v < to && cut.keeps(x, first + place);
+          float b, c;
+          w.of(x, b, c);
+          sum.add(k && v < from ? b : 0.f, c);
+          if (k && v >= from) put(x, first + place);
+        });
+        const uint64_t v = sum.warp_steps();
+        if (lane == 0) s.group[g] = v;
+        total += v;
+      });
+    } else {
+      each_left([&](float x, int token) {
+        const int v = coarse.place(x);
+        if (v >= to || !cut.keeps(x, token)) return;
+        if (v >= from) {
+          put(x, token);
+          return;
+        }
+        const uint64_t m = steps_of(x);
+        const int g = (token - first) / SMP_GROUP;
+        atomicAdd(part + 2 * g, (uint32_t)m & 0x1FFFFFu);
+        atomicAdd(part + 2 * g + 1, (uint32_t)(m >> 21));
+      });
+      __syncthreads();
+      for (int g = tid; g < groups; g += SMP_THREADS) {
+        const uint64_t v = part[2 * g] + ((uint64_t)part[2 * g + 1] << 21);
+        s.group[g] = v;
+        total += v;
+      }
+      total = warp_sum64(total);
+    }
+    __syncthreads();
+    listed = s.n_list <= (uint32_t)a.list_cap;
+    return sum_up(total).all;
+  }
+  __device__ __forceinline__ Sums sum_groups() {
+    __syncthreads();
+    uint64_t total = 0;
+    for (int g = tid; g < groups; g += SMP_THREADS) total += s.group[g];
+    return sum_up(warp_sum64(total));
   }
 
   // Tokens from m + `below` on.
@@ -807,7 +990,8 @@ struct Row {
     if (x > cut.x) {
       cut.x = x, cut.token = INT32_MAX;
       if (!solo) {
-        if (!listed && x > low) list(x);
+        if (grouped || (!listed && x > low)) list(x);
+        grouped = false;
         try_solo();
       }
     }
@@ -896,52 +1080,25 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
   const int64_t row = blockIdx.x / ctas;
   const int start = rank * a.per, n = max(0, min(a.per, a.V - start));  // this CTA's tokens
   const T* src = (const T*)a.x + row * a.stride + start;
-  const int phase = (int)((uintptr_t)src / sizeof(T) % W);  // the row's offset in 16 bytes, kept in shared memory
+  const int phase = (int)((uintptr_t)src / sizeof(T) % W);
   const int groups = (phase + n + SMP_GROUP - 1) / SMP_GROUP;
-  Row<T> R = {a, s, cluster, reinterpret_cast<uint4*>(smem_raw), start - phase, groups, ctas, rank, tid, tid & 31, tid >> 5, 0};
+  Row<T> R = {a, s, cluster, reinterpret_cast<const uint4*>(src - phase), reinterpret_cast<float2*>(smem_raw), phase, n,
+              start - phase, groups, ctas, rank, tid, tid & 31, tid >> 5, 0};
+  R.origin = 0.f, R.back = true;
   const Exp2Entry entry = kExp2Table[tid / 16];
   pdl_wait();
   // ---- what the row asks for
   const float t = a.temperature ? a.temperature[row] : 1.f, u = a.u[row];
   const float p = a.top_p ? a.top_p[row] : 1.f, least = a.min_p ? a.min_p[row] : 0.f;
   const int k = a.top_k ? a.top_k[row] : 0;
-  // ---- the row, its largest and smallest logit
-  T* data = reinterpret_cast<T*>(smem_raw) + phase;
+  // ---- its largest and smallest logit
   float mx = -INFINITY, mn = INFINITY;
-  const auto take = [&](float x) {
-    mx = fmaxf(mx, x);
-    mn = x > -INFINITY ? fminf(mn, x) : mn;
-  };
-  {
-    const int head = min(n, (W - phase) % W), words = (n - head) / W;
-    const uint4* from = reinterpret_cast<const uint4*>(src + head);
-    uint4* to = reinterpret_cast<uint4*>(data + head);
-    constexpr int BATCH = 8;
-    for (int i0 = tid; i0 < words; i0 += BATCH * SMP_THREADS) {
-      uint4 v[BATCH];
-#pragma unroll
-      for (int j = 0; j < BATCH; ++j)
-        if (i0 + j * SMP_THREADS < words) v[j] = from[i0 + j * SMP_THREADS];
-#pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        if (i0 + j * SMP_THREADS >= words) break;
-        to[i0 + j * SMP_THREADS] = v[j];
-        float x[W];
-        Words<T>::split(v[j], x);
-#pragma unroll
-        for (int e = 0; e < W; ++e) take(x[e]);
-      }
-    }
-    const int edges = head + (n - head) % W;
-    for (int i = tid; i < edges; i += SMP_THREADS) {
-      const int at = i < head ? i : head + words * W + i - head;
-      data[at] = src[at];
-      take((float)src[at]);
-    }
-    // (what is around it)
-    for (int i = tid; i < phase; i += SMP_THREADS) data[i - phase] = Words<T>::to(-INFINITY);
-    for (int i = n + tid; i < groups * SMP_GROUP - phase; i += SMP_THREADS) data[i] = Words<T>::to(-INFINITY);
-  }
+  R.each_group([&](int g) {
+    R.each_of(g, [&](int, float x, int) {
+      mx = fmaxf(mx, x);
+      mn = x > -INFINITY ? fminf(mn, x) : mn;
+    });
+  });
   // (the reciprocals come while the last loads are on their way)
   const float held = fminf(fmaxf(t, 1e-37f), 1e30f), lh = 1.44269502f, ll = 1.92596303e-08f;
   R.w.ch = __fdiv_rn(lh, held);
@@ -977,8 +1134,9 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
   }
   if (t == 0.f || k == 1 || p <= 0.f || least > 1.f) {  // the first of the largest
     uint32_t at = UINT32_MAX;
-    for (int g = R.warp; g < groups; g += SMP_WARPS)
+    R.each_group([&](int g) {
       R.each_of(g, [&](int, float x, int place) { at = x == mx ? min(at, (uint32_t)(R.first + place)) : at; });
+    });
     at = __reduce_min_sync(0xffffffffu, at);
     if (R.lane == 0) R.mine().sum[R.warp] = at;
     cluster.sync();
@@ -1002,12 +1160,12 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
   // ---- the kept weights, and where u falls (both factors are exact)
   const auto seek = [&](uint64_t total) { return min((uint64_t)((double)u * (double)total), total - 1); };
   if (R.solo) {
-    const uint64_t total = R.template weigh_kept<false, false>().all;
+    const uint64_t total = R.template weigh_kept<false>().all;
     R.draw_solo(seek(total), row, t, total);
     return;
   }
   const typename Row<T>::Sums sums =
-      R.cut.x == -INFINITY ? R.template weigh_all<false>() : R.template weigh_kept<false, true>();
+      R.grouped ? R.sum_groups() : R.cut.x == -INFINITY ? R.template weigh_all<false>(0.f) : R.weigh_groups();
   const uint64_t left = seek(sums.all);
   if (left >= sums.before && left < sums.before + sums.own) R.draw(left - sums.before, row, t, sums.all);
   cluster.sync();  // (a CTA's memory stays until the others have read it)
@@ -1022,19 +1180,16 @@ template <typename T>
 static cudaError_t launch_sample(SampleArgs a, int32_t rows, cudaStream_t stream) {
   static bool done[64];
   const auto kernel = sample_kernel<T>;
-  constexpr size_t AROUND = (SMP_GROUP + Words<T>::N) * sizeof(T);  // places before and behind a part
-  cudaError_t e = allow_smem(kernel, SMP_MAX_BYTES + AROUND, done);
+  cudaError_t e = allow_smem(kernel, SMP_LIST * sizeof(float2), done);
   if (e != cudaSuccess) return e;
-  const auto part = [&](int ctas) { return ((int64_t)a.V + ctas - 1) / ctas; };
+  // CTAs of a row: as many as fit the SMs at once, two on each, while a part is more than a few tokens a thread
   int ctas = 1;
-  // two CTAs an SM; and more while there are SMs without a row and a part is more than a
-  // few tokens a thread
-  constexpr int64_t HALF = 80 * 1024 / sizeof(T), FEW = 4 * SMP_THREADS;
-  while (ctas < ROW_CLUSTER && (part(ctas) > HALF || (2 * ctas * (int64_t)rows <= 2 * num_sms() && part(ctas) > FEW)))
-    ctas *= 2;
-  a.per = (int32_t)part(ctas);
-  const size_t smem = align_up((size_t)a.per * sizeof(T) + AROUND, 16);
-  return launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, smem, stream, true, a);
+  while (ctas < ROW_CLUSTER && 2 * ctas * (int64_t)rows <= 2 * num_sms() && a.V > 8 * SMP_THREADS * ctas) ctas *= 2;
+  a.per = (a.V + ctas - 1) / ctas;
+  a.list_cap = a.per < SMP_LIST ? a.per : SMP_LIST;
+  if (a.list_cap < SMP_SOLO) a.list_cap = SMP_SOLO < a.V ? SMP_SOLO : a.V;
+  return launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, a.list_cap * sizeof(float2), stream, true,
+                        a);
 }
 
 extern "C" pced_status pced_sample(const void* x, int32_t type, int64_t stride, int32_t rows, int32_t V, const float* u,
@@ -1051,7 +1206,7 @@ extern "C" pced_status pced_sample(const void* x, int32_t type, int64_t stride, 
   if (V > SMP_MAX_V) return fail(PCED_ERR_UNSUPPORTED, "%s: V above %d", fn, SMP_MAX_V);
   if ((int64_t)rows * ROW_CLUSTER > INT32_MAX) return fail(PCED_ERR_UNSUPPORTED, "%s: too many rows", fn);
   if (num_sms() <= 0) return fail(PCED_ERR_NO_DEVICE, "%s: no CUDA device", fn);
-  const SampleArgs a = {x, stride, V, 0, u, temperature, top_k, top_p, min_p, token, logprob, status};
+  const SampleArgs a = {x, stride, V, 0, 0, u, temperature, top_k, top_p, min_p, token, logprob, status};
   const cudaError_t e = type == PCED_IN_F32 ? launch_sample<float>(a, rows, (cudaStream_t)stream)
                                              : launch_sample<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "sample launch");
