@@ -30,8 +30,7 @@ namespace cg = cooperative_groups;
 struct SampleArgs {
   const void* x;
   int64_t stride;
-  int32_t V, per;    // tokens; of a CTA of the row's cluster
-  int32_t list_cap;  // tokens that a CTA's list takes
+  int32_t V, per;  // tokens; of a CTA of the row's cluster
   const float* u;
   const float* temperature;
   const int32_t* top_k;
@@ -49,8 +48,11 @@ constexpr int SMP_FEW = 512;          // tokens of a range that are ranked one b
 constexpr int SMP_EACH = 16;          // tokens of a lane in a group, whose weight is kept
 constexpr int SMP_GROUP = 32 * SMP_EACH;
 constexpr int SMP_FINE = 256;         // ranges that a cluster weighs (what its CTAs read of one another is slow)
-constexpr int SMP_LIST = 9216;        // tokens that a CTA's list takes (two CTAs an SM)
+constexpr int SMP_LIST = 4608;        // tokens that a CTA's list takes
 constexpr int SMP_SOLO = 4096;        // tokens of a row that one CTA goes on with alone
+constexpr int SMP_QUEUE = 32 * 8 + 32;  // tokens of a warp on their way to whole warps: half a group and a rest
+constexpr int SMP_RANK = 128;         // tokens that are ranked at once
+constexpr int64_t SMP_L2 = 100 << 20;   // bytes of rows that L2 keeps
 constexpr int SMP_MAX_V = 393216;     // (sets the groups)
 constexpr int SMP_MAX_GROUPS = SMP_MAX_V / SMP_GROUP + 1;
 constexpr int SMP_UNIT = 42;          // weights are counted in steps of 2^-42
@@ -128,6 +130,7 @@ struct Sum {
   }
 };
 static_assert(SMP_UNIT == 42, "18 + 24");
+static_assert(SMP_SOLO <= SMP_LIST, "one CTA's list");
 static_assert(SMP_BINS == 4 * SMP_FINE, "see keep_share");
 
 // Order of (logit, token) pairs: larger logits first, then lower tokens
@@ -196,7 +199,6 @@ struct SampleShared {
   uint32_t weight[3][SMP_BINS];  // their weights, 15 bits each
   uint64_t cand[SMP_FEW];
   uint64_t group[SMP_MAX_GROUPS];  // kept weight (on its way in two numbers, 21 bits in the first)
-  float2 queue[SMP_WARPS][64];     // tokens on their way to a whole warp
   uint32_t n_list, n_cand;
   int at[5];
   uint64_t wscan[SMP_WARPS];
@@ -323,25 +325,35 @@ struct Row {
       for (int i = tid; i < k; i += SMP_THREADS) f(left[i].x, __float_as_int(left[i].y));
       return;
     }
-    float2* const q = s.queue[warp];
+    float2* const q = left + SMP_LIST + warp * SMP_QUEUE;
     int held = 0;
     each_group([&](int g) {
       uint32_t take = 0;
       each_of(g, [&](int e, float x, int) { take |= (uint32_t)(x >= low) << e; });
       if (!__any_sync(0xffffffffu, take)) return;
-      each_of(g, [&](int e, float x, int place) {
-        const bool k = take >> e & 1u;
-        const uint32_t who = __ballot_sync(0xffffffffu, k);
-        if (!who) return;
-        if (k) q[held + __popc(who & ((1u << lane) - 1))] = make_float2(x, __int_as_float(first + place));
-        held += __popc(who);
-        if (held < 32) return;
-        held -= 32;  // (the last ones first)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t mine = take >> (8 * half) & 0xFFu;
+        const int k = __popc(mine);
+        int to = k;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, to, o);
+          if (lane >= o) to += y;
+        }
+        float2* at = q + held + to - k;
+        each_of(g, [&](int e, float x, int place) {
+          if (e / 8 == half && (take >> e & 1u)) *at++ = make_float2(x, __int_as_float(first + place));
+        });
+        held += __shfl_sync(0xffffffffu, to, 31);
         __syncwarp();
-        const float2 y = q[held + lane];
+        while (held >= 32) {  // (the last ones first)
+          held -= 32;
+          const float2 y = q[held + lane];
+          f(y.x, __float_as_int(y.y));
+        }
         __syncwarp();
-        f(y.x, __float_as_int(y.y));
-      });
+      }
     });
     __syncwarp();
     if (lane < held) f(q[lane].x, __float_as_int(q[lane].y));
@@ -365,7 +377,7 @@ struct Row {
       if (lane >= o) to += y;
     }
     const int total = __shfl_sync(0xffffffffu, to, ROW_CLUSTER - 1);
-    if (total > SMP_SOLO || total > a.list_cap) return;
+    if (total > SMP_SOLO) return;
     gone = rank != 0;
     // two warps for each CTA
     const int r = warp / 2, their_n = __shfl_sync(0xffffffffu, k, r), base = __shfl_sync(0xffffffffu, to, r) - their_n;
@@ -401,12 +413,12 @@ struct Row {
       if (lane == 31) base = (int)atomicAdd(&s.n_list, (uint32_t)to);
       base = __shfl_sync(0xffffffffu, base, 31) + to - k;
       each_of(g, [&](int e, float x, int place) {
-        if ((take >> e & 1u) && base < a.list_cap) left[base] = make_float2(x, __int_as_float(first + place));
+        if ((take >> e & 1u) && base < SMP_LIST) left[base] = make_float2(x, __int_as_float(first + place));
         base += take >> e & 1u;
       });
     });
     __syncthreads();
-    listed = s.n_list <= a.list_cap;
+    listed = s.n_list <= SMP_LIST;
   }
 
   // m, N and the table for temperature t (inverse: 1 / w.ch, entry: of the table)
@@ -770,7 +782,7 @@ struct Row {
         if (gone) return;
       }
     }
-    if (solo && solo <= SMP_FEW) {
+    if (solo && solo <= SMP_RANK) {
       if (solo > k) rank_few<false>((uint64_t)k, [](float, int) { return true; });
       return;
     }
@@ -829,7 +841,7 @@ struct Row {
       above = group_and_list(least, from, to, 32 * (int64_t)win.before > a.V);
     }
     uint64_t rest = target > above ? target - above : 1;
-    if (win.inside <= SMP_FEW) {
+    if (win.inside <= SMP_RANK) {
       rank_few<true>(rest, inside);
     } else {
       // the window's weight in finer ranges (a quarter of them where the cluster weighs)
@@ -932,7 +944,7 @@ struct Row {
     uint64_t total = 0;
     const auto put = [&](float x, int token) {
       const uint32_t i = atomicAdd(&s.n_list, 1u);
-      if (i < (uint32_t)a.list_cap) left[i] = make_float2(x, __int_as_float(token));
+      if (i < SMP_LIST) left[i] = make_float2(x, __int_as_float(token));
     };
     if (dense) {
       each_group([&](int g) {
@@ -971,7 +983,7 @@ struct Row {
       total = warp_sum64(total);
     }
     __syncthreads();
-    listed = s.n_list <= (uint32_t)a.list_cap;
+    listed = s.n_list <= SMP_LIST;
     return sum_up(total).all;
   }
   __device__ __forceinline__ Sums sum_groups() {
@@ -1180,16 +1192,18 @@ template <typename T>
 static cudaError_t launch_sample(SampleArgs a, int32_t rows, cudaStream_t stream) {
   static bool done[64];
   const auto kernel = sample_kernel<T>;
-  cudaError_t e = allow_smem(kernel, SMP_LIST * sizeof(float2), done);
+  cudaError_t e = allow_smem(kernel, (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2), done);
   if (e != cudaSuccess) return e;
-  // CTAs of a row: as many as fit the SMs at once, two on each, while a part is more than a few tokens a thread
+  // CTAs of a row: as many as fit the SMs at once, two on each, while a part is more than a few
+  // tokens a thread; and so many that the rows on the SMs fit L2 together
+  const int64_t slots = 2 * (int64_t)num_sms(), bytes = (int64_t)a.V * sizeof(T);
   int ctas = 1;
-  while (ctas < ROW_CLUSTER && 2 * ctas * (int64_t)rows <= 2 * num_sms() && a.V > 8 * SMP_THREADS * ctas) ctas *= 2;
+  while (ctas < ROW_CLUSTER && a.V > 8 * SMP_THREADS * ctas &&
+         (2 * ctas * (int64_t)rows <= slots || (rows < slots / ctas ? rows : slots / ctas) * bytes > SMP_L2))
+    ctas *= 2;
   a.per = (a.V + ctas - 1) / ctas;
-  a.list_cap = a.per < SMP_LIST ? a.per : SMP_LIST;
-  if (a.list_cap < SMP_SOLO) a.list_cap = SMP_SOLO < a.V ? SMP_SOLO : a.V;
-  return launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, a.list_cap * sizeof(float2), stream, true,
-                        a);
+  constexpr size_t smem = (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2);
+  return launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, smem, stream, true, a);
 }
 
 extern "C" pced_status pced_sample(const void* x, int32_t type, int64_t stride, int32_t rows, int32_t V, const float* u,
@@ -1206,7 +1220,7 @@ extern "C" pced_status pced_sample(const void* x, int32_t type, int64_t stride, 
   if (V > SMP_MAX_V) return fail(PCED_ERR_UNSUPPORTED, "%s: V above %d", fn, SMP_MAX_V);
   if ((int64_t)rows * ROW_CLUSTER > INT32_MAX) return fail(PCED_ERR_UNSUPPORTED, "%s: too many rows", fn);
   if (num_sms() <= 0) return fail(PCED_ERR_NO_DEVICE, "%s: no CUDA device", fn);
-  const SampleArgs a = {x, stride, V, 0, 0, u, temperature, top_k, top_p, min_p, token, logprob, status};
+  const SampleArgs a = {x, stride, V, 0, u, temperature, top_k, top_p, min_p, token, logprob, status};
   const cudaError_t e = type == PCED_IN_F32 ? launch_sample<float>(a, rows, (cudaStream_t)stream)
                                              : launch_sample<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "sample launch");
