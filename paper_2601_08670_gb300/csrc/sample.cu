@@ -200,6 +200,9 @@ struct SampleShared {
   uint64_t cand[SMP_FEW];
   uint64_t group[SMP_MAX_GROUPS];  // kept weight (on its way in two numbers, 21 bits in the first)
   uint32_t n_list, n_cand;
+  int from, to;                  // places of this CTA's part
+  float ym, whole, log2_range;   // log2 of the largest weight; N; log2 of weights at a range's ends, the difference
+  float thread_max[SMP_THREADS]; // the largest logit that a thread loaded first
   int at[5];
   uint64_t wscan[SMP_WARPS];
   uint32_t wkept[SMP_WARPS];
@@ -237,17 +240,14 @@ struct Row {
   cg::cluster_group cluster;
   const uint4* data;                   // this CTA's part of the row, from an address of 16 bytes on
   float2* left;                        // the list: (logit, token)
-  int phase, n;                        // the part's places are phase ... phase + n - 1
   int first, groups;                   // token of place 0
-  int ctas, rank, tid, lane, warp, turn;
-  float mx, mn;                        // of the row
+  int ctas, turn;
+  float mx;                            // the row's largest logit
   Weight w;
   float origin;                        // see moved()
   bool back;                           // see each_group()
-  float whole, ym;                     // N; log2 of the largest weight
   float alive;                         // smaller logits have weights that no cut asks about
   Ranges coarse;
-  float log2_range;                    // log2 of weights at a range's ends, the difference
   Cut cut;
   float low;                           // smaller logits are not kept
   bool listed;                         // the others' places are in the list (each CTA's own matter, as is `low`)
@@ -255,6 +255,10 @@ struct Row {
   bool gone;                           // ... another CTA
   bool grouped;                        // the groups' kept weight is known; the list has a part of the tokens only
 
+  static __device__ __forceinline__ int tid() { return threadIdx.x; }
+  static __device__ __forceinline__ int lane() { return threadIdx.x & 31; }
+  static __device__ __forceinline__ int warp() { return threadIdx.x >> 5; }
+  static __device__ __forceinline__ int rank() { return cg::this_cluster().block_rank(); }
   __device__ __forceinline__ typename SampleShared::Told& mine() { return s.told[turn & 1]; }
   __device__ __forceinline__ const typename SampleShared::Told& theirs(int r) {
     return cluster.map_shared_rank(&s, r)->told[turn & 1];
@@ -267,15 +271,15 @@ struct Row {
     return x;
   }
   __device__ __forceinline__ float at(int place) const {
-    if (place < phase || place >= phase + n) return -INFINITY;
+    if (place < s.from || place >= s.to) return -INFINITY;
     return moved((float)reinterpret_cast<const T*>(data)[place]);
   }
   // f(e, logit, place) for the SMP_EACH places of a lane in group g (-inf around the part)
   template <typename F>
   __device__ __forceinline__ void each_of(int g, F f) const {
     float x[TILES][W];
-    const int v0 = g * TILES * 32 + lane;
-    if (g * SMP_GROUP >= phase && (g + 1) * SMP_GROUP <= phase + n) {
+    const int v0 = g * TILES * 32 + lane();
+    if (g * SMP_GROUP >= s.from && (g + 1) * SMP_GROUP <= s.to) {
       uint4 w[TILES];
 #pragma unroll
       for (int t = 0; t < TILES; ++t) w[t] = data[v0 + t * 32];
@@ -285,12 +289,12 @@ struct Row {
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
         const int place = (v0 + t * 32) * W;
-        if (place >= phase && place + W <= phase + n) {
+        if (place >= s.from && place + W <= s.to) {
           Words<T>::split(data[v0 + t * 32], x[t]);
         } else {
 #pragma unroll
           for (int e = 0; e < W; ++e)
-            x[t][e] = place + e >= phase && place + e < phase + n ? (float)reinterpret_cast<const T*>(data)[place + e] : -INFINITY;
+            x[t][e] = place + e >= s.from && place + e < s.to ? (float)reinterpret_cast<const T*>(data)[place + e] : -INFINITY;
         }
       }
     }
@@ -310,7 +314,7 @@ struct Row {
   template <typename F>
   __device__ __forceinline__ void each_group(F f) {
     back = !back;
-    for (int i = warp; i < groups; i += SMP_WARPS) f(back ? groups - 1 - i : i);
+    for (int i = warp(); i < groups; i += SMP_WARPS) f(back ? groups - 1 - i : i);
   }
   // A barrier of the CTAs that still work on the row.
   __device__ __forceinline__ void meet() {
@@ -322,10 +326,10 @@ struct Row {
   __device__ __forceinline__ void each_left(F f) {
     if (listed) {
       const int k = solo ? solo : (int)s.n_list;
-      for (int i = tid; i < k; i += SMP_THREADS) f(left[i].x, __float_as_int(left[i].y));
+      for (int i = tid(); i < k; i += SMP_THREADS) f(left[i].x, __float_as_int(left[i].y));
       return;
     }
-    float2* const q = left + SMP_LIST + warp * SMP_QUEUE;
+    float2* const q = left + SMP_LIST + warp() * SMP_QUEUE;
     int held = 0;
     each_group([&](int g) {
       uint32_t take = 0;
@@ -339,7 +343,7 @@ struct Row {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int y = __shfl_up_sync(0xffffffffu, to, o);
-          if (lane >= o) to += y;
+          if (lane() >= o) to += y;
         }
         float2* at = q + held + to - k;
         each_of(g, [&](int e, float x, int place) {
@@ -349,14 +353,14 @@ struct Row {
         __syncwarp();
         while (held >= 32) {  // (the last ones first)
           held -= 32;
-          const float2 y = q[held + lane];
+          const float2 y = q[held + lane()];
           f(y.x, __float_as_int(y.y));
         }
         __syncwarp();
       }
     });
     __syncwarp();
-    if (lane < held) f(q[lane].x, __float_as_int(q[lane].y));
+    if (lane() < held) f(q[lane()].x, __float_as_int(q[lane()].y));
     __syncwarp();
   }
   // Where few tokens are left, CTA 0 takes them all (logit, token) and goes on alone: a barrier of
@@ -366,27 +370,27 @@ struct Row {
       if (listed) solo = s.n_list;
       return;
     }
-    if (tid == 0) mine().count = listed ? s.n_list : SMP_SOLO + 1;
+    if (tid() == 0) mine().count = listed ? s.n_list : SMP_SOLO + 1;
     cluster.sync();
-    const int k = lane < ctas ? (int)theirs(lane).count : 0;
+    const int k = lane() < ctas ? (int)theirs(lane()).count : 0;
     ++turn;
     int to = k;
 #pragma unroll
     for (int o = 1; o < ROW_CLUSTER; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, to, o);
-      if (lane >= o) to += y;
+      if (lane() >= o) to += y;
     }
     const int total = __shfl_sync(0xffffffffu, to, ROW_CLUSTER - 1);
     if (total > SMP_SOLO) return;
-    gone = rank != 0;
+    gone = rank() != 0;
     // two warps for each CTA
-    const int r = warp / 2, their_n = __shfl_sync(0xffffffffu, k, r), base = __shfl_sync(0xffffffffu, to, r) - their_n;
-    if (rank == 0 && r > 0 && r < ctas) {
+    const int r = warp() / 2, their_n = __shfl_sync(0xffffffffu, k, r), base = __shfl_sync(0xffffffffu, to, r) - their_n;
+    if (rank() == 0 && r > 0 && r < ctas) {
       const float2* theirs_ = cluster.map_shared_rank(left, r);
-      for (int i = tid & 63; i < their_n; i += 64) left[base + i] = theirs_[i];
+      for (int i = tid() & 63; i < their_n; i += 64) left[base + i] = theirs_[i];
     }
     cluster.sync();  // (CTA 0 has read the others' memory)
-    if (rank == 0) {
+    if (rank() == 0) {
       ctas = 1;
       solo = total;
     }
@@ -396,7 +400,7 @@ struct Row {
     low = low_;
     listed = false;
     __syncthreads();
-    if (tid == 0) s.n_list = 0;
+    if (tid() == 0) s.n_list = 0;
     __syncthreads();
     each_group([&](int g) {
       uint32_t take = 0;
@@ -407,10 +411,10 @@ struct Row {
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, to, o);
-        if (lane >= o) to += y;
+        if (lane() >= o) to += y;
       }
       int base = 0;
-      if (lane == 31) base = (int)atomicAdd(&s.n_list, (uint32_t)to);
+      if (lane() == 31) base = (int)atomicAdd(&s.n_list, (uint32_t)to);
       base = __shfl_sync(0xffffffffu, base, 31) + to - k;
       each_of(g, [&](int e, float x, int place) {
         if ((take >> e & 1u) && base < SMP_LIST) left[base] = make_float2(x, __int_as_float(first + place));
@@ -422,28 +426,30 @@ struct Row {
   }
 
   // m, N and the table for temperature t (inverse: 1 / w.ch, entry: of the table)
-  __device__ __forceinline__ void set_weights(float inverse, Exp2Entry entry) {
+  __device__ __forceinline__ void set_weights(float mn, float inverse, Exp2Entry entry) {
     if (!(fabsf(mx) * w.ch <= 8192.f)) {
       origin = mx;
-      thread_max = moved(thread_max);
+      s.thread_max[tid()] = moved(s.thread_max[tid()]);
       mn = mx == INFINITY ? 0.f : fmaxf(mn - mx, -3e38f);
       mx = 0.f;
     }
     const float y = __fmul_rn(mx, w.ch), top = ceilf(y);
-    ym = (y - top) + fmaf(mx, w.cl, fmaf(mx, w.ch, -y));
     w.floor = (top - SMP_LOWEST) * inverse;
     alive = (top - SMP_ALIVE) * inverse;
     low = alive;
     listed = gone = grouped = false;
     solo = 0;
-    w.table = &s.table[0][lane & 15];
-    const uint32_t j = tid / 16;
-    s.table[j][tid % 16] =
+    w.table = &s.table[0][lane() & 15];
+    const uint32_t j = tid() / 16;
+    s.table[j][tid() % 16] =
         make_float2(__uint_as_float(entry.bits - (j << 18) - ((uint32_t)(int)top << 23)), entry.rest);
     const float width = fminf((SMP_ALIVE + 1.f) * inverse, fmaxf(mx - mn, 1e-30f));
     coarse.set(mx, width);
-    log2_range = w.ch * width * (1.f / (SMP_BINS - 4));
-    whole = top;
+    if (tid() == 0) {
+      s.ym = (y - top) + fmaf(mx, w.cl, fmaf(mx, w.ch, -y));
+      s.log2_range = w.ch * width * (1.f / (SMP_BINS - 4));
+      s.whole = top;
+    }
     __syncthreads();
   }
 
@@ -452,21 +458,21 @@ struct Row {
     uint64_t all, before, own;
   };
   __device__ __forceinline__ Sums sum_up(uint64_t v) {
-    if (lane == 0) mine().sum[warp] = v;
+    if (lane() == 0) mine().sum[warp()] = v;
     meet();
     // a CTA's sixteen by four lanes
-    const int r = lane >> 2;
+    const int r = lane() >> 2;
     uint64_t of_cta = 0;
     if (r < ctas) {
-      const uint64_t* q = theirs(r).sum + (lane & 3) * (SMP_WARPS / 4);
+      const uint64_t* q = theirs(r).sum + (lane() & 3) * (SMP_WARPS / 4);
       const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(q), y = *reinterpret_cast<const ulonglong2*>(q + 2);
       of_cta = x.x + x.y + y.x + y.y;
     }
     of_cta += __shfl_xor_sync(0xffffffffu, of_cta, 1);
     of_cta += __shfl_xor_sync(0xffffffffu, of_cta, 2);
     Sums z;
-    z.own = __shfl_sync(0xffffffffu, of_cta, 4 * rank);
-    z.all = of_cta, z.before = r < rank ? of_cta : 0;
+    z.own = __shfl_sync(0xffffffffu, of_cta, 4 * rank());
+    z.all = of_cta, z.before = r < rank() ? of_cta : 0;
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) {
       z.all += __shfl_xor_sync(0xffffffffu, z.all, o);
@@ -489,7 +495,7 @@ struct Row {
         if (COUNT && x >= from) count_place(x);
       });
       const uint64_t v = sum.warp_steps();
-      if (lane == 0) s.group[g] = v;
+      if (lane() == 0) s.group[g] = v;
       total += v;
     });
     return sum_up(total);
@@ -511,7 +517,7 @@ struct Row {
     uint64_t total = 0;
     __syncthreads();
     if (listed) {
-      for (int g = tid; g < groups; g += SMP_THREADS) s.group[g] = 0;
+      for (int g = tid(); g < groups; g += SMP_THREADS) s.group[g] = 0;
       __syncthreads();
       uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
       each_left([&](float x, int token) {
@@ -522,7 +528,7 @@ struct Row {
         atomicAdd(part + 2 * g + 1, (uint32_t)(v >> 21));
       });
       __syncthreads();
-      for (int g = tid; g < groups; g += SMP_THREADS) {
+      for (int g = tid(); g < groups; g += SMP_THREADS) {
         const uint64_t v = part[2 * g] + ((uint64_t)part[2 * g + 1] << 21);
         s.group[g] = v;
         total += v;
@@ -541,7 +547,7 @@ struct Row {
           sum.add(k ? b : 0.f, c);
         });
         const uint64_t v = some ? sum.warp_steps() : 0;
-        if (lane == 0) s.group[g] = v;
+        if (lane() == 0) s.group[g] = v;
         total += v;
       });
     }
@@ -571,7 +577,7 @@ struct Row {
     static_assert(SMP_BINS == 2 * SMP_THREADS && ROW_CLUSTER == 8, "two ranges a thread");
     n[0] = n[1] = 0;
     m[0] = m[1] = 0;
-    if (PARTS == 3 && !solo && 2 * tid >= SMP_FINE) return;
+    if (PARTS == 3 && !solo && 2 * tid() >= SMP_FINE) return;
     constexpr int BATCH = PARTS == 3 ? 2 : 4;  // CTAs whose loads are in flight
 #pragma unroll
     for (int r0 = 0; r0 < ROW_CLUSTER; r0 += BATCH) {
@@ -582,10 +588,10 @@ struct Row {
         c[k] = make_uint2(0, 0);
         if (r0 + k >= ctas) continue;
         const SampleShared& o = *cluster.map_shared_rank(&s, r0 + k);
-        if (wide()) c[k] = *reinterpret_cast<const uint2*>(&o.count[2 * tid]);
-        else c[k].x = o.count[tid], c[k].y = c[k].x >> 16, c[k].x &= 0xFFFFu;
+        if (wide()) c[k] = *reinterpret_cast<const uint2*>(&o.count[2 * tid()]);
+        else c[k].x = o.count[tid()], c[k].y = c[k].x >> 16, c[k].x &= 0xFFFFu;
 #pragma unroll
-          for (int i = 0; i < PARTS; ++i) b[k][i] = *reinterpret_cast<const uint2*>(&o.weight[i][2 * tid]);
+          for (int i = 0; i < PARTS; ++i) b[k][i] = *reinterpret_cast<const uint2*>(&o.weight[i][2 * tid()]);
       }
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
@@ -606,16 +612,16 @@ struct Row {
     if (!MASS) m[0] = n[0], m[1] = n[1];
     uint64_t to = prefix(m[0] + m[1]);
     __syncthreads();
-    if (lane == 31) s.wscan[warp] = to;
-    if (tid == 0) s.border.found = false;
+    if (lane() == 31) s.wscan[warp()] = to;
+    if (tid() == 0) s.border.found = false;
     __syncthreads();
-    const uint64_t ahead = lane < warp ? s.wscan[lane] : 0;  // (warp < 16)
+    const uint64_t ahead = lane() < warp() ? s.wscan[lane()] : 0;  // (warp < 16)
     to += warp_sum64(ahead);
     uint64_t from = to - m[0] - m[1];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if (from < target && from + m[j] >= target) {
-        s.border.found = true, s.border.bin = 2 * tid + j, s.border.n = n[j], s.border.before = from;
+        s.border.found = true, s.border.bin = 2 * tid() + j, s.border.n = n[j], s.border.before = from;
       }
       from += m[j];
     }
@@ -625,7 +631,7 @@ struct Row {
 
   __device__ __forceinline__ void clear_ranges(bool mass) {
     __syncthreads();
-    for (int i = tid; i < SMP_BINS; i += SMP_THREADS) {
+    for (int i = tid(); i < SMP_BINS; i += SMP_THREADS) {
       s.count[i] = 0;
       if (mass) s.weight[0][i] = s.weight[1][i] = s.weight[2][i] = 0;
     }
@@ -661,10 +667,10 @@ struct Row {
       }
     });
     warp_bounds(lo, hi);
-    if (lane == 0) mine().lo[warp] = lo, mine().hi[warp] = hi;
+    if (lane() == 0) mine().lo[warp()] = lo, mine().hi[warp()] = hi;
     meet();
     lo = ~(uint64_t)0, hi = 0;
-    for (int i = lane; i < ctas * SMP_WARPS; i += 32) {
+    for (int i = lane(); i < ctas * SMP_WARPS; i += 32) {
       const auto& o = theirs(i / SMP_WARPS);
       lo = min(lo, o.lo[i % SMP_WARPS]), hi = max(hi, o.hi[i % SMP_WARPS]);
     }
@@ -709,7 +715,7 @@ struct Row {
   template <bool MASS, typename F>
   __device__ __forceinline__ void rank_few(uint64_t target, F in) {
     __syncthreads();
-    if (tid == 0) s.n_cand = 0, s.cut = 0;
+    if (tid() == 0) s.n_cand = 0, s.cut = 0;
     __syncthreads();
     each_left([&](float x, int token) {
       if (!in(x, token)) return;
@@ -722,29 +728,29 @@ struct Row {
   // Of the cluster's candidates the one that brings the sum of their weights to the target.
   __device__ __forceinline__ uint64_t rank_candidates(uint64_t target) {
     __syncthreads();
-    if (tid == 0) mine().count = s.n_cand;
+    if (tid() == 0) mine().count = s.n_cand;
     meet();
     // the candidates of all CTAs, two warps for each
     uint64_t *pairs = s.candidates(2), *weights = s.candidates(3);
-    const int their_n = lane < ctas ? (int)theirs(lane).count : 0;
+    const int their_n = lane() < ctas ? (int)theirs(lane()).count : 0;
     int to = their_n;
 #pragma unroll
     for (int o = 1; o < ROW_CLUSTER; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, to, o);
-      if (lane >= o) to += y;
+      if (lane() >= o) to += y;
     }
     const int total = __shfl_sync(0xffffffffu, to, ROW_CLUSTER - 1);
-    const int r = warp / 2, n = __shfl_sync(0xffffffffu, their_n, r), base = __shfl_sync(0xffffffffu, to, r) - n;
+    const int r = warp() / 2, n = __shfl_sync(0xffffffffu, their_n, r), base = __shfl_sync(0xffffffffu, to, r) - n;
     if (r < ctas) {
       SampleShared& o = *cluster.map_shared_rank(&s, r);
-      for (int i = tid & 63; i < n; i += 64)
+      for (int i = tid() & 63; i < n; i += 64)
         if (PCED_IN_BOUNDS(base + i < SMP_FEW, a.status))
           pairs[base + i] = o.candidates(0)[i], weights[base + i] = o.candidates(1)[i];
     }
     ++turn;
     __syncthreads();
-    if (tid < total) {
-      const uint64_t own = pairs[tid], ow = weights[tid];
+    if (tid() < total) {
+      const uint64_t own = pairs[tid()], ow = weights[tid()];
       uint64_t before = 0, last = ~(uint64_t)0;
 #pragma unroll 4
       for (int i = 0; i < total; ++i) {
@@ -766,7 +772,7 @@ struct Row {
     if (few || k <= a.V / SMP_EACH / 2) {
       clear_ranges(false);
       if (few) {
-        if (thread_max >= alive) count_in(coarse_of(thread_max));
+        if (s.thread_max[tid()] >= alive) count_in(coarse_of(s.thread_max[tid()]));
       } else {
         each_group([&](int g) {
           float top = -INFINITY;
@@ -806,10 +812,10 @@ struct Row {
       // Tokens of weight c weigh V c at most, so those of c = (1 - p) / 4 of all / V have no part in
       // the border; all is more than the threads' largest together.
       float b, c;
-      w.of(thread_max, b, c);
+      w.of(s.thread_max[tid()], b, c);
       const float some = (float)sum_up(warp_sum64((uint64_t)(b * (float)((uint64_t)1 << SMP_UNIT)))).all * UNIT;
       missed = 0.25f * (1.f - (float)share) * some;
-      counted = fmaxf(alive, (whole + log2f(missed / (float)a.V)) / w.ch);
+      counted = fmaxf(alive, (s.whole + log2f(missed / (float)a.V)) / w.ch);
       all = weigh_all<true>(counted).all;
     } else {
       all = weigh_kept<true>().all;
@@ -883,12 +889,12 @@ struct Row {
     uint32_t n[2];
     uint64_t places[2];
     gather_ranges<1>(n, places);
-    const float off = log2_range * (1.f / 120.f);  // (a 128th, and the roundings of a place)
+    const float off = s.log2_range * (1.f / 120.f);  // (a 128th, and the roundings of a place)
     float up[2], down[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float mean = n[j] ? ((float)places[j] / (float)n[j] - 1.f) * (1.f / 64) : 0.f;
-      const float y = ym - ((float)(2 * tid + j) + mean) * log2_range;
+      const float y = s.ym - ((float)(2 * tid() + j) + mean) * s.log2_range;
       up[j] = (float)n[j] * exp2f(y + off) * (1.f + 1.f / 4096);
       down[j] = (float)n[j] * exp2f(y - off);
     }
@@ -898,31 +904,31 @@ struct Row {
     for (int o = 1; o < 32; o <<= 1) {
       const float y = __shfl_up_sync(0xffffffffu, tu, o), z = __shfl_up_sync(0xffffffffu, td, o);
       const uint32_t c = __shfl_up_sync(0xffffffffu, tn, o);
-      if (lane >= o) tu += y, td += z, tn += c;
+      if (lane() >= o) tu += y, td += z, tn += c;
     }
     __syncthreads();
-    if (lane == 31) s.fscan[warp] = make_float2(tu, td), s.wkept[warp] = tn;
-    if (tid == 0) s.at[0] = s.at[1] = SMP_BINS, s.at[2] = s.at[3] = s.at[4] = 0;
+    if (lane() == 31) s.fscan[warp()] = make_float2(tu, td), s.wkept[warp()] = tn;
+    if (tid() == 0) s.at[0] = s.at[1] = SMP_BINS, s.at[2] = s.at[3] = s.at[4] = 0;
     __syncthreads();
     float all_up = 0.f, all_down = 0.f;
     for (int i = 0; i < SMP_WARPS; ++i) {
       const float2 o = s.fscan[i];
-      if (i < warp) tu += o.x, td += o.y, tn += s.wkept[i];
+      if (i < warp()) tu += o.x, td += o.y, tn += s.wkept[i];
       all_up += o.x, all_down += o.y;
     }
     const float slack = all * (1.f / (1 << 18));  // (sums in fp32)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float u = j ? tu : tu - up[1], d = j ? td : td - down[1];  // up to range 2 tid + j
-      if (fminf(u, all - (all_down - d)) + slack >= goal) atomicMin(&s.at[0], 2 * tid + j);
-      if (fmaxf(d, all - (all_up - u) - missed) - slack >= goal) atomicMin(&s.at[1], 2 * tid + j);
+      if (fminf(u, all - (all_down - d)) + slack >= goal) atomicMin(&s.at[0], 2 * tid() + j);
+      if (fmaxf(d, all - (all_up - u) - missed) - slack >= goal) atomicMin(&s.at[1], 2 * tid() + j);
     }
     __syncthreads();
     Window z;
     z.lo = s.at[0], z.hi = min(s.at[1], SMP_BINS - 1);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int b = 2 * tid + j;
+      const int b = 2 * tid() + j;
       const uint32_t c = j ? tn : tn - n[1];  // tokens up to range b
       if (b == z.lo - 1) s.at[2] = c;
       if (b == z.hi) s.at[3] = c;
@@ -937,8 +943,8 @@ struct Row {
     low = least;
     listed = false;
     __syncthreads();
-    if (tid == 0) s.n_list = 0;
-    for (int g = tid; g < groups; g += SMP_THREADS) s.group[g] = 0;
+    if (tid() == 0) s.n_list = 0;
+    for (int g = tid(); g < groups; g += SMP_THREADS) s.group[g] = 0;
     __syncthreads();
     uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
     uint64_t total = 0;
@@ -958,7 +964,7 @@ struct Row {
           if (k && v >= from) put(x, first + place);
         });
         const uint64_t v = sum.warp_steps();
-        if (lane == 0) s.group[g] = v;
+        if (lane() == 0) s.group[g] = v;
         total += v;
       });
     } else {
@@ -975,7 +981,7 @@ struct Row {
         atomicAdd(part + 2 * g + 1, (uint32_t)(m >> 21));
       });
       __syncthreads();
-      for (int g = tid; g < groups; g += SMP_THREADS) {
+      for (int g = tid(); g < groups; g += SMP_THREADS) {
         const uint64_t v = part[2 * g] + ((uint64_t)part[2 * g + 1] << 21);
         s.group[g] = v;
         total += v;
@@ -989,14 +995,14 @@ struct Row {
   __device__ __forceinline__ Sums sum_groups() {
     __syncthreads();
     uint64_t total = 0;
-    for (int g = tid; g < groups; g += SMP_THREADS) total += s.group[g];
+    for (int g = tid(); g < groups; g += SMP_THREADS) total += s.group[g];
     return sum_up(warp_sum64(total));
   }
 
   // Tokens from m + `below` on.
   __device__ __forceinline__ void keep_from(const double& below) {
     __syncthreads();
-    if (tid == 0) s.threshold = __double2float_ru((double)mx + below);
+    if (tid() == 0) s.threshold = __double2float_ru((double)mx + below);
     __syncthreads();
     const float x = s.threshold;
     if (x > cut.x) {
@@ -1014,7 +1020,7 @@ struct Row {
     // its group: each lane some of them in a row
     const int each = (groups + 31) / 32;
     uint64_t sum = 0;
-    for (int i = lane * each; i < min(groups, (lane + 1) * each); ++i) sum += s.group[i];
+    for (int i = lane() * each; i < min(groups, (lane() + 1) * each); ++i) sum += s.group[i];
     uint64_t to = prefix(sum);
     const int who = __ffs(__ballot_sync(0xffffffffu, to > left)) - 1;
     left -= __shfl_sync(0xffffffffu, to - sum, who);
@@ -1022,20 +1028,20 @@ struct Row {
     while (left >= s.group[g]) left -= s.group[g++];
     // a thread for each of its tokens
     static_assert(SMP_GROUP == SMP_THREADS, "a thread for each token of a group");
-    const int token = first + g * SMP_GROUP + tid;
-    const float x = at(g * SMP_GROUP + tid);
+    const int token = first + g * SMP_GROUP + tid();
+    const float x = at(g * SMP_GROUP + tid());
     const bool keep = x >= low && cut.keeps(x, token);
     const uint64_t m = keep ? steps_of(x) : 0;
     to = prefix(m);
-    if (lane == 31) s.wscan[warp] = to;
+    if (lane() == 31) s.wscan[warp()] = to;
     const uint32_t kept = __ballot_sync(0xffffffffu, keep);
-    if (lane == 0) s.wkept[warp] = kept;
+    if (lane() == 0) s.wkept[warp()] = kept;
     __syncthreads();
-    to += warp_sum64(lane < warp ? s.wscan[lane] : 0);
+    to += warp_sum64(lane() < warp() ? s.wscan[lane()] : 0);
     const bool mine_ = keep && to > left && to - m <= left;
     // (where rounding left the tokens' sum short of the group's: the last kept one)
-    const bool in_later_warps = __any_sync(0xffffffffu, lane > warp && lane < SMP_WARPS && s.wkept[lane & (SMP_WARPS - 1)]);
-    const bool last = !__syncthreads_or(mine_) && keep && !in_later_warps && !(kept >> lane >> 1);
+    const bool in_later_warps = __any_sync(0xffffffffu, lane() > warp() && lane() < SMP_WARPS && s.wkept[lane() & (SMP_WARPS - 1)]);
+    const bool last = !__syncthreads_or(mine_) && keep && !in_later_warps && !(kept >> lane() >> 1);
     if (mine_ || last) write(x, token, row, t, total);
   }
   // ... of the tokens that are left to this CTA: by ranges of tokens, then one by one
@@ -1043,7 +1049,7 @@ struct Row {
     const int shift = max(0, 22 - __clz(a.V));  // at most SMP_BINS ranges of at most SMP_FEW tokens
     static_assert(SMP_BINS == 1 << 10 && SMP_MAX_V <= SMP_BINS * SMP_FEW, "see there");
     clear_ranges(true);
-    if (tid == 0) s.n_cand = 0, s.cut = 0;
+    if (tid() == 0) s.n_cand = 0, s.cut = 0;
     each_left([&](float x, int token) {
       if (cut.keeps(x, token)) add_to_range(token >> shift, steps_of(x));
     });
@@ -1068,22 +1074,22 @@ struct Row {
       const float all = (float)total;
       const float rest = (float)((int64_t)(total - (uint64_t)all)) / all;
       const float log_all = logf(all * (1.f / (float)((uint64_t)1 << SMP_UNIT))) + rest;
-      a.logprob[row] = (mx == x ? 0.f : (x - mx) / t) - (log_all - ym * 0.693147181f);
+      a.logprob[row] = (mx == x ? 0.f : (x - mx) / t) - (log_all - s.ym * 0.693147181f);
     }
   }
   __device__ __forceinline__ uint64_t prefix(uint64_t v) const {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint64_t y = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += y;
+      if (lane() >= o) v += y;
     }
     return v;
   }
-  float thread_max;  // the largest logit that this thread loaded
 };
 
-template <typename T>
-__global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
+// ROOM: CTAs that an SM holds
+template <typename T, int ROOM>
+__global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   __shared__ __align__(16) SampleShared s;
   cg::cluster_group cluster = cg::this_cluster();
@@ -1094,9 +1100,11 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
   const T* src = (const T*)a.x + row * a.stride + start;
   const int phase = (int)((uintptr_t)src / sizeof(T) % W);
   const int groups = (phase + n + SMP_GROUP - 1) / SMP_GROUP;
-  Row<T> R = {a, s, cluster, reinterpret_cast<const uint4*>(src - phase), reinterpret_cast<float2*>(smem_raw), phase, n,
-              start - phase, groups, ctas, rank, tid, tid & 31, tid >> 5, 0};
+  Row<T> R = {a, s, cluster, reinterpret_cast<const uint4*>(src - phase), reinterpret_cast<float2*>(smem_raw), start - phase,
+              groups, ctas, 0};
   R.origin = 0.f, R.back = true;
+  if (tid == 0) s.from = phase, s.to = phase + n;
+  __syncthreads();
   const Exp2Entry entry = kExp2Table[tid / 16];
   pdl_wait();
   // ---- what the row asks for
@@ -1116,22 +1124,22 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
   R.w.ch = __fdiv_rn(lh, held);
   R.w.cl = __fdiv_rn(fmaf(-R.w.ch, held, lh) + ll, held);
   const float inverse = held * 0.693147181f;
-  R.thread_max = mx + 0.f;
+  s.thread_max[tid] = mx + 0.f;
   {
     const int hi = __reduce_max_sync(0xffffffffu, ordered(mx + 0.f)), lo = __reduce_min_sync(0xffffffffu, ordered(mn + 0.f));
-    if (R.lane == 0) R.mine().mx[R.warp] = hi, R.mine().mn[R.warp] = lo;
+    if (R.lane() == 0) R.mine().mx[R.warp()] = hi, R.mine().mn[R.warp()] = lo;
     cluster.barrier_arrive();
     if (tid == SMP_THREADS - 1 && least > 0.f) s.below = (double)t * log((double)least);  // (takes a microsecond)
     __syncwarp();
     cluster.barrier_wait();
-    const int r = R.lane >> 2;  // a CTA's sixteen by four lanes
+    const int r = R.lane() >> 2;  // a CTA's sixteen by four lanes
     int4 x = make_int4(INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN), y = make_int4(INT32_MAX, INT32_MAX, INT32_MAX, INT32_MAX);
     if (r < ctas) {
-      x = *reinterpret_cast<const int4*>(R.theirs(r).mx + 4 * (R.lane & 3));
-      y = *reinterpret_cast<const int4*>(R.theirs(r).mn + 4 * (R.lane & 3));
+      x = *reinterpret_cast<const int4*>(R.theirs(r).mx + 4 * (R.lane() & 3));
+      y = *reinterpret_cast<const int4*>(R.theirs(r).mn + 4 * (R.lane() & 3));
     }
     R.mx = mx = from_ordered(__reduce_max_sync(0xffffffffu, max(max(x.x, x.y), max(x.z, x.w))));
-    R.mn = mn = from_ordered(__reduce_min_sync(0xffffffffu, min(min(y.x, y.y), min(y.z, y.w))));
+    mn = from_ordered(__reduce_min_sync(0xffffffffu, min(min(y.x, y.y), min(y.z, y.w))));
     ++R.turn;
   }
   const bool bad = !(t >= 0.f) || !(u >= 0.f && u <= 1.f) || p != p || least != least;
@@ -1150,12 +1158,12 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
       R.each_of(g, [&](int, float x, int place) { at = x == mx ? min(at, (uint32_t)(R.first + place)) : at; });
     });
     at = __reduce_min_sync(0xffffffffu, at);
-    if (R.lane == 0) R.mine().sum[R.warp] = at;
+    if (R.lane() == 0) R.mine().sum[R.warp()] = at;
     cluster.sync();
-    if (rank == 0 && R.warp == 0) {
-      for (int i = R.lane; i < ctas * SMP_WARPS; i += 32) at = min(at, (uint32_t)R.theirs(i / SMP_WARPS).sum[i % SMP_WARPS]);
+    if (rank == 0 && R.warp() == 0) {
+      for (int i = R.lane(); i < ctas * SMP_WARPS; i += 32) at = min(at, (uint32_t)R.theirs(i / SMP_WARPS).sum[i % SMP_WARPS]);
       at = __reduce_min_sync(0xffffffffu, at);
-      if (R.lane == 0) {
+      if (R.lane() == 0) {
         a.token[row] = (int32_t)at;
         if (a.logprob) a.logprob[row] = 0.f;
       }
@@ -1163,7 +1171,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
     cluster.sync();
     return;
   }
-  R.set_weights(inverse, entry);
+  R.set_weights(mn, inverse, entry);
   // ---- cuts
   if (k > 1 && k < a.V) R.keep_top(k);
   if (!R.gone && p < 1.f) R.keep_share((double)p);
@@ -1188,12 +1196,17 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(SampleArgs a) {
 using namespace pced;
 using namespace pced_host;
 
-template <typename T>
-static cudaError_t launch_sample(SampleArgs a, int32_t rows, cudaStream_t stream) {
+template <typename T, int ROOM>
+static cudaError_t launch_sample(const SampleArgs& a, int32_t rows, int ctas, cudaStream_t stream) {
   static bool done[64];
-  const auto kernel = sample_kernel<T>;
-  cudaError_t e = allow_smem(kernel, (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2), done);
+  const auto kernel = sample_kernel<T, ROOM>;
+  constexpr size_t smem = (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2);
+  const cudaError_t e = allow_smem(kernel, smem, done);
   if (e != cudaSuccess) return e;
+  return launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, smem, stream, true, a);
+}
+template <typename T>
+static cudaError_t launch_sample_t(SampleArgs a, int32_t rows, cudaStream_t stream) {
   // CTAs of a row: as many as fit the SMs at once, two on each, while a part is more than a few
   // tokens a thread; and so many that the rows on the SMs fit L2 together
   const int64_t slots = 2 * (int64_t)num_sms(), bytes = (int64_t)a.V * sizeof(T);
@@ -1202,8 +1215,9 @@ static cudaError_t launch_sample(SampleArgs a, int32_t rows, cudaStream_t stream
          (2 * ctas * (int64_t)rows <= slots || (rows < slots / ctas ? rows : slots / ctas) * bytes > SMP_L2))
     ctas *= 2;
   a.per = (a.V + ctas - 1) / ctas;
-  constexpr size_t smem = (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2);
-  return launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, smem, stream, true, a);
+  // (one CTA an SM has twice the registers)
+  return (int64_t)rows * ctas <= num_sms() ? launch_sample<T, 1>(a, rows, ctas, stream)
+                                           : launch_sample<T, 2>(a, rows, ctas, stream);
 }
 
 extern "C" pced_status pced_sample(const void* x, int32_t type, int64_t stride, int32_t rows, int32_t V, const float* u,
@@ -1221,7 +1235,7 @@ extern "C" pced_status pced_sample(const void* x, int32_t type, int64_t stride, 
   if ((int64_t)rows * ROW_CLUSTER > INT32_MAX) return fail(PCED_ERR_UNSUPPORTED, "%s: too many rows", fn);
   if (num_sms() <= 0) return fail(PCED_ERR_NO_DEVICE, "%s: no CUDA device", fn);
   const SampleArgs a = {x, stride, V, 0, u, temperature, top_k, top_p, min_p, token, logprob, status};
-  const cudaError_t e = type == PCED_IN_F32 ? launch_sample<float>(a, rows, (cudaStream_t)stream)
-                                             : launch_sample<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
+  const cudaError_t e = type == PCED_IN_F32 ? launch_sample_t<float>(a, rows, (cudaStream_t)stream)
+                                             : launch_sample_t<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
   return e == cudaSuccess ? PCED_OK : cuda_status(e, "sample launch");
 }
