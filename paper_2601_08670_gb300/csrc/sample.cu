@@ -174,11 +174,7 @@ struct Ranges {
   float top, per;                           // the first one's upper end; ranges of a unit of x
   __device__ __forceinline__ void set(float top_, float width) {  // SMP_BINS - 4 ranges from top down
     top = top_;
-    per = (float)(SMP_BINS - 4) / width;
-  }
-  // a number that all of the ranges up to `bin` are above
-  __device__ __forceinline__ float below(int bin) const {
-    return bin >= SMP_BINS - 4 ? -INFINITY : top - ((float)bin + 1.25f) / per;
+    per = (float)(SMP_BINS - 4) / fmaxf(width, 1e-30f);
   }
   // (1 + 64 (top - x) per, rounded)
   __device__ __forceinline__ int place(float x) const {
@@ -201,7 +197,7 @@ struct SampleShared {
   uint64_t group[SMP_MAX_GROUPS];  // kept weight (on its way in two numbers, 21 bits in the first)
   uint32_t n_list, n_cand;
   int from, to;                  // places of this CTA's part
-  float ym, whole, log2_range;   // log2 of the largest weight; N; log2 of weights at a range's ends, the difference
+  float ym, inverse;             // log2 of the largest weight; t / log2(e)
   float thread_max[SMP_THREADS]; // the largest logit that a thread loaded first
   int at[5];
   uint64_t wscan[SMP_WARPS];
@@ -214,7 +210,7 @@ struct SampleShared {
   // what the cluster's warps tell one another: two of each, by turns, with a barrier of the
   // cluster between a write and its reads, so that the next write to one comes after them
   struct alignas(16) Told {
-    int mx[SMP_WARPS], mn[SMP_WARPS];
+    int mx[SMP_WARPS];
     uint64_t sum[SMP_WARPS], lo[SMP_WARPS], hi[SMP_WARPS];
     uint32_t count;
   } told[2];
@@ -247,7 +243,7 @@ struct Row {
   float origin;                        // see moved()
   bool back;                           // see each_group()
   float alive;                         // smaller logits have weights that no cut asks about
-  Ranges coarse;
+  float whole;                         // N: the largest weight lies in (1/2, 1] 2^N
   Cut cut;
   float low;                           // smaller logits are not kept
   bool listed;                         // the others' places are in the list (each CTA's own matter, as is `low`)
@@ -426,11 +422,10 @@ struct Row {
   }
 
   // m, N and the table for temperature t (inverse: 1 / w.ch, entry: of the table)
-  __device__ __forceinline__ void set_weights(float mn, float inverse, Exp2Entry entry) {
+  __device__ __forceinline__ void set_weights(float inverse, Exp2Entry entry) {
     if (!(fabsf(mx) * w.ch <= 8192.f)) {
       origin = mx;
       s.thread_max[tid()] = moved(s.thread_max[tid()]);
-      mn = mx == INFINITY ? 0.f : fmaxf(mn - mx, -3e38f);
       mx = 0.f;
     }
     const float y = __fmul_rn(mx, w.ch), top = ceilf(y);
@@ -443,12 +438,10 @@ struct Row {
     const uint32_t j = tid() / 16;
     s.table[j][tid() % 16] =
         make_float2(__uint_as_float(entry.bits - (j << 18) - ((uint32_t)(int)top << 23)), entry.rest);
-    const float width = fminf((SMP_ALIVE + 1.f) * inverse, fmaxf(mx - mn, 1e-30f));
-    coarse.set(mx, width);
+    whole = top;
     if (tid() == 0) {
       s.ym = (y - top) + fmaf(mx, w.cl, fmaf(mx, w.ch, -y));
-      s.log2_range = w.ch * width * (1.f / (SMP_BINS - 4));
-      s.whole = top;
+      s.inverse = inverse;
     }
     __syncthreads();
   }
@@ -553,10 +546,20 @@ struct Row {
     }
     return sum_up(total);
   }
-  __device__ __forceinline__ int coarse_of(float x) const { return min(coarse.place(x) >> 6, SMP_BINS - 1); }
+  // Where a logit lies below 2^N, in 2048ths of the weights' log2 (by the larger part of y, which
+  // rises with x; the fp32 number 4096 + such has them in its low bits), and its range, a 32nd.
+  __device__ __forceinline__ int place_of(float x) const {
+    const float p = __fmul_rn(fmaxf(x, w.floor), w.ch);
+    return __float_as_int(__fadd_rn(__fsub_rn(whole, p), 4096.f)) - __float_as_int(4096.f);
+  }
+  __device__ __forceinline__ int range_of(float x) const { return min(place_of(x) >> 6, SMP_BINS - 1); }
+  // a logit that those of the ranges up to `bin` are not below
+  __device__ __forceinline__ float below(int bin) const {
+    return bin >= SMP_BINS - 1 ? -INFINITY : (whole - ((float)bin + 1.125f) * (1.f / 32)) * s.inverse;
+  }
   // ... with its place in the range
   __device__ __forceinline__ void count_place(float x) {
-    const int v = coarse.place(x), bin = min(v >> 6, SMP_BINS - 1);
+    const int v = place_of(x), bin = min(v >> 6, SMP_BINS - 1);
     count_in(bin);
     atomicAdd(&s.weight[0][bin], (uint32_t)v & 63u);
   }
@@ -772,18 +775,18 @@ struct Row {
     if (few || k <= a.V / SMP_EACH / 2) {
       clear_ranges(false);
       if (few) {
-        if (s.thread_max[tid()] >= alive) count_in(coarse_of(s.thread_max[tid()]));
+        if (s.thread_max[tid()] >= alive) count_in(range_of(s.thread_max[tid()]));
       } else {
         each_group([&](int g) {
           float top = -INFINITY;
           each_of(g, [&](int, float x, int) { top = fmaxf(top, x); });
-          if (top >= alive) count_in(coarse_of(top));
+          if (top >= alive) count_in(range_of(top));
         });
       }
       meet();
       const Border b = find_border<false>((uint64_t)k);
       if (b.found) {
-        list(fmaxf(alive, coarse.below((int)b.bin)));
+        list(fmaxf(alive, below((int)b.bin)));
         try_solo();
         if (gone) return;
       }
@@ -793,12 +796,12 @@ struct Row {
       return;
     }
     clear_ranges(false);
-    each_left([&](float x, int) { count_in(coarse_of(x)); });
+    each_left([&](float x, int) { count_in(range_of(x)); });
     meet();
     const Border b = find_border<false>((uint64_t)k);
     if (!b.found) return;  // there are no more than k
-    if (!listed) list(fmaxf(alive, coarse.below((int)b.bin)));
-    cut_among<false>(b.n, k - b.before, [&](float x, int) { return coarse_of(x) == (int)b.bin; });
+    if (!listed) list(fmaxf(alive, below((int)b.bin)));
+    cut_among<false>(b.n, k - b.before, [&](float x, int) { return range_of(x) == (int)b.bin; });
   }
 
   // The shortest first part of the kept tokens that holds `share` of their weight.
@@ -815,7 +818,7 @@ struct Row {
       w.of(s.thread_max[tid()], b, c);
       const float some = (float)sum_up(warp_sum64((uint64_t)(b * (float)((uint64_t)1 << SMP_UNIT)))).all * UNIT;
       missed = 0.25f * (1.f - (float)share) * some;
-      counted = fmaxf(alive, (s.whole + log2f(missed / (float)a.V)) / w.ch);
+      counted = fmaxf(alive, (whole + log2f(missed / (float)a.V)) / w.ch);
       all = weigh_all<true>(counted).all;
     } else {
       all = weigh_kept<true>().all;
@@ -824,7 +827,7 @@ struct Row {
     const uint64_t target = want < 1.0 ? 1 : (uint64_t)want;
     const Window win = window((float)all * UNIT, (float)want * UNIT, missed);
     if (win.lo == SMP_BINS) return;  // all are kept
-    const float least = fmaxf(counted, coarse.below(win.hi));
+    const float least = fmaxf(counted, below(win.hi));
     if (!solo && win.through <= SMP_SOLO) {
       listed = false;
       list(least);
@@ -834,13 +837,13 @@ struct Row {
     const int from = 64 * win.lo, to = win.hi == SMP_BINS - 1 ? INT32_MAX : 64 * (win.hi + 1);
     const Cut old = cut;
     const auto inside = [&](float x, int token) {
-      const int v = coarse.place(x);
+      const int v = place_of(x);
       return x >= least && v >= from && v < to && old.keeps(x, token);
     };
     uint64_t above = 0;
     if (solo) {
       each_left([&](float x, int token) {
-        if (coarse.place(x) < from && old.keeps(x, token)) above += steps_of(x);
+        if (place_of(x) < from && old.keeps(x, token)) above += steps_of(x);
       });
       above = sum_up(warp_sum64(above)).all;
     } else {
@@ -852,8 +855,8 @@ struct Row {
     } else {
       // the window's weight in finer ranges (a quarter of them where the cluster weighs)
       Ranges fine;
-      fine.set(fminf(mx, mx - ((float)win.lo - 0.25f) / coarse.per),
-               fmaxf((float)(min(win.hi, SMP_BINS - 4) - win.lo) + 1.5f, 1.f) / coarse.per);
+      const float top = fminf(mx, (whole - ((float)win.lo - 0.125f) * (1.f / 32)) * s.inverse);
+      fine.set(top, win.hi == SMP_BINS - 1 ? top - least : ((float)(win.hi - win.lo) + 1.25f) * (1.f / 32) * s.inverse);
       const int shift = solo ? 6 : 8, bins = solo ? SMP_BINS : SMP_FINE;
       const auto bin_of = [&](float x) { return min(max(fine.place(x), 0) >> shift, bins - 1); };
       clear_ranges(true);
@@ -878,8 +881,8 @@ struct Row {
     }
   }
   // Ranges that can hold the border: a range's tokens weigh as many times the weight at their
-  // mean place, by what their places are rounded (a 128th of a range) more or less, and by the
-  // spread of a range more (2^-13 of it).  Summed from the first range on, and from the last
+  // mean place, by what their places are rounded more or less, and by the spread of a range more
+  // (2^-14 of it); the last one takes what lies lower too, and may weigh nothing.  Summed from the first range on, and from the last
   // one back, where `missed` comes on top, from the weight of all.
   struct Window {
     int lo, hi;                        // lo = SMP_BINS: no range
@@ -889,14 +892,14 @@ struct Row {
     uint32_t n[2];
     uint64_t places[2];
     gather_ranges<1>(n, places);
-    const float off = s.log2_range * (1.f / 120.f);  // (a 128th, and the roundings of a place)
+    const float off = 1.f / 4096 + fabsf(whole) * (1.f / (1 << 23));  // (the roundings of a place and of y)
     float up[2], down[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float mean = n[j] ? ((float)places[j] / (float)n[j] - 1.f) * (1.f / 64) : 0.f;
-      const float y = s.ym - ((float)(2 * tid() + j) + mean) * s.log2_range;
-      up[j] = (float)n[j] * exp2f(y + off) * (1.f + 1.f / 4096);
-      down[j] = (float)n[j] * exp2f(y - off);
+      const float mean = n[j] ? (float)places[j] / (float)n[j] : 0.f;
+      const float y = -(64.f * (float)(2 * tid() + j) + mean) * (1.f / 2048);
+      up[j] = (float)n[j] * exp2f(y + off) * (1.f + 1.f / 8192);
+      down[j] = 2 * tid() + j == SMP_BINS - 1 ? 0.f : (float)n[j] * exp2f(y - off);
     }
     float tu = up[0] + up[1], td = down[0] + down[1];
     uint32_t tn = n[0] + n[1];
@@ -948,6 +951,7 @@ struct Row {
     __syncthreads();
     uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
     uint64_t total = 0;
+    const bool none = cut.x == -INFINITY;
     const auto put = [&](float x, int token) {
       const uint32_t i = atomicAdd(&s.n_list, 1u);
       if (i < SMP_LIST) left[i] = make_float2(x, __int_as_float(token));
@@ -956,12 +960,12 @@ struct Row {
       each_group([&](int g) {
         Sum sum;
         each_of(g, [&](int, float x, int place) {
-          const int v = coarse.place(x);
-          const bool k = x >= low && v < to && cut.keeps(x, first + place);
+          const int v = place_of(x);
+          const bool k = none || cut.keeps(x, first + place);
           float b, c;
           w.of(x, b, c);
           sum.add(k && v < from ? b : 0.f, c);
-          if (k && v >= from) put(x, first + place);
+          if (v >= from && v < to && k && x >= low) put(x, first + place);
         });
         const uint64_t v = sum.warp_steps();
         if (lane() == 0) s.group[g] = v;
@@ -969,7 +973,7 @@ struct Row {
       });
     } else {
       each_left([&](float x, int token) {
-        const int v = coarse.place(x);
+        const int v = place_of(x);
         if (v >= to || !cut.keeps(x, token)) return;
         if (v >= from) {
           put(x, token);
@@ -1048,21 +1052,27 @@ struct Row {
   __device__ __forceinline__ void draw_solo(uint64_t left, int64_t row, float t, uint64_t total) {
     const int shift = max(0, 22 - __clz(a.V));  // at most SMP_BINS ranges of at most SMP_FEW tokens
     static_assert(SMP_BINS == 1 << 10 && SMP_MAX_V <= SMP_BINS * SMP_FEW, "see there");
-    clear_ranges(true);
-    if (tid() == 0) s.n_cand = 0, s.cut = 0;
-    each_left([&](float x, int token) {
-      if (cut.keeps(x, token)) add_to_range(token >> shift, steps_of(x));
-    });
+    int bin = -1;
+    uint64_t before = 0;
+    if (solo > SMP_RANK) {
+      clear_ranges(true);
+      each_left([&](float x, int token) {
+        if (cut.keeps(x, token)) add_to_range(token >> shift, steps_of(x));
+      });
+      __syncthreads();
+      const Border b = find_border<true>(left + 1);
+      bin = b.bin, before = b.before;
+    }
     __syncthreads();
-    const Border b = find_border<true>(left + 1);
-    const int bin = b.bin;
+    if (tid() == 0) s.n_cand = 0, s.cut = 0;
+    __syncthreads();
     each_left([&](float x, int token) {
-      if (token >> shift != bin || !cut.keeps(x, token)) return;
+      if ((bin >= 0 && token >> shift != bin) || !cut.keeps(x, token)) return;
       const uint32_t i = atomicAdd(&s.n_cand, 1u);
       if (PCED_IN_BOUNDS(i < SMP_FEW, a.status))
         s.candidates(0)[i] = (uint32_t)~token, s.candidates(1)[i] = steps_of(x);
     });
-    const int token_drawn = (int)~(uint32_t)rank_candidates(left + 1 - b.before);
+    const int token_drawn = (int)~(uint32_t)rank_candidates(left + 1 - before);
     each_left([&](float x, int token) {
       if (token == token_drawn) write(x, token, row, t, total);
     });
@@ -1111,14 +1121,9 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
   const float t = a.temperature ? a.temperature[row] : 1.f, u = a.u[row];
   const float p = a.top_p ? a.top_p[row] : 1.f, least = a.min_p ? a.min_p[row] : 0.f;
   const int k = a.top_k ? a.top_k[row] : 0;
-  // ---- its largest and smallest logit
-  float mx = -INFINITY, mn = INFINITY;
-  R.each_group([&](int g) {
-    R.each_of(g, [&](int, float x, int) {
-      mx = fmaxf(mx, x);
-      mn = x > -INFINITY ? fminf(mn, x) : mn;
-    });
-  });
+  // ---- its largest logit
+  float mx = -INFINITY;
+  R.each_group([&](int g) { R.each_of(g, [&](int, float x, int) { mx = fmaxf(mx, x); }); });
   // (the reciprocals come while the last loads are on their way)
   const float held = fminf(fmaxf(t, 1e-37f), 1e30f), lh = 1.44269502f, ll = 1.92596303e-08f;
   R.w.ch = __fdiv_rn(lh, held);
@@ -1126,20 +1131,16 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
   const float inverse = held * 0.693147181f;
   s.thread_max[tid] = mx + 0.f;
   {
-    const int hi = __reduce_max_sync(0xffffffffu, ordered(mx + 0.f)), lo = __reduce_min_sync(0xffffffffu, ordered(mn + 0.f));
-    if (R.lane() == 0) R.mine().mx[R.warp()] = hi, R.mine().mn[R.warp()] = lo;
+    const int hi = __reduce_max_sync(0xffffffffu, ordered(mx + 0.f));
+    if (R.lane() == 0) R.mine().mx[R.warp()] = hi;
     cluster.barrier_arrive();
     if (tid == SMP_THREADS - 1 && least > 0.f) s.below = (double)t * log((double)least);  // (takes a microsecond)
     __syncwarp();
     cluster.barrier_wait();
     const int r = R.lane() >> 2;  // a CTA's sixteen by four lanes
-    int4 x = make_int4(INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN), y = make_int4(INT32_MAX, INT32_MAX, INT32_MAX, INT32_MAX);
-    if (r < ctas) {
-      x = *reinterpret_cast<const int4*>(R.theirs(r).mx + 4 * (R.lane() & 3));
-      y = *reinterpret_cast<const int4*>(R.theirs(r).mn + 4 * (R.lane() & 3));
-    }
+    int4 x = make_int4(INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN);
+    if (r < ctas) x = *reinterpret_cast<const int4*>(R.theirs(r).mx + 4 * (R.lane() & 3));
     R.mx = mx = from_ordered(__reduce_max_sync(0xffffffffu, max(max(x.x, x.y), max(x.z, x.w))));
-    mn = from_ordered(__reduce_min_sync(0xffffffffu, min(min(y.x, y.y), min(y.z, y.w))));
     ++R.turn;
   }
   const bool bad = !(t >= 0.f) || !(u >= 0.f && u <= 1.f) || p != p || least != least;
@@ -1171,7 +1172,7 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
     cluster.sync();
     return;
   }
-  R.set_weights(mn, inverse, entry);
+  R.set_weights(inverse, entry);
   // ---- cuts
   if (k > 1 && k < a.V) R.keep_top(k);
   if (!R.gone && p < 1.f) R.keep_share((double)p);
