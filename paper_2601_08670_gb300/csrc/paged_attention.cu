@@ -21,9 +21,11 @@ namespace pced {
 // 64 rows of bf16 keys and values, as D/64 boxes of 64 columns
 template <int D_, bool PK>
 struct TileBf16 {
-  static constexpr int D = D_, STAGES = AttCfg<D>::STAGES, TILE_BYTES = AttCfg<D>::TILE_BYTES;
+  static constexpr int D = D_, TILE_BYTES = AttCfg<D>::TILE_BYTES;
   static constexpr int COLS = AttCfg<D>::BOXES, ROW_BYTES = 128;
   static constexpr bool SCALED = false;
+  static constexpr int stages(bool) { return AttCfg<D>::STAGES; }
+  static constexpr int producers(bool) { return 1; }
   // B column g of S^T = K Q^T is head g; with PK columns 4-7 repeat heads 0-3
   uint32_t qf[D / 16][2];
   __device__ __forceinline__ void load_q(const PagedAttArgs& a, int s, int h, int lane) {

@@ -23,7 +23,6 @@ namespace pced {
 constexpr int PATT_MAX_CTAS = 256;  // sizes the records and counters of the workspace
 constexpr int PATT_GRAN = 16;       // rows of a consumer warp, and of a small box
 constexpr int PATT_EPI = 4;         // epilogue warps
-constexpr int PATT_THREADS = (ATT_CONSUMERS + 1 + PATT_EPI) * 32;
 
 struct PagedAttArgs {
   pced_paged_cache c;
@@ -94,19 +93,25 @@ __device__ __forceinline__ bool bar_sync_warps(uint32_t bar, uint32_t& phase, in
 // Shared memory of a CTA over the tiles of `Tile`, which says what the pools hold and
 // does the math on it (TileBf16 in paged_attention.cu, TileE4m3 in paged_attention8.cu):
 //   D, PK                 head dim; whether the two parts of P share an MMA
-//   STAGES, TILE_BYTES    of the ring; bytes of K (or V) in a stage
+//   TILE_BYTES            of K (or V) in a stage
 //   COLS, ROW_BYTES       boxes side by side in a tile's rows, bytes of a box's row
 //   SCALED                whether a part's two scales come with it
+//   stages, producers     of the ring; warps that fill it, which take the CTA's tiles by turns
+//                         (small: every tile in boxes of 16 rows)
 //   load_q, math, fold, store   a consumer warp's queries, its part of a tile, its partials
-template <class Tile>
+constexpr size_t align16(size_t x) { return (x + 15) / 16 * 16; }
+template <class Tile, bool SMALL>
 struct PagedCfg {
   static constexpr int D = Tile::D;
-  static constexpr int STAGES = Tile::STAGES;  // odd: consecutive uses of a stage alternate warpgroups
+  static constexpr int STAGES = Tile::stages(SMALL);  // odd: consecutive uses of a stage alternate warpgroups
   static constexpr int STAGE_BYTES = 2 * Tile::TILE_BYTES;
   static constexpr int PARTIALS = AttCfg<D>::PARTIALS;
+  static constexpr int PRODUCERS = Tile::producers(SMALL);
+  static constexpr int SCALES_OF = SMALL ? ATT_BLOCK_N / PATT_GRAN : 1;  // blocks of a tile
+  static constexpr int THREADS = (ATT_CONSUMERS + PRODUCERS + PATT_EPI) * 32;
   static constexpr size_t BARS = (2 * STAGES + 4) * 8;
   static constexpr size_t DESC = (size_t)STAGES * 4;
-  static constexpr size_t SCALES = Tile::SCALED ? (size_t)STAGES * (ATT_BLOCK_N / PATT_GRAN) * 8 : 0;
+  static constexpr size_t SCALES = Tile::SCALED ? align16((size_t)STAGES * SCALES_OF * 8) : 0;
   static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE_BYTES + BARS + SCALES + (size_t)PARTIALS * 4 +
                                  (3 * PAGED_MAX_S + 1) * 4 + DESC + 64;
   static_assert(STAGES % 2 == 1 && (BARS + SCALES) % 16 == 0, "the partials are read as float4");
@@ -305,11 +310,11 @@ __device__ __forceinline__ bool finish_piece(const PagedAttArgs& a, const PagedP
 // SMALL: block_rows is no multiple of 64, so every tile comes in 16-row boxes,
 // each of its own block.
 template <class Tile, bool SMALL>
-__global__ void __launch_bounds__(PATT_THREADS, 1)
+__global__ void __launch_bounds__(PagedCfg<Tile, SMALL>::THREADS, 1)
     paged_attention_kernel(const __grid_constant__ CUtensorMap ktile, const __grid_constant__ CUtensorMap vtile,
                            const __grid_constant__ CUtensorMap kbox, const __grid_constant__ CUtensorMap vbox,
                            PagedAttArgs a) {
-  using C = PagedCfg<Tile>;
+  using C = PagedCfg<Tile, SMALL>;
   constexpr int D = Tile::D;
   constexpr int NG = ATT_BLOCK_N / PATT_GRAN;  // small boxes of a tile
   extern __shared__ uint8_t smem_raw[];
@@ -321,7 +326,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
   const uint32_t bar_empty = bar_full + C::STAGES * 8;
   const uint32_t bar_pfull = bar_empty + C::STAGES * 8, bar_pempty = bar_pfull + 8;
   const uint32_t bar_epi = bar_pempty + 8, bar_last = bar_epi + 8;
-  float2* scales = reinterpret_cast<float2*>(gbase + C::STAGES * C::STAGE_BYTES + C::BARS);  // [STAGES][NG]
+  float2* scales = reinterpret_cast<float2*>(gbase + C::STAGES * C::STAGE_BYTES + C::BARS);  // [STAGES][SCALES_OF]
   float* ms = reinterpret_cast<float*>(gbase + C::STAGES * C::STAGE_BYTES + C::BARS + C::SCALES);
   float* ls = ms + ATT_CONSUMERS * ATT_MAX_G;
   float* os = ls + ATT_CONSUMERS * ATT_MAX_G;
@@ -336,7 +341,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
 
   if (tid == 0) {
     for (int i = 0; i < C::STAGES; ++i) {
-      mbar_init(bar_full + 8 * i, Tile::SCALED ? 1 + NG : 1);
+      mbar_init(bar_full + 8 * i, Tile::SCALED ? 1 + C::SCALES_OF : 1);
       mbar_init(bar_empty + 8 * i, 4);  // the four warps of the consuming warpgroup
     }
     mbar_init(bar_pfull, ATT_CONSUMERS);
@@ -352,7 +357,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
     tma_prefetch_desc(&vbox);
   }
   pdl_wait();
-  for (int i = tid; i < S; i += PATT_THREADS) {
+  for (int i = tid; i < S; i += C::THREADS) {
     const int32_t n = paged_len(a.c, i, a.status);
     uint32_t rows = n;
     if (a.sel) rows = min((uint32_t)a.n_sel, (rows + P - 1) / P) * P;
@@ -384,19 +389,23 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
   const int32_t r_begin = (int32_t)min((int64_t)total, (int64_t)blockIdx.x * per);
   const int32_t r_end = min(total - r_begin, per) + r_begin;
 
-  if (warp == ATT_CONSUMERS) {
+  if (warp >= ATT_CONSUMERS && warp < ATT_CONSUMERS + C::PRODUCERS) {
     // ------------------------------------------------------------ producer
+    constexpr int NP = C::PRODUCERS;
+    // (A stage has one producer: it waits for every release of the stage in turn, so that the parity
+    // tells which; with two, one could take the release before the last for the last.)
+    static_assert(C::STAGES % NP == 0, "a stage is always the same producer's");
     const uint64_t pol = policy_evict_first();
-    uint32_t st = 0, ph = 0, it = 0;
+    uint32_t st = warp - ATT_CONSUMERS, ph = 0, it = st;
     bool ok = true;
-    for (int32_t p0 = r_begin; p0 < r_end && ok; p0 += 32) {
-      // this lane's tile: pool row of each of its parts, live rows of the parts
-      int32_t row[SMALL ? NG : 1];
+    for (int32_t p0 = r_begin + (int32_t)it; p0 < r_end && ok; p0 += 32 * NP) {
+      // this lane's tile: pool row of each of its parts, live rows of the parts, their pages
+      int32_t row[SMALL ? NG : 1], page[Tile::SCALED ? (SMALL ? NG : 1) : 1];
       uint32_t live4 = 0;
-      row[0] = 0;
-      const int nt = min(32, r_end - p0);
+      row[0] = page[0] = 0;
+      const int nt = min(32, (r_end - p0 + NP - 1) / NP);
       if (lane < nt) {
-        const PagedPiece pc = plan.at(p0 + lane, r_end);
+        const PagedPiece pc = plan.at(p0 + NP * lane, r_end);
         const int32_t n = lens[pc.s];
         const int32_t nb = (int32_t)((uint32_t)(n + P - 1) / (uint32_t)P);
         const int32_t* sel = a.sel ? a.sel + ((int64_t)pc.s * Hkv + pc.h) * a.n_sel : nullptr;
@@ -406,6 +415,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
           const uint32_t r = (uint32_t)pc.t0 * ATT_BLOCK_N + i * PATT_GRAN;  // row of the list
           const int32_t place = (int32_t)(r / (uint32_t)P), at = (int32_t)(r - (uint32_t)place * P);
           row[i] = 0;
+          if (Tile::SCALED) page[i] = 0;
           if (place >= places) continue;
           const int32_t j = sel ? sel[place] : place;
           if (j < 0 || j >= nb) {
@@ -416,6 +426,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
           if (blk < 0) continue;
           if (!PCED_IN_BOUNDS(in_pool(a.c, (int64_t)blk * Hkv + pc.h, at), a.status)) continue;
           row[i] = (blk * Hkv + pc.h) * P + at;
+          if (Tile::SCALED) page[i] = blk * Hkv + pc.h;
           const int32_t left = n - j * P - at;  // live rows from here on
           if (SMALL) {
             live4 |= (uint32_t)max(0, min(left, PATT_GRAN)) << (8 * i);
@@ -425,7 +436,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
           }
         }
       }
-      for (int t = 0; t < nt; ++t, ++it) {
+      for (int t = 0; t < nt; ++t, it += NP) {
         if (!mbar_wait_warp(bar_empty + 8 * st, ph ^ 1u, a.status)) {
           ok = false;
           break;
@@ -436,17 +447,16 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
         const uint32_t on = elect_one();
         if (on) desc[st] = lv;
         if constexpr (Tile::SCALED) {  // they come as the rows do: a load that waits would hold the copies up
-          int32_t rs = r0;
+          int32_t pg = __shfl_sync(0xffffffffu, page[0], t);
           if (SMALL) {
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {
-              const int32_t x = __shfl_sync(0xffffffffu, row[i], t);
-              if (i == lane) rs = x;
+            for (int i = 1; i < NG; ++i) {
+              const int32_t x = __shfl_sync(0xffffffffu, page[i], t);
+              if (i == lane) pg = x;
             }
           }
-          if (lane < NG) {
-            if (lv >> (8 * lane) & 0xFFu)
-              copy_async_8(smem_u32(scales + st * NG + lane), a.scale + (uint32_t)rs / (uint32_t)P);
+          if (lane < C::SCALES_OF) {
+            if (lv >> (8 * lane) & 0xFFu) copy_async_8(smem_u32(scales + st * C::SCALES_OF + lane), a.scale + pg);
             mbar_arrive_copies(fb);
           }
         }
@@ -475,23 +485,25 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
             tma_load_3d((v ? sv : sk) + (col * ATT_BLOCK_N + g * PATT_GRAN) * Tile::ROW_BYTES, v ? &vbox : &kbox, fb, 0,
                         rg, col, pol);
         }
-        if (++st == C::STAGES) {
-          st = 0;
+        st += NP;
+        if (st >= C::STAGES) {
+          st -= C::STAGES;
           ph ^= 1u;
         }
       }
     }
     if (!ok) {
-      // let copies already in flight land before the CTA exits
-      for (uint32_t j = (it >= C::STAGES ? it - C::STAGES : 0); j < it; ++j)
-        mbar_wait(bar_full + 8 * (j % C::STAGES), (j / C::STAGES) & 1u, a.status);
+      // let this warp's copies in flight land before the CTA exits: those of its tiles before `it`
+      // whose stage it has not waited for again
+      for (uint32_t j = it; j >= NP && it - (j - NP) <= C::STAGES; j -= NP)
+        mbar_wait(bar_full + 8 * ((j - NP) % C::STAGES), ((j - NP) / C::STAGES) & 1u, a.status);
     }
     return;
   }
 
-  if (warp > ATT_CONSUMERS) {
+  if (warp >= ATT_CONSUMERS + C::PRODUCERS) {
     // ------------------------------------------------------------ epilogue
-    const int et = tid - (ATT_CONSUMERS + 1) * 32;
+    const int et = tid - (ATT_CONSUMERS + C::PRODUCERS) * 32;
     // sequences without rows
     for (int s = blockIdx.x; s < S; s += gridDim.x)
       if (tiles[s] == 0) {
@@ -534,7 +546,7 @@ __global__ void __launch_bounds__(PATT_THREADS, 1)
       if (live) {
         const uint32_t sk = smem0 + st * C::STAGE_BYTES;
         tile.math(A, sk, sk + Tile::TILE_BYTES, kb, kb + live,
-                  Tile::SCALED ? scales[st * NG + (warp & 3)] : make_float2(1.f, 1.f), a.scale_log2, lane);
+                  Tile::SCALED ? scales[st * C::SCALES_OF + (SMALL ? warp & 3 : 0)] : make_float2(1.f, 1.f), a.scale_log2, lane);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_empty + 8 * st);
@@ -581,9 +593,9 @@ template <class Tile, bool SMALL>
 cudaError_t launch_paged(const CUtensorMap (&maps)[4], const PagedAttArgs& a, int ctas, cudaStream_t stream) {
   const auto kernel = paged_attention_kernel<Tile, SMALL>;
   static bool done[64];
-  const cudaError_t e = pced_host::allow_smem(kernel, PagedCfg<Tile>::SMEM, done);
+  const cudaError_t e = pced_host::allow_smem(kernel, PagedCfg<Tile, SMALL>::SMEM, done);
   if (e != cudaSuccess) return e;
-  return pced_host::launch_pdl(kernel, dim3(ctas), PATT_THREADS, PagedCfg<Tile>::SMEM, stream, maps[0], maps[1],
+  return pced_host::launch_pdl(kernel, dim3(ctas), PagedCfg<Tile, SMALL>::THREADS, PagedCfg<Tile, SMALL>::SMEM, stream, maps[0], maps[1],
                                maps[2], maps[3], a);
 }
 // Tile<D, PK>: PK where at most four heads share a row (hi and lo parts of P in one MMA)

@@ -21,9 +21,15 @@ constexpr float P8_LOW = 2048.f;  // factor of a probability's second part
 
 template <int D_, bool PK>
 struct TileE4m3 {
-  static constexpr int D = D_, STAGES = D == 128 ? 9 : 17, TILE_BYTES = ATT_BLOCK_N * D;
+  static constexpr int D = D_, TILE_BYTES = ATT_BLOCK_N * D;
   static constexpr int COLS = 1, ROW_BYTES = D;
   static constexpr bool SCALED = true;
+  // (small: eight copies a tile are more than one warp issues in time, 131,104 rows of 8 x 128
+  // in 16-row blocks 60 us with one, 48 with three.  Whole tiles: nine stages for seven, or three
+  // warps, make 9 x 2081 rows 14.0 and 14.3 us for 13.6, as copies in flight share the
+  // bandwidth and the first tile comes late; 272 ragged sequences gain 0.3 and 3 %)
+  static constexpr int stages(bool small) { return D == 128 ? (small ? 9 : 7) : (small ? 15 : 9); }
+  static constexpr int producers(bool small) { return small ? 3 : 1; }
   // The B operand of S^T = K Q^T, head g (with PK columns 4-7 repeat heads 0-3).  Of the
   // 32 channels that an ldmatrix of bytes brings, a thread has 4tq ... 4tq + 3 and the
   // same 16 further: the order of a sum's channels is free, so those are its k indexes.
@@ -65,19 +71,31 @@ struct TileE4m3 {
   // This warp's 16 rows [kb, kb + 16) of the tiles at sk, sv; rows >= nvalid are masked.
   __device__ __forceinline__ void math(WarpAcc<D>& A, uint32_t sk, uint32_t sv, int kb, int nvalid, float2 scales,
                                        float, int lane) const {
+    constexpr int N = D / 32;
     const int g = lane >> 2, tq = lane & 3, mat = lane >> 3, mr = lane & 7;
-    // ---- scores S^T (16 rows x 8 heads), four independent accumulation chains
-    float sc4[4][4] = {};
     const int row = kb + (mat & 1) * 8 + mr;
+    // (the loads all at once, those of V ahead of the softmax, and every sum taken up an MMA
+    // later: the instructions are issued in this order, so what waits holds up all that follows)
+    uint32_t rk[N][4], rv[N][4];
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      uint32_t r[4], a[8];
-      ldsm_x4(part(sk, row, 2 * j + (mat >> 1)), r[0], r[1], r[2], r[3]);
+    for (int j = 0; j < N; ++j) ldsm_x4(part(sk, row, 2 * j + (mat >> 1)), rk[j][0], rk[j][1], rk[j][2], rk[j][3]);
+    // ---- scores S^T (16 rows x 8 heads), four independent accumulation chains
+    float sc4[4][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e4m3_to_f16(r[i], a[2 * i], a[2 * i + 1]);
-      mma_f16(sc4[2 * j & 3], a[0], a[2], a[1], a[3], qf[j][0], qf[j][1]);
-      mma_f16(sc4[(2 * j + 1) & 3], a[4], a[6], a[5], a[7], qf[j][2], qf[j][3]);
+    for (int j = 0; j < N; ++j) {
+      uint32_t a[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e4m3_to_f16(rk[j][i], a[2 * i], a[2 * i + 1]);
+      if (j < 2) {
+        mma_f16_first(sc4[2 * j], a[0], a[2], a[1], a[3], qf[j][0], qf[j][1]);
+        mma_f16_first(sc4[2 * j + 1], a[4], a[6], a[5], a[7], qf[j][2], qf[j][3]);
+      } else {
+        mma_f16(sc4[2 * j & 3], a[0], a[2], a[1], a[3], qf[j][0], qf[j][1]);
+        mma_f16(sc4[(2 * j + 1) & 3], a[4], a[6], a[5], a[7], qf[j][2], qf[j][3]);
+      }
     }
+#pragma unroll
+    for (int j = 0; j < N; ++j) ldsm_x4_t(part(sv, row, 2 * j + (mat >> 1)), rv[j][0], rv[j][1], rv[j][2], rv[j][3]);
     const bool v0 = kb + g < nvalid, v1 = kb + g + 8 < nvalid;
     const float k0 = f0 * scales.x, k1 = f1 * scales.x;
     const float s0 = v0 ? ((sc4[0][0] + sc4[1][0]) + (sc4[2][0] + sc4[3][0])) * k0 : -INFINITY;
@@ -108,7 +126,7 @@ struct TileE4m3 {
       A.m1 = n1;
     }
     const float u0 = A.m0 == -INFINITY ? 0.f : A.m0, u1 = A.m1 == -INFINITY ? 0.f : A.m1;
-    const float p0 = exp2f(s0 - u0), p1 = exp2f(s1 - u1), p2 = exp2f(s2 - u0), p3 = exp2f(s3 - u1);
+    const float p0 = exp2_ftz(s0 - u0), p1 = exp2_ftz(s1 - u1), p2 = exp2_ftz(s2 - u0), p3 = exp2_ftz(s3 - u1);
     A.l0 += p0 + p2;
     A.l1 += p1 + p3;
     // ---- P^T as the B operand (rows x heads), in two parts
@@ -125,27 +143,31 @@ struct TileE4m3 {
     const int klo = kb + 2 * tq, khi = klo + 8;
     const uint32_t mlo = (klo < nvalid ? 0xFFFFu : 0u) | (klo + 1 < nvalid ? 0xFFFF0000u : 0u);
     const uint32_t mhi = (khi < nvalid ? 0xFFFFu : 0u) | (khi + 1 < nvalid ? 0xFFFF0000u : 0u);
+    const float low = scales.y * (1.f / P8_LOW);
+    float t[2][2][4], u[2][2][4];
+    const auto take_up = [&](int j) {
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      uint32_t r[4], a[8];
-      ldsm_x4_t(part(sv, row, 2 * j + (mat >> 1)), r[0], r[1], r[2], r[3]);
-      if (partial) r[0] &= mlo, r[1] &= mhi, r[2] &= mlo, r[3] &= mhi;
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e4m3_to_f16(__byte_perm(r[i], 0u, 0x3120), a[2 * i], a[2 * i + 1]);
+        for (int e = 0; e < 4; ++e) {
+          A.o[2 * j + i][e] = fmaf(t[j & 1][i][e], scales.y, A.o[2 * j + i][e]);
+          if (!PK) A.o[2 * j + i][e] = fmaf(u[j & 1][i][e], low, A.o[2 * j + i][e]);
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      uint32_t a[8];
+      if (partial) rv[j][0] &= mlo, rv[j][1] &= mhi, rv[j][2] &= mlo, rv[j][3] &= mhi;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e4m3_to_f16(__byte_perm(rv[j][i], 0u, 0x3120), a[2 * i], a[2 * i + 1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {  // channels 32j + 16i ...
-        float t[4] = {};
-        mma_f16(t, a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3], bh0, bh1);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) A.o[2 * j + i][e] = fmaf(t[e], scales.y, A.o[2 * j + i][e]);
-        if (!PK) {
-          float u[4] = {};
-          mma_f16(u, a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3], bl0, bl1);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) A.o[2 * j + i][e] = fmaf(u[e], scales.y * (1.f / P8_LOW), A.o[2 * j + i][e]);
-        }
+        mma_f16_first(t[j & 1][i], a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3], bh0, bh1);
+        if (!PK) mma_f16_first(u[j & 1][i], a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3], bl0, bl1);
       }
+      if (j > 0) take_up(j - 1);
     }
+    take_up(N - 1);
   }
   // the second parts' sums, in columns 4-7, to the first parts'
   static __device__ __forceinline__ void fold(WarpAcc<D>& A) {
