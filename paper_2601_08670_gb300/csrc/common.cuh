@@ -199,11 +199,21 @@ __device__ __forceinline__ void tma_prefetch_l2_3d(const void* tmap, int32_t x, 
                : "memory");
 }
 
-// 8 bytes global -> shared without waiting (8-byte aligned addresses), and an arrival on
-// `bar` once this thread's copies so far have landed (counted in the barrier's own number)
+// 8 or 16 bytes global -> shared without waiting (addresses aligned alike)
 __device__ __forceinline__ void copy_async_8(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// all but the last N groups of this thread's copies have landed
+template <int N>
+__device__ __forceinline__ void copy_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// an arrival on `bar` once this thread's copies so far have landed (counted in the
+// barrier's own number)
 __device__ __forceinline__ void mbar_arrive_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }

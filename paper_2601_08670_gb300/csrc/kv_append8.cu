@@ -9,7 +9,14 @@
 // smallest normal number.  Keys are rounded once, from the rotated fp32 ones.
 //
 // So every block and kv-head takes two passes over its new rows: their largest number,
-// then the bytes.  The second reads the rows from L2 again.
+// then the bytes.
+//
+// What bounds them (one GB300, GPU time in a graph): sixteen documents, 18,366 tokens of
+// 32 + 16 heads of 128, 427 MB in 90 us (4.8 TB/s, 70 % of the copy rate): a CTA's loads wait
+// for the block's largest number before the bytes can be written, with 16 warps an SM to
+// fill the time; queries alone, which are most of the bytes, would take 50.  32 tokens
+// behind each of 33 documents 8.9 us, nine sequences' next token 3.2 us (a launch and
+// four round trips: length, table, scale, write).
 #include <cuda_fp8.h>
 
 #include "kv_append.cuh"
@@ -29,21 +36,36 @@ __device__ __forceinline__ float scale_for(float top) {
   const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u);
   return __uint_as_float((uint32_t)(max(e, A8_LOWEST) + 127) << 23);
 }
-// |x|, 0 where it is not finite: that has no part in a scale
-__device__ __forceinline__ float size_of(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
+// The largest |x| of x, y and top; an infinity shows (what is no number does not).
 __device__ __forceinline__ float largest(const float (&x)[8], const float (&y)[8], float top) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(size_of(x[e]), size_of(y[e])));
+  for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(y[e])));
   return top;
 }
-// x inv as e4m3, rounded to nearest even; what is not finite: not a number
+// ... of the finite ones alone: infinities have no part in a scale
+__device__ __forceinline__ float largest_finite(const float (&x)[8], const float (&y)[8], float top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (fabsf(x[e]) < INFINITY) top = fmaxf(top, fabsf(x[e]));
+    if (fabsf(y[e]) < INFINITY) top = fmaxf(top, fabsf(y[e]));
+  }
+  return top;
+}
+// x inv as e4m3, rounded to nearest even.  An infinity would become the largest number: see drop_infinite.
 __device__ __forceinline__ uint32_t e4m3_pair(float x, float y, float inv) {
-  const float2 v = make_float2(fabsf(x) < INFINITY ? x * inv : NAN, fabsf(y) < INFINITY ? y * inv : NAN);
-  return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
+  return __nv_cvt_float2_to_fp8x2(make_float2(x * inv, y * inv), __NV_SATFINITE, __NV_E4M3);
 }
 __device__ __forceinline__ uint2 e4m3_8(const float (&x)[8], float inv) {
   return make_uint2(e4m3_pair(x[0], x[1], inv) | e4m3_pair(x[2], x[3], inv) << 16,
                     e4m3_pair(x[4], x[5], inv) | e4m3_pair(x[6], x[7], inv) << 16);
+}
+// infinities become not-a-number
+__device__ __forceinline__ void drop_infinite(float (&x)[8], float (&y)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (fabsf(x[e]) == INFINITY) x[e] = NAN;
+    if (fabsf(y[e]) == INFINITY) y[e] = NAN;
+  }
 }
 // four e4m3 numbers times `ratio`, rounded again
 __device__ __forceinline__ uint32_t move4(uint32_t w, float ratio) {
@@ -81,19 +103,20 @@ __device__ __forceinline__ float min_nan(float a, float b) {
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
-// eight channels' largest (up) or smallest keys as whole steps, into a block's summary
-__device__ __forceinline__ void update_bound(int8_t* at, const float (&k)[8], bool up, float inv, bool fresh) {
+// eight channels' largest (up) or smallest keys as whole steps, a byte each
+__device__ __forceinline__ uint2 bound_steps(const float (&k)[8], bool up, float inv) {
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     w[e / 4] |= ((uint32_t)(up ? steps_up(k[e], inv) : steps_down(k[e], inv)) & 0xFFu) << (8 * (e % 4));
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ uint2 merge_steps(uint2 a, uint2 b, bool up) {
+  return up ? make_uint2(__vmaxs4(a.x, b.x), __vmaxs4(a.y, b.y)) : make_uint2(__vmins4(a.x, b.x), __vmins4(a.y, b.y));
+}
+__device__ __forceinline__ void update_bound(int8_t* at, uint2 w, bool up, bool fresh) {
   uint2* p = reinterpret_cast<uint2*>(at);
-  if (!fresh) {
-    const uint2 old = *p;
-    w[0] = up ? __vmaxs4(w[0], old.x) : __vmins4(w[0], old.x);
-    w[1] = up ? __vmaxs4(w[1], old.y) : __vmins4(w[1], old.y);
-  }
-  *p = make_uint2(w[0], w[1]);
+  *p = fresh ? w : merge_steps(w, *p, up);
 }
 
 // The scale of a block after new rows whose largest number is `top`.
@@ -149,13 +172,12 @@ __global__ void __launch_bounds__(A8_ONE_THREADS) kv_append8_one_kernel(Append8A
     unpack8(r.b, y);
     if (rotated) rotate8(x, y, co, si);
     float top = largest(x, y, 0.f);
+    const bool infinite = top == INFINITY;
+    if (infinite) top = largest_finite(x, y, 0.f);
     const uint32_t unit = (LANES == 8 ? 0xFFu : 0xFu) << (lane & ~(LANES - 1));
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) top = fmaxf(top, __shfl_xor_sync(unit, top, o));
     const float sc = grown(s0, top, at == 0), inv = __fdiv_rn(1.f, sc);
-    uint8_t* row = (uint8_t*)(role ? a.c.v : a.c.k) + (page * P + at) * D + f;
-    *reinterpret_cast<uint2*>(row) = e4m3_8(x, inv);
-    *reinterpret_cast<uint2*>(row + D / 2) = e4m3_8(y, inv);
     if (f == 0) {
       if (sc != s0) a.scale[2 * page + role] = sc;
       ratio[role] = sc == s0 ? 1.f : __fdiv_rn(s0, sc);
@@ -165,10 +187,14 @@ __global__ void __launch_bounds__(A8_ONE_THREADS) kv_append8_one_kernel(Append8A
       int8_t* sum = a.c.summary + page * 2 * D + f;
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
-        update_bound(sum + which * D, x, !which, step, at == 0);
-        update_bound(sum + which * D + D / 2, y, !which, step, at == 0);
+        update_bound(sum + which * D, bound_steps(x, !which, step), !which, at == 0);
+        update_bound(sum + which * D + D / 2, bound_steps(y, !which, step), !which, at == 0);
       }
     }
+    if (infinite) drop_infinite(x, y);
+    uint8_t* row = (uint8_t*)(role ? a.c.v : a.c.k) + (page * P + at) * D + f;
+    *reinterpret_cast<uint2*>(row) = e4m3_8(x, inv);
+    *reinterpret_cast<uint2*>(row + D / 2) = e4m3_8(y, inv);
   }
   if (at == 0) return;
   __syncthreads();
@@ -180,8 +206,15 @@ __global__ void __launch_bounds__(A8_ONE_THREADS) kv_append8_one_kernel(Append8A
 
 // Any number of tokens: a CTA takes one item (the new rows of one block) and a kv-head,
 // or `heads` of them where items have few rows; D/16 lanes (a unit) share a row of a
-// kv-head and its group.
-constexpr int A8_CTAS = 5;  // CTAs that an SM holds
+// kv-head and its group.  A thread keeps its parts of the first rows in shared memory
+// between the passes (16 bytes beside those of its neighbours: no conflicts, and no
+// barrier), so that blocks of 64 rows and less are read once.
+// Sixteen documents: 115 us with the rows read again from L2, 111 kept, 104 with the kept
+// rows' copies under way before the queries, 90 us with four query heads' loads in flight
+// at 4 CTAs an SM instead of two at 6 (eight at 3: 107).
+constexpr int A8_CTAS = 4;   // CTAs that an SM holds
+constexpr int A8_HOLD = 4;   // rows of a unit that are kept
+constexpr int A8_HEADS = 4;  // query heads whose loads a thread has in flight
 
 template <int D>
 __global__ void __launch_bounds__(APP_THREADS, A8_CTAS) kv_append8_kernel(Append8Args a) {
@@ -189,8 +222,9 @@ __global__ void __launch_bounds__(APP_THREADS, A8_CTAS) kv_append8_kernel(Append
   const int tid = threadIdx.x, unit = tid / LANES, G = a.G, P = a.c.block_rows;
   const int heads = a.heads, per_item = a.c.Hkv / heads;
   const int h0 = (int)(blockIdx.x % per_item) * heads, mine = unit & (heads - 1), h = h0 + mine;
+  __shared__ uint4 kept[A8_HOLD][4][APP_THREADS];
+  __shared__ uint2 bounds[UNITS][2][D / 8];  // largest, smallest keys of a unit, in steps
   __shared__ float tops[UNITS][2];
-  __shared__ float bounds[UNITS][2][D];  // largest, smallest keys
   pdl_wait();
   const AppendItem it = find_item(a, blockIdx.x / per_item);
   if (it.s < 0) return;
@@ -198,48 +232,70 @@ __global__ void __launch_bounds__(APP_THREADS, A8_CTAS) kv_append8_kernel(Append
   const int64_t page = (int64_t)blk * a.c.Hkv + h;
   const int f = 8 * (tid % LANES), at = it.r0 % P;
   const bool fresh = at == 0;
+  float s0[2] = {0.f, 0.f};
+  if (blk >= 0) s0[0] = a.scale[2 * page], s0[1] = a.scale[2 * page + 1];
+  const int i0 = unit / heads, step = UNITS / heads;
+  // ---- the first rows on their way, a group of copies each
+#pragma unroll
+  for (int j = 0; j < A8_HOLD; ++j) {
+    const int i = i0 + j * step;
+    if (i < it.m) {
+      const __nv_bfloat16* kp = a.k + (it.t0 + i) * a.k_stride + h * D + f;
+      const __nv_bfloat16* vp = a.v + (it.t0 + i) * a.v_stride + h * D + f;
+      copy_async_16(smem_u32(&kept[j][0][tid]), kp);
+      copy_async_16(smem_u32(&kept[j][1][tid]), kp + D / 2);
+      copy_async_16(smem_u32(&kept[j][2][tid]), vp);
+      copy_async_16(smem_u32(&kept[j][3][tid]), vp + D / 2);
+    }
+    copy_async_commit();
+  }
   // ---- queries, and the largest of the keys and the values
   float top[2] = {0.f, 0.f};
-  float mx[16], mn[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) mx[e] = -INFINITY, mn[e] = INFINITY;
-  for (int i = unit / heads; i < it.m; i += UNITS / heads) {
+  bool infinite = false;  // among this thread's
+  for (int i = i0, j = 0; i < it.m; i += step, ++j) {
     const int64_t t = it.t0 + i;
+    HeadRow kr, vr;
+    if (j >= A8_HOLD) {
+      kr.load(a.k + t * a.k_stride + h * D + f, D / 2);
+      vr.load(a.v + t * a.v_stride + h * D + f, D / 2);
+    }
     float co[8], si[8];
     const bool rotated = a.rope && load_angles(a, D, a.positions ? a.positions[t] : it.r0 + i, f, co, si);
-    HeadRow kr, vr;
-    kr.load(a.k + t * a.k_stride + h * D + f, D / 2);
-    vr.load(a.v + t * a.v_stride + h * D + f, D / 2);
     const __nv_bfloat16* q = a.q + t * a.q_stride + (int64_t)h * G * D + f;
     __nv_bfloat16* qo = a.q_out + (t * a.Hq + h * G) * D + f;
-    for (int g0 = 0; g0 < G; g0 += 2) {
-      HeadRow x[2];
+    for (int g0 = 0; g0 < G; g0 += A8_HEADS) {
+      HeadRow x[A8_HEADS];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < A8_HEADS; ++u)
         if (g0 + u < G) x[u].load(q + (g0 + u) * D, D / 2);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < A8_HEADS; ++u) {
         if (g0 + u >= G) break;
         if (rotated) x[u].rotate(co, si);
         if (PCED_IN_BOUNDS(t < a.T, a.status)) x[u].store(qo + (g0 + u) * D, D / 2);
       }
     }
+    if (j < A8_HOLD) {  // (this thread's own copies: no barrier)
+      static_assert(A8_HOLD == 4, "the groups to wait for");
+      if (j == 0) copy_async_wait<3>();
+      else if (j == 1) copy_async_wait<2>();
+      else if (j == 2) copy_async_wait<1>();
+      else copy_async_wait<0>();
+      kr.a = kept[j][0][tid], kr.b = kept[j][1][tid], vr.a = kept[j][2][tid], vr.b = kept[j][3][tid];
+    }
     float x[8], y[8];
     unpack8(vr.a, x);
     unpack8(vr.b, y);
-    top[1] = largest(x, y, top[1]);
+    const float v = largest(x, y, 0.f);
+    top[1] = fmaxf(top[1], v < INFINITY ? v : largest_finite(x, y, 0.f));
     unpack8(kr.a, x);
     unpack8(kr.b, y);
     if (rotated) rotate8(x, y, co, si);
-    top[0] = largest(x, y, top[0]);
-    if (a.c.summary) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        mx[e] = max_nan(mx[e], x[e]), mn[e] = min_nan(mn[e], x[e]);
-        mx[8 + e] = max_nan(mx[8 + e], y[e]), mn[8 + e] = min_nan(mn[8 + e], y[e]);
-      }
-    }
+    const float k = largest(x, y, 0.f);
+    top[0] = fmaxf(top[0], k < INFINITY ? k : largest_finite(x, y, 0.f));
+    infinite |= v == INFINITY || k == INFINITY;
   }
+  copy_async_wait<0>();
   if (blk < 0) return;
   // ---- units of the same head meet
 #pragma unroll
@@ -248,68 +304,79 @@ __global__ void __launch_bounds__(APP_THREADS, A8_CTAS) kv_append8_kernel(Append
     for (int o = 1; o < LANES; o <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
     if (f == 0) tops[unit][i] = top[i];
   }
-  if (a.c.summary) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int d = f + (e < 8 ? e : D / 2 + e - 8);
-      bounds[unit][0][d] = mx[e];
-      bounds[unit][1][d] = mn[e];
-    }
-  }
   __syncthreads();
   float inv[2], ratio[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     for (int u = mine; u < UNITS; u += heads) top[i] = fmaxf(top[i], tops[u][i]);
-    const float s0 = a.scale[2 * page + i], sc = grown(s0, top[i], fresh);
+    const float sc = grown(s0[i], top[i], fresh);
     inv[i] = __fdiv_rn(1.f, sc);
-    ratio[i] = fresh || sc == s0 ? 1.f : __fdiv_rn(s0, sc);
+    ratio[i] = fresh || sc == s0[i] ? 1.f : __fdiv_rn(s0[i], sc);
     top[i] = sc;
   }
   // ---- the rows again, as bytes
-  for (int i = unit / heads; i < it.m; i += UNITS / heads) {
+  float mx[16], mn[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) mx[e] = -INFINITY, mn[e] = INFINITY;
+  for (int i = i0, j = 0; i < it.m; i += step, ++j) {
     const int64_t t = it.t0 + i;
+    HeadRow kr, vr;
+    if (j < A8_HOLD) {
+      kr.a = kept[j][0][tid], kr.b = kept[j][1][tid], vr.a = kept[j][2][tid], vr.b = kept[j][3][tid];
+    } else {
+      kr.load(a.k + t * a.k_stride + h * D + f, D / 2);
+      vr.load(a.v + t * a.v_stride + h * D + f, D / 2);
+    }
     float co[8], si[8];
     const bool rotated = a.rope && load_angles(a, D, a.positions ? a.positions[t] : it.r0 + i, f, co, si);
-    HeadRow kr, vr;
-    kr.load(a.k + t * a.k_stride + h * D + f, D / 2);
-    vr.load(a.v + t * a.v_stride + h * D + f, D / 2);
     if (!PCED_IN_BOUNDS(t < a.T && in_pool(a.c, page, at + i), a.status)) continue;
     const int64_t row = (page * P + at + i) * D + f;
     float x[8], y[8];
+    unpack8(vr.a, x);
+    unpack8(vr.b, y);
+    if (infinite) drop_infinite(x, y);
+    *reinterpret_cast<uint2*>((uint8_t*)a.c.v + row) = e4m3_8(x, inv[1]);
+    *reinterpret_cast<uint2*>((uint8_t*)a.c.v + row + D / 2) = e4m3_8(y, inv[1]);
     unpack8(kr.a, x);
     unpack8(kr.b, y);
     if (rotated) rotate8(x, y, co, si);
+    if (a.c.summary) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        mx[e] = max_nan(mx[e], x[e]), mn[e] = min_nan(mn[e], x[e]);
+        mx[8 + e] = max_nan(mx[8 + e], y[e]), mn[8 + e] = min_nan(mn[8 + e], y[e]);
+      }
+    }
+    if (infinite) drop_infinite(x, y);
     *reinterpret_cast<uint2*>((uint8_t*)a.c.k + row) = e4m3_8(x, inv[0]);
     *reinterpret_cast<uint2*>((uint8_t*)a.c.k + row + D / 2) = e4m3_8(y, inv[0]);
-    unpack8(vr.a, x);
-    unpack8(vr.b, y);
-    *reinterpret_cast<uint2*>((uint8_t*)a.c.v + row) = e4m3_8(x, inv[1]);
-    *reinterpret_cast<uint2*>((uint8_t*)a.c.v + row + D / 2) = e4m3_8(y, inv[1]);
   }
   // ---- the rows that the block held already: the units of a head share them
   if (!PCED_IN_BOUNDS(in_pool(a.c, page, at), a.status)) return;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
     if (ratio[i] != 1.f)
-      move_rows<D>((uint8_t*)(i ? a.c.v : a.c.k) + page * P * D, at, ratio[i], unit / heads * LANES + tid % LANES,
-                   APP_THREADS / heads);
-  __syncthreads();  // (all have read the old scales)
+      move_rows<D>((uint8_t*)(i ? a.c.v : a.c.k) + page * P * D, at, ratio[i], i0 * LANES + tid % LANES, APP_THREADS / heads);
+  if (a.c.summary) {  // (a unit without rows: bounds that change nothing)
+    const float steps = __fdiv_rn(1.f, a.c.key_step[h]);
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float k[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[e] = which ? mn[8 * half + e] : mx[8 * half + e];
+        bounds[unit][which][(f + half * (D / 2)) / 8] = bound_steps(k, !which, steps);
+      }
+  }
+  __syncthreads();  // (the bounds; and all have read the old scales)
   if (unit < heads && f == 0) a.scale[2 * page] = top[0], a.scale[2 * page + 1] = top[1];
   if (!a.c.summary) return;
-  for (int i = tid; i < heads * (D / 8); i += APP_THREADS) {  // eight channels of a head
-    const int hh = i / (D / 8), d = 8 * (i % (D / 8));
-    float hi[8], lo[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      hi[e] = -INFINITY, lo[e] = INFINITY;
-      for (int u = hh; u < UNITS; u += heads)
-        hi[e] = max_nan(hi[e], bounds[u][0][d + e]), lo[e] = min_nan(lo[e], bounds[u][1][d + e]);
-    }
-    int8_t* sum = a.c.summary + ((int64_t)blk * a.c.Hkv + h0 + hh) * 2 * D + d;
-    const float step = __fdiv_rn(1.f, a.c.key_step[h0 + hh]);
-    update_bound(sum, hi, true, step, fresh);
-    update_bound(sum + D, lo, false, step, fresh);
+  for (int i = tid; i < heads * 2 * (D / 8); i += APP_THREADS) {  // eight channels of a head
+    const int hh = i / (2 * (D / 8)), which = i / (D / 8) % 2, d = i % (D / 8);
+    uint2 w = bounds[hh][which][d];
+    for (int u = hh + heads; u < UNITS; u += heads) w = merge_steps(w, bounds[u][which][d], !which);
+    update_bound(a.c.summary + ((int64_t)blk * a.c.Hkv + h0 + hh) * 2 * D + which * D + 8 * d, w, !which, fresh);
   }
 }
 
