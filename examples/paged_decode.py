@@ -8,9 +8,11 @@ products between the library's operators.
     documents   kv_append of whole sequences, block_summaries
     each layer  kv_append -> block_select -> paged_attention
     each token  lm_head_logprobs -> logits_process -> contrastive_select, with the rows made logits again
-                before logits_process and normalised after it
+                before logits_process and normalised after it; or sample, from the experts' best scores
 
-Run: python examples/paged_decode.py [--steps 8] [--blocks 8]
+With --eight-bit the caches hold 8-bit numbers (half the memory): the same calls over a PagedCache8.
+
+Run: python examples/paged_decode.py [--steps 8] [--blocks 8] [--eight-bit] [--temperature 0.8 --top-p 0.95]
 """
 import argparse
 import math
@@ -54,10 +56,11 @@ class Model:
 
 
 class Loop:
-    """B queries of N experts and the amateur; `blocks` 0: attention over all blocks, else over so many."""
+    """B queries of N experts and the amateur; `blocks` 0: attention over all blocks, else over so many.  eight: 8-bit
+    caches.  sampling: keyword arguments of pced.sample, numbers for all queries (None: the best token)."""
 
     def __init__(self, model, B, N, lens, max_steps, beta, r, gamma=2.5, block_rows=16, blocks=0, penalties=None,
-                 mask=None):
+                 mask=None, eight=False, sampling=None, seed=0):
         m, dev = model, model.embed.device
         self.model, self.B, self.N, self.blocks, self.gamma = m, B, N, blocks, gamma
         S = B * (N + 1)
@@ -76,9 +79,19 @@ class Loop:
         def pool(dtype, *tail):
             return torch.zeros((sum(need), m.Hkv, *tail), dtype=dtype, device=dev)
 
-        self.caches = [pced.PagedCache(pool(torch.bfloat16, block_rows, m.D), pool(torch.bfloat16, block_rows, m.D),
-                                       table, self.seq_len, summary=pool(torch.int8, 2, m.D), key_step=step)
-                       for _ in range(m.L)]
+        def cache():
+            kind = torch.float8_e4m3fn if eight else torch.bfloat16
+            kv = [pool(kind, block_rows, m.D) for _ in range(2)]
+            more = dict(summary=pool(torch.int8, 2, m.D), key_step=step)
+            if eight:
+                return pced.PagedCache8(*kv, pool(torch.float32, 2), table, self.seq_len, **more)
+            return pced.PagedCache(*kv, table, self.seq_len, **more)
+
+        self.caches = [cache() for _ in range(m.L)]
+        self.sampling, self.random = None, torch.Generator(device=dev).manual_seed(seed)
+        if sampling is not None:
+            self.sampling = {n: torch.full((B,), v, device=dev, dtype=torch.int32 if n == "top_k" else torch.float32)
+                             for n, v in sampling.items()}
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.ws = pced.workspace(pced.paged_attention_workspace_size(S, m.Hq, m.Hkv, m.D), dev)
         self.beta, self.r = beta, r
@@ -96,7 +109,8 @@ class Loop:
         for layer, cache in enumerate(self.caches):
             _, k, v = self.model.project(layer, hidden)
             pced.kv_append(cache, None, k, v, rope=self.model.rope, tok_start=start, status=self.status)
-            pced.block_summaries(cache, status=self.status)  # (kv_append has made them; a cache loaded as it is needs this)
+            if not cache.eight:  # (kv_append has made them; a bf16 cache loaded as it is needs this)
+                pced.block_summaries(cache, status=self.status)
 
     def step(self):
         m, S = self.model, self.B * (self.N + 1)
@@ -121,11 +135,24 @@ class Loop:
                                 mask=self.mask, out=z, status=self.status)
             lp = z.log_softmax(1)  # (a mask that forbids everything leaves no distribution)
         self.logprobs = lp
-        token, expert, _ = pced.contrastive_select(lp, self.beta, self.r, self.gamma)
+        if self.sampling is None:
+            token, expert, _ = pced.contrastive_select(lp, self.beta, self.r, self.gamma)
+        else:
+            token, expert = self.draw(lp)
         self.history[:, self.t], self.expert[:, self.t] = token, expert
         self.n_history += 1
         self.t += 1
         return token, expert
+
+    def draw(self, lp):
+        """A token of every query from the experts' best contrastive scores, and the expert whose score it is."""
+        lp = lp.view(self.B, self.N + 1, -1)
+        beta = self.beta[..., None]
+        scores = (1 + beta) * lp[:, 1:] - beta * lp[:, :1] + self.gamma * self.r.log()[..., None]
+        best, expert = scores.max(1)
+        u = torch.rand(self.B, device=lp.device, generator=self.random)
+        token = pced.sample(best, u, status=self.status, **self.sampling)
+        return token, expert.gather(1, token.long()[:, None])[:, 0].int() + 1
 
     def device_status(self):
         return int(self.status.item()) | pced.device_status(self.ws)
@@ -135,6 +162,9 @@ def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=8)
     ap.add_argument("--blocks", type=int, default=8, help="blocks that attention reads (0: all)")
+    ap.add_argument("--eight-bit", action="store_true", help="8-bit caches")
+    ap.add_argument("--temperature", type=float, default=0.0, help="draw tokens (0: take the best)")
+    ap.add_argument("--top-p", type=float, default=1.0)
     args = ap.parse_args()
     torch.manual_seed(0)
     B, N = 2, 3
@@ -143,7 +173,8 @@ def main():
     beta = torch.full((B, N), 0.5, device="cuda")
     r = torch.rand((B, N), device="cuda")
     loop = Loop(model, B, N, lens, args.steps, beta, r, blocks=args.blocks,
-                penalties=torch.tensor([[1.1, 0.2, 0.2]] * B, device="cuda"))
+                penalties=torch.tensor([[1.1, 0.2, 0.2]] * B, device="cuda"), eight=args.eight_bit,
+                sampling=dict(temperature=args.temperature, top_p=args.top_p) if args.temperature > 0 else None)
     loop.load_documents(torch.randn((sum(lens), model.Hq * model.D), device="cuda"))
     for _ in range(args.steps):
         loop.step()
