@@ -29,7 +29,7 @@ FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "--expt-relaxe
          "-I", os.path.join(ROOT, "include")]
 SOURCES = ["attention.cu", "attention_noalloc.cu", "lm_head.cu", "lm_head_pair.cu", "select.cu", "adacad.cu", "aggregate.cu", "relevance.cu",
            "step.cu", "partition.cu", "host.cu", "kv_append.cu", "block_select.cu", "paged_attention.cu", "logits.cu",
-           "kv_append8.cu", "paged_attention8.cu", "sample.cu"]
+           "kv_append8.cu", "paged_attention8.cu", "sample.cu", "sample_bf16.cu"]
 CALLS = "pced_calls.so"
 
 
