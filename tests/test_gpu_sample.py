@@ -9,8 +9,8 @@ import sample_ref as ref
 pytestmark = pytest.mark.gpu
 
 # A weight is off by at most 2^-31 of itself (the table and the series, half a step of 2^-31 each; the series' own error
-# 2^-31; an argument off by 2^-31), and by a step of 2^-44; so are sums of them.  Where u (or p) lies nearer than twice that
-# to a border of two tokens, the neighbour is as right.
+# 2^-31; an argument off by 2^-31), sixteen of them together by a step of 2^-42 more; so are sums of them.  Where u (or p)
+# lies nearer than twice that to a border of two tokens, the neighbour is as right.
 MARGIN = 2.0 ** -30
 # logprob: fp32's rounding of a number below 32 (2^-20), and what the sum is off
 LOGPROB = 2.0 ** -19
