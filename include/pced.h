@@ -662,10 +662,11 @@ pced_status pced_paged_attention8(const pced_paged_cache8* cache, const void* q,
  * the first kept one, in the order of the vocabulary, with
  * sum_{v' <= v} w_v' > u sum w.  t = 0, k = 1, p <= 0 and min_p > 1 give the
  * first of the largest (logprob 0).  Logits of +inf share everything equally.
- * Weights are whole numbers of 2^-44 of the largest, exact to about 2^-32 of
- * themselves (a smaller one is never drawn), and added as such: the choice
+ * Weights are exact to about 2^-32 of themselves and are added in whole steps
+ * (2^-42 of the power of two from the largest up), sixteen at a time: the choice
  * depends on no order of sums and differs from that of exact sums in about one
- * row of a million.  Temperatures above 1e30 count as infinite.
+ * row of a million.  Weights below 2^-44 are nothing to a cut.  Temperatures
+ * count as 1e-37 at least and 1e30 at most.
  * A row whose logits are all -inf has token -1 and logprob -inf; so has one
  * with a parameter that is not a number, t < 0 or u outside [0, 1], which sets
  * PCED_DEV_BAD_PARAM.  V <= 393216.

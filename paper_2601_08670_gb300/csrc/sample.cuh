@@ -58,6 +58,8 @@ constexpr int64_t SMP_L2 = 100 << 20;   // bytes of rows that L2 keeps
 constexpr int SMP_MAX_V = 393216;     // (sets the groups)
 constexpr int SMP_MAX_GROUPS = SMP_MAX_V / SMP_GROUP + 1;
 constexpr int SMP_UNIT = 42;          // weights are counted in steps of 2^-42
+constexpr int SMP_PART = 14;          // bits of a weight that are added up in one number of 32
+constexpr int SMP_MAX_PER = (1 << 18) - 1;  // tokens of a CTA: as many such parts as fit, also of the uppermost
 constexpr float SMP_ALIVE = 44.f;     // -log2 of weights that no cut asks about
 constexpr float SMP_LOWEST = 100.f;   // ... and that are nothing
 
@@ -132,6 +134,8 @@ struct Sum {
   }
 };
 static_assert(SMP_UNIT == 42, "18 + 24");
+static_assert(((uint64_t)SMP_MAX_PER << SMP_PART) >> 32 == 0 && SMP_UNIT <= 3 * SMP_PART, "sums of parts, 2^SMP_UNIT itself among them");
+static_assert(SMP_MAX_V <= (int64_t)SMP_MAX_PER * ROW_CLUSTER, "parts of a row");
 static_assert(SMP_SOLO <= SMP_LIST, "one CTA's list");
 static_assert(SMP_BINS == 4 * SMP_FINE, "see keep_share");
 
@@ -194,7 +198,7 @@ struct Border {
 struct SampleShared {
   float2 table[32][16];
   uint32_t count[SMP_BINS];      // tokens of a range (16 bits each where a part has no more)
-  uint32_t weight[3][SMP_BINS];  // their weights, 15 bits each
+  uint32_t weight[3][SMP_BINS];  // their weights, SMP_PART bits each
   uint64_t cand[SMP_FEW];
   uint64_t group[SMP_MAX_GROUPS];  // kept weight (on its way in two numbers, 21 bits in the first)
   uint32_t n_list, n_cand;
@@ -603,7 +607,7 @@ struct Row {
         n[0] += c[k].x, n[1] += c[k].y;
         if (r0 + k >= ctas) continue;
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) m[0] += (uint64_t)b[k][i].x << (15 * i), m[1] += (uint64_t)b[k][i].y << (15 * i);
+        for (int i = 0; i < PARTS; ++i) m[0] += (uint64_t)b[k][i].x << (SMP_PART * i), m[1] += (uint64_t)b[k][i].y << (SMP_PART * i);
       }
     }
   }
@@ -651,9 +655,10 @@ struct Row {
   }
   __device__ __forceinline__ void add_to_range(int bin, uint64_t v) {
     count_in(bin);
-    atomicAdd(&s.weight[0][bin], (uint32_t)v & 0x7FFFu);
-    atomicAdd(&s.weight[1][bin], (uint32_t)(v >> 15) & 0x7FFFu);
-    atomicAdd(&s.weight[2][bin], (uint32_t)(v >> 30));
+    constexpr uint32_t MASK = (1u << SMP_PART) - 1;
+    atomicAdd(&s.weight[0][bin], (uint32_t)v & MASK);
+    atomicAdd(&s.weight[1][bin], (uint32_t)(v >> SMP_PART) & MASK);
+    atomicAdd(&s.weight[2][bin], (uint32_t)(v >> (2 * SMP_PART)));
   }
 
   // The cut among the tokens in(x, token), `n` of the cluster: the one that brings the sum
@@ -801,7 +806,10 @@ struct Row {
     each_left([&](float x, int) { count_in(range_of(x)); });
     meet();
     const Border b = find_border<false>((uint64_t)k);
-    if (!b.found) return;  // there are no more than k
+    if (!b.found) {  // there are no more than k; smaller ones may be among the first k, but are nothing
+      if (!solo) cut.x = low, cut.token = INT32_MAX;
+      return;
+    }
     if (!listed) list(fmaxf(alive, below((int)b.bin)));
     cut_among<false>(b.n, k - b.before, [&](float x, int) { return range_of(x) == (int)b.bin; });
   }
@@ -1036,7 +1044,8 @@ struct Row {
     static_assert(SMP_GROUP == SMP_THREADS, "a thread for each token of a group");
     const int token = first + g * SMP_GROUP + tid();
     const float x = at(g * SMP_GROUP + tid());
-    const bool keep = x >= low && cut.keeps(x, token);
+    // (without a cut the groups have the smallest weights too)
+    const bool keep = cut.x == -INFINITY ? x > -INFINITY : x >= low && cut.keeps(x, token);
     const uint64_t m = keep ? steps_of(x) : 0;
     to = prefix(m);
     if (lane() == 31) s.wscan[warp()] = to;
@@ -1180,7 +1189,7 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
   if (!R.gone && p < 1.f) R.keep_share((double)p);
   if (!R.gone && least > 0.f) R.keep_from(s.below);
   if (R.gone) return;
-  // ---- the kept weights, and where u falls (both factors are exact)
+  // ---- the kept weights, and where u falls (off by 2^-52)
   const auto seek = [&](uint64_t total) { return min((uint64_t)((double)u * (double)total), total - 1); };
   if (R.solo) {
     const uint64_t total = R.template weigh_kept<false>().all;
@@ -1210,7 +1219,7 @@ cudaError_t launch_sample_t(SampleArgs a, int32_t rows, cudaStream_t stream) {
   const int64_t slots = 2 * (int64_t)pced_host::num_sms(), bytes = (int64_t)a.V * sizeof(T);
   int ctas = 1;
   while (ctas < ROW_CLUSTER && a.V > 8 * SMP_THREADS * ctas &&
-         (2 * ctas * (int64_t)rows <= slots || (rows < slots / ctas ? rows : slots / ctas) * bytes > SMP_L2))
+         (a.V > SMP_MAX_PER * ctas || 2 * ctas * (int64_t)rows <= slots || (rows < slots / ctas ? rows : slots / ctas) * bytes > SMP_L2))
     ctas *= 2;
   a.per = (a.V + ctas - 1) / ctas;
   // (one CTA an SM has twice the registers)

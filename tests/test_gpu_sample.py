@@ -256,3 +256,53 @@ def test_another_stream_and_graph_replays(cuda_ok):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out.cpu(), want)
+
+
+@pytest.mark.parametrize("V,rows", [(151936, 160), (250001, 170), (300001, 153)])
+def test_one_value_almost_everywhere(cuda_ok, V, rows):
+    # a CTA's share of a row in one range, of weights with any low bits; p ends inside it
+    x = torch.zeros((rows, V), dtype=torch.bfloat16, device="cuda")
+    x[:, ::1000] = 1.0
+    t = np.linspace(0.31, 1.7, rows).astype(np.float32)
+    share = np.linspace(0.05, 0.97, rows).astype(np.float32)
+    u = numbers(rows, 4)
+    tok, lp = run(x, u, t=t, p=share)
+    for i in range(rows):
+        # (all ones first, then so many zeros that the share is reached)
+        ones, w = (V + 999) // 1000, np.exp(-1 / np.float64(t[i]))
+        all_ = ones + (V - ones) * w
+        want = np.float64(share[i]) * all_
+        zeros = max(0, int(np.ceil((want - ones) / w)))
+        if min(abs((want - ones) / w - z) for z in (zeros, zeros - 1)) * w < MARGIN * all_ or want < ones:
+            continue
+        # the kept zeros are the first ones; a thousand tokens are a one and 999 zeros
+        last = zeros + (zeros - 1) // 999 + 1 if zeros else 0  # tokens up to the last kept zero
+        total = ones + zeros * w
+        goal = np.float64(np.float32(u[i])) * total
+        order = np.arange(V)
+        kept = (order % 1000 == 0) | (order < last)
+        assert int(((order % 1000 != 0) & kept).sum()) == zeros
+        sums = np.cumsum(np.where(order % 1000 == 0, 1.0, w) * kept)
+        at = int(np.searchsorted(sums, goal, side="right"))
+        if np.abs(sums - goal).min() < MARGIN * total:
+            continue
+        assert tok[i] == at, i
+        want_lp = np.log((1.0 if at % 1000 == 0 else w) / total)
+        assert abs(lp[i] - want_lp) <= LOGPROB * max(1.0, abs(want_lp))
+
+
+@pytest.mark.parametrize("u", [0.0, 1.0])
+@pytest.mark.parametrize("k", [0, 5, 50, 3000])
+def test_the_smallest_weights_beside_a_large_one(cuda_ok, u, k):
+    # weights of 2^-45 of the largest, at the ends of the order: some token is drawn, and one that is kept
+    for V in (600, 5000, 128256):
+        x = torch.zeros((3, V), device="cuda")
+        x[:, V // 2] = 45 * float(np.log(2))
+        x[1, :V // 4] = -float("inf")
+        x[2] += torch.linspace(-1e-3, 1e-3, V, device="cuda")
+        tok, lp = run(x, np.full(3, u), k=None if k == 0 else np.full(3, k))
+        h = x.cpu().numpy()
+        for i in range(3):
+            assert 0 <= tok[i] < V and np.isfinite(h[i, tok[i]]) and np.isfinite(lp[i])
+            if 0 < k < V:
+                assert tok[i] in ref.order(h[i].astype(np.float64))[:k]
