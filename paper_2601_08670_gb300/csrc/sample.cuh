@@ -46,6 +46,7 @@ struct SampleArgs {
 constexpr int SMP_THREADS = 512;
 constexpr int SMP_WARPS = SMP_THREADS / 32;
 constexpr int SMP_BINS = 1024;        // ranges
+constexpr int SMP_COARSE = 2 * SMP_BINS;  // ranges of all weights, a 64th of their log2 each
 constexpr int SMP_FEW = 512;          // tokens of a range that are ranked one by one
 constexpr int SMP_EACH = 16;          // tokens of a lane in a group, whose weight is kept
 constexpr int SMP_GROUP = 32 * SMP_EACH;
@@ -197,15 +198,16 @@ struct Border {
 
 struct SampleShared {
   float2 table[32][16];
-  uint32_t count[SMP_BINS];      // tokens of a range (16 bits each where a part has no more)
-  uint32_t weight[3][SMP_BINS];  // their weights, SMP_PART bits each
+  // tokens of the ranges, then their weights, SMP_PART bits each (of SMP_BINS ranges); or the
+  // tokens of SMP_COARSE ranges (16 bits each where a part has no more)
+  uint32_t ranges[4][SMP_BINS];
   uint64_t cand[SMP_FEW];
   uint64_t group[SMP_MAX_GROUPS];  // kept weight (on its way in two numbers, 21 bits in the first)
   uint32_t n_list, n_cand;
   int from, to;                  // places of this CTA's part
   float ym, inverse;             // log2 of the largest weight; t / log2(e)
   float thread_max[SMP_THREADS]; // the largest logit that a thread loaded first
-  int at[5];
+  int at[4];
   uint64_t wscan[SMP_WARPS];
   uint32_t wkept[SMP_WARPS];
   float2 fscan[SMP_WARPS];
@@ -223,7 +225,7 @@ struct SampleShared {
 
   // When a range is ranked the histograms are free: this CTA's candidates and their weights,
   // all the cluster's and theirs.
-  __device__ __forceinline__ uint64_t* candidates(int which) { return which ? reinterpret_cast<uint64_t*>(weight[which - 1]) : cand; }
+  __device__ __forceinline__ uint64_t* candidates(int which) { return which ? reinterpret_cast<uint64_t*>(ranges[which]) : cand; }
 };
 static_assert(SMP_BINS * 4 >= SMP_FEW * 8, "room for the candidates");
 
@@ -491,7 +493,7 @@ struct Row {
         float b, c;
         w.of(x, b, c);
         sum.add(b, c);
-        if (COUNT && x >= from) count_place(x);
+        if (COUNT) count_coarse(x, from);
       });
       const uint64_t v = sum.warp_steps();
       if (lane() == 0) s.group[g] = v;
@@ -507,7 +509,7 @@ struct Row {
     each_left([&](float x, int token) {
       if (!cut.keeps(x, token)) return;
       total += steps_of(x);
-      if (COUNT) count_place(x);
+      if (COUNT) count_coarse(x, alive);
     });
     return sum_up(warp_sum64(total));
   }
@@ -553,26 +555,31 @@ struct Row {
     return sum_up(total);
   }
   // Where a logit lies below 2^N, in 2048ths of the weights' log2 (by the larger part of y, which
-  // rises with x; the fp32 number 4096 + such has them in its low bits), and its range, a 32nd.
-  __device__ __forceinline__ int place_of(float x) const {
-    const float p = __fmul_rn(fmaxf(x, w.floor), w.ch);
-    return __float_as_int(__fadd_rn(__fsub_rn(whole, p), 4096.f)) - __float_as_int(4096.f);
+  // rises with x, and is at most N; the fp32 number 4096 + such has them in its low bits), and its
+  // range, a 32nd.
+  __device__ __forceinline__ float place_float(float x) const {
+    return __fsub_rn(whole + 4096.f, __fmul_rn(fmaxf(x, w.floor), w.ch));
   }
+  __device__ __forceinline__ int place_of(float x) const { return __float_as_int(place_float(x)) - __float_as_int(4096.f); }
   __device__ __forceinline__ int range_of(float x) const { return min(place_of(x) >> 6, SMP_BINS - 1); }
-  // a logit that those of the ranges up to `bin` are not below
-  __device__ __forceinline__ float below(int bin) const {
-    return bin >= SMP_BINS - 1 ? -INFINITY : (whole - ((float)bin + 1.125f) * (1.f / 32)) * s.inverse;
+  // a logit that those of the ranges up to `bin` are not below (which are `per` of log2)
+  __device__ __forceinline__ float below(int bin, int bins = SMP_BINS, float per = 1.f / 32) const {
+    return bin >= bins - 1 ? -INFINITY : (whole - ((float)bin + 1.25f) * per) * s.inverse;
   }
-  // ... with its place in the range
-  __device__ __forceinline__ void count_place(float x) {
-    const int v = place_of(x), bin = min(v >> 6, SMP_BINS - 1);
-    count_in(bin);
-    atomicAdd(&s.weight[0][bin], (uint32_t)v & 63u);
+  // Counts x in its coarse range if it is `from` or more (alive at least).  (A predicate, no
+  // branch: with branches around the atomics, and more instructions for places, this and
+  // group_and_list took 77 instructions a token, now NN; 272 rows of 151936, p = 0.9: 203 and XX us.)
+  __device__ __forceinline__ void count_coarse(float x, float from) {
+    const int narrow = !wide(), bin = min((int)(__float_as_uint(place_float(x)) >> 5 & 0x3FFFFu), SMP_COARSE - 1);
+    const uint32_t at = smem_u32(&s.ranges[0][0]) + ((bin >> narrow) << 2), n = 1u << ((bin & narrow) << 4);
+    asm volatile("{\n.reg .pred p;\nsetp.ge.f32 p, %2, %3;\n@p red.shared.add.u32 [%0], %1;\n}" ::"r"(at), "r"(n), "f"(x), "f"(from)
+                 : "memory");
   }
   __device__ __forceinline__ bool wide() const { return a.per > 0xFFFF; }
   __device__ __forceinline__ void count_in(int bin) {
-    if (wide()) atomicAdd(&s.count[bin], 1u);
-    else atomicAdd(&s.count[bin >> 1], 1u << (16 * (bin & 1)));
+    uint32_t* const n = &s.ranges[0][0];
+    if (wide()) atomicAdd(n + bin, 1u);
+    else atomicAdd(n + (bin >> 1), 1u << (16 * (bin & 1)));
   }
   static __device__ __forceinline__ uint64_t warp_sum64(uint64_t v) {
 #pragma unroll
@@ -580,14 +587,14 @@ struct Row {
     return v;
   }
 
-  // Two ranges' tokens of the cluster, each thread its own; PARTS 3: and weights, 1: and the sum of their places.
-  template <int PARTS>
+  // Two ranges' tokens of the cluster, each thread its own; MASS: and their weights.
+  template <bool MASS>
   __device__ __forceinline__ void gather_ranges(uint32_t (&n)[2], uint64_t (&m)[2]) {
     static_assert(SMP_BINS == 2 * SMP_THREADS && ROW_CLUSTER == 8, "two ranges a thread");
     n[0] = n[1] = 0;
     m[0] = m[1] = 0;
-    if (PARTS == 3 && !solo && 2 * tid() >= SMP_FINE) return;
-    constexpr int BATCH = PARTS == 3 ? 2 : 4;  // CTAs whose loads are in flight
+    if (MASS && !solo && 2 * tid() >= SMP_FINE) return;
+    constexpr int PARTS = MASS ? 3 : 0, BATCH = MASS ? 2 : 4;  // CTAs whose loads are in flight
 #pragma unroll
     for (int r0 = 0; r0 < ROW_CLUSTER; r0 += BATCH) {
       if (r0 >= ctas) break;
@@ -597,10 +604,10 @@ struct Row {
         c[k] = make_uint2(0, 0);
         if (r0 + k >= ctas) continue;
         const SampleShared& o = *cluster.map_shared_rank(&s, r0 + k);
-        if (wide()) c[k] = *reinterpret_cast<const uint2*>(&o.count[2 * tid()]);
-        else c[k].x = o.count[tid()], c[k].y = c[k].x >> 16, c[k].x &= 0xFFFFu;
+        if (wide()) c[k] = *reinterpret_cast<const uint2*>(&o.ranges[0][2 * tid()]);
+        else c[k].x = o.ranges[0][tid()], c[k].y = c[k].x >> 16, c[k].x &= 0xFFFFu;
 #pragma unroll
-          for (int i = 0; i < PARTS; ++i) b[k][i] = *reinterpret_cast<const uint2*>(&o.weight[i][2 * tid()]);
+        for (int i = 0; i < PARTS; ++i) b[k][i] = *reinterpret_cast<const uint2*>(&o.ranges[1 + i][2 * tid()]);
       }
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
@@ -617,7 +624,7 @@ struct Row {
   __device__ __forceinline__ Border find_border(uint64_t target) {
     uint32_t n[2];
     uint64_t m[2];
-    gather_ranges<MASS ? 3 : 0>(n, m);
+    gather_ranges<MASS>(n, m);
     if (!MASS) m[0] = n[0], m[1] = n[1];
     uint64_t to = prefix(m[0] + m[1]);
     __syncthreads();
@@ -641,8 +648,8 @@ struct Row {
   __device__ __forceinline__ void clear_ranges(bool mass) {
     __syncthreads();
     for (int i = tid(); i < SMP_BINS; i += SMP_THREADS) {
-      s.count[i] = 0;
-      if (mass) s.weight[0][i] = s.weight[1][i] = s.weight[2][i] = 0;
+      s.ranges[0][i] = 0;
+      if (mass) s.ranges[1][i] = s.ranges[2][i] = s.ranges[3][i] = 0;
     }
     __syncthreads();
   }
@@ -656,9 +663,9 @@ struct Row {
   __device__ __forceinline__ void add_to_range(int bin, uint64_t v) {
     count_in(bin);
     constexpr uint32_t MASK = (1u << SMP_PART) - 1;
-    atomicAdd(&s.weight[0][bin], (uint32_t)v & MASK);
-    atomicAdd(&s.weight[1][bin], (uint32_t)(v >> SMP_PART) & MASK);
-    atomicAdd(&s.weight[2][bin], (uint32_t)(v >> (2 * SMP_PART)));
+    atomicAdd(&s.ranges[1][bin], (uint32_t)v & MASK);
+    atomicAdd(&s.ranges[2][bin], (uint32_t)(v >> SMP_PART) & MASK);
+    atomicAdd(&s.ranges[3][bin], (uint32_t)(v >> (2 * SMP_PART)));
   }
 
   // The cut among the tokens in(x, token), `n` of the cluster: the one that brings the sum
@@ -836,37 +843,35 @@ struct Row {
     const double want = ceil(share * (double)all);
     const uint64_t target = want < 1.0 ? 1 : (uint64_t)want;
     const Window win = window((float)all * UNIT, (float)want * UNIT, missed);
-    if (win.lo == SMP_BINS) return;  // all are kept
-    const float least = fmaxf(counted, below(win.hi));
+    if (win.lo == SMP_COARSE) return;  // all are kept
+    // the border lies among the logits from `least` on and below `above` (of which all are kept so far)
+    const float least = fmaxf(counted, below(win.hi, SMP_COARSE, 1.f / 64));
+    const float above = win.lo == 0 ? INFINITY : (whole - ((float)win.lo - 0.25f) * (1.f / 64)) * s.inverse;
     if (!solo && win.through <= SMP_SOLO) {
       listed = false;
       list(least);
       try_solo();
       if (gone) return;
     }
-    const int from = 64 * win.lo, to = win.hi == SMP_BINS - 1 ? INT32_MAX : 64 * (win.hi + 1);
     const Cut old = cut;
-    const auto inside = [&](float x, int token) {
-      const int v = place_of(x);
-      return x >= least && v >= from && v < to && old.keeps(x, token);
-    };
-    uint64_t above = 0;
+    const auto inside = [&](float x, int token) { return x >= least && x < above && old.keeps(x, token); };
+    uint64_t before = 0;
     if (solo) {
-      each_left([&](float x, int token) {
-        if (place_of(x) < from && old.keeps(x, token)) above += steps_of(x);
+      each_left([&](float x, int) {
+        if (x >= above) before += steps_of(x);
       });
-      above = sum_up(warp_sum64(above)).all;
+      before = sum_up(warp_sum64(before)).all;
     } else {
-      above = group_and_list(least, from, to, 32 * (int64_t)win.before > a.V);
+      before = group_and_list(least, above, 32 * (int64_t)win.before > a.V);
     }
-    uint64_t rest = target > above ? target - above : 1;
+    const uint64_t rest = target > before ? target - before : 1;
     if (win.inside <= SMP_RANK) {
       rank_few<true>(rest, inside);
     } else {
       // the window's weight in finer ranges (a quarter of them where the cluster weighs)
       Ranges fine;
-      const float top = fminf(mx, (whole - ((float)win.lo - 0.125f) * (1.f / 32)) * s.inverse);
-      fine.set(top, win.hi == SMP_BINS - 1 ? top - least : ((float)(win.hi - win.lo) + 1.25f) * (1.f / 32) * s.inverse);
+      const float top = fminf(mx, above);
+      fine.set(top, top - least);
       const int shift = solo ? 6 : 8, bins = solo ? SMP_BINS : SMP_FINE;
       const auto bin_of = [&](float x) { return min(max(fine.place(x), 0) >> shift, bins - 1); };
       clear_ranges(true);
@@ -890,29 +895,41 @@ struct Row {
       grouped = true;
     }
   }
-  // Ranges that can hold the border: a range's tokens weigh as many times the weight at their
-  // mean place, by what their places are rounded more or less, and by the spread of a range more
-  // (2^-14 of it); the last one takes what lies lower too, and may weigh nothing.  Summed from the first range on, and from the last
-  // one back, where `missed` comes on top, from the weight of all.
+  // Ranges that can hold the border.  A range's tokens weigh between as many times the weights at
+  // its ends (a little apart, as places are rounded); the last one takes what lies lower too, and
+  // may weigh nothing.  Summed from the first range on, and from the last one back, where `missed`
+  // comes on top, from the weight of all: half a percent of the smaller of both sides.
   struct Window {
-    int lo, hi;                        // lo = SMP_BINS: no range
-    uint32_t before, inside, through;  // tokens before them, in them, in all up to one behind them
+    int lo, hi;                        // lo = SMP_COARSE: no range
+    uint32_t before, inside, through;  // tokens up to two before them, from there on up to one behind them, in all
   };
   __device__ __forceinline__ Window window(float all, float goal, float missed) {
-    uint32_t n[2];
-    uint64_t places[2];
-    gather_ranges<1>(n, places);
-    const float off = 1.f / 4096 + fabsf(whole) * (1.f / (1 << 23));  // (the roundings of a place and of y)
-    float up[2], down[2];
+    static_assert(SMP_COARSE == 4 * SMP_THREADS, "four ranges a thread");
+    uint32_t n[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float mean = n[j] ? (float)places[j] / (float)n[j] : 0.f;
-      const float y = -(64.f * (float)(2 * tid() + j) + mean) * (1.f / 2048);
-      up[j] = (float)n[j] * exp2f(y + off) * (1.f + 1.f / 8192);
-      down[j] = 2 * tid() + j == SMP_BINS - 1 ? 0.f : (float)n[j] * exp2f(y - off);
+    for (int r = 0; r < ROW_CLUSTER; ++r) {
+      if (r >= ctas) break;
+      const uint32_t* o = &cluster.map_shared_rank(&s, r)->ranges[0][0];
+      uint4 c;
+      if (wide()) {
+        c = *reinterpret_cast<const uint4*>(o + 4 * tid());
+      } else {
+        const uint2 h = *reinterpret_cast<const uint2*>(o + 2 * tid());
+        c = make_uint4(h.x & 0xFFFFu, h.x >> 16, h.y & 0xFFFFu, h.y >> 16);
+      }
+      n[0] += c.x, n[1] += c.y, n[2] += c.z, n[3] += c.w;
     }
-    float tu = up[0] + up[1], td = down[0] + down[1];
-    uint32_t tn = n[0] + n[1];
+    const float off = 1.f / 4096 + (fabsf(whole) + 64.f) * (1.f / (1 << 23));  // (the roundings of a place and of y)
+    const float upper = exp2f((float)tid() * (-4.f / 64) + off) * (1.f + 1.f / (1 << 20)), ratio = exp2f(-1.f / 64 - 2.f * off);
+    float up[4], down[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      constexpr float STEP[4] = {1.f, 0.989228f, 0.978572f, 0.968031f};  // 2^(-j / 64), and up
+      up[j] = (float)n[j] * (upper * STEP[j]);
+      down[j] = 4 * tid() + j == SMP_COARSE - 1 ? 0.f : up[j] * ratio * (1.f - 1.f / (1 << 17));
+    }
+    float tu = (up[0] + up[1]) + (up[2] + up[3]), td = (down[0] + down[1]) + (down[2] + down[3]);
+    uint32_t tn = n[0] + n[1] + n[2] + n[3];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const float y = __shfl_up_sync(0xffffffffu, tu, o), z = __shfl_up_sync(0xffffffffu, td, o);
@@ -921,7 +938,7 @@ struct Row {
     }
     __syncthreads();
     if (lane() == 31) s.fscan[warp()] = make_float2(tu, td), s.wkept[warp()] = tn;
-    if (tid() == 0) s.at[0] = s.at[1] = SMP_BINS, s.at[2] = s.at[3] = s.at[4] = 0;
+    if (tid() == 0) s.at[0] = s.at[1] = SMP_COARSE, s.at[2] = s.at[3] = 0;
     __syncthreads();
     float all_up = 0.f, all_down = 0.f;
     for (int i = 0; i < SMP_WARPS; ++i) {
@@ -930,29 +947,34 @@ struct Row {
       all_up += o.x, all_down += o.y;
     }
     const float slack = all * (1.f / (1 << 18));  // (sums in fp32)
+    {
+      float u = tu, d = td;  // up to range 4 tid + j
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float u = j ? tu : tu - up[1], d = j ? td : td - down[1];  // up to range 2 tid + j
-      if (fminf(u, all - (all_down - d)) + slack >= goal) atomicMin(&s.at[0], 2 * tid() + j);
-      if (fmaxf(d, all - (all_up - u) - missed) - slack >= goal) atomicMin(&s.at[1], 2 * tid() + j);
+      for (int j = 3; j >= 0; --j) {
+        if (fminf(u, all - (all_down - d)) + slack >= goal) atomicMin(&s.at[0], 4 * tid() + j);
+        if (fmaxf(d, all - (all_up - u) - missed) - slack >= goal) atomicMin(&s.at[1], 4 * tid() + j);
+        u -= up[j], d -= down[j];
+      }
     }
     __syncthreads();
     Window z;
-    z.lo = s.at[0], z.hi = min(s.at[1], SMP_BINS - 1);
+    z.lo = s.at[0], z.hi = min(s.at[1], SMP_COARSE - 1);
+    {
+      uint32_t c = tn;  // tokens up to range b
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int b = 2 * tid() + j;
-      const uint32_t c = j ? tn : tn - n[1];  // tokens up to range b
-      if (b == z.lo - 1) s.at[2] = c;
-      if (b == z.hi) s.at[3] = c;
-      if (b == min(z.hi + 1, SMP_BINS - 1)) s.at[4] = c;
+      for (int j = 3; j >= 0; --j) {
+        const int b = 4 * tid() + j;
+        if (b == z.lo - 2) s.at[2] = c;
+        if (b == min(z.hi + 1, SMP_COARSE - 1)) s.at[3] = c;
+        c -= n[j];
+      }
     }
     meet();  // (all have read the ranges)
-    z.before = s.at[2], z.inside = s.at[3] - s.at[2], z.through = s.at[4];
+    z.before = s.at[2], z.through = s.at[3], z.inside = z.through - z.before;
     return z;
   }
-  // Weight by groups of the kept tokens before place `from`; the list of those up to `to`.
-  __device__ __forceinline__ uint64_t group_and_list(float least, int from, int to, bool dense) {
+  // Weight by groups of the tokens from `above` on; the list of the kept ones below it from `least` on.
+  __device__ __forceinline__ uint64_t group_and_list(float least, float above, bool dense) {
     low = least;
     listed = false;
     __syncthreads();
@@ -961,31 +983,33 @@ struct Row {
     __syncthreads();
     uint32_t* const part = reinterpret_cast<uint32_t*>(s.group);
     uint64_t total = 0;
-    const bool none = cut.x == -INFINITY;
     const auto put = [&](float x, int token) {
+      if (!cut.keeps(x, token)) return;
       const uint32_t i = atomicAdd(&s.n_list, 1u);
       if (i < SMP_LIST) left[i] = make_float2(x, __int_as_float(token));
     };
     if (dense) {
       each_group([&](int g) {
         Sum sum;
-        each_of(g, [&](int, float x, int place) {
-          const int v = place_of(x);
-          const bool k = none || cut.keeps(x, first + place);
+        uint32_t take = 0;
+        each_of(g, [&](int e, float x, int) {
           float b, c;
           w.of(x, b, c);
-          sum.add(k && v < from ? b : 0.f, c);
-          if (v >= from && v < to && k && x >= low) put(x, first + place);
+          sum.add(x >= above ? b : 0.f, c);
+          take |= (uint32_t)(x >= least && x < above) << e;
         });
         const uint64_t v = sum.warp_steps();
         if (lane() == 0) s.group[g] = v;
         total += v;
+        for (; take; take &= take - 1) {  // (few)
+          const int e = __ffs(take) - 1, place = ((g * TILES + e / W) * 32 + lane()) * W + e % W;
+          put(at(place), first + place);
+        }
+        __syncwarp();
       });
     } else {
       each_left([&](float x, int token) {
-        const int v = place_of(x);
-        if (v >= to || !cut.keeps(x, token)) return;
-        if (v >= from) {
+        if (x < above) {
           put(x, token);
           return;
         }
