@@ -55,7 +55,7 @@ constexpr int SMP_LIST = 4608;        // tokens that a CTA's list takes
 constexpr int SMP_SOLO = 4096;        // tokens of a row that one CTA goes on with alone
 constexpr int SMP_QUEUE = 32 * 8 + 32;  // tokens of a warp on their way to whole warps: half a group and a rest
 constexpr int SMP_RANK = 128;         // tokens that are ranked at once
-constexpr int64_t SMP_L2 = 100 << 20;   // bytes of rows that L2 keeps
+constexpr int SMP_LONG = 65536;       // tokens of a row that two CTAs share where rows wait
 constexpr int SMP_MAX_V = 393216;     // (sets the groups)
 constexpr int SMP_MAX_GROUPS = SMP_MAX_V / SMP_GROUP + 1;
 constexpr int SMP_UNIT = 42;          // weights are counted in steps of 2^-42
@@ -566,9 +566,9 @@ struct Row {
   __device__ __forceinline__ float below(int bin, int bins = SMP_BINS, float per = 1.f / 32) const {
     return bin >= bins - 1 ? -INFINITY : (whole - ((float)bin + 1.25f) * per) * s.inverse;
   }
-  // Counts x in its coarse range if it is `from` or more (alive at least).  (A predicate, no
-  // branch: with branches around the atomics, and more instructions for places, this and
-  // group_and_list took 77 instructions a token, now NN; 272 rows of 151936, p = 0.9: 203 and XX us.)
+  // Counts x in its coarse range if it is `from` or more (alive at least); a predicate, no branch:
+  // with one, and a second atomic for a mean in ranges twice as wide, 272 rows of 151936 at
+  // p = 0.9 take 203 us for 190.
   __device__ __forceinline__ void count_coarse(float x, float from) {
     const int narrow = !wide(), bin = min((int)(__float_as_uint(place_float(x)) >> 5 & 0x3FFFFu), SMP_COARSE - 1);
     const uint32_t at = smem_u32(&s.ranges[0][0]) + ((bin >> narrow) << 2), n = 1u << ((bin & narrow) << 4);
@@ -1227,28 +1227,69 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
   cluster.sync();  // (a CTA's memory stays until the others have read it)
 }
 
+constexpr size_t SMP_SMEM = (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2);
+
 template <typename T, int ROOM>
 static cudaError_t launch_sample(const SampleArgs& a, int32_t rows, int ctas, cudaStream_t stream) {
   static bool done[64];
   const auto kernel = sample_kernel<T, ROOM>;
-  constexpr size_t smem = (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2);
-  const cudaError_t e = pced_host::allow_smem(kernel, smem, done);
+  const cudaError_t e = pced_host::allow_smem(kernel, SMP_SMEM, done);
   if (e != cudaSuccess) return e;
-  return pced_host::launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, smem, stream, true, a);
+  return pced_host::launch_cluster(kernel, dim3((unsigned)(rows * ctas)), ctas, SMP_THREADS, SMP_SMEM, stream, true, a);
+}
+// Whether the SMs hold so many clusters of `ctas` at once, ROOM CTAs on each (not whenever the SMs'
+// number allows it: a cluster lies within a part of the device).
+template <typename T, int ROOM>
+static cudaError_t all_at_once(int32_t rows, int ctas, bool& yes) {
+  static int cache[64][ROW_CLUSTER + 1];
+  static bool done[64];
+  const auto kernel = sample_kernel<T, ROOM>;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = pced_host::allow_smem(kernel, SMP_SMEM, done);
+  if (e != cudaSuccess) return e;
+  if (!cache[dev][ctas]) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas), cfg.blockDim = dim3(SMP_THREADS), cfg.dynamicSmemBytes = SMP_SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)ctas, 1, 1};
+    cfg.attrs = attr, cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    cache[dev][ctas] = n;
+  }
+  yes = rows <= cache[dev][ctas];
+  return cudaSuccess;
 }
 template <typename T>
 cudaError_t launch_sample_t(SampleArgs a, int32_t rows, cudaStream_t stream) {
-  // CTAs of a row: as many as fit the SMs at once, two on each, while a part is more than a few
-  // tokens a thread; and so many that the rows on the SMs fit L2 together
-  const int64_t slots = 2 * (int64_t)pced_host::num_sms(), bytes = (int64_t)a.V * sizeof(T);
-  int ctas = 1;
-  while (ctas < ROW_CLUSTER && a.V > 8 * SMP_THREADS * ctas &&
-         (a.V > SMP_MAX_PER * ctas || 2 * ctas * (int64_t)rows <= slots || (rows < slots / ctas ? rows : slots / ctas) * bytes > SMP_L2))
-    ctas *= 2;
+  // CTAs of a row: eight or four with an SM each (and twice the registers), else four or two with
+  // half an SM, as long as all rows run at once and a part is more than a few tokens a thread.  fp32, us
+  // at p = 0.9 with 1, 2, 4, 8 on an SM each | on half of one: a row of 128256 78, 49, 34, 30 | 79, 50, 37,
+  // 33; 19 of 151936 88, 55, 38, 64 (not all at once) | 90, 57, 40, 48; 38 of them 88, 55, 73, 96 | 90, 57,
+  // 56, 82; 152 of them 112, 131, 200, 358 | 113, 104, 154, 236.  Where the requests differ
+  // the longest rules, and more CTAs gain: mixed cuts, 38 rows 117, 69, 73, - | 125, 74, 52, 52.  More rows
+  // than that run two a row if that is long, so that those waiting fill the gaps: 272 of 151936 at
+  // p = 0.9 178 with one, 191 with two, mixed cuts 196 and 152; of 65536 mixed 90 and 83, of 32768 60 and 69.
+  const auto long_enough = [&](int ctas) { return a.V > 4 * SMP_THREADS * ctas; };
+  bool yes = false;
+  cudaError_t e = cudaSuccess;
+  int ctas = 0;
+  const int alone[] = {8, 4}, shared[] = {4, 2};
+  static_assert(ROW_CLUSTER == 8, "the largest of these");
+  bool room = false;
+  for (int n : alone)
+    if (!ctas && e == cudaSuccess && long_enough(n) && (e = all_at_once<T, 1>(rows, n, yes)) == cudaSuccess && yes) ctas = n, room = true;
+  for (int n : shared)
+    if (!ctas && e == cudaSuccess && long_enough(n) && (e = all_at_once<T, 2>(rows, n, yes)) == cudaSuccess && yes) ctas = n;
+  if (e != cudaSuccess) return e;
+  if (!ctas) ctas = a.V >= SMP_LONG ? 2 : 1;
+  if (ctas == 1 && rows <= pced_host::num_sms()) room = true;
+  while (a.V > SMP_MAX_PER * ctas) ctas *= 2;
   a.per = (a.V + ctas - 1) / ctas;
-  // (one CTA an SM has twice the registers)
-  return (int64_t)rows * ctas <= pced_host::num_sms() ? launch_sample<T, 1>(a, rows, ctas, stream)
-                                           : launch_sample<T, 2>(a, rows, ctas, stream);
+  return room ? launch_sample<T, 1>(a, rows, ctas, stream) : launch_sample<T, 2>(a, rows, ctas, stream);
 }
 // (a translation unit each: they compile for a minute)
 extern template cudaError_t launch_sample_t<float>(SampleArgs, int32_t, cudaStream_t);
