@@ -849,7 +849,7 @@ struct Row {
     }
     const double want = ceil(share * (double)all);
     const uint64_t target = want < 1.0 ? 1 : (uint64_t)want;
-    const Window win = window((float)all * UNIT, (float)want * UNIT, missed);
+    const Window win = window((float)all * UNIT, (float)want * UNIT, 1.01f * missed);  // (`counted` is rounded)
     if (win.lo == SMP_COARSE) return;  // all are kept
     // the border lies among the logits from `least` on and below `above` (of which all are kept so far)
     const float least = fmaxf(counted, below(win.hi, SMP_COARSE, 1.f / 64));
