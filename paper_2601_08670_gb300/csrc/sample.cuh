@@ -142,7 +142,8 @@ struct Sum {
   }
 };
 static_assert(SMP_UNIT == 42, "18 + 24");
-static_assert(((uint64_t)SMP_MAX_PER << SMP_PART) >> 32 == 0 && SMP_UNIT <= 3 * SMP_PART, "sums of parts, 2^SMP_UNIT itself among them");
+static_assert(((uint64_t)SMP_MAX_PER << SMP_PART) >> 32 == 0 && SMP_UNIT <= 3 * SMP_PART,
+              "sums of parts, 2^SMP_UNIT itself among them");
 static_assert(SMP_MAX_V <= (int64_t)SMP_MAX_PER * ROW_CLUSTER, "parts of a row");
 static_assert(SMP_SOLO <= SMP_LIST, "one CTA's list");
 static_assert(SMP_BINS == 4 * SMP_FINE, "see keep_share");
@@ -1288,7 +1289,8 @@ cudaError_t launch_sample_t(SampleArgs a, int32_t rows, cudaStream_t stream) {
   static_assert(ROW_CLUSTER == 8, "the largest of these");
   bool room = false;
   for (int n : alone)
-    if (!ctas && e == cudaSuccess && long_enough(n) && (e = all_at_once<T, 1>(rows, n, yes)) == cudaSuccess && yes) ctas = n, room = true;
+    if (!ctas && e == cudaSuccess && long_enough(n) && (e = all_at_once<T, 1>(rows, n, yes)) == cudaSuccess && yes)
+      ctas = n, room = true;
   for (int n : shared)
     if (!ctas && e == cudaSuccess && long_enough(n) && (e = all_at_once<T, 2>(rows, n, yes)) == cudaSuccess && yes) ctas = n;
   if (e != cudaSuccess) return e;

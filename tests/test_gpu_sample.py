@@ -95,6 +95,12 @@ def test_the_largest_vocabularies(cuda_ok, V, bf16):
           low=[0, 0, 0, 0, 1e-3])
 
 
+@pytest.mark.parametrize("rows", [10, 19, 38, 64, 120, 160])
+@pytest.mark.parametrize("V", [9000, 70_001])
+def test_rows_split_over_any_number_of_ctas(cuda_ok, rows, V):
+    check(logits(rows, V, rows, rows % 3 == 1), numbers(rows, V), near=1, **mixed(rows, rows + V))
+
+
 def test_every_border_of_a_few_tokens(cuda_ok):
     # u just below and just above each border: whole numbers as weights, so that the borders are known
     w = np.array([3, 1, 4, 1, 5, 9, 2, 6], np.float64)
