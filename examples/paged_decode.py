@@ -57,7 +57,8 @@ class Model:
 
 class Loop:
     """B queries of N experts and the amateur; `blocks` 0: attention over all blocks, else over so many.  eight: 8-bit
-    caches.  sampling: keyword arguments of pced.sample, numbers for all queries (None: the best token)."""
+    caches.  sampling: keyword arguments of pced.sample, numbers for all queries (None: the best token).  A query whose
+    mask forbids everything has token -1 of expert 0."""
 
     def __init__(self, model, B, N, lens, max_steps, beta, r, gamma=2.5, block_rows=16, blocks=0, penalties=None,
                  mask=None, eight=False, sampling=None, seed=0):
@@ -116,7 +117,8 @@ class Loop:
         m, S = self.model, self.B * (self.N + 1)
         last = self.history[:, self.t - 1] if self.t else torch.zeros(self.B, dtype=torch.int32,
                                                                       device=self.seq_len.device)
-        x = m.embed[last.long()].float().repeat_interleave(self.N + 1, 0)
+        # (a query without a token, -1, goes on as from token 0)
+        x = m.embed[last.clamp(min=0).long()].float().repeat_interleave(self.N + 1, 0)
         self.seq_len += 1
         for layer, cache in enumerate(self.caches):
             q, k, v = m.project(layer, x)
@@ -137,6 +139,8 @@ class Loop:
         self.logprobs = lp
         if self.sampling is None:
             token, expert, _ = pced.contrastive_select(lp, self.beta, self.r, self.gamma)
+            none = token >= lp.shape[1]  # (no score was a number)
+            token, expert = torch.where(none, -1, token), torch.where(none, 0, expert)
         else:
             token, expert = self.draw(lp)
         self.history[:, self.t], self.expert[:, self.t] = token, expert
@@ -152,7 +156,8 @@ class Loop:
         best, expert = scores.max(1)
         u = torch.rand(self.B, device=lp.device, generator=self.random)
         token = pced.sample(best, u, status=self.status, **self.sampling)
-        return token, expert.gather(1, token.long()[:, None])[:, 0].int() + 1
+        of_token = expert.gather(1, token.clamp(min=0).long()[:, None])[:, 0].int() + 1
+        return token, torch.where(token < 0, 0, of_token)
 
     def device_status(self):
         return int(self.status.item()) | pced.device_status(self.ws)
