@@ -349,8 +349,8 @@ class PagedCache:
     and their addresses taken once: change their contents, not their storage (the fields take no other tensor; for
     one, make another PagedCache).  They lie on one CUDA device, which is the current one when the calls are made."""
 
-    _TAKEN = frozenset(["k", "v", "scale", "block_table", "seq_len", "summary", "key_step", "num_blocks", "Hkv",
-                        "block_rows", "D", "S", "max_blocks"])
+    _TAKEN = frozenset(["k", "v", "block_table", "seq_len", "summary", "key_step", "num_blocks", "Hkv", "block_rows",
+                        "D", "S", "max_blocks"])
     _NUMBERS, _NAME = torch.bfloat16, "bf16"
     eight = False  # whether k and v are 8-bit numbers with scales
 
@@ -409,6 +409,7 @@ class PagedCache8(PagedCache):
     them, block_select reads the summaries, which kv_append keeps; block_summaries reads bf16 keys and takes a PagedCache
     alone."""
 
+    _TAKEN = PagedCache._TAKEN | {"scale"}
     _NUMBERS, _NAME = torch.float8_e4m3fn, "e4m3"
     eight = True
 
