@@ -666,7 +666,7 @@ pced_status pced_paged_attention8(const pced_paged_cache8* cache, const void* q,
  * (2^-42 of the power of two from the largest up), sixteen at a time: the choice
  * depends on no order of sums and differs from that of exact sums in about one
  * row of a million.  Weights below 2^-44 are nothing to a cut.  Temperatures
- * count as 1e-37 at least and 1e30 at most.
+ * count as 1e-37 at least and 1e30 at most, to weights, min_p and logprob alike.
  * A row whose logits are all -inf has token -1 and logprob -inf; so has one
  * with a parameter that is not a number, t < 0 or u outside [0, 1], which sets
  * PCED_DEV_BAD_PARAM.  V <= 393216.

@@ -221,7 +221,7 @@ struct SampleShared {
   float2 fscan[SMP_WARPS];
   Border border;
   float threshold;
-  double below;  // of a min_p: t log(p)
+  double below;  // of a min_p: t log(p), t the temperature that counts
   uint64_t cut;
   // what the cluster's warps tell one another: two of each, by turns, with a barrier of the
   // cluster between a write and its reads, so that the next write to one comes after them
@@ -1167,7 +1167,7 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
   // ---- its largest logit
   float mx = -INFINITY;
   R.each_group([&](int g) { R.each_of(g, [&](int, float x, int) { mx = fmaxf(mx, x); }); });
-  // (the reciprocals come while the last loads are on their way)
+  // (the reciprocals come while the last loads are on their way; held: the temperature that counts)
   const float held = fminf(fmaxf(t, 1e-37f), 1e30f), lh = 1.44269502f, ll = 1.92596303e-08f;
   R.w.ch = __fdiv_rn(lh, held);
   R.w.cl = __fdiv_rn(fmaf(-R.w.ch, held, lh) + ll, held);
@@ -1177,7 +1177,7 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
     const int hi = __reduce_max_sync(0xffffffffu, ordered(mx + 0.f));
     if (R.lane() == 0) R.mine().mx[R.warp()] = hi;
     cluster.barrier_arrive();
-    if (tid == SMP_THREADS - 1 && least > 0.f) s.below = (double)t * log((double)least);  // (takes a microsecond)
+    if (tid == SMP_THREADS - 1 && least > 0.f) s.below = (double)held * log((double)least);  // (takes a microsecond)
     __syncwarp();
     cluster.barrier_wait();
     const int r = R.lane() >> 2;  // a CTA's sixteen by four lanes
@@ -1225,13 +1225,13 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
   const auto seek = [&](uint64_t total) { return min((uint64_t)((double)u * (double)total), total - 1); };
   if (R.solo) {
     const uint64_t total = R.template weigh_kept<false>().all;
-    R.draw_solo(seek(total), row, t, total);
+    R.draw_solo(seek(total), row, held, total);
     return;
   }
   const typename Row<T>::Sums sums =
       R.grouped ? R.sum_groups() : R.cut.x == -INFINITY ? R.template weigh_all<false>(0.f) : R.weigh_groups();
   const uint64_t left = seek(sums.all);
-  if (left >= sums.before && left < sums.before + sums.own) R.draw(left - sums.before, row, t, sums.all);
+  if (left >= sums.before && left < sums.before + sums.own) R.draw(left - sums.before, row, held, sums.all);
   cluster.sync();  // (a CTA's memory stays until the others have read it)
 }
 
