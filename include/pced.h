@@ -662,7 +662,7 @@ pced_status pced_paged_attention8(const pced_paged_cache8* cache, const void* q,
  * the first kept one, in the order of the vocabulary, with
  * sum_{v' <= v} w_v' > u sum w.  t = 0, k = 1, p <= 0 and min_p > 1 give the
  * first of the largest (logprob 0).  Logits of +inf share everything equally.
- * Weights are exact to about 2^-32 of themselves and are added in whole steps
+ * Weights are exact to 2^-30 of themselves (most to 2^-32) and are added in whole steps
  * (2^-42 of the power of two from the largest up), sixteen at a time: the choice
  * depends on no order of sums and differs from that of exact sums in about one
  * row of a million.  Weights below 2^-44 are nothing to a cut.  Temperatures

@@ -8,8 +8,8 @@
 //
 // A sum over a vocabulary decides at which token u falls, and its error counts 150,000
 // times (every border of two tokens is a place to be wrong): with weights of 24 bits one row
-// in some thousands gets another token than in 64 bits.  So weights are exact to about
-// 2^-32 of themselves, and are added without further loss (see Sum).
+// in some thousands gets another token than in 64 bits.  So weights are exact to 2^-30
+// of themselves, and are added without further loss (see Sum).
 //
 // A cluster of CTAs reads a row two to four times, from L2 after the first: for its largest logit,
 // for its weights, for what a cut leaves.  A cut is found by counting the tokens in equal
@@ -71,44 +71,56 @@ constexpr int SMP_MAX_PER = (1 << 18) - 1;  // tokens of a CTA: as many such par
 constexpr float SMP_ALIVE = 44.f;     // -log2 of weights that no cut asks about
 constexpr float SMP_LOWEST = 100.f;   // ... and that are nothing
 
-// {2^(j / 32) as fp32, what it is short of, relative}
+// {2^(j / 64) as fp32, log2 of what it has to be multiplied by}
 struct Exp2Entry {
   uint32_t bits;
   float rest;
 };
-__device__ const Exp2Entry kExp2Table[32] = {
-    {0x3F800000u, 0.f}, {0x3F82CD87u, -4.70845762e-08f}, {0x3F85AAC3u, 4.62854715e-08f}, {0x3F88980Fu, -5.56042252e-08f},
-    {0x3F8B95C2u, -1.19921575e-08f}, {0x3F8EA43Au, -4.87760623e-08f}, {0x3F91C3D3u, 4.72978243e-08f}, {0x3F94F4F0u, -3.48144269e-08f},
-    {0x3F9837F0u, 3.19341815e-08f}, {0x3F9B8D3Au, -2.68866653e-08f}, {0x3F9EF532u, 3.62105723e-08f}, {0x3FA27043u, 1.11842102e-09f},
-    {0x3FA5FED7u, -3.09907193e-08f}, {0x3FA9A15Bu, -2.63830096e-08f}, {0x3FAD583Fu, -7.47521334e-09f}, {0x3FB123F6u, -4.24563567e-08f},
-    {0x3FB504F3u, 1.71142709e-08f}, {0x3FB8FBAFu, 2.30019666e-08f}, {0x3FBD08A4u, -3.04768335e-08f}, {0x3FC12C4Du, -1.65385377e-08f},
-    {0x3FC5672Au, 5.23333421e-09f}, {0x3FC9B9BEu, -3.5920646e-08f}, {0x3FCE248Cu, 6.10759177e-09f}, {0x3FD2A81Eu, -3.11405444e-08f},
-    {0x3FD744FDu, -1.47196051e-08f}, {0x3FDBFBB8u, -2.82181016e-08f}, {0x3FE0CCDFu, -5.25879518e-09f}, {0x3FE5B907u, -6.36038733e-09f},
-    {0x3FEAC0C7u, -6.12825968e-09f}, {0x3FEFE4BAu, -2.48804088e-08f}, {0x3FF5257Du, 5.14060927e-09f}, {0x3FFA83B3u, -8.69726691e-09f}};
+constexpr int SMP_EXP2 = 64;
+__device__ const Exp2Entry kExp2Table[SMP_EXP2] = {
+    {0x3F800000u, 0.f}, {0x3F8164D2u, -8.15134182e-09f}, {0x3F82CD87u, -6.79286885e-08f}, {0x3F843A29u, -3.92309936e-08f},
+    {0x3F85AAC3u, 6.67758187e-08f}, {0x3F871F62u, -6.70637164e-08f}, {0x3F88980Fu, -8.02199409e-08f}, {0x3F8A14D5u, 7.30413632e-08f},
+    {0x3F8B95C2u, -1.73010264e-08f}, {0x3F8D1ADFu, 5.57574609e-08f}, {0x3F8EA43Au, -7.03689835e-08f}, {0x3F9031DCu, 4.00033358e-08f},
+    {0x3F91C3D3u, 6.82363321e-08f}, {0x3F935A2Bu, 2.74734742e-08f}, {0x3F94F4F0u, -5.02265998e-08f}, {0x3F96942Du, 3.14805497e-08f},
+    {0x3F9837F0u, 4.60712819e-08f}, {0x3F99E046u, -6.0841586e-08f}, {0x3F9B8D3Au, -3.87892598e-08f}, {0x3F9D3EDAu, -4.85744387e-08f},
+    {0x3F9EF532u, 5.22408143e-08f}, {0x3FA0B051u, 8.41478265e-09f}, {0x3FA27043u, 1.61354052e-09f}, {0x3FA43516u, -4.29211156e-08f},
+    {0x3FA5FED7u, -4.47101591e-08f}, {0x3FA7CD94u, -3.84792926e-08f}, {0x3FA9A15Bu, -3.80626375e-08f}, {0x3FAB7A3Au, -3.72789515e-08f},
+    {0x3FAD583Fu, -1.07844533e-08f}, {0x3FAF3B79u, -4.05290344e-08f}, {0x3FB123F6u, -6.12515763e-08f}, {0x3FB311C4u, 8.96096175e-09f},
+    {0x3FB504F3u, 2.46906744e-08f}, {0x3FB6FD92u, -1.35528202e-08f}, {0x3FB8FBAFu, 3.3184822e-08f}, {0x3FBAFF5Bu, -3.58339562e-08f},
+    {0x3FBD08A4u, -4.39687788e-08f}, {0x3FBF179Au, -3.30846959e-08f}, {0x3FC12C4Du, -2.38600659e-08f}, {0x3FC346CDu, -1.6670608e-08f},
+    {0x3FC5672Au, 7.55010543e-09f}, {0x3FC78D75u, -2.3842496e-08f}, {0x3FC9B9BEu, -5.18225391e-08f}, {0x3FCBEC15u, -4.440113e-10f},
+    {0x3FCE248Cu, 8.8113925e-09f}, {0x3FD06334u, -1.52952193e-08f}, {0x3FD2A81Eu, -4.49263098e-08f}, {0x3FD4F35Bu, -3.39957644e-08f},
+    {0x3FD744FDu, -2.12359019e-08f}, {0x3FD99D16u, -2.43133815e-08f}, {0x3FDBFBB8u, -4.07101162e-08f}, {0x3FDE60F5u, -4.85806915e-08f},
+    {0x3FE0CCDFu, -7.58683782e-09f}, {0x3FE33F89u, 4.34195506e-08f}, {0x3FE5B907u, -9.17609899e-09f}, {0x3FE8396Au, 2.97107601e-08f},
+    {0x3FEAC0C7u, -8.84121043e-09f}, {0x3FED4F30u, 1.11787655e-08f}, {0x3FEFE4BAu, -3.58948427e-08f}, {0x3FF28177u, 2.14003624e-08f},
+    {0x3FF5257Du, 7.41633155e-09f}, {0x3FF7D0DFu, 3.99192928e-08f}, {0x3FFA83B3u, -1.25475035e-08f}, {0x3FFD3E0Cu, 4.39907888e-09f}};
 
 // What a row's weights are made with.  y = x log2(e) / t, from a factor in two parts, is
-// p + low, p rounded to q / 32 + r, q whole; w = 2^(y - N), N the ceiling of the largest
-// y (so the largest weight lies in (1/2, 1]).  2^(q / 32 - N) comes from a table that the
+// p + low, p rounded to q / 64, q whole, what is left r; w = 2^(y - N), N the ceiling of the largest
+// y (so the largest weight lies in (1/2, 1]).  2^(q / 64 - N) comes from a table that the
 // row's CTA makes (16 copies side by side, so that a warp's lanes do not meet on banks),
-// 2^r - 1 from its series to r^4, of which the rest is below 2^-36 of it.
+// and what its number is short of goes into r; 2^r - 1 comes from its series to r^3.
+// Off by at most 2^-30 of itself: r's rounding (at most 2^-31, times ln 2), the last product's and the inner
+// sum's (2^-32 each), what the series leaves out (2^-34.7), and y's (2^-34 at |y| = 8192).
 struct Weight {
   float ch, cl;            // ch + cl = log2(e) / t
   float floor;             // logits are taken as this at least: 2^-SMP_LOWEST
   const float2* table;     // this lane's copy
   // a (1 + g): the weight
   __device__ __forceinline__ void of(float x, float& a, float& g) const {
-    constexpr float MAGIC = 393216.f;  // 1.5 2^18: sums with it are rounded to 32nds; its low bits are 0
+    constexpr float MAGIC = 196608.f;  // 1.5 2^17: sums with it are rounded to 64ths; its low bits are 0
     x = fmaxf(x, floor);               // (also of what is not a number)
     const float p = __fmul_rn(x, ch);
     const float low = fmaf(x, cl, fmaf(x, ch, -p));
     const float shifted = __fadd_rn(p, MAGIC);
-    const float r = __fadd_rn(__fsub_rn(p, __fsub_rn(shifted, MAGIC)), low);
     const uint32_t q = __float_as_uint(shifted);
-    const float2 e = *reinterpret_cast<const float2*>(reinterpret_cast<const char*>(table) + (q << 7 & 0xF80u));
-    a = __uint_as_float(__float_as_uint(e.x) + (q << 18));  // (the entries make up for what q's low bits add)
-    g = fmaf(r, fmaf(r, fmaf(r, fmaf(r, 9.61812911e-3f, 5.55041087e-2f), 2.40226507e-1f), 6.93147181e-1f), e.y);
+    const float2 e = *reinterpret_cast<const float2*>(reinterpret_cast<const char*>(table) + (q << 7 & 0x1F80u));
+    const float r = __fadd_rn(__fsub_rn(p, __fsub_rn(shifted, MAGIC)), __fadd_rn(low, e.y));
+    a = __uint_as_float(__float_as_uint(e.x) + (q << 17));  // (the entries make up for what q's low bits add)
+    g = __fmul_rn(r, fmaf(r, fmaf(r, 5.55041087e-2f, 2.40226507e-1f), 6.93147181e-1f));
   }
 };
+static_assert(SMP_EXP2 == 64, "the bits of q");
 
 // A sum of weights, at most SMP_EACH of them: what fits the grid of 2^-18 that numbers from
 // 32 to 64 have is added exactly, the rest, below 2^-19 each, beside it.
@@ -205,7 +217,7 @@ struct Border {
 };
 
 struct SampleShared {
-  float2 table[32][16];
+  float2 table[SMP_EXP2][16];
   // tokens of the ranges, then their weights, SMP_PART bits each (of SMP_BINS ranges); or the
   // tokens of SMP_COARSE ranges (16 bits each where a part has no more)
   uint32_t ranges[4][SMP_BINS];
@@ -437,8 +449,8 @@ struct Row {
     listed = s.n_list <= SMP_LIST;
   }
 
-  // m, N and the table for temperature t (inverse: 1 / w.ch, entry: of the table)
-  __device__ __forceinline__ void set_weights(float inverse, Exp2Entry entry) {
+  // m, N and the table for temperature t (inverse: 1 / w.ch, entries: this thread's of the table)
+  __device__ __forceinline__ void set_weights(float inverse, const Exp2Entry (&entries)[2]) {
     if (!(fabsf(mx) * w.ch <= 8192.f)) {
       origin = mx;
       s.thread_max[tid()] = moved(s.thread_max[tid()]);
@@ -451,9 +463,12 @@ struct Row {
     listed = gone = grouped = false;
     solo = 0;
     w.table = &s.table[0][lane() & 15];
-    const uint32_t j = tid() / 16;
-    s.table[j][tid() % 16] =
-        make_float2(__uint_as_float(entry.bits - (j << 18) - ((uint32_t)(int)top << 23)), entry.rest);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t j = tid() / 16 + i * (SMP_THREADS / 16);
+      s.table[j][tid() % 16] =
+          make_float2(__uint_as_float(entries[i].bits - (j << 17) - ((uint32_t)(int)top << 23)), entries[i].rest);
+    }
     whole = top;
     if (tid() == 0) {
       s.ym = (y - top) + fmaf(mx, w.cl, fmaf(mx, w.ch, -y));
@@ -1158,7 +1173,8 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
   R.origin = 0.f, R.back = true;
   if (tid == 0) s.from = phase, s.to = phase + n;
   __syncthreads();
-  const Exp2Entry entry = kExp2Table[tid / 16];
+  static_assert(SMP_EXP2 == 2 * (SMP_THREADS / 16), "two entries a thread");
+  const Exp2Entry entries[2] = {kExp2Table[tid / 16], kExp2Table[tid / 16 + SMP_THREADS / 16]};
   pdl_wait();
   // ---- what the row asks for
   const float t = a.temperature ? a.temperature[row] : 1.f, u = a.u[row];
@@ -1215,7 +1231,7 @@ __global__ void __launch_bounds__(SMP_THREADS, ROOM) sample_kernel(SampleArgs a)
     cluster.sync();
     return;
   }
-  R.set_weights(inverse, entry);
+  R.set_weights(inverse, entries);
   // ---- cuts
   if (k > 1 && k < a.V) R.keep_top(k);
   if (!R.gone && p < 1.f) R.keep_share((double)p);
