@@ -599,7 +599,8 @@ pced_status pced_logits_process(const float* x, float* y, int64_t stride, int32_
  *   scale        fp32 [num_blocks][Hkv][2] (8-byte aligned): what a block's
  *                numbers are multiples of, the keys' (0) and the values' (1)
  * pced_kv_append8 writes powers of two there, from 2^-100 on; a cache of the
- * caller's own making may hold any finite scales above 0.  pages alone serves
+ * caller's own making may hold any finite scales above 0 (attention keeps fewer
+ * bits of values' scales below 2^-111).  pages alone serves
  * pced_block_select, which reads the summaries; pced_block_summaries, which reads
  * bf16 keys, must not be given it.
  * ======================================================================== */

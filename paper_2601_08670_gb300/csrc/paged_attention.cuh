@@ -32,6 +32,7 @@ struct PagedAttArgs {
   const int32_t* sel;
   int32_t n_sel;
   float scale_log2;
+  float up;  // what the sums of the values have to be multiplied by (1, or what Tile::math keeps them down by)
   void* out;
   int32_t out_bf16;
   float* lse;
@@ -121,7 +122,7 @@ struct PagedCfg {
 // Writes four outputs of a finished segment, normalised.
 __device__ __forceinline__ void write_out(const PagedAttArgs& a, int s, int h, int D, int hh, int idx0, float mx,
                                           float lsum, const float (&acc)[4]) {
-  const float w = mx == -INFINITY ? 0.f : 1.f / lsum;
+  const float w = mx == -INFINITY ? 0.f : a.up / lsum;
   float y[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) y[j] = mx == -INFINITY ? 0.f : acc[j] * w;
@@ -641,6 +642,7 @@ inline pced_status paged_attention_args(const pced_paged_cache* cache, const voi
   a.Hq = Hq, a.G = Hq / c.Hkv;
   a.sel = sel, a.n_sel = n_sel;
   a.scale_log2 = scale * 1.4426950408889634f;
+  a.up = 1.f;
   a.out = out, a.out_bf16 = out_type == PCED_OUT_BF16;
   a.lse = lse;
   a.scale = nullptr;

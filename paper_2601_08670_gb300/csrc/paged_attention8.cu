@@ -10,7 +10,8 @@
 // so that its largest part lies in [2^14, 2^15) (a part below 2^-28 of it loses bits,
 // which the sum does not keep either), probabilities are counted from 2^7 at the
 // reference (at most 2^15 until it moves), their first 11 bits in one part, the rest, times
-// 2^11, in the other: 23 bits, as a sum in fp32 keeps.
+// 2^11, in the other: 23 bits, as a sum in fp32 keeps.  The values' sums are kept 2^-15 down, so that
+// they overflow no sooner than with probabilities up to 1 (scales below 2^-111 lose bits by it).
 //
 // What bounds it (one GB300, GPU time in a graph): 272 ragged sequences of 32/8 heads of
 // 128, 665 MB in 128 us (5.2 TB/s, 77 % of the copy rate; the bf16 operator needs 193 for
@@ -27,6 +28,7 @@ namespace pced {
 constexpr float P8_RAISE = 7.f;   // log2 of a probability at the reference
 constexpr float P8_SLACK = 15.f;  // log2 of the largest one
 constexpr float P8_LOW = 2048.f;  // factor of a probability's second part
+constexpr float P8_UP = 32768.f;  // 2^P8_SLACK, by which the sums of the values are kept down
 
 template <int D_, bool PK>
 struct TileE4m3 {
@@ -152,14 +154,14 @@ struct TileE4m3 {
     const int klo = kb + 2 * tq, khi = klo + 8;
     const uint32_t mlo = (klo < nvalid ? 0xFFFFu : 0u) | (klo + 1 < nvalid ? 0xFFFF0000u : 0u);
     const uint32_t mhi = (khi < nvalid ? 0xFFFFu : 0u) | (khi + 1 < nvalid ? 0xFFFF0000u : 0u);
-    const float low = scales.y * (1.f / P8_LOW);
+    const float high = scales.y * (1.f / P8_UP), low = high * (1.f / P8_LOW);
     float t[2][2][4], u[2][2][4];
     const auto take_up = [&](int j) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          A.o[2 * j + i][e] = fmaf(t[j & 1][i][e], scales.y, A.o[2 * j + i][e]);
+          A.o[2 * j + i][e] = fmaf(t[j & 1][i][e], high, A.o[2 * j + i][e]);
           if (!PK) A.o[2 * j + i][e] = fmaf(u[j & 1][i][e], low, A.o[2 * j + i][e]);
         }
     };
@@ -234,6 +236,7 @@ extern "C" pced_status pced_paged_attention8(const pced_paged_cache8* cache, con
   if (st != PCED_OK) return st;
   const pced_paged_cache& c = a.c;
   a.scale = reinterpret_cast<const float2*>(cache->scale);
+  a.up = P8_UP;
   const uint64_t rows = (uint64_t)c.num_blocks * c.Hkv * c.block_rows;
   CUtensorMap maps[4];
   const void* pools[2] = {c.k, c.v};
