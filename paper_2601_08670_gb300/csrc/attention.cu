@@ -1432,7 +1432,7 @@ int att_step_seg_lead(int seg_cost) { return env_int("PCED_ATT_LEAD", seg_cost /
 
 // cudaFuncSetAttribute once per kernel and device
 template <typename K>
-static cudaError_t set_smem_once(K kernel, size_t bytes, bool* done) {
+static cudaError_t set_smem_once(K kernel, size_t bytes, std::atomic<bool>* done) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -1448,7 +1448,7 @@ static cudaError_t set_smem_once(K kernel, size_t bytes, bool* done) {
 template <int D, bool PK>
 static cudaError_t launch_split(const CUtensorMap& kmap, const CUtensorMap& vmap, const AttArgs& a, int ctas,
                                 cudaStream_t stream) {
-  static bool configured[64];
+  static std::atomic<bool> configured[64];
   cudaError_t e = set_smem_once(att_split_kernel<D, PK>, AttCfg<D>::SMEM, configured);
   if (e != cudaSuccess) return e;
   return pced_host::launch_cluster(att_split_kernel<D, PK>, dim3(ctas), a.fused ? ctas : 0, ATT_THREADS,
@@ -1494,7 +1494,7 @@ cudaError_t att_layer_launch(int D, const CUtensorMap& kmap, const CUtensorMap& 
 template <int D, bool PK>
 static cudaError_t launch_step(const CUtensorMap& kmap, const CUtensorMap& vmap, const StepAttArgs& a, int ctas,
                                cudaStream_t stream) {
-  static bool configured[64];
+  static std::atomic<bool> configured[64];
   const StepSmem SL = step_smem(D, a.G);
   cudaError_t e = set_smem_once(att_step_kernel<D, PK>, 227 * 1024, configured);
   if (e != cudaSuccess) return e;

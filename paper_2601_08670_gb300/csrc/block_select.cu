@@ -323,7 +323,7 @@ extern "C" pced_status pced_block_select(const pced_paged_cache* cache, const vo
   a.status = status;
   const auto kernel = c.D == 128 ? block_select_kernel<128> : block_select_kernel<64>;
   const size_t smem = (size_t)c.max_blocks * 4;
-  static bool done[2][64];
+  static std::atomic<bool> done[2][64];
   cudaError_t e = allow_smem(kernel, BSEL_MAX_BLOCKS * 4, done[c.D == 128]);
   if (e != cudaSuccess) return cuda_status(e, "block_select shared memory");
   // CTAs of a row: more while there are fewer than two for every SM and the blocks

@@ -32,23 +32,21 @@ pced_status cuda_status(cudaError_t e, const char* what) {
 }
 
 int num_sms() {
-  static int cache[64];
-  static bool init[64];
+  static std::atomic<int> cache[64];  // (0: not asked yet; host threads call at the same time)
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
     cudaGetLastError();
     return 0;
   }
-  if (!init[dev]) {
-    int n = 0;
+  int n = cache[dev];
+  if (!n) {
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
       cudaGetLastError();
       return 0;
     }
     cache[dev] = n;
-    init[dev] = true;
   }
-  return cache[dev];
+  return n;
 }
 
 int row_cluster(int64_t rows) {
@@ -62,14 +60,15 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 static EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
+  static std::atomic<EncodeTiledFn> held{nullptr};
+  EncodeTiledFn fn = held;
   if (!fn) {
     void* ptr = nullptr;
     cudaDriverEntryPointQueryResult q;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
             cudaSuccess &&
         q == cudaDriverEntryPointSuccess)
-      fn = (EncodeTiledFn)ptr;
+      held = fn = (EncodeTiledFn)ptr;
     else
       cudaGetLastError();
   }

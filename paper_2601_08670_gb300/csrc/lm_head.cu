@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(LM_THREADS, 1)
 cudaError_t lm_head_launch(const LmMaps& m, const LmGeom& g, const LmArgs& a, cudaStream_t stream) {
   if (g.pair) return lm_head_pair_launch(m, g, a, stream);
   // the shared-memory limit is an attribute of the kernel on each device
-  static bool configured[64];
+  static std::atomic<bool> configured[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;

@@ -89,9 +89,10 @@ pced_status make_tmap_kv_part(CUtensorMap* map, const void* base, uint64_t rows,
 // ... over a pool of `rows` rows of D bytes, box_rows whole rows in a copy, swizzled
 // over D bytes (16-byte part c of row r lies at c ^ (r & 7), for D = 64 at c ^ (r >> 1 & 3))
 pced_status make_tmap_bytes(CUtensorMap* map, const void* base, uint64_t rows, uint32_t D, uint32_t box_rows);
-// more than 48 KB of dynamic shared memory for a kernel: asked for once per device
+// more than 48 KB of dynamic shared memory for a kernel: asked for once per device (host
+// threads call at the same time)
 template <typename K>
-inline cudaError_t allow_smem(K kernel, size_t bytes, bool (&done)[64]) {
+inline cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<bool> (&done)[64]) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;

@@ -593,7 +593,7 @@ inline size_t place_records(PagedAttArgs* a, void* ws, int32_t G, int32_t D) {
 template <class Tile, bool SMALL>
 cudaError_t launch_paged(const CUtensorMap (&maps)[4], const PagedAttArgs& a, int ctas, cudaStream_t stream) {
   const auto kernel = paged_attention_kernel<Tile, SMALL>;
-  static bool done[64];
+  static std::atomic<bool> done[64];
   const cudaError_t e = pced_host::allow_smem(kernel, PagedCfg<Tile, SMALL>::SMEM, done);
   if (e != cudaSuccess) return e;
   return pced_host::launch_pdl(kernel, dim3(ctas), PagedCfg<Tile, SMALL>::THREADS, PagedCfg<Tile, SMALL>::SMEM, stream, maps[0], maps[1],

@@ -1255,7 +1255,7 @@ constexpr size_t SMP_SMEM = (SMP_LIST + SMP_WARPS * SMP_QUEUE) * sizeof(float2);
 
 template <typename T, int ROOM>
 static cudaError_t launch_sample(const SampleArgs& a, int32_t rows, int ctas, cudaStream_t stream) {
-  static bool done[64];
+  static std::atomic<bool> done[64];
   const auto kernel = sample_kernel<T, ROOM>;
   const cudaError_t e = pced_host::allow_smem(kernel, SMP_SMEM, done);
   if (e != cudaSuccess) return e;
@@ -1265,26 +1265,26 @@ static cudaError_t launch_sample(const SampleArgs& a, int32_t rows, int ctas, cu
 // number allows it: a cluster lies within a part of the device).
 template <typename T, int ROOM>
 static cudaError_t all_at_once(int32_t rows, int ctas, bool& yes) {
-  static int cache[64][ROW_CLUSTER + 1];
-  static bool done[64];
+  static std::atomic<int> cache[64][ROW_CLUSTER + 1];  // (0: not asked yet)
+  static std::atomic<bool> done[64];
   const auto kernel = sample_kernel<T, ROOM>;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = pced_host::allow_smem(kernel, SMP_SMEM, done);
   if (e != cudaSuccess) return e;
-  if (!cache[dev][ctas]) {
+  int held = cache[dev][ctas];
+  if (!held) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas), cfg.blockDim = dim3(SMP_THREADS), cfg.dynamicSmemBytes = SMP_SMEM;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim = {(unsigned)ctas, 1, 1};
     cfg.attrs = attr, cfg.numAttrs = 1;
-    int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&held, kernel, &cfg);
     if (e != cudaSuccess) return e;
-    cache[dev][ctas] = n;
+    cache[dev][ctas] = held;
   }
-  yes = rows <= cache[dev][ctas];
+  yes = rows <= held;
   return cudaSuccess;
 }
 template <typename T>
