@@ -97,6 +97,7 @@ __global__ void __launch_bounds__(APP_ONE_THREADS) kv_append_one_kernel(AppendAr
 // Sixteen documents: 134 us with a unit per head's row (angles read again for every
 // head), 89 us this way at 2 CTAs of 256 threads an SM, 81 us at 3, 78 us with an
 // item's heads side by side in the grid, 76 us with 6 CTAs of 128 threads.
+constexpr int APP_CLUSTER = 8;  // most CTAs of an item and kv-head
 constexpr int APP_CTAS = 6;     // CTAs that an SM holds
 constexpr int APP_HEADS = 3;  // heads whose loads a thread has in flight (six, at 2/3 of the CTAs: 1 % less time)
 
@@ -314,7 +315,7 @@ extern "C" pced_status pced_kv_append(const pced_paged_cache* cache, const void*
                    (cudaStream_t)stream, a);
   } else {
     const int units = APP_THREADS / (c.D / 16);
-    const int64_t items = append_items(a, units);
+    const int64_t items = append_items(a, units, APP_CLUSTER);
     if (!items) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
     const int64_t groups = items * (c.Hkv / a.heads);
     // rows of a full item, about; CTAs of a cluster for them, while that leaves each its units' worth and all

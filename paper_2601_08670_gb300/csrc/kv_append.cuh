@@ -27,7 +27,6 @@ struct AppendArgs {
 };
 
 constexpr int APP_THREADS = 128;
-constexpr int APP_CLUSTER = 8;  // most CTAs of an item and kv-head
 
 // tokens [t0, t0 + m) of one sequence, which go to rows r0 ... of one block
 struct AppendItem {
@@ -191,11 +190,12 @@ inline pced_status append_args(const pced_paged_cache* cache, const void* q, int
 
 // Items of a call with tok_start (blocks touched: at most two more than whole ones for
 // every sequence with tokens) and the kv-heads that a CTA takes of one, so that its
-// `units` have a row each where items have few; 0 items: too many
-inline int64_t append_items(AppendArgs& a, int units) {
+// `units` have a row each where items have few; 0 items: too many for a grid of up to `cluster`
+// CTAs each
+inline int64_t append_items(AppendArgs& a, int units, int cluster) {
   const pced_paged_cache& c = a.c;
   const int64_t items = (int64_t)a.T / c.block_rows + 2 * (int64_t)(a.T < c.S ? a.T : c.S);
-  if (items * c.Hkv * APP_CLUSTER >= (INT64_C(1) << 31)) return 0;
+  if (items * c.Hkv * cluster >= (INT64_C(1) << 31)) return 0;
   const int64_t rows = a.T / items > 0 ? a.T / items : 1;  // of an item, about
   a.heads = 1;
   while (2 * a.heads * rows <= units && c.Hkv % (2 * a.heads) == 0) a.heads *= 2;

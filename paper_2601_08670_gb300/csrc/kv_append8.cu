@@ -404,7 +404,7 @@ extern "C" pced_status pced_kv_append8(const pced_paged_cache8* cache, const voi
     e = launch_pdl(c.D == 128 ? kv_append8_one_kernel<128> : kv_append8_one_kernel<64>, dim3(c.Hkv, c.S), threads, 0,
                    (cudaStream_t)stream, a);
   } else {
-    const int64_t items = append_items(a, APP_THREADS / (c.D / 16));
+    const int64_t items = append_items(a, APP_THREADS / (c.D / 16), 1);
     if (!items) return fail(PCED_ERR_UNSUPPORTED, "%s: too many tokens", fn);
     e = launch_pdl(c.D == 128 ? kv_append8_kernel<128> : kv_append8_kernel<64>,
                    dim3((unsigned)(items * (c.Hkv / a.heads))), APP_THREADS, 0, (cudaStream_t)stream, a);
