@@ -623,7 +623,8 @@ typedef struct pced_paged_cache8 {
  * what falls below e4m3's smallest numbers, and nothing else.  Rows appended one
  * by one and at once can differ by that, and by the scale that the block had when
  * they came.
- * The summaries are of the rotated fp32 keys.
+ * The summaries are of the rotated fp32 keys, which the stored ones can exceed by
+ * their rounding (1/16 of themselves).
  * ------------------------------------------------------------------------ */
 pced_status pced_kv_append8(const pced_paged_cache8* cache, const void* q, int64_t q_stride, const void* k,
                             int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int32_t Hq,
@@ -633,8 +634,9 @@ pced_status pced_kv_append8(const pced_paged_cache8* cache, const void* q, int64
 /* ------------------------------------------------------------------------
  * pced_paged_attention8 -- pced_paged_attention over an 8-bit cache, of the
  * numbers that the bytes stand for (times their scale); arguments, conditions and
- * the workspace (pced_paged_attention_workspace_size) are its.  Queries are not
- * rounded, probabilities are held to 23 bits, sums in fp32.
+ * the workspace (pced_paged_attention_workspace_size) are its.  Parts of a query
+ * below 2^-31 of its head's largest lose bits, all others are exact;
+ * probabilities are held to 23 bits (there 24), sums in fp32.
  * ------------------------------------------------------------------------ */
 pced_status pced_paged_attention8(const pced_paged_cache8* cache, const void* q, int64_t q_stride, int32_t Hq,
                                   const int32_t* sel, int32_t n_sel, int64_t total_rows, float scale, void* out,
@@ -663,14 +665,18 @@ pced_status pced_paged_attention8(const pced_paged_cache8* cache, const void* q,
  * the first kept one, in the order of the vocabulary, with
  * sum_{v' <= v} w_v' > u sum w.  t = 0, k = 1, p <= 0 and min_p > 1 give the
  * first of the largest (logprob 0).  Logits of +inf share everything equally.
- * Weights are exact to 2^-30 of themselves (most to 2^-32) and are added in whole steps
- * (2^-42 of the power of two from the largest up), sixteen at a time: the choice
- * depends on no order of sums and differs from that of exact sums in about one
- * row of a million.  Weights below 2^-44 are nothing to a cut.  Temperatures
- * count as 1e-37 at least and 1e30 at most, to weights, min_p and logprob alike.
+ * Weights are exact to 2^-30 of themselves (most to 2^-32), sixteen at a time are
+ * added and rounded to whole steps (2^-42 of the power of two from the largest up),
+ * which are added exactly: the choice differs from that of exact sums in about one
+ * row of some millions.  The same call gives the same tokens.  Which sixteen go
+ * together follows a row's address and how many CTAs share it, so with other rows
+ * beside it, at another address or on another device a sum can differ by some
+ * steps, and a token where u (or p) lies as near to a border.  Weights below 2^-44
+ * are nothing to a cut.  Temperatures count as 1e-37 at least and 1e30 at most, to
+ * weights, min_p and logprob alike.
  * A row whose logits are all -inf has token -1 and logprob -inf; so has one
  * with a parameter that is not a number, t < 0 or u outside [0, 1], which sets
- * PCED_DEV_BAD_PARAM.  V <= 393216.
+ * PCED_DEV_BAD_PARAM.  u = 1 gives the last kept token of a weight that counts.  V <= 393216.
  * ------------------------------------------------------------------------ */
 #define PCED_IN_F32 0
 #define PCED_IN_BF16 1

@@ -406,8 +406,8 @@ class PagedCache8(PagedCache):
     and the other tensors of a PagedCache.
 
     kv_append writes numbers and scales (rows of another cache become bytes by appending them), paged_attention reads
-    them, block_select reads the summaries, which kv_append keeps; block_summaries reads bf16 keys and takes a PagedCache
-    alone."""
+    them, block_select reads the summaries, which kv_append keeps; block_summaries reads bf16 keys and takes a
+    PagedCache alone."""
 
     _TAKEN = PagedCache._TAKEN | {"scale"}
     _NUMBERS, _NAME = torch.float8_e4m3fn, "e4m3"
@@ -436,9 +436,10 @@ def rope_table(theta: float, D: int, rows: int, device="cuda") -> torch.Tensor:
 def kv_append(cache: PagedCache, q, k, v, rope=None, tok_start=None, positions=None, q_out=None, status=None,
               stream=None):
     """pced_kv_append (pced_kv_append8 for a PagedCache8): k, v bf16 [T, Hkv, D] into the last rows of the sequences,
-    q bf16 [T, Hq, D] (or None) rotated into q_out, which is returned.  The parts of one projection's output need no copies (strides between
-    tokens).  rope: fp32 [rows, D] (rope_table), None: no rotation; tok_start: int32 [S + 1], None: one token per
-    sequence; positions: int32 [T], None: the rows themselves.  Device conditions go to the int32 tensor status."""
+    q bf16 [T, Hq, D] (or None) rotated into q_out, which is returned.  The parts of one projection's output need no
+    copies (strides between tokens).  rope: fp32 [rows, D] (rope_table), None: no rotation; tok_start: int32 [S + 1],
+    None: one token per sequence; positions: int32 [T], None: the rows themselves.  Device conditions go to the int32
+    tensor status."""
     if q_out is None and q is not None:
         q_out = _empty((q.shape[0], q.shape[1], cache.D), torch.bfloat16, q.device, stream)
     native = _calls or _native()
@@ -480,9 +481,9 @@ def paged_attention_workspace_size(S, Hq, Hkv, D) -> int:
 def paged_attention(cache: PagedCache, q, sel=None, total_rows: int = 0, scale=None, out=None, lse=None, ws=None,
                     stream=None):
     """pced_paged_attention (pced_paged_attention8 for a PagedCache8): q bf16 [S, Hq, D] over the cache, or over the
-    blocks sel int32 [S, Hkv, n_sel]; returns out [S, Hq, D], fp32 unless a bf16 `out` is passed.  lse: fp32 [S, Hq] that receives the log of the softmax's sum.
-    total_rows: upper bound of the rows attended to (of one kv-head, over all sequences), 0: unknown.  A workspace of
-    the caller's own is zeroed before its first use (workspace())."""
+    blocks sel int32 [S, Hkv, n_sel]; returns out [S, Hq, D], fp32 unless a bf16 `out` is passed.  lse: fp32 [S, Hq]
+    that receives the log of the softmax's sum.  total_rows: upper bound of the rows attended to (of one kv-head, over
+    all sequences), 0: unknown.  A workspace of the caller's own is zeroed before its first use (workspace())."""
     if out is None:
         out = _empty((cache.S, q.shape[1], cache.D), torch.float32, q.device, stream)
     if ws is None:

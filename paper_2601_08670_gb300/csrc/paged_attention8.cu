@@ -7,7 +7,7 @@
 // scores and the scale of the values the factor with which the warp's sums are added.
 // The bytes become fp16 in registers, which holds every e4m3 number, and the products
 // run as fp16 mma.sync.  fp16's range is met by powers of two: a head's query is scaled
-// so that its largest part lies in [2^14, 2^15) (a part below 2^-28 of it loses bits,
+// so that its largest part lies in [2^14, 2^15) (a part below 2^-31 of it loses bits,
 // which the sum does not keep either), probabilities are counted from 2^7 at the
 // reference (at most 2^15 until it moves), their first 11 bits in one part, the rest, times
 // 2^11, in the other: 23 bits, as a sum in fp32 keeps.  The values' sums are kept 2^-15 down, so that

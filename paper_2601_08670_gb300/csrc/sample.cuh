@@ -9,7 +9,7 @@
 // A sum over a vocabulary decides at which token u falls, and its error counts 150,000
 // times (every border of two tokens is a place to be wrong): with weights of 24 bits one row
 // in some thousands gets another token than in 64 bits.  So weights are exact to 2^-30
-// of themselves, and are added without further loss (see Sum).
+// of themselves, and are added with 2^-42 lost in sixteen (see Sum).
 //
 // A cluster of CTAs reads a row two to four times, from L2 after the first: for its largest logit,
 // for its weights, for what a cut leaves.  A cut is found by counting the tokens in equal
@@ -20,11 +20,13 @@
 // logits, say) are split by (logit, token) pairs as 64-bit numbers, again and again: pairs are
 // distinct, so that ends.  Few tokens that are left go to one CTA, which ends alone.
 //
-// What bounds it (one GB300, GPU time in a graph).  Many rows: instructions.  A weight and its sum
-// take about 24 a token, 272 rows of 151936 fp32 logits without a cut 84 us (48 of them for the
-// largest logit, at 3.4 TB/s), top 50 81, p = 0.9 190 (a count and a second weight, and about
-// 45,000 cycles a CTA of small steps between barriers), mixed cuts 148 of a floor of 24.5.  Few rows:
-// those steps.  A row of 128256 4.8 us at t = 0, 9.3 without a cut, 12.5 for the top 50, 29 for
+// What bounds it (one GB300, GPU time in a graph).  Many rows: 272 of 151936 fp32 logits 48 us for
+// the largest logit alone (3.4 TB/s, half of the copy rate: a warp has one group's loads in flight),
+// without a cut 84 (a weight and its sum take about 24 instructions a token), top 50 79 (the same
+// first pass and one that lists), p = 0.9 190 (a count and a second weight, and about 45,000 cycles a
+// CTA of small steps between barriers), mixed cuts 142 to 154 of a floor of 24.5; the warps issue
+// in 35 to 60 % of the slots, so loads and barriers are waited for as well.  Few rows:
+// those steps.  A row of 128256 5.0 us at t = 0, 9.4 without a cut, 12.7 for the top 50, 29 for
 // p = 0.9; a barrier of a cluster costs 900 cycles, what its CTAs read of one another 10 bytes a clock.
 #pragma once
 
